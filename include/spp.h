@@ -335,6 +335,114 @@ spp_status adapter_predict_static(const void* adapter_a, const void* adapter_b, 
                                   int32_t n, int32_t r, const float* x_dev, int32_t B, float* s_out_dev,
                                   void* hip_stream);
 
+/* ------------------------------------- attention over a 4-bit key/value cache
+ *
+ * The operators of the attention in front of an MoE layer, on explicit device
+ * pointers like adapter_predict_static: no context, no allocation, no host
+ * wait, the work enqueued on hip_stream of the current device (every pointer
+ * belongs to that device), so a call can be captured into a graph.  A call
+ * with nothing to do (T = 0, n_seq = 0) returns SPP_OK and enqueues nothing.
+ * Errors: EINVAL before anything is enqueued (NULL or misaligned pointer, bad
+ * shape or stride, a workspace that is too small), EHIP.  What only the device
+ * can see (slots, page ids, lengths) cannot be refused: each call says what an
+ * entry out of range does, and none makes it read or write outside the cache
+ * and the rows it was given.
+ *
+ * Cache: n_pages pages of `page` tokens, one block per page p and key/value
+ * head h at byte (p * n_kv_heads + h) * page * (d + d/16), d = head_dim:
+ *   key codes [page][d/2], value codes [page][d/2], key scales [d/32][page],
+ *   value scales [d/32][page].
+ * A byte of codes holds elements 2j (low nibble) and 2j+1.  A code is a sign
+ * bit (8) and the magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (codes 0..7); an
+ * element is its code's value times 2^(s - 127), s the scale byte of its
+ * block of 32 elements.  s = 255 makes the block NaN.  4.25 bits an element.
+ * The format is the one gfx950 converts to bf16 in hardware, exactly.
+ * A slot names a token's place in the cache: p * page + offset. */
+typedef struct {
+  int32_t n_heads;     /* query heads, a multiple of n_kv_heads */
+  int32_t n_kv_heads;  /* key/value heads; query head i reads key/value head i / (n_heads / n_kv_heads) */
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t page;        /* tokens per page: 16, 32, 64, 128 or 256 */
+  int32_t n_pages;     /* pages of the cache */
+} spp_attn_desc;
+
+/* Bytes of a cache of this shape; 0 for a bad one (spp_last_error says why). */
+size_t spp_kv4_cache_bytes(const spp_attn_desc* desc);
+
+/* Rotary angles over several position axes (time, height and width of an
+ * image's tokens; text tokens have the same position on each):
+ *   angle = pos[axis_of[i]][t] * inv_freq[i], formed and reduced in 64 bits;
+ *   table[t][0][i] = cos(angle), table[t][1][i] = sin(angle).
+ * pos: dev int32, axis a at pos + a * pos_stride, [T] each; n_axes: 1 to 4;
+ * axis_of: host int32 [n_freq], the axis each frequency turns with (runs of
+ * axes, or interleaved ones), or NULL (all axis 0); inv_freq: dev fp32
+ * [n_freq]; n_freq: a multiple of 8, at most 64; table: dev fp32
+ * [T][2][n_freq], 16-byte aligned.  One table serves every layer of a step. */
+spp_status spp_rotary_table(const int32_t* pos, int64_t pos_stride, int32_t n_axes, const int32_t* axis_of,
+                            const float* inv_freq, int32_t n_freq, int32_t T, float* table, void* hip_stream);
+
+/* Rotate T tokens' queries and keys and write their keys and values into the
+ * cache.  q: dev [T][n_heads][d] in dtype, token t at q + t * q_stride
+ * elements; k, v the same with n_kv_heads heads and k_stride, v_stride (rows
+ * of one fused product need no copies).  q_out (row stride q_out_stride)
+ * receives the rotated queries in dtype; q_out may be q with the same stride.
+ * q and q_out both NULL: keys and values only.  table: of spp_rotary_table,
+ * [T][2][n_freq], 2 * n_freq <= d; element i < n_freq turns with element
+ * i + n_freq, elements from 2 * n_freq on stay.  n_freq = 0 (table NULL): no
+ * rotation.  Every product and sum of the rotation is rounded to fp32; keys
+ * are not rounded to dtype before they are quantised.
+ * slots: dev int64 [T]; a token whose slot is outside [0, n_pages * page) is
+ * not written (its query is rotated all the same).  Where two tokens of a call
+ * have one slot, that slot holds parts of both.
+ * A block of 32 elements takes the smallest scale with no magnitude above
+ * 7 * 2^(s-127), 2 <= s <= 252, and each element the nearest code (ties to
+ * the even one): no element is off by more than half of its step, except that
+ * magnitudes above 7 * 2^125 become 6 * 2^125.  A block with an infinity or
+ * a NaN becomes a NaN block.  Pointers 16-byte aligned, strides multiples of
+ * 16 bytes, at least a row. */
+spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int32_t dtype, const void* q, int64_t q_stride,
+                         void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, const void* v,
+                         int64_t v_stride, const float* table, int32_t n_freq, const int64_t* slots, int32_t T,
+                         void* hip_stream);
+
+/* Read T tokens' keys and values back: k_out, v_out dev [T][n_kv_heads][d] in
+ * dtype with their row strides (exact in either dtype); either may be NULL.
+ * The rows of a token whose slot is outside [0, n_pages * page) are left as
+ * they were.  Alignment as for spp_kv4_store. */
+spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dtype, const int64_t* slots, int32_t T,
+                        void* k_out, int64_t k_stride, void* v_out, int64_t v_stride, void* hip_stream);
+
+/* Attention of n_seq sequences' query tokens over their cached tokens:
+ *   out[i] = sum_t softmax_t(scale * q[i] . k[t]) v[t].
+ * q, out: dev [n_tokens][n_heads][d] in dtype with their row strides (out may
+ * be q with the same stride).  q_start: dev int32 [n_seq + 1], sequence b has
+ * the query tokens q_start[b] .. q_start[b+1] - 1; NULL: one each (n_tokens =
+ * n_seq).  kv_len: dev int32 [n_seq], cached tokens of each; token t of
+ * sequence b is in page pages[b * pages_stride + t / page] (dev int32).
+ * causal = 1: the queries are the sequence's last tokens, query j of n sees
+ * cached tokens t <= kv_len - n + j; 0: every query sees all of them.  A
+ * query that sees no token gives zeros.  Rows of no sequence are left as they
+ * were.  What a query does not see does not reach it, NaN blocks and pages of
+ * unseen tokens included; a NaN key or value block that it sees makes its row
+ * (the block's elements for a value) NaN.
+ * max_q: at least the most query tokens of a sequence (tokens past it are left
+ * as they were); max_kv: about the most cached tokens (a hint for the split of
+ * the work, never for the result's correctness).  kv_len below 0 counts as 0;
+ * a sequence with more tokens than its page table row names (pages_stride *
+ * page), or with a page id outside [0, n_pages) among those a query sees,
+ * gives that query NaN.
+ * Scores and softmax statistics are fp32; bf16 queries are exact operands,
+ * probabilities are rounded to bf16 for the value product (their sum is not);
+ * fp32 queries and probabilities go in as three bf16 terms each.
+ * workspace: dev, spp_kv4_attend_workspace bytes (16-byte aligned, any
+ * contents), held by the call until the stream has passed it: calls (and
+ * captured graphs) that may run at the same time need one each. */
+size_t spp_kv4_attend_workspace(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, int32_t max_kv);
+spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cache, int32_t dtype, const void* q, int64_t q_stride,
+                          const int32_t* q_start, const int32_t* kv_len, const int32_t* pages, int64_t pages_stride,
+                          int32_t n_seq, int32_t n_tokens, int32_t max_q, int32_t max_kv, int32_t causal, float scale,
+                          void* out, int64_t out_stride, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ------------------------------------------------------ inspection / runs */
 
 /* Slot table of layer l: experts_out host int32 [S] (-1 = EMPTY), stamps_out

@@ -43,7 +43,7 @@ def build(verbose: bool = True, sanitize: str = "") -> str:
     os.makedirs(out_dir, exist_ok=True)
     inc = ["-I" + INCLUDE, "-I" + CSRC]
     objs = []
-    for src in ("spp_kernels.hip", "spp_static.hip"):
+    for src in ("spp_kernels.hip", "spp_static.hip", "spp_attn.hip"):
         obj = os.path.join(out_dir, src.replace(".hip", ".o"))
         _run([HIPCC, *DEVICE_FLAGS, *inc, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)

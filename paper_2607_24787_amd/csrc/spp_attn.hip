@@ -1,0 +1,907 @@
+// Attention over a 4-bit key/value cache: rotary tables, the store that
+// rotates and quantises, the load that reads back, and the attention itself.
+// The cache's format and the calls' contracts are in spp.h.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "spp.h"
+#include "spp_internal.h"
+
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMaxFreq = 64;
+constexpr uint32_t kExpMask = 0x7f800000u;
+constexpr int kNanByte = 255;
+constexpr int kMinByte = 2;    // scale 2^-125: every nonzero value of a block stays a normal number
+constexpr int kMaxByte = 252;  // scale 2^125: 6 * 2^125 is the largest that is finite in bf16 and fp32
+
+// ------------------------------------------------------------------ the cache
+
+struct Cache {
+  const uint8_t* base;
+  uint64_t page_bytes;  // all heads of a page
+  uint32_t head_bytes;  // one head of a page
+  int page, shift;      // tokens per page and its logarithm
+  int n_pages;
+};
+
+// Offsets within a (page, head) block of head size D.
+template <int D>
+struct Block {
+  static __device__ __forceinline__ uint32_t codes(int page, int kv, int off) {
+    return static_cast<uint32_t>((kv * page + off) * (D / 2));
+  }
+  static __device__ __forceinline__ uint32_t scales(int page, int kv, int block, int off) {
+    return static_cast<uint32_t>(page * D + (kv * (D / 32) + block) * page + off);
+  }
+};
+
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Two codes of byte SEL of w to bf16, times the power of two in `scale`'s
+// exponent field (its other bits do not count; exponent 255 gives NaN).
+template <int SEL>
+__device__ __forceinline__ uint32_t cvt2(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
+}
+
+// 8 codes to 8 bf16, in order
+__device__ __forceinline__ u32x4 cvt8(uint32_t w, float scale) {
+  return u32x4{cvt2<0>(w, scale), cvt2<1>(w, scale), cvt2<2>(w, scale), cvt2<3>(w, scale)};
+}
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+}
+
+// 8 consecutive elements of a row (16-byte aligned)
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float* f) {
+  if constexpr (std::is_same<T, float>::value) {
+    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = a[i], f[4 + i] = b[i];
+  } else {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[2 * i] = bf16_lo(a[i]), f[2 * i + 1] = bf16_hi(a[i]);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float* f) {
+  if constexpr (std::is_same<T, float>::value) {
+    reinterpret_cast<f32x4*>(p)[0] = f32x4{f[0], f[1], f[2], f[3]};
+    reinterpret_cast<f32x4*>(p)[1] = f32x4{f[4], f[5], f[6], f[7]};
+  } else {
+    *reinterpret_cast<u32x4*>(p) =
+        u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+  }
+}
+
+// --------------------------------------------------------------- rotary table
+
+struct TableArgs {
+  const int32_t* pos;
+  int64_t pos_stride;
+  const float* inv_freq;
+  float* table;
+  uint32_t axes[kMaxFreq / 16];  // two bits per frequency
+  int F, T;
+};
+
+constexpr int kTableFreqs = 4;  // per thread: 16-byte stores
+
+// The angle in turns, reduced to [-1/2, 1/2] in 64 bits; what is left of it
+// beyond fp32 goes in by the first term of the addition theorem.
+__global__ __launch_bounds__(256) void rotary_table_kernel(TableArgs a) {
+  const uint32_t per = static_cast<uint32_t>(a.F / kTableFreqs);
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  const uint32_t t = i / per;
+  if (t >= static_cast<uint32_t>(a.T)) return;
+  const int f0 = static_cast<int>(i - t * per) * kTableFreqs;
+  f32x4 c, s;
+#pragma unroll
+  for (int k = 0; k < kTableFreqs; ++k) {
+    const int f = f0 + k;
+    const int axis = static_cast<int>(a.axes[f / 16] >> (2 * (f % 16))) & 3;
+    const double angle = static_cast<double>(a.pos[axis * a.pos_stride + t]) * static_cast<double>(a.inv_freq[f]);
+    double turns = angle * 0.15915494309189533577;
+    turns -= rint(turns);
+    const double half = 2.0 * turns;  // in units of pi
+    const float hi = static_cast<float>(half);
+    const float lo = static_cast<float>((half - static_cast<double>(hi)) * 3.14159265358979323846);
+    const float ch = cospif(hi), sh = sinpif(hi);
+    c[k] = fmaf(-lo, sh, ch);
+    s[k] = fmaf(lo, ch, sh);
+  }
+  float* row = a.table + static_cast<size_t>(t) * 2 * a.F + f0;
+  *reinterpret_cast<f32x4*>(row) = c;
+  *reinterpret_cast<f32x4*>(row + a.F) = s;
+}
+
+// ----------------------------------------------------------------- store, load
+
+struct StoreArgs {
+  Cache cache;
+  const void *q, *k, *v;
+  void* q_out;
+  int64_t q_stride, q_out_stride, k_stride, v_stride;
+  const float* table;
+  const int64_t* slots;
+  int Hq, Hkv, F;  // Hq = 0: no queries
+  int T;
+};
+
+// Codes (one word) and scale byte of this lane's 8 elements of a block of 32,
+// which lanes 4j .. 4j+3 hold together.
+__device__ __forceinline__ uint32_t quantise8(const float* y, uint32_t* byte) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(y[i]) & 0x7fffffffu);  // ordered as the magnitudes are; NaN above infinity
+  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
+  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
+  if (top >= kExpMask) {
+    *byte = kNanByte;
+    return 0u;
+  }
+  // top = 1.m * 2^(E-127) <= 7 * 2^e = 1.75 * 2^(e+2)
+  const int E = static_cast<int>(top >> 23);
+  int s = (top & 0x7fffffu) <= 0x600000u ? E - 2 : E - 1;
+  s = min(max(s, kMinByte), kMaxByte);
+  const float scale = scale_of(static_cast<uint32_t>(s));
+  *byte = static_cast<uint32_t>(s);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], scale, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], scale, 3);
+  return w;
+}
+
+// Each product and the sum rounded, not contracted: what is quantised next is
+// then the same number wherever it is formed.
+__device__ __forceinline__ float turn(float y, float z, float c, float s, bool first) {
+#pragma clang fp contract(off)
+  const float p = y * c, r = z * s;
+  return first ? p - r : p + r;
+}
+
+// D/8 lanes per head, 8 elements each; a thread reads its elements and those
+// they turn with before it writes, and a head lies within one wave, so the
+// queries may be rotated in place.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv4_store_kernel(StoreArgs a) {
+  constexpr int L = D / 8;
+  const uint32_t heads = static_cast<uint32_t>(a.Hq + 2 * a.Hkv);
+  const uint32_t unit = blockIdx.x * (256u / L) + threadIdx.x / L;
+  const uint32_t t = unit / heads;
+  if (t >= static_cast<uint32_t>(a.T)) return;
+  int h = static_cast<int>(unit - t * heads);
+  const int e0 = static_cast<int>(threadIdx.x % L) * 8;
+  const int kind = h < a.Hq ? 0 : (h < a.Hq + a.Hkv ? 1 : 2);
+  h -= kind == 0 ? 0 : (kind == 1 ? a.Hq : a.Hq + a.Hkv);
+  const T* row = kind == 0   ? reinterpret_cast<const T*>(a.q) + static_cast<int64_t>(t) * a.q_stride
+                 : kind == 1 ? reinterpret_cast<const T*>(a.k) + static_cast<int64_t>(t) * a.k_stride
+                             : reinterpret_cast<const T*>(a.v) + static_cast<int64_t>(t) * a.v_stride;
+  row += h * D;
+  const int64_t slot = a.slots[t];
+  float y[8];
+  load8(row + e0, y);
+  if (kind < 2 && e0 < 2 * a.F) {
+    float z[8], c[8], s[8];
+    const bool first = e0 < a.F;
+    const int f0 = first ? e0 : e0 - a.F;
+    load8(row + (first ? e0 + a.F : f0), z);
+    const float* tab = a.table + static_cast<size_t>(t) * 2 * a.F + f0;
+    load8(tab, c);
+    load8(tab + a.F, s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = turn(y[i], z[i], c[i], s[i], first);
+  }
+  if (kind == 0) {
+    store8(reinterpret_cast<T*>(a.q_out) + static_cast<int64_t>(t) * a.q_out_stride + h * D + e0, y);
+    return;
+  }
+  uint32_t byte;
+  const uint32_t w = quantise8(y, &byte);
+  if (static_cast<uint64_t>(slot) >= static_cast<uint64_t>(a.cache.n_pages) << a.cache.shift) return;
+  const int off = static_cast<int>(slot) & (a.cache.page - 1);
+  uint8_t* blk = const_cast<uint8_t*>(a.cache.base) + static_cast<uint64_t>(slot >> a.cache.shift) * a.cache.page_bytes +
+                 static_cast<uint64_t>(h) * a.cache.head_bytes;
+  *reinterpret_cast<uint32_t*>(blk + Block<D>::codes(a.cache.page, kind - 1, off) + e0 / 2) = w;
+  if (e0 % 32 == 0) blk[Block<D>::scales(a.cache.page, kind - 1, e0 / 32, off)] = static_cast<uint8_t>(byte);
+}
+
+struct LoadArgs {
+  Cache cache;
+  const int64_t* slots;
+  void *k, *v;  // either may be NULL
+  int64_t k_stride, v_stride;
+  int Hkv, T;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv4_load_kernel(LoadArgs a) {
+  constexpr int L = D / 8;
+  const uint32_t both = a.k && a.v ? 2u : 1u;
+  const uint32_t heads = static_cast<uint32_t>(a.Hkv) * both;
+  const uint32_t unit = blockIdx.x * (256u / L) + threadIdx.x / L;
+  const uint32_t t = unit / heads;
+  if (t >= static_cast<uint32_t>(a.T)) return;
+  int h = static_cast<int>(unit - t * heads);
+  const int kv = both == 2u ? (h >= a.Hkv ? 1 : 0) : (a.k ? 0 : 1);
+  if (both == 2u) h -= kv * a.Hkv;
+  const int e0 = static_cast<int>(threadIdx.x % L) * 8;
+  const int64_t slot = a.slots[t];
+  if (static_cast<uint64_t>(slot) >= static_cast<uint64_t>(a.cache.n_pages) << a.cache.shift) return;
+  const int off = static_cast<int>(slot) & (a.cache.page - 1);
+  const uint8_t* blk = a.cache.base + static_cast<uint64_t>(slot >> a.cache.shift) * a.cache.page_bytes +
+                       static_cast<uint64_t>(h) * a.cache.head_bytes;
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + Block<D>::codes(a.cache.page, kv, off) + e0 / 2);
+  const uint32_t byte = blk[Block<D>::scales(a.cache.page, kv, e0 / 32, off)];
+  const u32x4 b = cvt8(w, scale_of(byte));
+  T* out = kv ? reinterpret_cast<T*>(a.v) + static_cast<int64_t>(t) * a.v_stride
+              : reinterpret_cast<T*>(a.k) + static_cast<int64_t>(t) * a.k_stride;
+  out += h * D + e0;
+  if constexpr (std::is_same<T, float>::value) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[2 * i] = bf16_lo(b[i]), f[2 * i + 1] = bf16_hi(b[i]);
+    store8(out, f);
+  } else {
+    *reinterpret_cast<u32x4*>(out) = b;
+  }
+}
+
+// ------------------------------------------------------------------- attention
+
+struct AttendArgs {
+  Cache cache;
+  const void* q;
+  void* out;
+  int64_t q_stride, out_stride;
+  const int32_t *q_start, *kv_len, *pages;
+  int64_t pages_stride;
+  int n_seq, n_tokens, Hkv, G;  // G: query heads per key/value head
+  int causal;
+  float scale_log2;  // scale * log2(e): the softmax runs on powers of two
+};
+
+constexpr int kWaves = 4;
+constexpr int kTile = 32;  // cached tokens per step: one 16x16x32 product over them
+
+// The rows of a sequence's key/value head are its query tokens times the G
+// heads that share it, token-major: row r is token r / G, head r % G.
+struct Seq {
+  int q0, nq;     // first query token, count
+  int len;        // cached tokens (at most what the page table row names)
+  bool overlong;  // it has more than that
+  __device__ __forceinline__ int limit(const AttendArgs& a, int row) const {
+    return a.causal ? max(0, len - nq + row / a.G + 1) : len;
+  }
+};
+
+__device__ __forceinline__ Seq sequence(const AttendArgs& a, int b) {
+  Seq s;
+  if (a.q_start) {
+    s.q0 = min(max(a.q_start[b], 0), a.n_tokens);
+    s.nq = min(max(a.q_start[b + 1], s.q0), a.n_tokens) - s.q0;
+  } else {
+    s.q0 = b;
+    s.nq = 1;
+  }
+  const int64_t room = a.pages_stride * a.cache.page;
+  s.len = max(a.kv_len[b], 0);
+  s.overlong = s.len > room;
+  if (s.overlong) s.len = static_cast<int>(room);
+  return s;
+}
+
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// fp32 as three bf16 terms that add up to it (24 significant bits); for bf16
+// one term, the value rounded to it.
+template <int NS>
+__device__ __forceinline__ void split8(const float* f, u32x4* out) {
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = f[i];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = pack_bf16(r[2 * i], r[2 * i + 1]);
+      out[s][i] = w;
+      if (s + 1 < NS) {
+        r[2 * i] -= bf16_lo(w);
+        r[2 * i + 1] -= bf16_hi(w);
+      }
+    }
+  }
+}
+
+// One step's share of a lane (c = lane % 16, g = lane / 16).  Keys: tokens
+// kt = 8 (c/4) + c%4 and kt + 4 of the tile, elements g*D/4 .. of each (so the
+// four lanes of a token read its whole row in one piece, and a lane needs one
+// scale).  Values: tokens 8g .. 8g+7, elements c*D/16 .. of each.
+template <int D>
+struct Tile {
+  static constexpr int KW = D / 32;  // words of a lane's key codes
+  uint32_t k[2][KW];
+  uint32_t ks[2];
+  uint32_t v[8];  // D = 64: 16 bits each
+  u32x2 vs;       // scale bytes of the 8 tokens
+};
+
+// Page ids of a lane's key tokens and value tokens (they differ where a tile
+// spans two pages); -1: none
+struct Pids {
+  int k, v;
+};
+
+__device__ __forceinline__ Pids page_ids(const AttendArgs& a, const int32_t* pages, int t0, int c, int g) {
+  const int ik = (t0 + (c >> 2) * 8) >> a.cache.shift, iv = (t0 + g * 8) >> a.cache.shift;
+  Pids p;
+  p.k = ik < a.pages_stride ? pages[ik] : -1;
+  p.v = iv < a.pages_stride ? pages[iv] : -1;
+  return p;
+}
+
+template <int D>
+__device__ __forceinline__ void load_tile(const AttendArgs& a, const uint8_t* head, Pids pid, int t0, int c, int g,
+                                          Tile<D>& t) {
+  const int page = a.cache.page;
+  const bool kbad = static_cast<uint32_t>(pid.k) >= static_cast<uint32_t>(a.cache.n_pages);
+  const bool vbad = static_cast<uint32_t>(pid.v) >= static_cast<uint32_t>(a.cache.n_pages);
+  // a page that is none: its keys are NaN, which makes NaN of every row that
+  // sees them; page 0 stands in for the loads
+  const uint8_t* kb = head + static_cast<uint64_t>(kbad ? 0 : pid.k) * a.cache.page_bytes;
+  const uint8_t* vb = head + static_cast<uint64_t>(vbad ? 0 : pid.v) * a.cache.page_bytes;
+  const int ko = (t0 + (c >> 2) * 8 + (c & 3)) & (page - 1), vo = (t0 + g * 8) & (page - 1);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint8_t* p = kb + Block<D>::codes(page, 0, ko + 4 * i) + g * (D / 8);
+    if constexpr (D == 128) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) t.k[i][j] = w[j];
+    } else {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+      t.k[i][0] = w[0], t.k[i][1] = w[1];
+    }
+    const uint32_t byte = kb[Block<D>::scales(page, 0, g * (D / 4) / 32, ko + 4 * i)];
+    t.ks[i] = kbad ? static_cast<uint32_t>(kNanByte) : byte;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint8_t* p = vb + Block<D>::codes(page, 1, vo + j) + c * (D / 32);
+    if constexpr (D == 128)
+      t.v[j] = *reinterpret_cast<const uint32_t*>(p);
+    else
+      t.v[j] = *reinterpret_cast<const uint16_t*>(p);
+  }
+  t.vs = *reinterpret_cast<const u32x2*>(vb + Block<D>::scales(page, 1, c * (D / 16) / 32, vo));
+}
+
+// O += V^T P^T over a tile: product n takes element c * D/16 + n of every
+// lane, so a lane's codes become operands by pairing tokens (one permutation
+// per pair).  frag(n, A operand) is called for n = 0 .. D/16 - 1.
+template <int D, int B = 0, typename Fn>
+__device__ __forceinline__ void value_frags(const uint32_t* w, const float* sc, Fn frag) {
+  uint32_t x[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = cvt2<B>(w[j], sc[j]);
+  u32x4 lo, hi;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    lo[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x05040100u);
+    hi[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x07060302u);
+  }
+  frag(2 * B, lo);
+  frag(2 * B + 1, hi);
+  if constexpr (B + 1 < D / 32) value_frags<D, B + 1>(w, sc, frag);
+}
+
+template <typename T, int D, int R>
+__global__ __launch_bounds__(64 * kWaves) void kv4_attend_kernel(AttendArgs a) {
+  constexpr int NS = std::is_same<T, float>::value ? 3 : 1;  // bf16 terms of a query and of a probability
+  constexpr int KW = D / 32, NT = D / 16;
+  constexpr int kRows = 16 * R, kPad = 4;
+  __shared__ float s_o[kWaves][16][D + kPad];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+
+  const int heads = a.n_seq * a.Hkv;
+  const int bh = static_cast<int>(blockIdx.x) % heads, rt = static_cast<int>(blockIdx.x) / heads;
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const Seq seq = sequence(a, b);
+  const int nrows = seq.nq * a.G, row0 = rt * kRows;
+  if (row0 >= nrows) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = lane & 15, g = lane >> 4;
+  const int last = min(row0 + kRows, nrows) - 1;
+
+  // queries: the B operand of K Q^T; step j covers elements g*D/4 + 8j ..
+  u32x4 qf[R][NS][KW];
+  int limit[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = min(row0 + r * 16 + c, last);  // rows past the last repeat it and are not stored
+    limit[r] = seq.limit(a, row);
+    const int tok = row / a.G, hq = h * a.G + row - tok * a.G;
+    const T* qp = reinterpret_cast<const T*>(a.q) + static_cast<int64_t>(seq.q0 + tok) * a.q_stride + hq * D + g * (D / 4);
+#pragma unroll
+    for (int j = 0; j < KW; ++j) {
+      if constexpr (NS == 1) {
+        qf[r][0][j] = *reinterpret_cast<const u32x4*>(qp + 8 * j);
+      } else {
+        float f[8];
+        load8(qp + 8 * j, f);
+        u32x4 parts[NS];
+        split8<NS>(f, parts);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) qf[r][s][j] = parts[s];
+      }
+    }
+  }
+
+  const int lim_min = seq.limit(a, row0), lim_max = seq.limit(a, last);
+  const int tiles = (lim_max + kTile - 1) / kTile;
+  const int32_t* pages = a.pages + static_cast<int64_t>(b) * a.pages_stride;
+  const uint8_t* head = a.cache.base + static_cast<uint64_t>(h) * a.cache.head_bytes;
+
+  f32x4 o[R][NT];
+  float m[R], l[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) o[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  for (int tile = wave; tile < tiles; tile += kWaves) {
+    const int t0 = tile * kTile;
+    Tile<D> t;
+    load_tile<D>(a, head, page_ids(a, pages, t0, c, g), t0, c, g, t);
+    const bool masked = t0 + kTile > lim_min;
+
+    // scores: lane holds tokens 8g + 4i + e of its row c
+    f32x4 s[R][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) s[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const float sc = scale_of(t.ks[i]);
+#pragma unroll
+      for (int j = 0; j < KW; ++j) {
+        const u32x4 kf = cvt8(t.k[i][j], sc);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int n = 0; n < NS; ++n) s[r][i] = mfma(kf, qf[r][NS - 1 - n][j], s[r][i]);
+      }
+    }
+
+    u32x4 pf[R][NS];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (t0 + 8 * g + 4 * i + e >= limit[r]) s[r][i][e] = -INFINITY;
+      }
+      float top = s[r][0][0];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[r][i][e]);
+      top *= a.scale_log2;
+      // The running maximum moves only when a score passes it by 2^8: the
+      // probabilities stay below 2^8, far from fp32's range, and most steps
+      // neither reduce across lanes nor rescale.
+      if (__any(top > m[r] + 8.f)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = top > m[r] + 8.f ? top : m[r];  // a row's bits do not depend on the rows beside it
+        const float alpha = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[r] - now);
+        m[r] = now;
+        l[r] *= alpha;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[r][n] *= alpha;
+      }
+      const float ref = m[r] == -INFINITY ? 0.f : m[r];  // nothing seen yet: every power is 0
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[4 * i + e] = __builtin_amdgcn_exp2f(fmaf(s[r][i][e], a.scale_log2, -ref));
+          l[r] += p[4 * i + e];
+        }
+      split8<NS>(p, pf[r]);
+    }
+
+    float sc[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sc[j] = scale_of((t.vs[0] >> (8 * j)) & 255u);
+      sc[4 + j] = scale_of((t.vs[1] >> (8 * j)) & 255u);
+    }
+    bool special = false;  // a value that is not finite in a tile with masked places
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) special |= __float_as_uint(sc[j]) > (static_cast<uint32_t>(kMaxByte) << 23);
+    }
+    if (!__any(special)) {
+      value_frags<D>(t.v, sc, [&](int n, u32x4 vf) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int k = 0; k < NS; ++k) o[r][n] = mfma(vf, pf[r][NS - 1 - k], o[r][n]);
+      });
+    } else {
+      // zero times such a value is NaN: token by token, into the rows that see it
+      for (int j = 0; j < kTile; ++j) {
+        uint32_t w[8];
+        float sj[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const bool mine = 8 * g + k == j;
+          w[k] = mine ? t.v[k] : 0u;
+          sj[k] = mine ? sc[k] : 1.f;
+        }
+        value_frags<D>(w, sj, [&](int n, u32x4 vf) {
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            f32x4 y = o[r][n];
+#pragma unroll
+            for (int k = 0; k < NS; ++k) y = mfma(vf, pf[r][NS - 1 - k], y);
+            if (t0 + j < limit[r]) o[r][n] = y;
+          }
+        });
+      }
+    }
+  }
+
+  // the waves' parts join: weights 2^(m_w - max m)
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    l[r] += __shfl_xor(l[r], 16);
+    l[r] += __shfl_xor(l[r], 32);
+    if (r > 0) __syncthreads();
+    if (g == 0) {
+      s_m[wave][c] = m[r];
+      s_l[wave][c] = l[r];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)  // A row 4g + e is elements (4g + e) * NT + n
+#pragma unroll
+      for (int n = 0; n < NT; n += 4)
+        *reinterpret_cast<f32x4*>(&s_o[wave][c][(4 * g + e) * NT + n]) =
+            f32x4{o[r][n][e], o[r][n + 1][e], o[r][n + 2][e], o[r][n + 3][e]};
+    __syncthreads();
+    constexpr int kPer = D / 16;  // elements per thread: 16 threads per row
+    const int rr = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * kPer;
+    const int row = row0 + r * 16 + rr;
+    if (row >= nrows) continue;
+    float top = s_m[0][rr];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][rr]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, y[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) y[k] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(s_m[w][rr] - ref);
+      sum += f * s_l[w][rr];
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) y[k] += f * s_o[w][rr][e0 + k];
+    }
+    const bool empty = seq.limit(a, row) <= 0;
+    const float inv = 1.f / sum;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) y[k] = empty ? 0.f : (seq.overlong ? NAN : y[k] * inv);
+    const int tok = row / a.G, hq = h * a.G + row - tok * a.G;
+    T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(seq.q0 + tok) * a.out_stride + hq * D + e0;
+    if constexpr (kPer == 8) {
+      store8(op, y);
+    } else if constexpr (NS == 3) {
+      *reinterpret_cast<f32x4*>(op) = f32x4{y[0], y[1], y[2], y[3]};
+    } else {
+      *reinterpret_cast<u32x2*>(op) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    }
+  }
+}
+
+// ------------------------------------------------------------------ host side
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+spp_status bad(const char* why) { return spp::set_error(SPP_EINVAL, why); }
+
+const char* desc_why(const spp_attn_desc* d) {
+  if (!d) return "desc is NULL";
+  if (d->n_kv_heads < 1 || d->n_heads < 1 || d->n_heads > 1024 || d->n_heads % d->n_kv_heads != 0)
+    return "n_heads must be a multiple of n_kv_heads, both at least 1 and n_heads at most 1024";
+  if (d->head_dim != 64 && d->head_dim != 128) return "head_dim must be 64 or 128";
+  if (d->page != 16 && d->page != 32 && d->page != 64 && d->page != 128 && d->page != 256)
+    return "page must be 16, 32, 64, 128 or 256";
+  if (d->n_pages < 1) return "n_pages must be at least 1";
+  return nullptr;
+}
+
+Cache cache_of(const spp_attn_desc* d, const void* base) {
+  Cache c;
+  c.base = static_cast<const uint8_t*>(base);
+  c.head_bytes = static_cast<uint32_t>(d->page * (d->head_dim + d->head_dim / 16));
+  c.page_bytes = static_cast<uint64_t>(c.head_bytes) * static_cast<uint64_t>(d->n_kv_heads);
+  c.page = d->page;
+  c.shift = __builtin_ctz(static_cast<unsigned>(d->page));
+  c.n_pages = d->n_pages;
+  return c;
+}
+
+constexpr int64_t kMaxUnits = int64_t{1} << 30;  // so that 32-bit indices of threads and units hold
+
+// Rows [T][heads][d] at a stride of `stride` elements
+const char* rows_why(const void* p, int64_t stride, int heads, int d, int elem) {
+  if (stride < static_cast<int64_t>(heads) * d) return "a row stride is smaller than its row";
+  if (stride > kMaxUnits) return "a row stride is larger than 2^30 elements";
+  if (!aligned16(p) || stride * elem % 16 != 0) return "rows must be 16-byte aligned, their stride a multiple of 16 bytes";
+  return nullptr;
+}
+
+// Bytes from the first row's start to the last one's end
+uint64_t extent(int64_t stride, int64_t T, int heads, int d, int elem) {
+  return static_cast<uint64_t>((T - 1) * stride + static_cast<int64_t>(heads) * d) * static_cast<uint64_t>(elem);
+}
+
+bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+const char* dtype_why(int32_t dtype) {
+  return dtype == SPP_DTYPE_F32 || dtype == SPP_DTYPE_BF16 ? nullptr : "dtype must be 0 (f32) or 1 (bf16)";
+}
+
+spp_status launched() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SPP_OK : spp::set_error(SPP_EHIP, hipGetErrorString(e));
+}
+
+#define SPP_BAD(expr)                   \
+  do {                                  \
+    if (const char* w_ = (expr)) return bad(w_); \
+  } while (0)
+
+template <typename T>
+void launch_store(const StoreArgs& a, int d, unsigned grid, hipStream_t st) {
+  if (d == 128)
+    hipLaunchKernelGGL((kv4_store_kernel<T, 128>), dim3(grid), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((kv4_store_kernel<T, 64>), dim3(grid), dim3(256), 0, st, a);
+}
+
+template <typename T>
+void launch_load(const LoadArgs& a, int d, unsigned grid, hipStream_t st) {
+  if (d == 128)
+    hipLaunchKernelGGL((kv4_load_kernel<T, 128>), dim3(grid), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((kv4_load_kernel<T, 64>), dim3(grid), dim3(256), 0, st, a);
+}
+
+template <typename T>
+void launch_attend(const AttendArgs& a, int d, unsigned grid, hipStream_t st) {
+  if (d == 128)
+    hipLaunchKernelGGL((kv4_attend_kernel<T, 128, 1>), dim3(grid), dim3(64 * kWaves), 0, st, a);
+  else
+    hipLaunchKernelGGL((kv4_attend_kernel<T, 64, 1>), dim3(grid), dim3(64 * kWaves), 0, st, a);
+}
+
+}  // namespace
+
+extern "C" size_t spp_kv4_cache_bytes(const spp_attn_desc* desc) {
+  if (const char* w = desc_why(desc)) return bad(w), 0;
+  return static_cast<size_t>(cache_of(desc, nullptr).page_bytes) * static_cast<size_t>(desc->n_pages);
+}
+
+extern "C" spp_status spp_rotary_table(const int32_t* pos, int64_t pos_stride, int32_t n_axes, const int32_t* axis_of,
+                                       const float* inv_freq, int32_t n_freq, int32_t T, float* table,
+                                       void* hip_stream) {
+  if (n_axes < 1 || n_axes > 4) return bad("n_axes must be in [1, 4]");
+  if (n_freq < 8 || n_freq > kMaxFreq || n_freq % 8 != 0) return bad("n_freq must be a multiple of 8 in [8, 64]");
+  if (T < 0 || static_cast<int64_t>(T) * n_freq > kMaxUnits) return bad("T must be >= 0, T * n_freq at most 2^30");
+  TableArgs a{};
+  for (int i = 0; axis_of && i < n_freq; ++i) {
+    if (axis_of[i] < 0 || axis_of[i] >= n_axes) return bad("axis_of names an axis outside [0, n_axes)");
+    a.axes[i / 16] |= static_cast<uint32_t>(axis_of[i]) << (2 * (i % 16));
+  }
+  if (T == 0) return SPP_OK;
+  if (!pos || !inv_freq || !table) return bad("pos, inv_freq and table must not be NULL");
+  if ((n_axes > 1 && pos_stride < T) || pos_stride > int64_t{1} << 40) return bad("pos_stride must be at least T");
+  if (!aligned16(table)) return bad("table must be 16-byte aligned");
+  a.pos = pos;
+  a.pos_stride = pos_stride;
+  a.inv_freq = inv_freq;
+  a.table = table;
+  a.F = n_freq;
+  a.T = T;
+  const int64_t threads = static_cast<int64_t>(T) * (n_freq / kTableFreqs);
+  hipLaunchKernelGGL(rotary_table_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0,
+                     static_cast<hipStream_t>(hip_stream), a);
+  return launched();
+}
+
+extern "C" spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int32_t dtype, const void* q,
+                                    int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k,
+                                    int64_t k_stride, const void* v, int64_t v_stride, const float* table,
+                                    int32_t n_freq, const int64_t* slots, int32_t T, void* hip_stream) {
+  SPP_BAD(desc_why(desc));
+  SPP_BAD(dtype_why(dtype));
+  const int d = desc->head_dim, elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
+  if (n_freq < 0 || n_freq % 8 != 0 || 2 * n_freq > d) return bad("n_freq must be a multiple of 8, at most head_dim / 2");
+  if ((table != nullptr) != (n_freq > 0) && T > 0) return bad("table must be given iff n_freq > 0");
+  if ((q != nullptr) != (q_out != nullptr)) return bad("q and q_out must be given together");
+  const int Hq = q ? desc->n_heads : 0;
+  if (T < 0 || static_cast<int64_t>(T) * (desc->n_heads + 2 * desc->n_kv_heads) > kMaxUnits)
+    return bad("T must be >= 0, T * (n_heads + 2 n_kv_heads) at most 2^30");
+  if (T == 0) return SPP_OK;
+  if (!cache || !k || !v || !slots) return bad("cache, k, v and slots must not be NULL");
+  if (!aligned16(cache)) return bad("cache must be 16-byte aligned");
+  if (table && !aligned16(table)) return bad("table must be 16-byte aligned");
+  SPP_BAD(rows_why(k, k_stride, desc->n_kv_heads, d, elem));
+  SPP_BAD(rows_why(v, v_stride, desc->n_kv_heads, d, elem));
+  if (q) {
+    SPP_BAD(rows_why(q, q_stride, desc->n_heads, d, elem));
+    SPP_BAD(rows_why(q_out, q_out_stride, desc->n_heads, d, elem));
+    const bool same = q == q_out && q_stride == q_out_stride;
+    const uint64_t out_bytes = extent(q_out_stride, T, desc->n_heads, d, elem);
+    if (!same && overlap(q, extent(q_stride, T, desc->n_heads, d, elem), q_out, out_bytes))
+      return bad("q_out must be q with the same stride, or not overlap it");
+  }
+  StoreArgs a{};
+  a.cache = cache_of(desc, cache);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.q_stride = q_stride;
+  a.q_out_stride = q_out_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.table = table;
+  a.slots = slots;
+  a.Hq = Hq;
+  a.Hkv = desc->n_kv_heads;
+  a.F = n_freq;
+  a.T = T;
+  const int per = 256 / (d / 8);
+  const int64_t units = static_cast<int64_t>(T) * (Hq + 2 * desc->n_kv_heads);
+  const unsigned grid = static_cast<unsigned>((units + per - 1) / per);
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (dtype == SPP_DTYPE_BF16)
+    launch_store<__bf16>(a, d, grid, st);
+  else
+    launch_store<float>(a, d, grid, st);
+  return launched();
+}
+
+extern "C" spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dtype, const int64_t* slots,
+                                   int32_t T, void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
+                                   void* hip_stream) {
+  SPP_BAD(desc_why(desc));
+  SPP_BAD(dtype_why(dtype));
+  const int d = desc->head_dim, elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
+  if (T < 0 || static_cast<int64_t>(T) * 2 * desc->n_kv_heads > kMaxUnits)
+    return bad("T must be >= 0, T * 2 n_kv_heads at most 2^30");
+  if (T == 0 || (!k_out && !v_out)) return SPP_OK;
+  if (!cache || !slots) return bad("cache and slots must not be NULL");
+  if (!aligned16(cache)) return bad("cache must be 16-byte aligned");
+  if (k_out) SPP_BAD(rows_why(k_out, k_stride, desc->n_kv_heads, d, elem));
+  if (v_out) SPP_BAD(rows_why(v_out, v_stride, desc->n_kv_heads, d, elem));
+  LoadArgs a{};
+  a.cache = cache_of(desc, cache);
+  a.slots = slots;
+  a.k = k_out;
+  a.v = v_out;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.Hkv = desc->n_kv_heads;
+  a.T = T;
+  const int per = 256 / (d / 8);
+  const int64_t units = static_cast<int64_t>(T) * desc->n_kv_heads * (k_out && v_out ? 2 : 1);
+  const unsigned grid = static_cast<unsigned>((units + per - 1) / per);
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (dtype == SPP_DTYPE_BF16)
+    launch_load<__bf16>(a, d, grid, st);
+  else
+    launch_load<float>(a, d, grid, st);
+  return launched();
+}
+
+namespace {
+
+const char* attend_why(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, int32_t max_kv) {
+  if (const char* w = desc_why(desc)) return w;
+  if (n_seq < 0 || max_q < 1 || max_kv < 0) return "n_seq and max_kv must be >= 0, max_q >= 1";
+  if (static_cast<int64_t>(n_seq) * max_q * desc->n_heads > kMaxUnits) return "n_seq * max_q * n_heads must be at most 2^30";
+  return nullptr;
+}
+
+}  // namespace
+
+extern "C" size_t spp_kv4_attend_workspace(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, int32_t max_kv) {
+  if (const char* w = attend_why(desc, n_seq, max_q, max_kv)) return bad(w), 0;
+  return 16;
+}
+
+extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cache, int32_t dtype, const void* q,
+                                     int64_t q_stride, const int32_t* q_start, const int32_t* kv_len,
+                                     const int32_t* pages, int64_t pages_stride, int32_t n_seq, int32_t n_tokens,
+                                     int32_t max_q, int32_t max_kv, int32_t causal, float scale, void* out,
+                                     int64_t out_stride, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  SPP_BAD(attend_why(desc, n_seq, max_q, max_kv));
+  SPP_BAD(dtype_why(dtype));
+  const int d = desc->head_dim, elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
+  if (causal != 0 && causal != 1) return bad("causal must be 0 or 1");
+  if (!(scale > 0.f) || !std::isfinite(scale)) return bad("scale must be finite and positive");
+  if (n_tokens < 0 || static_cast<int64_t>(n_tokens) * desc->n_heads > kMaxUnits)
+    return bad("n_tokens must be >= 0, n_tokens * n_heads at most 2^30");
+  if (!q_start && n_tokens != n_seq) return bad("without q_start every sequence has one query token: n_tokens must be n_seq");
+  if (n_seq == 0 || n_tokens == 0) return SPP_OK;
+  if (!cache || !q || !kv_len || !pages || !out) return bad("cache, q, kv_len, pages and out must not be NULL");
+  if (!aligned16(cache)) return bad("cache must be 16-byte aligned");
+  if (pages_stride < 1 || pages_stride > INT32_MAX || pages_stride * desc->page > INT32_MAX - 1024)
+    return bad("pages_stride must be at least 1, pages_stride * page below 2^31 - 1024");
+  SPP_BAD(rows_why(q, q_stride, desc->n_heads, d, elem));
+  SPP_BAD(rows_why(out, out_stride, desc->n_heads, d, elem));
+  const bool same = q == out && q_stride == out_stride;
+  if (!same && overlap(q, extent(q_stride, n_tokens, desc->n_heads, d, elem), out,
+                       extent(out_stride, n_tokens, desc->n_heads, d, elem)))
+    return bad("out must be q with the same stride, or not overlap it");
+  if (!workspace || !aligned16(workspace)) return bad("workspace must not be NULL, and 16-byte aligned");
+  if (workspace_bytes < spp_kv4_attend_workspace(desc, n_seq, max_q, max_kv)) return bad("the workspace is too small");
+  AttendArgs a{};
+  a.cache = cache_of(desc, cache);
+  a.q = q;
+  a.out = out;
+  a.q_stride = q_stride;
+  a.out_stride = out_stride;
+  a.q_start = q_start;
+  a.kv_len = kv_len;
+  a.pages = pages;
+  a.pages_stride = pages_stride;
+  a.n_seq = n_seq;
+  a.n_tokens = n_tokens;
+  a.Hkv = desc->n_kv_heads;
+  a.G = desc->n_heads / desc->n_kv_heads;
+  a.causal = causal;
+  a.scale_log2 = scale * 1.44269504088896340736f;
+  const int64_t rows = static_cast<int64_t>(max_q) * a.G;
+  const int64_t grid = (rows + 15) / 16 * n_seq * a.Hkv;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  (void)workspace;
+  if (dtype == SPP_DTYPE_BF16)
+    launch_attend<__bf16>(a, d, static_cast<unsigned>(grid), st);
+  else
+    launch_attend<float>(a, d, static_cast<unsigned>(grid), st);
+  return launched();
+}

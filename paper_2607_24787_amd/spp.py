@@ -35,6 +35,10 @@ class ModelDesc(ctypes.Structure):
                                        "has_proj")] + [("rms_eps", c_float), ("expert_codec", c_int32)]
 
 
+class AttnDesc(ctypes.Structure):
+    _fields_ = [(f, c_int32) for f in ("n_heads", "n_kv_heads", "head_dim", "page", "n_pages")]
+
+
 class LayerStats(ctypes.Structure):
     _fields_ = ([(f, c_int32) for f in ("hits", "misses", "prefetched", "prefetch_used", "ready_on_time",
                                         "token_hits", "waited")]
@@ -84,6 +88,17 @@ _SIGS = {
     "spp_last_error": (c_char_p, []),
     "adapter_predict_static": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int32,
                                          c_void_p, c_void_p]),
+    "spp_kv4_cache_bytes": (c_size_t, [POINTER(AttnDesc)]),
+    "spp_rotary_table": (c_int32, [c_void_p, c_int64, c_int32, POINTER(c_int32), c_void_p, c_int32, c_int32, c_void_p,
+                                   c_void_p]),
+    "spp_kv4_store": (c_int32, [POINTER(AttnDesc), c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                c_int64, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int32, c_void_p]),
+    "spp_kv4_load": (c_int32, [POINTER(AttnDesc), c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_int64, c_void_p,
+                               c_int64, c_void_p]),
+    "spp_kv4_attend_workspace": (c_size_t, [POINTER(AttnDesc), c_int32, c_int32, c_int32]),
+    "spp_kv4_attend": (c_int32, [POINTER(AttnDesc), c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_void_p,
+                                 c_int64, c_int32, c_int32, c_int32, c_int32, c_int32, c_float, c_void_p, c_int64,
+                                 c_void_p, c_size_t, c_void_p]),
     "spp_get_slot_table": (c_int32, [c_void_p, c_int32, POINTER(c_int32), POINTER(c_int64)]),
     "spp_set_slot_table": (c_int32, [c_void_p, c_int32, POINTER(c_int32), POINTER(c_int64)]),
     "spp_get_clock": (c_int32, [c_void_p, POINTER(c_int64)]),
@@ -291,6 +306,78 @@ def spp_decode_step(ctx, L: int, h_in_dev: int, h_out_dev: int, h_scratch_dev: i
                                  B, M_max, topk.ctypes.data_as(POINTER(c_int32)),
                                  gates.ctypes.data_as(POINTER(c_float)), st))
     return topk, gates, list(st)
+
+
+# ---------------------------------------- attention over a 4-bit key/value cache
+
+def make_attn_desc(n_heads, n_kv_heads, head_dim, page, n_pages) -> AttnDesc:
+    return AttnDesc(n_heads, n_kv_heads, head_dim, page, n_pages)
+
+
+def spp_kv4_cache_bytes(desc: AttnDesc) -> int:
+    n = int(lib().spp_kv4_cache_bytes(byref(desc)))
+    if n == 0:
+        raise SppError(SPP_EINVAL, spp_last_error())
+    return n
+
+
+def spp_rotary_table(pos_dev: int, pos_stride: int, n_axes: int, axis_of, inv_freq_dev: int, T: int, table_dev: int,
+                     stream: int = 0):
+    """cos and sin of the T tokens' angles into table_dev (fp32 [T, 2, len(axis_of)]); axis_of: the axis of each
+    frequency (host ints)."""
+    a, p = _i32(axis_of)
+    _check(lib().spp_rotary_table(pos_dev or None, pos_stride, n_axes, p, inv_freq_dev or None, a.size, T,
+                                  table_dev or None, stream or None))
+
+
+def rotary_axes(sections, interleaved: bool):
+    """axis_of for `sections` frequencies per axis: in runs (all of axis 0, then axis 1, ...), or interleaved (frequency i
+    turns with axis i mod n while that axis has frequencies left, else with axis 0)."""
+    sections = np.asarray(sections, dtype=np.int32)
+    n = sections.size
+    if n < 1 or sections.min() < 0:
+        raise ValueError("sections: a count of frequencies for each axis")
+    if not interleaved:
+        return np.repeat(np.arange(n, dtype=np.int32), sections)
+    i = np.arange(int(sections.sum()), dtype=np.int32)
+    axis = np.where(i // n < sections[i % n], i % n, 0).astype(np.int32)
+    if not np.array_equal(np.bincount(axis, minlength=n), sections):
+        raise ValueError("these sections do not interleave: an axis other than the first has too many")
+    return axis
+
+
+def spp_kv4_store(desc: AttnDesc, cache_dev: int, dtype: int, q_dev: int, q_stride: int, q_out_dev: int,
+                  q_out_stride: int, k_dev: int, k_stride: int, v_dev: int, v_stride: int, table_dev: int, n_freq: int,
+                  slots_dev: int, T: int, stream: int = 0):
+    """Rotate T tokens' queries (into q_out) and keys, quantise keys and values into the cache at their slots."""
+    _check(lib().spp_kv4_store(byref(desc), cache_dev or None, dtype, q_dev or None, q_stride, q_out_dev or None,
+                               q_out_stride, k_dev or None, k_stride, v_dev or None, v_stride, table_dev or None, n_freq,
+                               slots_dev or None, T, stream or None))
+
+
+def spp_kv4_load(desc: AttnDesc, cache_dev: int, dtype: int, slots_dev: int, T: int, k_out_dev: int, k_stride: int,
+                 v_out_dev: int, v_stride: int, stream: int = 0):
+    """The keys and values at T slots, in dtype; either output may be 0."""
+    _check(lib().spp_kv4_load(byref(desc), cache_dev or None, dtype, slots_dev or None, T, k_out_dev or None, k_stride,
+                              v_out_dev or None, v_stride, stream or None))
+
+
+def spp_kv4_attend_workspace(desc: AttnDesc, n_seq: int, max_q: int, max_kv: int) -> int:
+    n = int(lib().spp_kv4_attend_workspace(byref(desc), n_seq, max_q, max_kv))
+    if n == 0:
+        raise SppError(SPP_EINVAL, spp_last_error())
+    return n
+
+
+def spp_kv4_attend(desc: AttnDesc, cache_dev: int, dtype: int, q_dev: int, q_stride: int, q_start_dev: int,
+                   kv_len_dev: int, pages_dev: int, pages_stride: int, n_seq: int, n_tokens: int, max_q: int,
+                   max_kv: int, causal: bool, scale: float, out_dev: int, out_stride: int, workspace_dev: int,
+                   workspace_bytes: int, stream: int = 0):
+    """Attention of n_seq sequences' n_tokens queries over their cached tokens, into out_dev."""
+    _check(lib().spp_kv4_attend(byref(desc), cache_dev or None, dtype, q_dev or None, q_stride, q_start_dev or None,
+                                kv_len_dev or None, pages_dev or None, pages_stride, n_seq, n_tokens, max_q, max_kv,
+                                int(causal), scale, out_dev or None, out_stride, workspace_dev or None, workspace_bytes,
+                                stream or None))
 
 
 def spp_last_error() -> str:
