@@ -355,7 +355,8 @@ spp_status adapter_predict_static(const void* adapter_a, const void* adapter_b, 
  * A byte of codes holds elements 2j (low nibble) and 2j+1.  A code is a sign
  * bit (8) and the magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (codes 0..7); an
  * element is its code's value times 2^(s - 127), s the scale byte of its
- * block of 32 elements.  s = 255 makes the block NaN.  4.25 bits an element.
+ * block of 32 elements.  s = 255 makes the block NaN;
+ * 253 and 254 do not occur.  4.25 bits an element.
  * The format is the one gfx950 converts to bf16 in hardware, exactly.
  * A slot names a token's place in the cache: p * page + offset. */
 typedef struct {

@@ -3,6 +3,7 @@
 // The cache's format and the calls' contracts are in spp.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -276,6 +277,9 @@ struct AttendArgs {
   int64_t pages_stride;
   int n_seq, n_tokens, Hkv, G;  // G: query heads per key/value head
   int causal;
+  int row_tiles, nsplit, min_tiles;  // row tiles of the grid; parts a row tile's tokens are split into, each of
+                                     // at least min_tiles tiles
+  float* part;                       // [row_tiles][nsplit][n_seq * Hkv] partial rows, if nsplit > 1
   float scale_log2;  // scale * log2(e): the softmax runs on powers of two
 };
 
@@ -307,6 +311,26 @@ __device__ __forceinline__ Seq sequence(const AttendArgs& a, int b) {
   s.overlong = s.len > room;
   if (s.overlong) s.len = static_cast<int>(room);
   return s;
+}
+
+// The part of its tiles that a split takes.  Goes by the device's lengths, so
+// that the splits of a sequence share its tiles whatever the caller's hint was.
+struct Parts {
+  int each, count;
+};
+
+__device__ __forceinline__ Parts parts_of(const AttendArgs& a, int tiles) {
+  Parts p;
+  p.each = max((tiles + a.nsplit - 1) / a.nsplit, a.min_tiles);
+  p.count = max((tiles + p.each - 1) / p.each, 1);
+  return p;
+}
+
+// Partial rows of one (row tile, split, sequence and head): [rows][D] sums, then
+// [rows][2] their maximum and sum of probabilities.
+template <int D>
+__device__ __forceinline__ float* part_of(const AttendArgs& a, int rows, int rt, int split, int bh) {
+  return a.part + (static_cast<size_t>(rt * a.nsplit + split) * (a.n_seq * a.Hkv) + bh) * rows * (D + 2);
 }
 
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
@@ -413,11 +437,38 @@ __device__ __forceinline__ void value_frags(const uint32_t* w, const float* sc, 
   }
   frag(2 * B, lo);
   frag(2 * B + 1, hi);
+  __builtin_amdgcn_sched_barrier(0);  // the next elements are not converted ahead: registers
   if constexpr (B + 1 < D / 32) value_frags<D, B + 1>(w, sc, frag);
 }
 
+template <typename T>
+__device__ __forceinline__ T* out_row(const AttendArgs& a, const Seq& seq, int h, int row, int d) {
+  const int tok = row / a.G, hq = h * a.G + row - tok * a.G;
+  return reinterpret_cast<T*>(a.out) + static_cast<int64_t>(seq.q0 + tok) * a.out_stride + hq * d;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_n(T* p, const float* y) {
+  if constexpr (N == 8) {
+    store8(p, y);
+  } else if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = y[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) reinterpret_cast<uint32_t*>(p)[i / 2] = pack_bf16(y[i], y[i + 1]);
+  }
+}
+
+// Waves per SIMD that the registers of a variant leave without spilling.
 template <typename T, int D, int R>
-__global__ __launch_bounds__(64 * kWaves) void kv4_attend_kernel(AttendArgs a) {
+constexpr int waves_for() {
+  const int w = R == 1 ? 4 : (R == 2 ? 2 : 1);
+  return std::is_same<T, float>::value && D == 128 && w > 1 ? w / 2 : w;
+}
+
+template <typename T, int D, int R>
+__global__ __launch_bounds__(64 * kWaves, (waves_for<T, D, R>())) void kv4_attend_kernel(AttendArgs a) {
   constexpr int NS = std::is_same<T, float>::value ? 3 : 1;  // bf16 terms of a query and of a probability
   constexpr int KW = D / 32, NT = D / 16;
   constexpr int kRows = 16 * R, kPad = 4;
@@ -425,14 +476,29 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_attend_kernel(AttendArgs a) {
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
 
   const int heads = a.n_seq * a.Hkv;
-  const int bh = static_cast<int>(blockIdx.x) % heads, rt = static_cast<int>(blockIdx.x) / heads;
+  const int bh = static_cast<int>(blockIdx.x) % heads, rest = static_cast<int>(blockIdx.x) / heads;
+  const int split = rest % a.nsplit, rt = a.row_tiles - 1 - rest / a.nsplit;  // the rows that see most first
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;
   const Seq seq = sequence(a, b);
   const int nrows = seq.nq * a.G, row0 = rt * kRows;
   if (row0 >= nrows) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int last = min(row0 + kRows, nrows) - 1;
+  const int lim_min = seq.limit(a, row0), lim_max = seq.limit(a, last);
+  const int tiles = (lim_max + kTile - 1) / kTile;
+  const Parts parts = parts_of(a, tiles);
+  if (split >= parts.count) return;
+  const int begin = split * parts.each, end = min(tiles, begin + parts.each);
+
+  const int32_t* pages = a.pages + static_cast<int64_t>(b) * a.pages_stride;
+  const uint8_t* head = a.cache.base + static_cast<uint64_t>(h) * a.cache.head_bytes;
+  // two steps ahead the page ids, one step ahead the codes and scales
+  int tile = begin + wave;
+  Pids pid = page_ids(a, pages, tile * kTile, c, g);
+  Tile<D> next;
+  if (tile < end) load_tile<D>(a, head, pid, tile * kTile, c, g, next);
+  pid = page_ids(a, pages, (tile + kWaves) * kTile, c, g);
 
   // queries: the B operand of K Q^T; step j covers elements g*D/4 + 8j ..
   u32x4 qf[R][NS][KW];
@@ -450,34 +516,34 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_attend_kernel(AttendArgs a) {
       } else {
         float f[8];
         load8(qp + 8 * j, f);
-        u32x4 parts[NS];
-        split8<NS>(f, parts);
+        u32x4 terms[NS];
+        split8<NS>(f, terms);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) qf[r][s][j] = parts[s];
+        for (int s = 0; s < NS; ++s) qf[r][s][j] = terms[s];
       }
     }
   }
 
-  const int lim_min = seq.limit(a, row0), lim_max = seq.limit(a, last);
-  const int tiles = (lim_max + kTile - 1) / kTile;
-  const int32_t* pages = a.pages + static_cast<int64_t>(b) * a.pages_stride;
-  const uint8_t* head = a.cache.base + static_cast<uint64_t>(h) * a.cache.head_bytes;
-
-  f32x4 o[R][NT];
-  float m[R], l[R];
+  const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+  f32x4 o[R][NT], l[R];  // l: every element the sum of its row's probabilities, as rounded for the product
+  float m[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = -INFINITY;
-    l[r] = 0.f;
+    l[r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < NT; ++n) o[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  for (int tile = wave; tile < tiles; tile += kWaves) {
+  for (; tile < end; tile += kWaves) {
     const int t0 = tile * kTile;
-    Tile<D> t;
-    load_tile<D>(a, head, page_ids(a, pages, t0, c, g), t0, c, g, t);
+    Tile<D> t = next;
+    if (tile + kWaves < end) {
+      load_tile<D>(a, head, pid, t0 + kWaves * kTile, c, g, next);
+      pid = page_ids(a, pages, t0 + 2 * kWaves * kTile, c, g);
+    }
     const bool masked = t0 + kTile > lim_min;
+    __builtin_amdgcn_sched_barrier(0);
 
     // scores: lane holds tokens 8g + 4i + e of its row c
     f32x4 s[R][2];
@@ -495,99 +561,106 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_attend_kernel(AttendArgs a) {
           for (int n = 0; n < NS; ++n) s[r][i] = mfma(kf, qf[r][NS - 1 - n][j], s[r][i]);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
 
-    u32x4 pf[R][NS];
+    if (masked) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (masked) {
+      for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (t0 + 8 * g + 4 * i + e >= limit[r]) s[r][i][e] = -INFINITY;
-      }
-      float top = s[r][0][0];
+    }
+    float top[R];
+    bool moves = false;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+    for (int r = 0; r < R; ++r) {
+      top[r] = s[r][0][0];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[r][i][e]);
-      top *= a.scale_log2;
-      // The running maximum moves only when a score passes it by 2^8: the
-      // probabilities stay below 2^8, far from fp32's range, and most steps
-      // neither reduce across lanes nor rescale.
-      if (__any(top > m[r] + 8.f)) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float now = top > m[r] + 8.f ? top : m[r];  // a row's bits do not depend on the rows beside it
+      for (int k = 1; k < 8; ++k) top[r] = fmaxf(top[r], s[r][k / 4][k % 4]);
+      top[r] *= a.scale_log2;
+      moves |= top[r] > m[r] + 8.f;
+    }
+    // The running maximum moves only when a score passes it by 2^8: the
+    // probabilities stay below 2^8, far from fp32's range, and most steps
+    // neither reduce across lanes nor rescale.
+    if (__any(moves)) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        top[r] = fmaxf(top[r], __shfl_xor(top[r], 16));
+        top[r] = fmaxf(top[r], __shfl_xor(top[r], 32));
+        const float now = top[r] > m[r] + 8.f ? top[r] : m[r];  // a row's bits do not depend on the rows beside it
         const float alpha = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[r] - now);
         m[r] = now;
         l[r] *= alpha;
 #pragma unroll
         for (int n = 0; n < NT; ++n) o[r][n] *= alpha;
       }
+    }
+    u32x4 pf[R][NS];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
       const float ref = m[r] == -INFINITY ? 0.f : m[r];  // nothing seen yet: every power is 0
       float p[8];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[4 * i + e] = __builtin_amdgcn_exp2f(fmaf(s[r][i][e], a.scale_log2, -ref));
-          l[r] += p[4 * i + e];
-        }
+      for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(fmaf(s[r][k / 4][k % 4], a.scale_log2, -ref));
       split8<NS>(p, pf[r]);
+#pragma unroll
+      for (int k = 0; k < NS; ++k) l[r] = mfma(ones, pf[r][NS - 1 - k], l[r]);
     }
 
     float sc[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      sc[j] = scale_of((t.vs[0] >> (8 * j)) & 255u);
-      sc[4 + j] = scale_of((t.vs[1] >> (8 * j)) & 255u);
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t w = t.vs[j / 4];
+      sc[j] = __uint_as_float(j % 4 == 3 ? w >> 1 : w << (23 - 8 * (j % 4)));  // only the exponent field counts
     }
-    bool special = false;  // a value that is not finite in a tile with masked places
     if (masked) {
+      // Zero times a value that is not finite is NaN, so none goes into the
+      // product of a tile with masked places: what no row sees may hold
+      // anything, and where some rows see a NaN block they get their NaN here.
+      int poisoned = INT32_MAX;  // the first such token of this lane's block
 #pragma unroll
-      for (int j = 0; j < 8; ++j) special |= __float_as_uint(sc[j]) > (static_cast<uint32_t>(kMaxByte) << 23);
-    }
-    if (!__any(special)) {
-      value_frags<D>(t.v, sc, [&](int n, u32x4 vf) {
+      for (int j = 7; j >= 0; --j) {
+        const int token = t0 + 8 * g + j;
+        const bool special = ((t.vs[j / 4] >> (8 * (j % 4))) & 255u) > kMaxByte;
+        if (special && token < lim_max) poisoned = token;
+        if (special || token >= lim_max) {
+          t.v[j] = 0u;
+          sc[j] = 1.f;
+        }
+      }
+      if (__any(poisoned != INT32_MAX)) {
+        // this lane's sums are of block g (D = 128) or g / 2
+        const int from = D == 128 ? 4 * g : 8 * (g >> 1);
+        int first = INT32_MAX;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) first = min(first, __shfl(poisoned, 16 * k + from));
 #pragma unroll
         for (int r = 0; r < R; ++r)
+          if (first < limit[r]) {
 #pragma unroll
-          for (int k = 0; k < NS; ++k) o[r][n] = mfma(vf, pf[r][NS - 1 - k], o[r][n]);
-      });
-    } else {
-      // zero times such a value is NaN: token by token, into the rows that see it
-      for (int j = 0; j < kTile; ++j) {
-        uint32_t w[8];
-        float sj[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const bool mine = 8 * g + k == j;
-          w[k] = mine ? t.v[k] : 0u;
-          sj[k] = mine ? sc[k] : 1.f;
-        }
-        value_frags<D>(w, sj, [&](int n, u32x4 vf) {
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            f32x4 y = o[r][n];
-#pragma unroll
-            for (int k = 0; k < NS; ++k) y = mfma(vf, pf[r][NS - 1 - k], y);
-            if (t0 + j < limit[r]) o[r][n] = y;
+            for (int n = 0; n < NT; ++n) o[r][n] = f32x4{NAN, NAN, NAN, NAN};
           }
-        });
       }
     }
+    value_frags<D>(t.v, sc, [&](int n, u32x4 vf) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int k = 0; k < NS; ++k) o[r][n] = mfma(vf, pf[r][NS - 1 - k], o[r][n]);
+    });
   }
 
   // the waves' parts join: weights 2^(m_w - max m)
+  float* part = parts.count > 1 ? part_of<D>(a, kRows, rt, split, bh) : nullptr;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    l[r] += __shfl_xor(l[r], 16);
-    l[r] += __shfl_xor(l[r], 32);
     if (r > 0) __syncthreads();
     if (g == 0) {
       s_m[wave][c] = m[r];
-      s_l[wave][c] = l[r];
+      s_l[wave][c] = l[r][0];
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)  // A row 4g + e is elements (4g + e) * NT + n
@@ -614,20 +687,75 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_attend_kernel(AttendArgs a) {
 #pragma unroll
       for (int k = 0; k < kPer; ++k) y[k] += f * s_o[w][rr][e0 + k];
     }
+    if (part) {
+      const int at = r * 16 + rr;
+#pragma unroll
+      for (int k = 0; k < kPer; k += 4)
+        *reinterpret_cast<f32x4*>(part + at * D + e0 + k) = f32x4{y[k], y[k + 1], y[k + 2], y[k + 3]};
+      if (e0 == 0) *reinterpret_cast<float2*>(part + kRows * D + 2 * at) = make_float2(top, sum);
+      continue;
+    }
     const bool empty = seq.limit(a, row) <= 0;
     const float inv = 1.f / sum;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) y[k] = empty ? 0.f : (seq.overlong ? NAN : y[k] * inv);
-    const int tok = row / a.G, hq = h * a.G + row - tok * a.G;
-    T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(seq.q0 + tok) * a.out_stride + hq * D + e0;
-    if constexpr (kPer == 8) {
-      store8(op, y);
-    } else if constexpr (NS == 3) {
-      *reinterpret_cast<f32x4*>(op) = f32x4{y[0], y[1], y[2], y[3]};
-    } else {
-      *reinterpret_cast<u32x2*>(op) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
-    }
+    store_n<T, kPer>(out_row<T>(a, seq, h, row, D) + e0, y);
   }
+}
+
+// Joins the parts of one row: one workgroup per (row, sequence and head), its
+// waves over the parts, in a fixed order.
+template <typename T, int D, int R>
+__global__ __launch_bounds__(64 * kWaves) void kv4_join_kernel(AttendArgs a) {
+  constexpr int kRows = 16 * R, kPer = D / 64;
+  __shared__ float s_y[kWaves][D], s_sum[kWaves];
+  const int heads = a.n_seq * a.Hkv;
+  const int bh = static_cast<int>(blockIdx.x) % heads, row = static_cast<int>(blockIdx.x) / heads;
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const Seq seq = sequence(a, b);
+  const int nrows = seq.nq * a.G;
+  if (row >= nrows) return;
+  const int rt = row / kRows, at = row - rt * kRows;
+  const int last = min((rt + 1) * kRows, nrows) - 1;
+  const Parts parts = parts_of(a, (seq.limit(a, last) + kTile - 1) / kTile);
+  if (parts.count == 1) return;  // written whole
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const size_t stride = static_cast<size_t>(heads) * kRows * (D + 2);  // from a split to the next
+  const float* part = part_of<D>(a, kRows, rt, 0, bh);
+  const float* ml = part + kRows * D + 2 * at;
+  float top = -INFINITY;
+  for (int s = lane; s < parts.count; s += 64) top = fmaxf(top, ml[s * stride]);
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, y[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) y[k] = 0.f;
+#pragma unroll 4
+  for (int s = wave; s < parts.count; s += kWaves) {
+    const float2 p = *reinterpret_cast<const float2*>(ml + s * stride);
+    const float f = __builtin_amdgcn_exp2f(p.x - ref);
+    sum += f * p.y;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) y[k] += f * part[s * stride + at * D + lane * kPer + k];
+  }
+  if (lane == 0) s_sum[wave] = sum;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) s_y[wave][lane * kPer + k] = y[k];
+  __syncthreads();
+  if (wave != 0) return;
+  sum = s_sum[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    sum += s_sum[w];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) y[k] += s_y[w][lane * kPer + k];
+  }
+  const float inv = 1.f / sum;
+  const bool empty = seq.limit(a, row) <= 0;
+  T* out = out_row<T>(a, seq, h, row, D) + lane * kPer;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) out[k] = static_cast<T>(empty ? 0.f : (seq.overlong ? NAN : y[k] * inv));
 }
 
 // ------------------------------------------------------------------ host side
@@ -708,12 +836,52 @@ void launch_load(const LoadArgs& a, int d, unsigned grid, hipStream_t st) {
     hipLaunchKernelGGL((kv4_load_kernel<T, 64>), dim3(grid), dim3(256), 0, st, a);
 }
 
+// How a call's work is cut: rows per workgroup, row tiles, and parts of a row
+// tile's tokens.  Goes by the caller's bounds alone, so that the workspace can
+// be sized without a device.
+struct Cut {
+  int R, row_tiles, nsplit;
+  int64_t items;  // row tiles of every sequence and head
+};
+
+constexpr int kMinTiles = 8;       // two steps a wave
+constexpr int kWantGroups = 1024;  // workgroups that fill 256 compute units
+
+Cut cut_of(const spp_attn_desc* d, bool f32, int32_t n_seq, int32_t max_q, int32_t max_kv) {
+  Cut c;
+  const int64_t rows = static_cast<int64_t>(max_q) * (d->n_heads / d->n_kv_heads);
+  c.R = rows <= 16 ? 1 : (rows <= 32 || (f32 && d->head_dim == 128) ? 2 : 4);
+  c.row_tiles = static_cast<int>((rows + 16 * c.R - 1) / (16 * c.R));
+  c.items = static_cast<int64_t>(n_seq) * d->n_kv_heads * c.row_tiles;
+  const int64_t tiles = (static_cast<int64_t>(max_kv) + kTile - 1) / kTile;
+  const int64_t want = (kWantGroups + c.items - 1) / (c.items > 0 ? c.items : 1);
+  const int64_t most = (tiles + kMinTiles - 1) / kMinTiles;
+  c.nsplit = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
+  return c;
+}
+
+size_t part_bytes(const Cut& c, int d) {
+  return c.nsplit > 1 ? static_cast<size_t>(c.items) * c.nsplit * (16 * c.R) * (d + 2) * sizeof(float) : 0;
+}
+
+template <typename T, int D, int R>
+void launch_attend_r(const AttendArgs& a, int64_t rows, hipStream_t st) {
+  const unsigned heads = static_cast<unsigned>(a.n_seq * a.Hkv);
+  hipLaunchKernelGGL((kv4_attend_kernel<T, D, R>), dim3(heads * a.row_tiles * a.nsplit), dim3(64 * kWaves), 0, st, a);
+  if (a.nsplit > 1)
+    hipLaunchKernelGGL((kv4_join_kernel<T, D, R>), dim3(heads * static_cast<unsigned>(rows)), dim3(64 * kWaves), 0, st, a);
+}
+
 template <typename T>
-void launch_attend(const AttendArgs& a, int d, unsigned grid, hipStream_t st) {
-  if (d == 128)
-    hipLaunchKernelGGL((kv4_attend_kernel<T, 128, 1>), dim3(grid), dim3(64 * kWaves), 0, st, a);
-  else
-    hipLaunchKernelGGL((kv4_attend_kernel<T, 64, 1>), dim3(grid), dim3(64 * kWaves), 0, st, a);
+void launch_attend(const AttendArgs& a, int d, int R, int64_t rows, hipStream_t st) {
+  if (d == 128) {
+    if (R == 4) {
+      if constexpr (!std::is_same<T, float>::value) launch_attend_r<T, 128, 4>(a, rows, st);
+    } else {
+      R == 1 ? launch_attend_r<T, 128, 1>(a, rows, st) : launch_attend_r<T, 128, 2>(a, rows, st);
+    }
+  } else
+    R == 1 ? launch_attend_r<T, 64, 1>(a, rows, st) : R == 2 ? launch_attend_r<T, 64, 2>(a, rows, st) : launch_attend_r<T, 64, 4>(a, rows, st);
 }
 
 }  // namespace
@@ -850,7 +1018,9 @@ const char* attend_why(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, 
 
 extern "C" size_t spp_kv4_attend_workspace(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, int32_t max_kv) {
   if (const char* w = attend_why(desc, n_seq, max_q, max_kv)) return bad(w), 0;
-  return 16;
+  const size_t a = part_bytes(cut_of(desc, false, n_seq, max_q, max_kv), desc->head_dim);
+  const size_t b = part_bytes(cut_of(desc, true, n_seq, max_q, max_kv), desc->head_dim);
+  return std::max<size_t>(16, std::max(a, b));
 }
 
 extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cache, int32_t dtype, const void* q,
@@ -895,13 +1065,16 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
   a.G = desc->n_heads / desc->n_kv_heads;
   a.causal = causal;
   a.scale_log2 = scale * 1.44269504088896340736f;
+  const Cut cut = cut_of(desc, dtype == SPP_DTYPE_F32, n_seq, max_q, max_kv);
+  a.row_tiles = cut.row_tiles;
+  a.nsplit = cut.nsplit;
+  a.min_tiles = kMinTiles;
+  a.part = static_cast<float*>(workspace);
   const int64_t rows = static_cast<int64_t>(max_q) * a.G;
-  const int64_t grid = (rows + 15) / 16 * n_seq * a.Hkv;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  (void)workspace;
   if (dtype == SPP_DTYPE_BF16)
-    launch_attend<__bf16>(a, d, static_cast<unsigned>(grid), st);
+    launch_attend<__bf16>(a, d, cut.R, rows, st);
   else
-    launch_attend<float>(a, d, static_cast<unsigned>(grid), st);
+    launch_attend<float>(a, d, cut.R, rows, st);
   return launched();
 }
