@@ -435,9 +435,11 @@ spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dt
  * Scores and softmax statistics are fp32; bf16 queries are exact operands,
  * probabilities are rounded to bf16 for the value product (their sum is not);
  * fp32 queries and probabilities go in as three bf16 terms each.
- * workspace: dev, spp_kv4_attend_workspace bytes (16-byte aligned, any
- * contents), held by the call until the stream has passed it: calls (and
- * captured graphs) that may run at the same time need one each. */
+ * workspace: dev, spp_kv4_attend_workspace bytes for these sizes (16-byte
+ * aligned), all zero before its first call; each call leaves it fit for the
+ * next one of any sizes that it is large enough for.  A call holds it until the
+ * stream has passed it: calls (and captured graphs) that may run at the same
+ * time need one each. */
 size_t spp_kv4_attend_workspace(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, int32_t max_kv);
 spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cache, int32_t dtype, const void* q, int64_t q_stride,
                           const int32_t* q_start, const int32_t* kv_len, const int32_t* pages, int64_t pages_stride,

@@ -277,9 +277,13 @@ struct AttendArgs {
   int64_t pages_stride;
   int n_seq, n_tokens, Hkv, G;  // G: query heads per key/value head
   int causal;
-  int row_tiles, nsplit, min_tiles;  // row tiles of the grid; parts a row tile's tokens are split into, each of
-                                     // at least min_tiles tiles
-  float* part;                       // [row_tiles][nsplit][n_seq * Hkv] partial rows, if nsplit > 1
+  int planes, row_tiles;  // a plane: one key/value head and row tile (Hkv * row_tiles of them)
+  int units;              // about the parts that a plane's cached tokens are cut into; 0: a part is a whole sequence
+  int min_tiles;          // tiles of the smallest part
+  int sum_shift;          // see place_of
+  int join_apart;         // parts are joined by a launch of their own
+  unsigned* count;        // [planes][n_seq] finished parts; zero between calls
+  float* part;            // [planes][units + n_seq] partial rows
   float scale_log2;  // scale * log2(e): the softmax runs on powers of two
 };
 
@@ -313,24 +317,70 @@ __device__ __forceinline__ Seq sequence(const AttendArgs& a, int b) {
   return s;
 }
 
-// The part of its tiles that a split takes.  Goes by the device's lengths, so
-// that the splits of a sequence share its tiles whatever the caller's hint was.
-struct Parts {
-  int each, count;
-};
-
-__device__ __forceinline__ Parts parts_of(const AttendArgs& a, int tiles) {
-  Parts p;
-  p.each = max((tiles + a.nsplit - 1) / a.nsplit, a.min_tiles);
-  p.count = max((tiles + p.each - 1) / p.each, 1);
-  return p;
+__device__ __forceinline__ int tiles_of(const AttendArgs& a, int i) {
+  if (i >= a.n_seq) return 0;
+  const int64_t len = min(static_cast<int64_t>(max(a.kv_len[i], 0)), a.pages_stride * a.cache.page);
+  return static_cast<int>((len + kTile - 1) / kTile);
 }
 
-// Partial rows of one (row tile, split, sequence and head): [rows][D] sums, then
-// [rows][2] their maximum and sum of probabilities.
-template <int D>
-__device__ __forceinline__ float* part_of(const AttendArgs& a, int rows, int rt, int split, int bh) {
-  return a.part + (static_cast<size_t>(rt * a.nsplit + split) * (a.n_seq * a.Hkv) + bh) * rows * (D + 2);
+// Inclusive sums over the wave's lanes (all of them active)
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes below within 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 to the second 16, lane 47 to the last
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
+  return x;
+}
+
+// Part p of a plane: tiles [first, first + each) of sequence b, which is its
+// part p - base.
+struct Place {
+  int b, base, each;
+};
+
+// A plane's parts are equal pieces of all its sequences' tiles, at most
+// units + n_seq of them (one at least for each sequence), so that a batch of
+// very different lengths keeps every workgroup about as long.  Every wave
+// finds its part by itself, from the lengths on the device: a scan over 64
+// sequences at a time.  b >= 0: the place of that sequence's first part instead.
+__device__ __forceinline__ Place place_of(const AttendArgs& a, int p, int b, int lane) {
+  const int mine = tiles_of(a, lane);
+  const uint32_t up = (1u << a.sum_shift) - 1u;  // sums in units of 2^sum_shift tiles fit 31 bits
+  uint32_t total = (static_cast<uint32_t>(mine) + up) >> a.sum_shift;
+  for (int i = 64 + lane; i - lane < a.n_seq; i += 64) total += (static_cast<uint32_t>(tiles_of(a, i)) + up) >> a.sum_shift;
+  total = __builtin_amdgcn_readlane(wave_scan(static_cast<int>(total)), 63);
+  uint32_t each = ((total + static_cast<uint32_t>(a.units) - 1) / static_cast<uint32_t>(a.units)) << a.sum_shift;
+  each = (max(each, static_cast<uint32_t>(a.min_tiles)) + kWaves - 1) / kWaves * kWaves;  // whole steps of a workgroup
+  Place at;
+  at.b = -1;
+  at.base = 0;
+  at.each = static_cast<int>(min(each, 1u << 30));
+  for (int i0 = 0; i0 < a.n_seq; i0 += 64) {
+    const int t = i0 == 0 ? mine : tiles_of(a, i0 + lane);
+    const int n = i0 + lane < a.n_seq ? max(1, static_cast<int>((static_cast<uint32_t>(t) + at.each - 1) / static_cast<uint32_t>(at.each))) : 0;
+    const int sum = wave_scan(n);
+    const uint64_t past = __ballot(b < 0 ? at.base + sum > p : i0 + lane == b);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      at.b = i0 + l;
+      at.base += __builtin_amdgcn_readlane(sum - n, l);
+      return at;
+    }
+    at.base += __builtin_amdgcn_readlane(sum, 63);
+  }
+  return at;
+}
+
+// Two floats (8-byte aligned) written and read at agent scope
+__device__ __forceinline__ void put2(float* p, float x, float y) {
+  const uint64_t v = static_cast<uint64_t>(__float_as_uint(y)) << 32 | __float_as_uint(x);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get2(const float* p) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float(static_cast<uint32_t>(v)), __uint_as_float(static_cast<uint32_t>(v >> 32)));
 }
 
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
@@ -448,48 +498,79 @@ __device__ __forceinline__ T* out_row(const AttendArgs& a, const Seq& seq, int h
 }
 
 template <typename T, int N>
+__device__ __forceinline__ void store_n(T* p, const float* y);
+
+// N elements of a finished row: its sums over the sum of its probabilities
+template <typename T, int N>
+__device__ __forceinline__ void finish(const AttendArgs& a, const Seq& seq, int h, int row, int d, int e0, float sum,
+                                       const float* y) {
+  const bool empty = seq.limit(a, row) <= 0;
+  const float inv = 1.f / sum;
+  float v[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = empty ? 0.f : (seq.overlong ? NAN : y[k] * inv);
+  store_n<T, N>(out_row<T>(a, seq, h, row, d) + e0, v);
+}
+
+template <typename T, int N>
 __device__ __forceinline__ void store_n(T* p, const float* y) {
   if constexpr (N == 8) {
     store8(p, y);
-  } else if constexpr (std::is_same<T, float>::value) {
+  } else if constexpr (N == 1 || std::is_same<T, float>::value) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) p[i] = y[i];
+    for (int i = 0; i < N; ++i) p[i] = static_cast<T>(y[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < N; i += 2) reinterpret_cast<uint32_t*>(p)[i / 2] = pack_bf16(y[i], y[i + 1]);
   }
 }
 
-// Waves per SIMD that the registers of a variant leave without spilling.
-template <typename T, int D, int R>
-constexpr int waves_for() {
+// Workgroups per compute unit (waves per SIMD) that the registers of a variant
+// leave without spilling.
+constexpr int resident(bool f32, int d, int R) {
   const int w = R == 1 ? 4 : (R == 2 ? 2 : 1);
-  return std::is_same<T, float>::value && D == 128 && w > 1 ? w / 2 : w;
+  return f32 && d == 128 && w > 1 ? w / 2 : w;
 }
 
 template <typename T, int D, int R>
-__global__ __launch_bounds__(64 * kWaves, (waves_for<T, D, R>())) void kv4_attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value, D, R)) void kv4_attend_kernel(AttendArgs a) {
+  constexpr int W = kWaves;
   constexpr int NS = std::is_same<T, float>::value ? 3 : 1;  // bf16 terms of a query and of a probability
   constexpr int KW = D / 32, NT = D / 16;
   constexpr int kRows = 16 * R, kPad = 4;
-  __shared__ float s_o[kWaves][16][D + kPad];
-  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  __shared__ float s_o[W][16][D + kPad];
+  __shared__ float s_m[W][16], s_l[W][16];
+  __shared__ unsigned s_done;
 
-  const int heads = a.n_seq * a.Hkv;
-  const int bh = static_cast<int>(blockIdx.x) % heads, rest = static_cast<int>(blockIdx.x) / heads;
-  const int split = rest % a.nsplit, rt = a.row_tiles - 1 - rest / a.nsplit;  // the rows that see most first
-  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  int b, h, rt, p = 0, split = 0, each = 1 << 30;
+  if (a.units > 0) {
+    const int plane = static_cast<int>(blockIdx.x) % a.planes;
+    p = static_cast<int>(blockIdx.x) / a.planes;
+    h = plane % a.Hkv, rt = plane / a.Hkv;
+    const Place at = place_of(a, p, -1, lane);
+    if (at.b < 0) return;
+    b = at.b, split = p - at.base, each = at.each;
+  } else {
+    // the row tiles of one sequence and head are a multiple of 8 workgroups
+    // apart, which brings them to one XCD and the cached rows into its L2; the
+    // rows that see most go first
+    const int heads = a.n_seq * a.Hkv, step = a.row_tiles > 1 ? (heads + 7) / 8 * 8 : heads;
+    const int bh = static_cast<int>(blockIdx.x) % step;
+    if (bh >= heads) return;
+    rt = a.row_tiles - 1 - static_cast<int>(blockIdx.x) / step;
+    b = bh / a.Hkv, h = bh - b * a.Hkv;
+  }
   const Seq seq = sequence(a, b);
   const int nrows = seq.nq * a.G, row0 = rt * kRows;
   if (row0 >= nrows) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 15, g = lane >> 4;
   const int last = min(row0 + kRows, nrows) - 1;
   const int lim_min = seq.limit(a, row0), lim_max = seq.limit(a, last);
   const int tiles = (lim_max + kTile - 1) / kTile;
-  const Parts parts = parts_of(a, tiles);
-  if (split >= parts.count) return;
-  const int begin = split * parts.each, end = min(tiles, begin + parts.each);
+  const int parts = max(1, static_cast<int>((static_cast<uint32_t>(tiles) + each - 1) / static_cast<uint32_t>(each)));
+  if (split >= parts) return;
+  const int begin = split * each, end = min(tiles, begin + each);
 
   const int32_t* pages = a.pages + static_cast<int64_t>(b) * a.pages_stride;
   const uint8_t* head = a.cache.base + static_cast<uint64_t>(h) * a.cache.head_bytes;
@@ -498,7 +579,7 @@ __global__ __launch_bounds__(64 * kWaves, (waves_for<T, D, R>())) void kv4_atten
   Pids pid = page_ids(a, pages, tile * kTile, c, g);
   Tile<D> next;
   if (tile < end) load_tile<D>(a, head, pid, tile * kTile, c, g, next);
-  pid = page_ids(a, pages, (tile + kWaves) * kTile, c, g);
+  pid = page_ids(a, pages, (tile + W) * kTile, c, g);
 
   // queries: the B operand of K Q^T; step j covers elements g*D/4 + 8j ..
   u32x4 qf[R][NS][KW];
@@ -535,12 +616,12 @@ __global__ __launch_bounds__(64 * kWaves, (waves_for<T, D, R>())) void kv4_atten
     for (int n = 0; n < NT; ++n) o[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  for (; tile < end; tile += kWaves) {
+  for (; tile < end; tile += W) {
     const int t0 = tile * kTile;
     Tile<D> t = next;
-    if (tile + kWaves < end) {
-      load_tile<D>(a, head, pid, t0 + kWaves * kTile, c, g, next);
-      pid = page_ids(a, pages, t0 + 2 * kWaves * kTile, c, g);
+    if (tile + W < end) {
+      load_tile<D>(a, head, pid, t0 + W * kTile, c, g, next);
+      pid = page_ids(a, pages, t0 + 2 * W * kTile, c, g);
     }
     const bool masked = t0 + kTile > lim_min;
     __builtin_amdgcn_sched_barrier(0);
@@ -653,8 +734,11 @@ __global__ __launch_bounds__(64 * kWaves, (waves_for<T, D, R>())) void kv4_atten
     });
   }
 
-  // the waves' parts join: weights 2^(m_w - max m)
-  float* part = parts.count > 1 ? part_of<D>(a, kRows, rt, split, bh) : nullptr;
+  // the waves' sums join: weights 2^(m_w - max m)
+  const size_t part_floats = static_cast<size_t>(kRows) * (D + 2);  // [rows][D] sums, then [rows] maximum, sum
+  float* plane_parts = a.part + static_cast<size_t>(rt * a.Hkv + h) * (a.units + a.n_seq) * part_floats;
+  float* part = plane_parts + static_cast<size_t>(p) * part_floats;
+  constexpr int kPer = 16 * D / (64 * W), kThr = D / kPer;  // elements per thread, threads per row
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (r > 0) __syncthreads();
@@ -669,93 +753,172 @@ __global__ __launch_bounds__(64 * kWaves, (waves_for<T, D, R>())) void kv4_atten
         *reinterpret_cast<f32x4*>(&s_o[wave][c][(4 * g + e) * NT + n]) =
             f32x4{o[r][n][e], o[r][n + 1][e], o[r][n + 2][e], o[r][n + 3][e]};
     __syncthreads();
-    constexpr int kPer = D / 16;  // elements per thread: 16 threads per row
-    const int rr = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * kPer;
+    const int rr = threadIdx.x / kThr, e0 = (threadIdx.x % kThr) * kPer;
     const int row = row0 + r * 16 + rr;
     if (row >= nrows) continue;
     float top = s_m[0][rr];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][rr]);
+    for (int w = 1; w < W; ++w) top = fmaxf(top, s_m[w][rr]);
     const float ref = top == -INFINITY ? 0.f : top;
     float sum = 0.f, y[kPer];
 #pragma unroll
     for (int k = 0; k < kPer; ++k) y[k] = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float f = __builtin_amdgcn_exp2f(s_m[w][rr] - ref);
       sum += f * s_l[w][rr];
 #pragma unroll
       for (int k = 0; k < kPer; ++k) y[k] += f * s_o[w][rr][e0 + k];
     }
-    if (part) {
+    if (parts > 1) {
       const int at = r * 16 + rr;
+      float* to = part + at * D + e0;
+      if (a.join_apart) {
 #pragma unroll
-      for (int k = 0; k < kPer; k += 4)
-        *reinterpret_cast<f32x4*>(part + at * D + e0 + k) = f32x4{y[k], y[k + 1], y[k + 2], y[k + 3]};
-      if (e0 == 0) *reinterpret_cast<float2*>(part + kRows * D + 2 * at) = make_float2(top, sum);
+        for (int k = 0; k < kPer; k += 4) *reinterpret_cast<f32x4*>(to + k) = f32x4{y[k], y[k + 1], y[k + 2], y[k + 3]};
+        if (e0 == 0) *reinterpret_cast<float2*>(part + kRows * D + 2 * at) = make_float2(top, sum);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kPer; k += 2) put2(to + k, y[k], y[k + 1]);
+        if (e0 == 0) put2(part + kRows * D + 2 * at, top, sum);
+      }
       continue;
     }
-    const bool empty = seq.limit(a, row) <= 0;
-    const float inv = 1.f / sum;
+    finish<T, kPer>(a, seq, h, row, D, e0, sum, y);
+  }
+  if (parts == 1 || a.join_apart) return;
+
+  // The workgroup that finishes a sequence's parts last joins them, in their
+  // order.  Parts pass between XCDs, whose L2 caches do not see each other:
+  // they are written and read at agent scope, past those caches, and counted
+  // only when every write has arrived.  (Fences in their place write back and
+  // drop whole caches: one token against 131,072 took 92 us instead of 20.)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    unsigned* count = a.count + static_cast<size_t>(rt * a.Hkv + h) * a.n_seq + b;
+    const unsigned before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (before + 1 >= static_cast<unsigned>(parts)) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s_done = before + 1;
+  }
+  __syncthreads();
+  const unsigned done = __builtin_amdgcn_readfirstlane(s_done);
+  if (done < static_cast<unsigned>(parts)) return;
+  const float* all = part - static_cast<size_t>(split) * part_floats;
+  constexpr int kCols = D / 4, kSlots = 64 * W / kCols;  // a slot of threads takes a row of a group of parts
+  const int slot = threadIdx.x / kCols, col = threadIdx.x % kCols, rows = last - row0 + 1;
+  const int groups = max(1, kSlots / rows);
+  float* s_y = &s_o[0][0][0];  // [kSlots][D], then sums in s_l
+  float* s_sum = &s_l[0][0];
+  static_assert(sizeof(s_o) >= sizeof(float) * kSlots * D && sizeof(s_l) >= sizeof(float) * kSlots, "join buffers");
+  for (int at = slot % (groups > 1 ? rows : kSlots), grp = groups > 1 ? slot / rows : 0; at < rows; at += kSlots) {
+    const float* ml = all + kRows * D + 2 * at;
+    float top = -INFINITY;
+    for (int k = col; k < parts; k += kCols) top = fmaxf(top, get2(ml + k * part_floats).x);
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) y[k] = empty ? 0.f : (seq.overlong ? NAN : y[k] * inv);
-    store_n<T, kPer>(out_row<T>(a, seq, h, row, D) + e0, y);
+    for (int k = 1; k < kCols; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (grp < groups) {
+#pragma unroll 8
+      for (int k = grp; k < parts; k += groups) {
+        const float2 v = get2(ml + k * part_floats);
+        const float* from = all + k * part_floats + at * D + 4 * col;
+        const float2 lo = get2(from), hi = get2(from + 2);
+        const float f = __builtin_amdgcn_exp2f(v.x - ref);
+        sum += f * v.y;
+        y += f * f32x4{lo.x, lo.y, hi.x, hi.y};
+      }
+    }
+    if (groups > 1) {
+      *reinterpret_cast<f32x4*>(s_y + slot * D + 4 * col) = y;
+      if (col == 0) s_sum[slot] = sum;
+      __syncthreads();
+      if (slot >= rows) return;
+      for (int k = 1; k < groups; ++k) {
+        sum += s_sum[slot + k * rows];
+        y += *reinterpret_cast<const f32x4*>(s_y + (slot + k * rows) * D + 4 * col);
+      }
+    }
+    const float v[4] = {y[0], y[1], y[2], y[3]};
+    // a count beyond the parts: the workspace was not zero, and nothing is known of the parts
+    finish<T, 4>(a, seq, h, row0 + at, D, 4 * col, done > static_cast<unsigned>(parts) ? NAN : sum, v);
   }
 }
 
-// Joins the parts of one row: one workgroup per (row, sequence and head), its
-// waves over the parts, in a fixed order.
+// Joins the parts of one row: one workgroup per (row, head and sequence).  A
+// wave takes every W-th part, its loads all in flight at once, since this
+// kernel is bound by their latency; then the waves' sums join.
+constexpr int kJoinWaves = 16, kJoinBatch = 16;
 template <typename T, int D, int R>
-__global__ __launch_bounds__(64 * kWaves) void kv4_join_kernel(AttendArgs a) {
-  constexpr int kRows = 16 * R, kPer = D / 64;
-  __shared__ float s_y[kWaves][D], s_sum[kWaves];
+__global__ __launch_bounds__(64 * kJoinWaves) void kv4_join_kernel(AttendArgs a) {
+  constexpr int kRows = 16 * R, kPer = D / 64, W = kJoinWaves;
+  __shared__ float s_y[W][D], s_sum[W], s_m[W];
   const int heads = a.n_seq * a.Hkv;
   const int bh = static_cast<int>(blockIdx.x) % heads, row = static_cast<int>(blockIdx.x) / heads;
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Place at = place_of(a, 0, b, lane);
   const Seq seq = sequence(a, b);
   const int nrows = seq.nq * a.G;
   if (row >= nrows) return;
-  const int rt = row / kRows, at = row - rt * kRows;
-  const int last = min((rt + 1) * kRows, nrows) - 1;
-  const Parts parts = parts_of(a, (seq.limit(a, last) + kTile - 1) / kTile);
-  if (parts.count == 1) return;  // written whole
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const size_t stride = static_cast<size_t>(heads) * kRows * (D + 2);  // from a split to the next
-  const float* part = part_of<D>(a, kRows, rt, 0, bh);
-  const float* ml = part + kRows * D + 2 * at;
-  float top = -INFINITY;
-  for (int s = lane; s < parts.count; s += 64) top = fmaxf(top, ml[s * stride]);
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, y[kPer];
+  const int rt = row / kRows, ri = row - rt * kRows;
+  const int tiles = (seq.limit(a, min((rt + 1) * kRows, nrows) - 1) + kTile - 1) / kTile;
+  const int parts = max(1, static_cast<int>((static_cast<uint32_t>(tiles) + at.each - 1) / static_cast<uint32_t>(at.each)));
+  if (parts == 1) return;  // written whole
+  constexpr size_t kStride = static_cast<size_t>(kRows) * (D + 2);
+  const float* part = a.part + (static_cast<size_t>(rt * a.Hkv + h) * (a.units + a.n_seq) + at.base) * kStride;
+  float top = -INFINITY, sum = 0.f, y[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) y[k] = 0.f;
-#pragma unroll 4
-  for (int s = wave; s < parts.count; s += kWaves) {
-    const float2 p = *reinterpret_cast<const float2*>(ml + s * stride);
-    const float f = __builtin_amdgcn_exp2f(p.x - ref);
-    sum += f * p.y;
+  for (int p0 = wave; p0 < parts; p0 += W * kJoinBatch) {
+    float2 ml[kJoinBatch];
+    float v[kJoinBatch][kPer];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) y[k] += f * part[s * stride + at * D + lane * kPer + k];
+    for (int i = 0; i < kJoinBatch; ++i) {
+      const float* from = part + min(p0 + W * i, parts - 1) * kStride;
+      ml[i] = *reinterpret_cast<const float2*>(from + kRows * D + 2 * ri);
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) v[i][k] = from[ri * D + lane * kPer + k];
+    }
+    float now = top;
+#pragma unroll
+    for (int i = 0; i < kJoinBatch; ++i)
+      if (p0 + W * i < parts) now = fmaxf(now, ml[i].x);
+    const float ref = now == -INFINITY ? 0.f : now, keep = __builtin_amdgcn_exp2f(top - ref);
+    sum *= keep;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) y[k] *= keep;
+    top = now;
+#pragma unroll
+    for (int i = 0; i < kJoinBatch; ++i) {
+      if (p0 + W * i >= parts) continue;
+      const float f = __builtin_amdgcn_exp2f(ml[i].x - ref);
+      sum += f * ml[i].y;
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) y[k] += f * v[i][k];
+    }
   }
-  if (lane == 0) s_sum[wave] = sum;
+  if (lane == 0) s_sum[wave] = sum, s_m[wave] = top;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) s_y[wave][lane * kPer + k] = y[k];
   __syncthreads();
   if (wave != 0) return;
-  sum = s_sum[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
-    sum += s_sum[w];
+  for (int w = 0; w < W; ++w) top = fmaxf(top, s_m[w]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) y[k] += s_y[w][lane * kPer + k];
+  for (int k = 0; k < kPer; ++k) y[k] = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const float f = __builtin_amdgcn_exp2f(s_m[w] - ref);
+    sum += f * s_sum[w];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) y[k] += f * s_y[w][lane * kPer + k];
   }
-  const float inv = 1.f / sum;
-  const bool empty = seq.limit(a, row) <= 0;
-  T* out = out_row<T>(a, seq, h, row, D) + lane * kPer;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) out[k] = static_cast<T>(empty ? 0.f : (seq.overlong ? NAN : y[k] * inv));
+  finish<T, kPer>(a, seq, h, row, D, lane * kPer, sum, y);
 }
 
 // ------------------------------------------------------------------ host side
@@ -836,52 +999,66 @@ void launch_load(const LoadArgs& a, int d, unsigned grid, hipStream_t st) {
     hipLaunchKernelGGL((kv4_load_kernel<T, 64>), dim3(grid), dim3(256), 0, st, a);
 }
 
-// How a call's work is cut: rows per workgroup, row tiles, and parts of a row
-// tile's tokens.  Goes by the caller's bounds alone, so that the workspace can
-// be sized without a device.
+// How a call's work is cut: rows per workgroup, row tiles, waves per workgroup,
+// and about how many parts a plane's cached tokens make.  Goes by the caller's
+// bounds alone, so that the workspace can be sized without a device.
 struct Cut {
-  int R, row_tiles, nsplit;
-  int64_t items;  // row tiles of every sequence and head
+  int R, row_tiles, planes, units;
+  bool join_apart;
 };
 
-constexpr int kMinTiles = 8;       // two steps a wave
-constexpr int kWantGroups = 1024;  // workgroups that fill 256 compute units
+constexpr int kCUs = 256;
+constexpr int kMinTiles = 2 * kWaves;
+constexpr int kFusedParts = 32;
+
+// The counters stand at the workspace's start and take the same room in every
+// call, so that no call's partial rows come to lie where another one counts.
+constexpr int kMaxItems = 4 * kCUs * 4;
+constexpr size_t kCountBytes = kMaxItems * sizeof(unsigned);
 
 Cut cut_of(const spp_attn_desc* d, bool f32, int32_t n_seq, int32_t max_q, int32_t max_kv) {
-  Cut c;
+  Cut c{};
   const int64_t rows = static_cast<int64_t>(max_q) * (d->n_heads / d->n_kv_heads);
   c.R = rows <= 16 ? 1 : (rows <= 32 || (f32 && d->head_dim == 128) ? 2 : 4);
   c.row_tiles = static_cast<int>((rows + 16 * c.R - 1) / (16 * c.R));
-  c.items = static_cast<int64_t>(n_seq) * d->n_kv_heads * c.row_tiles;
+  c.planes = d->n_kv_heads * c.row_tiles;
+  const int64_t items = static_cast<int64_t>(n_seq) * c.planes;
+  const int fit = resident(f32, d->head_dim, c.R);
   const int64_t tiles = (static_cast<int64_t>(max_kv) + kTile - 1) / kTile;
-  const int64_t want = (kWantGroups + c.items - 1) / (c.items > 0 ? c.items : 1);
-  const int64_t most = (tiles + kMinTiles - 1) / kMinTiles;
-  c.nsplit = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
+  if (items == 0 || tiles <= kMinTiles || items >= std::min((c.R == 4 ? 2 : 4) * kCUs * fit, kMaxItems)) return c;
+  c.units = static_cast<int>(std::max<int64_t>(1, kCUs * fit / c.planes - n_seq / 2));
+  c.join_apart = std::min<int64_t>(c.units / n_seq, tiles / kMinTiles) >= kFusedParts;
   return c;
 }
 
-size_t part_bytes(const Cut& c, int d) {
-  return c.nsplit > 1 ? static_cast<size_t>(c.items) * c.nsplit * (16 * c.R) * (d + 2) * sizeof(float) : 0;
+size_t part_bytes(const Cut& c, int32_t n_seq, int d) {
+  return c.units > 0 ? static_cast<size_t>(c.planes) * (c.units + n_seq) * (16 * c.R) * (d + 2) * sizeof(float) : 0;
 }
 
-template <typename T, int D, int R>
-void launch_attend_r(const AttendArgs& a, int64_t rows, hipStream_t st) {
-  const unsigned heads = static_cast<unsigned>(a.n_seq * a.Hkv);
-  hipLaunchKernelGGL((kv4_attend_kernel<T, D, R>), dim3(heads * a.row_tiles * a.nsplit), dim3(64 * kWaves), 0, st, a);
-  if (a.nsplit > 1)
-    hipLaunchKernelGGL((kv4_join_kernel<T, D, R>), dim3(heads * static_cast<unsigned>(rows)), dim3(64 * kWaves), 0, st, a);
+template <typename T, int D>
+void launch_attend_d(const AttendArgs& a, const Cut& c, int64_t rows, hipStream_t st) {
+  constexpr bool f32 = std::is_same<T, float>::value;
+  const int heads = a.n_seq * a.Hkv;
+  const dim3 grid(c.units > 0 ? static_cast<unsigned>(c.units + a.n_seq) * static_cast<unsigned>(c.planes)
+                              : static_cast<unsigned>(c.row_tiles > 1 ? (heads + 7) / 8 * 8 : heads) *
+                                    static_cast<unsigned>(c.row_tiles));
+  const dim3 join(static_cast<unsigned>(heads) * static_cast<unsigned>(rows));
+  const auto run = [&](auto r) {
+    constexpr int R = decltype(r)::value;
+    hipLaunchKernelGGL((kv4_attend_kernel<T, D, R>), grid, dim3(64 * kWaves), 0, st, a);
+    if (c.join_apart) hipLaunchKernelGGL((kv4_join_kernel<T, D, R>), join, dim3(64 * kJoinWaves), 0, st, a);
+  };
+  if (c.R == 1)
+    run(std::integral_constant<int, 1>());
+  else if (c.R == 2)
+    run(std::integral_constant<int, 2>());
+  else if constexpr (!(f32 && D == 128))
+    run(std::integral_constant<int, 4>());
 }
 
 template <typename T>
-void launch_attend(const AttendArgs& a, int d, int R, int64_t rows, hipStream_t st) {
-  if (d == 128) {
-    if (R == 4) {
-      if constexpr (!std::is_same<T, float>::value) launch_attend_r<T, 128, 4>(a, rows, st);
-    } else {
-      R == 1 ? launch_attend_r<T, 128, 1>(a, rows, st) : launch_attend_r<T, 128, 2>(a, rows, st);
-    }
-  } else
-    R == 1 ? launch_attend_r<T, 64, 1>(a, rows, st) : R == 2 ? launch_attend_r<T, 64, 2>(a, rows, st) : launch_attend_r<T, 64, 4>(a, rows, st);
+void launch_attend(const AttendArgs& a, int d, const Cut& c, int64_t rows, hipStream_t st) {
+  d == 128 ? launch_attend_d<T, 128>(a, c, rows, st) : launch_attend_d<T, 64>(a, c, rows, st);
 }
 
 }  // namespace
@@ -1018,9 +1195,12 @@ const char* attend_why(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, 
 
 extern "C" size_t spp_kv4_attend_workspace(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, int32_t max_kv) {
   if (const char* w = attend_why(desc, n_seq, max_q, max_kv)) return bad(w), 0;
-  const size_t a = part_bytes(cut_of(desc, false, n_seq, max_q, max_kv), desc->head_dim);
-  const size_t b = part_bytes(cut_of(desc, true, n_seq, max_q, max_kv), desc->head_dim);
-  return std::max<size_t>(16, std::max(a, b));
+  size_t most = 16;
+  for (bool f32 : {false, true}) {
+    const Cut c = cut_of(desc, f32, n_seq, max_q, max_kv);
+    if (c.units > 0) most = std::max(most, kCountBytes + part_bytes(c, n_seq, desc->head_dim));
+  }
+  return most;
 }
 
 extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cache, int32_t dtype, const void* q,
@@ -1066,15 +1246,18 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
   a.causal = causal;
   a.scale_log2 = scale * 1.44269504088896340736f;
   const Cut cut = cut_of(desc, dtype == SPP_DTYPE_F32, n_seq, max_q, max_kv);
+  a.planes = cut.planes;
   a.row_tiles = cut.row_tiles;
-  a.nsplit = cut.nsplit;
+  a.units = cut.units;
   a.min_tiles = kMinTiles;
-  a.part = static_cast<float*>(workspace);
-  const int64_t rows = static_cast<int64_t>(max_q) * a.G;
+  a.join_apart = cut.join_apart;
+  while (n_seq >> a.sum_shift > 16) ++a.sum_shift;  // a sequence has at most 2^26 tiles
+  a.count = static_cast<unsigned*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kCountBytes);
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (dtype == SPP_DTYPE_BF16)
-    launch_attend<__bf16>(a, d, cut.R, rows, st);
+    launch_attend<__bf16>(a, d, cut, static_cast<int64_t>(max_q) * a.G, st);
   else
-    launch_attend<float>(a, d, cut.R, rows, st);
+    launch_attend<float>(a, d, cut, static_cast<int64_t>(max_q) * a.G, st);
   return launched();
 }

@@ -89,7 +89,7 @@ _SIGS = {
     "adapter_predict_static": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int32,
                                          c_void_p, c_void_p]),
     "spp_kv4_cache_bytes": (c_size_t, [POINTER(AttnDesc)]),
-    "spp_rotary_table": (c_int32, [c_void_p, c_int64, c_int32, POINTER(c_int32), c_void_p, c_int32, c_int32, c_void_p,
+    "spp_rotary_table": (c_int32, [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_void_p,
                                    c_void_p]),
     "spp_kv4_store": (c_int32, [POINTER(AttnDesc), c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
                                 c_int64, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int32, c_void_p]),
@@ -325,9 +325,8 @@ def spp_rotary_table(pos_dev: int, pos_stride: int, n_axes: int, axis_of, inv_fr
                      stream: int = 0):
     """cos and sin of the T tokens' angles into table_dev (fp32 [T, 2, len(axis_of)]); axis_of: the axis of each
     frequency (host ints)."""
-    a, p = _i32(axis_of)
-    _check(lib().spp_rotary_table(pos_dev or None, pos_stride, n_axes, p, inv_freq_dev or None, a.size, T,
-                                  table_dev or None, stream or None))
+    a = np.ascontiguousarray(axis_of, dtype=np.int32)
+    _check(lib().spp_rotary_table(pos_dev, pos_stride, n_axes, a.ctypes.data, inv_freq_dev, a.size, T, table_dev, stream))
 
 
 def rotary_axes(sections, interleaved: bool):
@@ -350,16 +349,16 @@ def spp_kv4_store(desc: AttnDesc, cache_dev: int, dtype: int, q_dev: int, q_stri
                   q_out_stride: int, k_dev: int, k_stride: int, v_dev: int, v_stride: int, table_dev: int, n_freq: int,
                   slots_dev: int, T: int, stream: int = 0):
     """Rotate T tokens' queries (into q_out) and keys, quantise keys and values into the cache at their slots."""
-    _check(lib().spp_kv4_store(byref(desc), cache_dev or None, dtype, q_dev or None, q_stride, q_out_dev or None,
-                               q_out_stride, k_dev or None, k_stride, v_dev or None, v_stride, table_dev or None, n_freq,
-                               slots_dev or None, T, stream or None))
+    _check(lib().spp_kv4_store(byref(desc), cache_dev, dtype, q_dev, q_stride, q_out_dev,
+                               q_out_stride, k_dev, k_stride, v_dev, v_stride, table_dev, n_freq,
+                               slots_dev, T, stream))
 
 
 def spp_kv4_load(desc: AttnDesc, cache_dev: int, dtype: int, slots_dev: int, T: int, k_out_dev: int, k_stride: int,
                  v_out_dev: int, v_stride: int, stream: int = 0):
     """The keys and values at T slots, in dtype; either output may be 0."""
-    _check(lib().spp_kv4_load(byref(desc), cache_dev or None, dtype, slots_dev or None, T, k_out_dev or None, k_stride,
-                              v_out_dev or None, v_stride, stream or None))
+    _check(lib().spp_kv4_load(byref(desc), cache_dev, dtype, slots_dev, T, k_out_dev, k_stride,
+                              v_out_dev, v_stride, stream))
 
 
 def spp_kv4_attend_workspace(desc: AttnDesc, n_seq: int, max_q: int, max_kv: int) -> int:
@@ -374,10 +373,10 @@ def spp_kv4_attend(desc: AttnDesc, cache_dev: int, dtype: int, q_dev: int, q_str
                    max_kv: int, causal: bool, scale: float, out_dev: int, out_stride: int, workspace_dev: int,
                    workspace_bytes: int, stream: int = 0):
     """Attention of n_seq sequences' n_tokens queries over their cached tokens, into out_dev."""
-    _check(lib().spp_kv4_attend(byref(desc), cache_dev or None, dtype, q_dev or None, q_stride, q_start_dev or None,
-                                kv_len_dev or None, pages_dev or None, pages_stride, n_seq, n_tokens, max_q, max_kv,
-                                int(causal), scale, out_dev or None, out_stride, workspace_dev or None, workspace_bytes,
-                                stream or None))
+    _check(lib().spp_kv4_attend(byref(desc), cache_dev, dtype, q_dev, q_stride, q_start_dev,
+                                kv_len_dev, pages_dev, pages_stride, n_seq, n_tokens, max_q, max_kv,
+                                int(causal), scale, out_dev, out_stride, workspace_dev, workspace_bytes,
+                                stream))
 
 
 def spp_last_error() -> str:

@@ -97,7 +97,9 @@ class Setup:
         max_q = max(self.nq + [1]) if max_q is None else max_q
         max_kv = max(self.kv) if max_kv is None else max_kv
         size = spp.spp_kv4_attend_workspace(self.desc, len(self.kv), max_q, max_kv)
-        ws = torch.full((size + 64,), 255, dtype=torch.uint8, device="cuda") if ws is None else ws
+        if ws is None:
+            ws = torch.zeros(size + 64, dtype=torch.uint8, device="cuda")
+            ws[size:] = 255
         q = self.q if q is None else q
         out = torch.full_like(q, 7.0) if out is None else out
         row = self.H * self.d
@@ -108,7 +110,7 @@ class Setup:
                            out_stride or row, ws.data_ptr(), size, _stream())
         if wait:
             torch.cuda.synchronize()
-            assert int(ws[size:].min()) == 255    # nothing past the workspace
+            assert int(ws[-64:].min()) == 255    # nothing past the workspace
         return out
 
     def check(self, out, causal=True, kv_len=None, untouched=7.0):
