@@ -532,6 +532,43 @@ constexpr int resident(bool f32, int d, int R) {
   return f32 && d == 128 && w > 1 ? w / 2 : w;
 }
 
+// N elements of a row joined from parts, in their order: each part a maximum,
+// a sum of probabilities and N sums relative to that maximum.
+template <int N>
+struct Joined {
+  float top = -INFINITY, sum = 0.f, y[N] = {};
+
+  // Parts first, first + step, ... below count; read(k, (maximum, sum), sums)
+  // reads part k.  B of them are read before the first is used: the joins are
+  // bound by the latency of these reads.
+  template <int B, typename Fn>
+  __device__ __forceinline__ void take(int count, int first, int step, Fn read) {
+    for (int k0 = first; k0 < count; k0 += step * B) {
+      float2 ml[B];
+      float v[B][N];
+#pragma unroll
+      for (int i = 0; i < B; ++i) read(min(k0 + step * i, count - 1), ml[i], v[i]);
+      float now = top;
+#pragma unroll
+      for (int i = 0; i < B; ++i)
+        if (k0 + step * i < count) now = fmaxf(now, ml[i].x);
+      const float ref = now == -INFINITY ? 0.f : now, keep = __builtin_amdgcn_exp2f(top - ref);
+      top = now;
+      sum *= keep;
+#pragma unroll
+      for (int n = 0; n < N; ++n) y[n] *= keep;
+#pragma unroll
+      for (int i = 0; i < B; ++i) {
+        if (k0 + step * i >= count) continue;
+        const float f = __builtin_amdgcn_exp2f(ml[i].x - ref);
+        sum += f * ml[i].y;
+#pragma unroll
+        for (int n = 0; n < N; ++n) y[n] += f * v[i][n];
+      }
+    }
+  }
+};
+
 template <typename T, int D, int R>
 __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value, D, R)) void kv4_attend_kernel(AttendArgs a) {
   constexpr int W = kWaves;
@@ -808,42 +845,34 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
   constexpr int kCols = D / 4, kSlots = 64 * W / kCols;  // a slot of threads takes a row of a group of parts
   const int slot = threadIdx.x / kCols, col = threadIdx.x % kCols, rows = last - row0 + 1;
   const int groups = max(1, kSlots / rows);
-  float* s_y = &s_o[0][0][0];  // [kSlots][D], then sums in s_l
-  float* s_sum = &s_l[0][0];
+  float* s_y = &s_o[0][0][0];  // [kSlots][D]
+  float *s_sum = &s_l[0][0], *s_top = &s_m[0][0];
   static_assert(sizeof(s_o) >= sizeof(float) * kSlots * D && sizeof(s_l) >= sizeof(float) * kSlots, "join buffers");
-  for (int at = slot % (groups > 1 ? rows : kSlots), grp = groups > 1 ? slot / rows : 0; at < rows; at += kSlots) {
-    const float* ml = all + kRows * D + 2 * at;
-    float top = -INFINITY;
-    for (int k = col; k < parts; k += kCols) top = fmaxf(top, get2(ml + k * part_floats).x);
-#pragma unroll
-    for (int k = 1; k < kCols; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (grp < groups) {
-#pragma unroll 8
-      for (int k = grp; k < parts; k += groups) {
-        const float2 v = get2(ml + k * part_floats);
-        const float* from = all + k * part_floats + at * D + 4 * col;
-        const float2 lo = get2(from), hi = get2(from + 2);
-        const float f = __builtin_amdgcn_exp2f(v.x - ref);
-        sum += f * v.y;
-        y += f * f32x4{lo.x, lo.y, hi.x, hi.y};
-      }
-    }
+  for (int at = groups > 1 ? slot % rows : slot, grp = groups > 1 ? slot / rows : 0; at < rows; at += kSlots) {
+    Joined<4> j;
+    if (grp < groups)
+      j.template take<8>(parts, grp, groups, [&](int k, float2& ml, float* v) {
+        const float* from = all + k * part_floats;
+        ml = get2(from + kRows * D + 2 * at);
+        const float2 lo = get2(from + at * D + 4 * col), hi = get2(from + at * D + 4 * col + 2);
+        v[0] = lo.x, v[1] = lo.y, v[2] = hi.x, v[3] = hi.y;
+      });
     if (groups > 1) {
-      *reinterpret_cast<f32x4*>(s_y + slot * D + 4 * col) = y;
-      if (col == 0) s_sum[slot] = sum;
+      *reinterpret_cast<f32x4*>(s_y + slot * D + 4 * col) = f32x4{j.y[0], j.y[1], j.y[2], j.y[3]};
+      if (col == 0) s_sum[slot] = j.sum, s_top[slot] = j.top;
       __syncthreads();
       if (slot >= rows) return;
-      for (int k = 1; k < groups; ++k) {
-        sum += s_sum[slot + k * rows];
-        y += *reinterpret_cast<const f32x4*>(s_y + (slot + k * rows) * D + 4 * col);
-      }
+      Joined<4> whole;
+      whole.template take<1>(groups, 0, 1, [&](int k, float2& ml, float* v) {
+        const int from = slot + k * rows;
+        ml = make_float2(s_top[from], s_sum[from]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = s_y[from * D + 4 * col + i];
+      });
+      j = whole;
     }
-    const float v[4] = {y[0], y[1], y[2], y[3]};
     // a count beyond the parts: the workspace was not zero, and nothing is known of the parts
-    finish<T, 4>(a, seq, h, row0 + at, D, 4 * col, done > static_cast<unsigned>(parts) ? NAN : sum, v);
+    finish<T, 4>(a, seq, h, row0 + at, D, 4 * col, done > static_cast<unsigned>(parts) ? NAN : j.sum, j.y);
   }
 }
 
@@ -869,56 +898,25 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv4_join_kernel(AttendArgs a)
   if (parts == 1) return;  // written whole
   constexpr size_t kStride = static_cast<size_t>(kRows) * (D + 2);
   const float* part = a.part + (static_cast<size_t>(rt * a.Hkv + h) * (a.units + a.n_seq) + at.base) * kStride;
-  float top = -INFINITY, sum = 0.f, y[kPer];
+  Joined<kPer> j;
+  j.template take<kJoinBatch>(parts, wave, W, [&](int k, float2& ml, float* v) {
+    const float* from = part + k * kStride;
+    ml = *reinterpret_cast<const float2*>(from + kRows * D + 2 * ri);
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) y[k] = 0.f;
-  for (int p0 = wave; p0 < parts; p0 += W * kJoinBatch) {
-    float2 ml[kJoinBatch];
-    float v[kJoinBatch][kPer];
+    for (int i = 0; i < kPer; ++i) v[i] = from[ri * D + lane * kPer + i];
+  });
+  if (lane == 0) s_sum[wave] = j.sum, s_m[wave] = j.top;
 #pragma unroll
-    for (int i = 0; i < kJoinBatch; ++i) {
-      const float* from = part + min(p0 + W * i, parts - 1) * kStride;
-      ml[i] = *reinterpret_cast<const float2*>(from + kRows * D + 2 * ri);
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) v[i][k] = from[ri * D + lane * kPer + k];
-    }
-    float now = top;
-#pragma unroll
-    for (int i = 0; i < kJoinBatch; ++i)
-      if (p0 + W * i < parts) now = fmaxf(now, ml[i].x);
-    const float ref = now == -INFINITY ? 0.f : now, keep = __builtin_amdgcn_exp2f(top - ref);
-    sum *= keep;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) y[k] *= keep;
-    top = now;
-#pragma unroll
-    for (int i = 0; i < kJoinBatch; ++i) {
-      if (p0 + W * i >= parts) continue;
-      const float f = __builtin_amdgcn_exp2f(ml[i].x - ref);
-      sum += f * ml[i].y;
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) y[k] += f * v[i][k];
-    }
-  }
-  if (lane == 0) s_sum[wave] = sum, s_m[wave] = top;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) s_y[wave][lane * kPer + k] = y[k];
+  for (int k = 0; k < kPer; ++k) s_y[wave][lane * kPer + k] = j.y[k];
   __syncthreads();
   if (wave != 0) return;
+  Joined<kPer> whole;
+  whole.template take<W>(W, 0, 1, [&](int k, float2& ml, float* v) {
+    ml = make_float2(s_m[k], s_sum[k]);
 #pragma unroll
-  for (int w = 0; w < W; ++w) top = fmaxf(top, s_m[w]);
-  const float ref = top == -INFINITY ? 0.f : top;
-  sum = 0.f;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) y[k] = 0.f;
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    const float f = __builtin_amdgcn_exp2f(s_m[w] - ref);
-    sum += f * s_sum[w];
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) y[k] += f * s_y[w][lane * kPer + k];
-  }
-  finish<T, kPer>(a, seq, h, row, D, lane * kPer, sum, y);
+    for (int i = 0; i < kPer; ++i) v[i] = s_y[k][lane * kPer + i];
+  });
+  finish<T, kPer>(a, seq, h, row, D, lane * kPer, whole.sum, whole.y);
 }
 
 // ------------------------------------------------------------------ host side
