@@ -259,7 +259,8 @@ spp_status expert_cache_issue_prefetch(spp_ctx* ctx, int32_t target_layer, const
 
 /* One MoE layer of one decode step (sections "Problem Formulation" through
  * "Window-Aware Prefetch Budgeting"):
- *   u = h (+ P rms(h) if has_proj); x = rms(u) (fp32, no learned scale);
+ *   u = h (+ P rms(h) if has_proj; + W_o o with spp_set_attention);
+ *   x = rms(u) (fp32, no learned scale);
  *   z = W_r x (fp32); T_b = Top_K(z_b), lowest index first on ties;
  *   g_b = softmax(z_b) renormalised over T_b;
  *   if l < L-1 and M_max >= 0: s = sum_b softmax(B A x_b);
@@ -435,16 +436,45 @@ spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dt
  * Scores and softmax statistics are fp32; bf16 queries are exact operands,
  * probabilities are rounded to bf16 for the value product (their sum is not);
  * fp32 queries and probabilities go in as three bf16 terms each.
- * workspace: dev, spp_kv4_attend_workspace bytes for these sizes (16-byte
- * aligned), all zero before its first call; each call leaves it fit for the
- * next one of any sizes that it is large enough for.  A call holds it until the
- * stream has passed it: calls (and captured graphs) that may run at the same
- * time need one each. */
+ * workspace: dev, 16-byte aligned, all zero before its first call; each call
+ * leaves it fit for the next.  spp_kv4_attend_workspace gives the bytes for
+ * every call of at most these sizes, in either dtype.  A call holds it until
+ * the stream has passed it: calls (and captured graphs) that may run at the
+ * same time need one each.  One that was not zero may give NaN or leave rows
+ * unwritten. */
 size_t spp_kv4_attend_workspace(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, int32_t max_kv);
 spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cache, int32_t dtype, const void* q, int64_t q_stride,
                           const int32_t* q_start, const int32_t* kv_len, const int32_t* pages, int64_t pages_stride,
                           int32_t n_seq, int32_t n_tokens, int32_t max_q, int32_t max_kv, int32_t causal, float scale,
                           void* out, int64_t out_stride, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The attention of a context's layers, in place of u = h (contexts without the
+ * stand-in projection):
+ *   q, k, v = W_qkv rms(h) (rounded to dtype), q and k turned by the step's
+ *   angles; k, v of each token written to the layer's cache; o = each token's
+ *   queries against its own sequence's cached tokens, itself included, scores
+ *   scaled by 1 / sqrt(head_dim) (rounded to dtype); u = h + W_o o (fp32).
+ * spp_set_attention, once per context, before its first layer call: the heads
+ * and the cache's shape, the rotary frequencies (n_axes, axis_of, inv_freq,
+ * n_freq as for spp_rotary_table, inv_freq kept; n_freq 0: no rotation) and
+ * about how many tokens a sequence comes to (a hint).  n_heads * head_dim at
+ * most 4096 (bf16) or 2048 (fp32).  Allocates the context's buffers; ESTATE if
+ * it was set before.
+ * spp_bind_attention, for every layer: w_qkv dev [(n_heads + 2 n_kv_heads) *
+ * head_dim][D] (queries, keys, values), w_o dev [D][n_heads * head_dim], cache
+ * dev spp_kv4_cache_bytes bytes, all 16-byte aligned.
+ * spp_attention_step, before the layer calls of each decode step of B tokens,
+ * one per sequence: pos (dev int32, axis a at pos + a * pos_stride, [B] each),
+ * slots (dev int64 [B], where each token's key and value go), kv_len (dev int32
+ * [B], the sequences' lengths with this token), pages as for spp_kv4_attend.
+ * The arrays are read by the step's layer calls on the compute stream: they
+ * stay as they are until that work is done.  A layer call without a step of
+ * its B is refused (ESTATE). */
+spp_status spp_set_attention(spp_ctx* ctx, const spp_attn_desc* desc, int32_t n_axes, const int32_t* axis_of,
+                             const float* inv_freq, int32_t n_freq, int32_t max_kv);
+spp_status spp_bind_attention(spp_ctx* ctx, int32_t l, const void* w_qkv, const void* w_o, void* cache);
+spp_status spp_attention_step(spp_ctx* ctx, int32_t B, const int32_t* pos, int64_t pos_stride, const int64_t* slots,
+                              const int32_t* kv_len, const int32_t* pages, int64_t pages_stride);
 
 /* ------------------------------------------------------ inspection / runs */
 

@@ -921,6 +921,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv4_join_kernel(AttendArgs a)
 
 // ------------------------------------------------------------------ host side
 
+bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 spp_status bad(const char* why) { return spp::set_error(SPP_EINVAL, why); }
@@ -1014,16 +1015,22 @@ constexpr int kFusedParts = 32;
 constexpr int kMaxItems = 4 * kCUs * 4;
 constexpr size_t kCountBytes = kMaxItems * sizeof(unsigned);
 
+// Sixteens of rows a workgroup takes of a sequence's `rows`
+int rows_per_group(bool f32, int d, int64_t rows) { return rows <= 16 ? 1 : (rows <= 32 || (f32 && d == 128) ? 2 : 4); }
+
+// Row tiles, over all sequences and heads, below which tokens are split
+int split_below(bool f32, int d, int R) { return std::min((R == 4 ? 2 : 4) * kCUs * resident(f32, d, R), kMaxItems); }
+
 Cut cut_of(const spp_attn_desc* d, bool f32, int32_t n_seq, int32_t max_q, int32_t max_kv) {
   Cut c{};
   const int64_t rows = static_cast<int64_t>(max_q) * (d->n_heads / d->n_kv_heads);
-  c.R = rows <= 16 ? 1 : (rows <= 32 || (f32 && d->head_dim == 128) ? 2 : 4);
+  c.R = rows_per_group(f32, d->head_dim, rows);
   c.row_tiles = static_cast<int>((rows + 16 * c.R - 1) / (16 * c.R));
   c.planes = d->n_kv_heads * c.row_tiles;
   const int64_t items = static_cast<int64_t>(n_seq) * c.planes;
   const int fit = resident(f32, d->head_dim, c.R);
   const int64_t tiles = (static_cast<int64_t>(max_kv) + kTile - 1) / kTile;
-  if (items == 0 || tiles <= kMinTiles || items >= std::min((c.R == 4 ? 2 : 4) * kCUs * fit, kMaxItems)) return c;
+  if (items == 0 || tiles <= kMinTiles || items >= split_below(f32, d->head_dim, c.R)) return c;
   c.units = static_cast<int>(std::max<int64_t>(1, kCUs * fit / c.planes - n_seq / 2));
   c.join_apart = std::min<int64_t>(c.units / n_seq, tiles / kMinTiles) >= kFusedParts;
   return c;
@@ -1080,7 +1087,8 @@ extern "C" spp_status spp_rotary_table(const int32_t* pos, int64_t pos_stride, i
   if (T == 0) return SPP_OK;
   if (!pos || !inv_freq || !table) return bad("pos, inv_freq and table must not be NULL");
   if ((n_axes > 1 && pos_stride < T) || pos_stride > int64_t{1} << 40) return bad("pos_stride must be at least T");
-  if (!aligned16(table)) return bad("table must be 16-byte aligned");
+  if (!aligned16(table) || !aligned(pos, 4) || !aligned(inv_freq, 4))
+    return bad("table must be 16-byte aligned, pos and inv_freq aligned to their elements");
   a.pos = pos;
   a.pos_stride = pos_stride;
   a.inv_freq = inv_freq;
@@ -1108,7 +1116,7 @@ extern "C" spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int3
     return bad("T must be >= 0, T * (n_heads + 2 n_kv_heads) at most 2^30");
   if (T == 0) return SPP_OK;
   if (!cache || !k || !v || !slots) return bad("cache, k, v and slots must not be NULL");
-  if (!aligned16(cache)) return bad("cache must be 16-byte aligned");
+  if (!aligned16(cache) || !aligned(slots, 8)) return bad("cache must be 16-byte aligned, slots 8-byte aligned");
   if (table && !aligned16(table)) return bad("table must be 16-byte aligned");
   SPP_BAD(rows_why(k, k_stride, desc->n_kv_heads, d, elem));
   SPP_BAD(rows_why(v, v_stride, desc->n_kv_heads, d, elem));
@@ -1157,7 +1165,7 @@ extern "C" spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache,
     return bad("T must be >= 0, T * 2 n_kv_heads at most 2^30");
   if (T == 0 || (!k_out && !v_out)) return SPP_OK;
   if (!cache || !slots) return bad("cache and slots must not be NULL");
-  if (!aligned16(cache)) return bad("cache must be 16-byte aligned");
+  if (!aligned16(cache) || !aligned(slots, 8)) return bad("cache must be 16-byte aligned, slots 8-byte aligned");
   if (k_out) SPP_BAD(rows_why(k_out, k_stride, desc->n_kv_heads, d, elem));
   if (v_out) SPP_BAD(rows_why(v_out, v_stride, desc->n_kv_heads, d, elem));
   LoadArgs a{};
@@ -1193,11 +1201,19 @@ const char* attend_why(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, 
 
 extern "C" size_t spp_kv4_attend_workspace(const spp_attn_desc* desc, int32_t n_seq, int32_t max_q, int32_t max_kv) {
   if (const char* w = attend_why(desc, n_seq, max_q, max_kv)) return bad(w), 0;
+  // bounds of cut_of over every smaller size: a part for each item, and as many as fill the device
   size_t most = 16;
-  for (bool f32 : {false, true}) {
-    const Cut c = cut_of(desc, f32, n_seq, max_q, max_kv);
-    if (c.units > 0) most = std::max(most, kCountBytes + part_bytes(c, n_seq, desc->head_dim));
-  }
+  const int64_t rows = static_cast<int64_t>(max_q) * (desc->n_heads / desc->n_kv_heads);
+  if ((static_cast<int64_t>(max_kv) + kTile - 1) / kTile <= kMinTiles) return most;
+  for (bool f32 : {false, true})
+    for (int R : {1, 2, 4}) {
+      if (R > rows_per_group(f32, desc->head_dim, rows)) continue;
+      const bool longest = R == rows_per_group(f32, desc->head_dim, kMaxUnits);
+      const int64_t row_tiles = longest ? (rows + 16 * R - 1) / (16 * R) : 1;
+      const int64_t items = std::min<int64_t>(n_seq * desc->n_kv_heads * row_tiles, split_below(f32, desc->head_dim, R) - 1);
+      const int64_t parts = std::max<int64_t>(kCUs * resident(f32, desc->head_dim, R), items) + items;
+      most = std::max(most, kCountBytes + static_cast<size_t>(parts) * (16 * R) * (desc->head_dim + 2) * sizeof(float));
+    }
   return most;
 }
 
@@ -1216,7 +1232,8 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
   if (!q_start && n_tokens != n_seq) return bad("without q_start every sequence has one query token: n_tokens must be n_seq");
   if (n_seq == 0 || n_tokens == 0) return SPP_OK;
   if (!cache || !q || !kv_len || !pages || !out) return bad("cache, q, kv_len, pages and out must not be NULL");
-  if (!aligned16(cache)) return bad("cache must be 16-byte aligned");
+  if (!aligned16(cache) || !aligned(kv_len, 4) || !aligned(pages, 4) || !aligned(q_start, 4))
+    return bad("cache must be 16-byte aligned, q_start, kv_len and pages aligned to their elements");
   if (pages_stride < 1 || pages_stride > INT32_MAX || pages_stride * desc->page > INT32_MAX - 1024)
     return bad("pages_stride must be at least 1, pages_stride * page below 2^31 - 1024");
   SPP_BAD(rows_why(q, q_stride, desc->n_heads, d, elem));
@@ -1226,7 +1243,8 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
                        extent(out_stride, n_tokens, desc->n_heads, d, elem)))
     return bad("out must be q with the same stride, or not overlap it");
   if (!workspace || !aligned16(workspace)) return bad("workspace must not be NULL, and 16-byte aligned");
-  if (workspace_bytes < spp_kv4_attend_workspace(desc, n_seq, max_q, max_kv)) return bad("the workspace is too small");
+  const Cut cut = cut_of(desc, dtype == SPP_DTYPE_F32, n_seq, max_q, max_kv);
+  if (cut.units > 0 && workspace_bytes < kCountBytes + part_bytes(cut, n_seq, d)) return bad("the workspace is too small");
   AttendArgs a{};
   a.cache = cache_of(desc, cache);
   a.q = q;
@@ -1243,7 +1261,6 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
   a.G = desc->n_heads / desc->n_kv_heads;
   a.causal = causal;
   a.scale_log2 = scale * 1.44269504088896340736f;
-  const Cut cut = cut_of(desc, dtype == SPP_DTYPE_F32, n_seq, max_q, max_kv);
   a.planes = cut.planes;
   a.row_tiles = cut.row_tiles;
   a.units = cut.units;

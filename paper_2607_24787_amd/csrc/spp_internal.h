@@ -129,12 +129,21 @@ struct CombineArgs {
   void* out;             // [D] storage dtype
 };
 
+// Products of B rows with a weight [rows, D]:
+//   kProjPrologue  u = h + P rms(h) (rows = D)
+//   kProjNorm      out = P rms(h), in the storage dtype
+//   kProjAdd       u = res + P h
+enum { kProjPrologue = 0, kProjNorm = 1, kProjAdd = 2 };
 struct ProjArgs {
-  const void* h;   // [B, D]
-  const void* P;   // [D, D]
-  float* u;        // [B, D]
+  const void* h;    // [B, D]
+  const void* P;    // [rows, D]
+  float* u;         // [B, rows]
   int B, D;
   float eps;
+  int rows;
+  int mode;
+  const void* res;  // [B, rows], kProjAdd
+  void* out;        // [B, rows], kProjNorm
 };
 
 hipError_t launch_router(const RouterArgs& a, int dtype, hipStream_t st);

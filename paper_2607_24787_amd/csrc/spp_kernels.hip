@@ -2585,14 +2585,15 @@ __global__ __launch_bounds__(64 * kCombWaves) void ffn_combine_batched_kernel(Co
   store_elem<T>(a.out, o + 3, res.w + y[3]);
 }
 
-// Stand-in projection prologue: u = h + P rms(h) (fp32 result).  One wave per row of P.
-template <typename T, int NCH, bool FULL>
+// The products in front of a layer (ProjArgs): the stand-in projection u = h + P
+// rms(h), or those before and behind the attention.  One wave per row of P.
+template <typename T, int NCH, bool FULL, int MODE>
 __global__ __launch_bounds__(kThreads) void proj_kernel(ProjArgs a) {
   constexpr int V = Vec<T>::N;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int D = a.D, nch = D / V;
   const int row = blockIdx.x * kWaves + wave;
-  if (row >= D) return;
+  if (row >= a.rows) return;
   const T* prow = reinterpret_cast<const T*>(a.P) + static_cast<size_t>(row) * D;
   uint4 w[NCH];
   load_chunks<NCH, FULL>(prow, lane, nch, w);
@@ -2600,17 +2601,18 @@ __global__ __launch_bounds__(kThreads) void proj_kernel(ProjArgs a) {
   // unpacked weights are hoisted out of the token loop, which waits for them
   uint4 hr[NCH];
   load_chunks<NCH, FULL>(a.h, lane, nch, hr);
-  float res = load_elem<T>(a.h, row);
+  const void* added = MODE == kProjAdd ? a.res : a.h;
+  float res = MODE == kProjNorm ? 0.f : load_elem<T>(added, row);
   for (int b = 0; b < a.B; ++b) {
     const T* hb = reinterpret_cast<const T*>(a.h) + static_cast<size_t>(b) * D;
     if (b > 0) {
       load_chunks<NCH, FULL>(hb, lane, nch, hr);
-      res = load_elem<T>(hb, row);
+      if (MODE != kProjNorm) res = load_elem<T>(added, static_cast<size_t>(b) * a.rows + row);
     }
     float xv[NCH][V];
 #pragma unroll
     for (int j = 0; j < NCH; ++j) unpack<T>(hr[j], xv[j]);
-    const float inv = rms_scale<T, NCH>(xv, D, a.eps);
+    const float inv = MODE == kProjAdd ? 1.f : rms_scale<T, NCH>(xv, D, a.eps);
     float acc = 0.f;
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
@@ -2620,7 +2622,11 @@ __global__ __launch_bounds__(kThreads) void proj_kernel(ProjArgs a) {
       for (int v = 0; v < V; ++v) acc += wf[v] * (xv[j][v] * inv);
     }
     acc = wave_sum(acc);
-    if (lane == 0) a.u[static_cast<size_t>(b) * D + row] = res + acc;
+    if (lane != 0) continue;
+    if (MODE == kProjNorm)
+      store_elem<T>(a.out, static_cast<size_t>(b) * a.rows + row, acc);
+    else
+      a.u[static_cast<size_t>(b) * a.rows + row] = res + acc;
   }
 }
 
@@ -2782,7 +2788,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void router_rows_kernel(RouterArgs 
   }
 }
 
-// Stand-in projection for a batch (bf16, B > 1) on MFMA.  h and P are bf16, so
+// The same products for a batch (bf16, B > 1) on MFMA.  h and P are bf16, so
 // their products are exact on the bf16 MFMA; the normalisation moves to the
 // epilogue,
 //   u[b][o] = h[b][o] + (sum_i P[o][i] h[b][i]) / sqrt(mean_i h[b][i]^2 + eps),
@@ -2799,6 +2805,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void router_rows_kernel(RouterArgs 
 // last token and are not stored.
 constexpr int kProjWaves = 8;
 constexpr int kProjRB = 2;  // 16-row blocks of P per workgroup (D a multiple of 256)
+template <int MODE>
 __global__ __launch_bounds__(64 * kProjWaves) void proj_mfma_kernel(ProjArgs a) {
   __shared__ f32x4 s_acc[kProjWaves][kProjRB][64];
   __shared__ float s_ss[kProjWaves][16];
@@ -2865,10 +2872,12 @@ __global__ __launch_bounds__(64 * kProjWaves) void proj_mfma_kernel(ProjArgs a) 
     const int b = b0 + t;
     if (b < a.B) {
       const int o = o0 + 16 * wave + krow;
-      const float inv = 1.0f / sqrtf(sst / static_cast<float>(D) + a.eps);
-      const size_t idx = static_cast<size_t>(b) * D + o;
-      a.u[idx] = __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(a.h)[idx]) << 16) +
-                 inv * y[j];
+      const float inv = MODE == kProjAdd ? 1.f : 1.0f / sqrtf(sst / static_cast<float>(D) + a.eps);
+      const size_t idx = static_cast<size_t>(b) * a.rows + o;
+      if (MODE == kProjNorm)
+        store_elem<uint16_t>(a.out, idx, inv * y[j]);
+      else
+        a.u[idx] = load_elem<uint16_t>(MODE == kProjAdd ? a.res : a.h, idx) + inv * y[j];
     }
   }
 }
@@ -3084,17 +3093,24 @@ hipError_t ffn_t(const FfnArgs& a, int grid, hipStream_t st, hipEvent_t start, h
   return full_rows<T>(a.D) ? ffn_tf<T, true>(a, grid, st, start, stop) : ffn_tf<T, false>(a, grid, st, start, stop);
 }
 
-template <typename T, bool FULL>
+template <typename T, bool FULL, int MODE>
 hipError_t proj_tf(const ProjArgs& a, hipStream_t st) {
-  const int grid = (a.D + kWaves - 1) / kWaves;
+  const int grid = (a.rows + kWaves - 1) / kWaves;
   SPP_DISPATCH_NCH(nch_for<T>(a.D),
-                   hipLaunchKernelGGL((proj_kernel<T, NCH, FULL>), dim3(grid), dim3(kThreads), 0, st, a));
+                   hipLaunchKernelGGL((proj_kernel<T, NCH, FULL, MODE>), dim3(grid), dim3(kThreads), 0, st, a));
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t proj_t(const ProjArgs& a, hipStream_t st) {
-  return full_rows<T>(a.D) ? proj_tf<T, true>(a, st) : proj_tf<T, false>(a, st);
+template <int MODE>
+hipError_t proj_m(const ProjArgs& a, int dtype, hipStream_t st) {
+  if (dtype == 1 && a.B > 1 && a.D % 256 == 0 && a.rows % (16 * kProjRB) == 0) {
+    hipLaunchKernelGGL((proj_mfma_kernel<MODE>), dim3(a.rows / (16 * kProjRB), (a.B + 15) / 16), dim3(64 * kProjWaves),
+                       0, st, a);
+    return hipGetLastError();
+  }
+  if (dtype == 1)
+    return full_rows<uint16_t>(a.D) ? proj_tf<uint16_t, true, MODE>(a, st) : proj_tf<uint16_t, false, MODE>(a, st);
+  return full_rows<float>(a.D) ? proj_tf<float, true, MODE>(a, st) : proj_tf<float, false, MODE>(a, st);
 }
 
 }  // namespace
@@ -3231,11 +3247,12 @@ hipError_t launch_combine(const CombineArgs& a, int dtype, hipStream_t st) {
 }
 
 hipError_t launch_proj(const ProjArgs& a, int dtype, hipStream_t st) {
-  if (dtype == 1 && a.B > 1 && a.D % 256 == 0) {
-    hipLaunchKernelGGL(proj_mfma_kernel, dim3(a.D / (16 * kProjRB), (a.B + 15) / 16), dim3(64 * kProjWaves), 0, st, a);
-    return hipGetLastError();
+  switch (a.mode) {
+    case kProjPrologue: return proj_m<kProjPrologue>(a, dtype, st);
+    case kProjNorm: return proj_m<kProjNorm>(a, dtype, st);
+    case kProjAdd: return proj_m<kProjAdd>(a, dtype, st);
+    default: return hipErrorInvalidValue;
   }
-  return dtype == 1 ? proj_t<uint16_t>(a, st) : proj_t<float>(a, st);
 }
 
 hipError_t launch_ffn_grouped(const GroupArgs& a, hipStream_t st, hipEvent_t start, hipEvent_t stop) {

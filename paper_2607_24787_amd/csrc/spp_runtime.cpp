@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <chrono>
+#include <climits>
 #include <immintrin.h>
 #include <cmath>
 #include <cstring>
@@ -66,6 +67,8 @@ struct LayerState {
   const void* Bm = nullptr;
   const void* proj = nullptr;
   const void* shared = nullptr;
+  const void *w_qkv = nullptr, *w_o = nullptr;  // attention (spp_bind_attention)
+  void* kv_cache = nullptr;
   const uint8_t* host_store = nullptr;
   const uint8_t* host_store_dev = nullptr;  // its device-visible address (read by the copy kernel)
   uint8_t* slots = nullptr;
@@ -85,6 +88,25 @@ struct LayerState {
   uint64_t slot_tab_version = 0;          // the policy version it holds (0: none)
 };
 
+// The attention in front of every layer (spp_set_attention), and the step it is at
+struct Attention {
+  bool on = false;
+  spp_attn_desc desc{};
+  int32_t n_axes = 1, n_freq = 0, max_kv = 0;
+  int32_t axis_of[64] = {};  // n_freq of them
+  const float* inv_freq = nullptr;
+  // per step, shared by every layer: rotary table; per layer: products and sums
+  float* table = nullptr;  // [max_batch, 2, n_freq]
+  void* qkv = nullptr;     // [max_batch, (n_heads + 2 n_kv_heads) head_dim]
+  void* out = nullptr;     // [max_batch, n_heads head_dim]
+  void* workspace = nullptr;
+  size_t workspace_bytes = 0;
+  int32_t B = 0;  // tokens of the step that was set; 0: none
+  const int64_t* slots = nullptr;
+  const int32_t *kv_len = nullptr, *pages = nullptr;
+  int64_t pages_stride = 0;
+};
+
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 }  // namespace
@@ -101,6 +123,7 @@ struct spp_ctx {
   size_t elem = 0, blob_bytes = 0, stride = 0;
   std::vector<LayerState> layers;
   float* u_dev = nullptr;      // [maxB, D] prologue output
+  Attention attn;
   float* x_dev = nullptr;      // [maxB, D] router input
   float* zbuf = nullptr;       // [maxB, n + r]
   uint64_t* ztag = nullptr;    // [n + r] batch-1 router values tagged with their launch's seq (zero: none yet)
@@ -590,7 +613,8 @@ void free_ctx(spp_ctx* c) {
   for (void* p : {static_cast<void*>(c->u_dev), static_cast<void*>(c->x_dev), static_cast<void*>(c->zbuf),
                   static_cast<void*>(c->ztag), static_cast<void*>(c->res_dev), static_cast<void*>(c->counter),
                   static_cast<void*>(c->slot_tabs),
-                  static_cast<void*>(c->partial), static_cast<void*>(c->probe_dev)})
+                  static_cast<void*>(c->partial), static_cast<void*>(c->probe_dev), static_cast<void*>(c->attn.table),
+                  c->attn.qkv, c->attn.out, c->attn.workspace})
     if (p) (void)hipFree(p);
   if (c->rec_host) (void)hipHostFree(c->rec_host);
   if (c->xh_dev) (void)hipFree(c->xh_dev);
@@ -905,6 +929,9 @@ spp_status launch_groups(spp_ctx* c, const LayerState& ls, int32_t b0, int32_t B
   return SPP_OK;
 }
 
+// Whether u differs from the layer's input (u_dev holds it then)
+bool has_prologue(const spp_ctx* c) { return c->d.has_proj || c->attn.on; }
+
 spp_status combine_batch(spp_ctx* c, int32_t b0, int32_t B, const void* h_in, void* h_out) {
   const spp_model_desc& d = c->d;
   const size_t row_bytes = static_cast<size_t>(d.D) * c->elem;
@@ -918,7 +945,7 @@ spp_status combine_batch(spp_ctx* c, int32_t b0, int32_t B, const void* h_in, vo
   cb.n_shared = d.n_shared;
   cb.D = d.D;
   cb.res_h = static_cast<const uint8_t*>(h_in) + b0 * row_bytes;
-  cb.res_u = d.has_proj ? c->u_dev + static_cast<size_t>(b0) * d.D : nullptr;
+  cb.res_u = has_prologue(c) ? c->u_dev + static_cast<size_t>(b0) * d.D : nullptr;
   cb.out = static_cast<uint8_t*>(h_out) + b0 * row_bytes;
   SPP_HIP(spp::launch_combine_batched(cb, d.dtype, c->compute));
   c->stats.ffn_launches += 1;
@@ -1074,14 +1101,37 @@ spp_status combine_token(spp_ctx* c, const Flight& fl, int32_t b, int grid) {
   ca.nparts = grid;
   ca.D = c->d.D;
   ca.res_h = static_cast<const uint8_t*>(fl.h_in) + row * c->elem;
-  ca.res_u = c->d.has_proj ? c->u_dev + row : nullptr;
+  ca.res_u = has_prologue(c) ? c->u_dev + row : nullptr;
   ca.out = static_cast<uint8_t*>(fl.h_out) + row * c->elem;
   SPP_HIP(spp::launch_combine(ca, c->d.dtype, c->compute));
   c->stats.ffn_launches += 1;
   return SPP_OK;
 }
 
-// Enqueue one layer call: projection and router, and, for a device-routable
+// u = h + W_o attention(W_qkv rms(h)): the queries, keys and values of the B
+// tokens in one product, rotated, the new tokens written to the layer's cache,
+// each token against its own sequence, and the product back with the residual.
+spp_status attention_prologue(spp_ctx* c, const LayerState& ls, const void* h_in, int32_t B) {
+  const spp_model_desc& d = c->d;
+  Attention& at = c->attn;
+  const int32_t hd = at.desc.head_dim, q = at.desc.n_heads * hd, kv = at.desc.n_kv_heads * hd, wide = q + 2 * kv;
+  uint8_t* rows = static_cast<uint8_t*>(at.qkv);
+  spp::ProjArgs in{h_in, ls.w_qkv, nullptr, B, d.D, d.rms_eps, wide, spp::kProjNorm, nullptr, at.qkv};
+  SPP_HIP(spp::launch_proj(in, d.dtype, c->compute));
+  if (spp_status s = spp_kv4_store(&at.desc, ls.kv_cache, d.dtype, rows, wide, rows, wide, rows + q * c->elem, wide,
+                                   rows + (q + kv) * c->elem, wide, at.n_freq ? at.table : nullptr, at.n_freq, at.slots,
+                                   B, c->compute))
+    return s;
+  if (spp_status s = spp_kv4_attend(&at.desc, ls.kv_cache, d.dtype, rows, wide, nullptr, at.kv_len, at.pages,
+                                    at.pages_stride, B, B, 1, at.max_kv, 1, 1.0f / std::sqrt(static_cast<float>(hd)),
+                                    at.out, q, at.workspace, at.workspace_bytes, c->compute))
+    return s;
+  spp::ProjArgs out{at.out, ls.w_o, c->u_dev, B, q, d.rms_eps, d.D, spp::kProjAdd, h_in, nullptr};
+  SPP_HIP(spp::launch_proj(out, d.dtype, c->compute));
+  return SPP_OK;
+}
+
+// Enqueue one layer call: prologue and router, and, for a device-routable
 // layer, its FFN and combine.
 spp_status layer_begin(spp_ctx* c, int32_t l, const void* h_in, void* h_out, int32_t B, int32_t M_max, Flight* out) {
   if (spp_status s = check_layer(c, l, true)) return s;
@@ -1091,6 +1141,8 @@ spp_status layer_begin(spp_ctx* c, int32_t l, const void* h_in, void* h_out, int
   if (B < 1 || B > d.max_batch) return fail(SPP_EINVAL, "B must be in [1, max_batch]");
   if (M_max < -1) return fail(SPP_EINVAL, "M_max must be >= -1");
   LayerState& ls = c->layers[l];
+  if (c->attn.on && !ls.kv_cache) return fail(SPP_ESTATE, "the layer's attention is not bound");
+  if (c->attn.on && c->attn.B != B) return fail(SPP_ESTATE, "no attention step was set for this batch");
   Flight& fl = *out;
   fl.l = l;
   fl.B = B;
@@ -1117,8 +1169,10 @@ spp_status layer_begin(spp_ctx* c, int32_t l, const void* h_in, void* h_out, int
     SPP_HIP(hipEventRecord(ts.ev[kEvStart], c->compute));
   }
   if (d.has_proj) {
-    spp::ProjArgs pa{h_in, ls.proj, c->u_dev, B, d.D, d.rms_eps};
+    spp::ProjArgs pa{h_in, ls.proj, c->u_dev, B, d.D, d.rms_eps, d.D, spp::kProjPrologue, nullptr, nullptr};
     SPP_HIP(spp::launch_proj(pa, dt, c->compute));
+  } else if (c->attn.on) {
+    if (spp_status s = attention_prologue(c, ls, h_in, B)) return s;
   }
   fl.seq = next_router_seq(c);
   fl.set = next_rec_set(c);
@@ -1126,7 +1180,7 @@ spp_status layer_begin(spp_ctx* c, int32_t l, const void* h_in, void* h_out, int
   const size_t bkmax = static_cast<size_t>(d.max_batch) * d.K;
   spp::RouterArgs ra{};
   ra.h = h_in;
-  ra.u = d.has_proj ? c->u_dev : nullptr;
+  ra.u = has_prologue(c) ? c->u_dev : nullptr;
   ra.Wr = ls.router_w;
   ra.A = fl.adapter_on ? ls.A : nullptr;
   ra.Bm = ls.Bm;
@@ -1539,6 +1593,88 @@ spp_status spp_bind_layer(spp_ctx* c, int32_t l, const void* router_w, const voi
   ls.shared = shared_blobs;
   ls.host_store = static_cast<const uint8_t*>(host_store);
   ls.bound = true;
+  return SPP_OK;
+}
+
+spp_status spp_set_attention(spp_ctx* c, const spp_attn_desc* desc, int32_t n_axes, const int32_t* axis_of,
+                             const float* inv_freq, int32_t n_freq, int32_t max_kv) {
+  if (spp_status s = check_ctx(c)) return s;
+  const spp_model_desc& d = c->d;
+  if (spp_kv4_cache_bytes(desc) == 0) return SPP_EINVAL;  // the message is set
+  if (d.has_proj) return fail(SPP_EINVAL, "a context with the stand-in projection takes no attention");
+  const int64_t q = static_cast<int64_t>(desc->n_heads) * desc->head_dim;
+  const int64_t wide = q + 2 * static_cast<int64_t>(desc->n_kv_heads) * desc->head_dim;
+  if ((q * static_cast<int64_t>(c->elem) / 16 + 63) / 64 > 8)
+    return fail(SPP_EINVAL, "n_heads * head_dim too large (at most 4096 bf16 / 2048 fp32)");
+  if (n_freq < 0 || n_freq % 8 != 0 || 2 * n_freq > desc->head_dim)
+    return fail(SPP_EINVAL, "n_freq must be a multiple of 8, at most head_dim / 2");
+  if (n_axes < 1 || n_axes > 4) return fail(SPP_EINVAL, "n_axes must be in [1, 4]");
+  if ((inv_freq != nullptr) != (n_freq > 0)) return fail(SPP_EINVAL, "inv_freq must be given iff n_freq > 0");
+  for (int32_t i = 0; axis_of && i < n_freq; ++i)
+    if (axis_of[i] < 0 || axis_of[i] >= n_axes) return fail(SPP_EINVAL, "axis_of names an axis outside [0, n_axes)");
+  if (max_kv < 1) return fail(SPP_EINVAL, "max_kv must be >= 1");
+  if (c->attn.on) return fail(SPP_ESTATE, "the context's attention is already set");
+  Attention at;
+  at.desc = *desc;
+  at.n_axes = n_axes;
+  at.n_freq = n_freq;
+  at.max_kv = max_kv;
+  if (axis_of) std::copy(axis_of, axis_of + n_freq, at.axis_of);
+  at.inv_freq = inv_freq;
+  at.workspace_bytes = spp_kv4_attend_workspace(desc, d.max_batch, 1, max_kv);
+  if (at.workspace_bytes == 0) return SPP_EINVAL;
+  const size_t B = static_cast<size_t>(d.max_batch);
+  const auto undo = [&](spp_status s, const char* why) {
+    for (void* p : {static_cast<void*>(at.table), at.qkv, at.out, at.workspace})
+      if (p) (void)hipFree(p);
+    return fail(s, why);
+  };
+  if ((n_freq && hipMalloc(&at.table, B * 2 * n_freq * sizeof(float)) != hipSuccess) ||
+      hipMalloc(&at.qkv, B * wide * c->elem) != hipSuccess || hipMalloc(&at.out, B * q * c->elem) != hipSuccess ||
+      hipMalloc(&at.workspace, at.workspace_bytes) != hipSuccess)
+    return undo(SPP_ENOMEM, "attention buffer allocation failed");
+  // zero once; every call leaves it zero where it counts
+  if (hipMemsetAsync(at.workspace, 0, at.workspace_bytes, c->compute) != hipSuccess)
+    return undo(SPP_EHIP, "clearing the attention workspace failed");
+  at.on = true;
+  c->attn = at;
+  return SPP_OK;
+}
+
+spp_status spp_bind_attention(spp_ctx* c, int32_t l, const void* w_qkv, const void* w_o, void* cache) {
+  if (spp_status s = check_layer(c, l, false)) return s;
+  if (!c->attn.on) return fail(SPP_ESTATE, "spp_set_attention comes first");
+  if (!w_qkv || !w_o || !cache) return fail(SPP_EINVAL, "w_qkv, w_o and cache must not be NULL");
+  for (const void* p : {w_qkv, w_o, static_cast<const void*>(cache)})
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return fail(SPP_EINVAL, "w_qkv, w_o and cache must be 16-byte aligned");
+  LayerState& ls = c->layers[l];
+  ls.w_qkv = w_qkv;
+  ls.w_o = w_o;
+  ls.kv_cache = cache;
+  return SPP_OK;
+}
+
+spp_status spp_attention_step(spp_ctx* c, int32_t B, const int32_t* pos, int64_t pos_stride, const int64_t* slots,
+                              const int32_t* kv_len, const int32_t* pages, int64_t pages_stride) {
+  if (spp_status s = check_ctx(c)) return s;
+  Attention& at = c->attn;
+  if (!at.on) return fail(SPP_ESTATE, "spp_set_attention comes first");
+  if (B < 1 || B > c->d.max_batch) return fail(SPP_EINVAL, "B must be in [1, max_batch]");
+  if (!slots || !kv_len || !pages) return fail(SPP_EINVAL, "slots, kv_len and pages must not be NULL");
+  if (pages_stride < 1 || pages_stride > (INT32_MAX - 1024) / at.desc.page)
+    return fail(SPP_EINVAL, "pages_stride must be at least 1, pages_stride * page below 2^31 - 1024");
+  if (reinterpret_cast<uintptr_t>(slots) % 8 != 0 || reinterpret_cast<uintptr_t>(kv_len) % 4 != 0 ||
+      reinterpret_cast<uintptr_t>(pages) % 4 != 0)
+    return fail(SPP_EINVAL, "slots, kv_len and pages must be aligned to their elements");
+  if (at.n_freq)
+    if (spp_status s = spp_rotary_table(pos, pos_stride, at.n_axes, at.axis_of, at.inv_freq, at.n_freq, B, at.table,
+                                        c->compute))
+      return s;
+  at.B = B;
+  at.slots = slots;
+  at.kv_len = kv_len;
+  at.pages = pages;
+  at.pages_stride = pages_stride;
   return SPP_OK;
 }
 

@@ -25,6 +25,62 @@ def _torch_from_storage(a: np.ndarray, device):
     return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(device)
 
 
+class PagedAttention:
+    """The attention of a stack's layers: weights, 4-bit key/value caches, and where a decode step stands in them.
+
+    Each of the batch's sequences owns ``kv_tokens / kv_page`` pages of every
+    layer's cache.  ``next_token`` appends one token to the first B sequences.
+    """
+
+    def __init__(self, stack: "OffloadedMoEStack"):
+        import torch
+        from workload import gen
+
+        cfg, self.stack, dev = stack.cfg, stack, stack.device
+        self.per_seq = -(-cfg.kv_tokens // cfg.kv_page)
+        n_pages = cfg.batch * self.per_seq
+        self.desc = spp.make_attn_desc(cfg.attn_heads, cfg.attn_kv_heads, cfg.head_dim, cfg.kv_page, n_pages)
+        axes = spp.rotary_axes(cfg.rotary_sections, cfg.rotary_interleaved)
+        self.inv_freq = torch.from_numpy(gen.rotary_frequencies(cfg)).to(dev)
+        spp.spp_set_attention(stack.ctx, self.desc, len(cfg.rotary_sections), axes,
+                              self.inv_freq.data_ptr() if axes.size else 0, cfg.kv_tokens)
+        self.weights, self.caches = [], []
+        for l in range(cfg.L):
+            self.weights.append([_torch_from_storage(w, dev) for w in gen.attention_weights(cfg, l)])
+            self.caches.append(torch.zeros(spp.spp_kv4_cache_bytes(self.desc), dtype=torch.uint8, device=dev))
+            spp.spp_bind_attention(stack.ctx, l, *(w.data_ptr() for w in self.weights[l]), self.caches[l].data_ptr())
+        # page i of sequence b is page i * batch + b of the cache
+        self.pages = torch.arange(n_pages, dtype=torch.int32, device=dev).reshape(self.per_seq, cfg.batch).T.contiguous()
+        self.kv_len = torch.zeros(cfg.batch, dtype=torch.int32, device=dev)
+        self.slots = torch.zeros(cfg.batch, dtype=torch.int64, device=dev)
+        self.pos = torch.zeros((len(cfg.rotary_sections), cfg.batch), dtype=torch.int32, device=dev)
+        self.length = np.zeros(cfg.batch, dtype=np.int64)
+
+    def reset(self):
+        """Every sequence is empty again."""
+        with self.stack.torch.cuda.stream(self.stack.stream):
+            self.kv_len.zero_()
+        self.length[:] = 0
+
+    def next_token(self, B: int, positions=None):
+        """One more token of the first B sequences, at positions [axes, B] (default: its place in the sequence, on every axis)."""
+        cfg, torch = self.stack.cfg, self.stack.torch
+        if self.length[:B].max() >= self.per_seq * cfg.kv_page:
+            raise ValueError("a sequence's pages are full")
+        with torch.cuda.stream(self.stack.stream):
+            at = self.kv_len[:B].long()
+            page = self.pages[:B].gather(1, (at // cfg.kv_page)[:, None])[:, 0].long()
+            self.slots[:B] = page * cfg.kv_page + at % cfg.kv_page
+            if positions is None:
+                self.pos[:, :B] = self.kv_len[:B]
+            else:
+                self.pos[:, :B] = torch.from_numpy(np.ascontiguousarray(positions, dtype=np.int32)).to(self.pos.device)
+            self.kv_len[:B] += 1
+        self.length[:B] += 1
+        spp.spp_attention_step(self.stack.ctx, B, self.pos.data_ptr(), cfg.batch, self.slots.data_ptr(),
+                               self.kv_len.data_ptr(), self.pages.data_ptr(), self.per_seq)
+
+
 class OffloadedMoEStack:
     """One spp context over a whole synthetic stack (all L layers).
 
@@ -106,6 +162,7 @@ class OffloadedMoEStack:
                                self.proj[l].data_ptr() if self.proj[l] is not None else 0,
                                self.shared[l].data_ptr() if self.shared[l] is not None else 0,
                                self.host[l % self.host_layers].data_ptr())
+        self.attention = PagedAttention(self) if cfg.attn_heads else None
         self.resident = list(range(min(self.S, cfg.n))) if resident is None else list(resident)
         self.reset()
         # ping-pong hidden-state buffers [B, D] in the storage dtype
@@ -113,10 +170,16 @@ class OffloadedMoEStack:
         self.hbuf = [torch.empty(nbytes, dtype=torch.uint8, device=self.device) for _ in range(2)]
 
     def reset(self):
-        """Initial slot tables (the resident set in slots 0.., stamp 0) and step clock 0."""
+        """Initial slot tables (the resident set in slots 0.., stamp 0), step clock 0, and empty sequences."""
         for l in range(self.cfg.L):
             spp.spp_set_resident(self.ctx, l, self.resident)
         spp.spp_set_clock(self.ctx, 0)
+        if self.attention:
+            self.attention.reset()
+
+    def _next_token(self, B: Optional[int]):
+        if self.attention:
+            self.attention.next_token(self.cfg.batch if B is None else B)
 
     def _to_storage(self, v):
         from workload.gen import f32_to_bf16_bits
@@ -149,6 +212,7 @@ class OffloadedMoEStack:
         """One decode step through all layers; returns the per-layer (topk, gates, stats)."""
         if h_storage is not None:
             self.upload_hidden(h_storage, 0)
+        self._next_token(B)
         out = []
         src = 0
         for l in range(self.cfg.L):
@@ -160,6 +224,7 @@ class OffloadedMoEStack:
     def step_from(self, h_in_ptr: int, M_max: int, B: Optional[int] = None):
         """One decode step whose layer-0 input is read from device address ``h_in_ptr``."""
         B = self.cfg.batch if B is None else B
+        self._next_token(B)
         out = []
         src_ptr = h_in_ptr
         dst = 0
@@ -175,6 +240,7 @@ class OffloadedMoEStack:
         (spp_decode_step); the output lands in hbuf[0].  Returns the per-layer
         (topk, gates, stats) like step_from."""
         B = self.cfg.batch if B is None else B
+        self._next_token(B)
         topk, gates, stats = spp.spp_decode_step(self.ctx, self.cfg.L, h_in_ptr, self.hbuf[0].data_ptr(),
                                                  self.hbuf[1].data_ptr(), B, self.cfg.K, M_max)
         self.last_buf = 0

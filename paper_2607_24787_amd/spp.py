@@ -99,6 +99,9 @@ _SIGS = {
     "spp_kv4_attend": (c_int32, [POINTER(AttnDesc), c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_void_p,
                                  c_int64, c_int32, c_int32, c_int32, c_int32, c_int32, c_float, c_void_p, c_int64,
                                  c_void_p, c_size_t, c_void_p]),
+    "spp_set_attention": (c_int32, [c_void_p, POINTER(AttnDesc), c_int32, POINTER(c_int32), c_void_p, c_int32, c_int32]),
+    "spp_bind_attention": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
+    "spp_attention_step": (c_int32, [c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64]),
     "spp_get_slot_table": (c_int32, [c_void_p, c_int32, POINTER(c_int32), POINTER(c_int64)]),
     "spp_set_slot_table": (c_int32, [c_void_p, c_int32, POINTER(c_int32), POINTER(c_int64)]),
     "spp_get_clock": (c_int32, [c_void_p, POINTER(c_int64)]),
@@ -377,6 +380,23 @@ def spp_kv4_attend(desc: AttnDesc, cache_dev: int, dtype: int, q_dev: int, q_str
                                 kv_len_dev, pages_dev, pages_stride, n_seq, n_tokens, max_q, max_kv,
                                 int(causal), scale, out_dev, out_stride, workspace_dev, workspace_bytes,
                                 stream))
+
+
+def spp_set_attention(ctx, desc: AttnDesc, n_axes: int, axis_of, inv_freq_dev: int, max_kv: int):
+    """Attention in front of every layer of the context; axis_of: the axis of each rotary frequency (empty: no rotation)."""
+    a, p = _i32(axis_of)
+    _check(lib().spp_set_attention(c_void_p(ctx), byref(desc), n_axes, p, inv_freq_dev, a.size, max_kv))
+
+
+def spp_bind_attention(ctx, l: int, w_qkv_dev: int, w_o_dev: int, cache_dev: int):
+    _check(lib().spp_bind_attention(c_void_p(ctx), l, w_qkv_dev, w_o_dev, cache_dev))
+
+
+def spp_attention_step(ctx, B: int, pos_dev: int, pos_stride: int, slots_dev: int, kv_len_dev: int, pages_dev: int,
+                       pages_stride: int):
+    """The positions, slots, lengths and pages (device) of the next decode step's B tokens."""
+    _check(lib().spp_attention_step(c_void_p(ctx), B, pos_dev, pos_stride, slots_dev, kv_len_dev, pages_dev,
+                                    pages_stride))
 
 
 def spp_last_error() -> str:

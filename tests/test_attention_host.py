@@ -1,5 +1,4 @@
 """CPU tests of the attention operators: the plain forms on hand-worked values, the entry points' refusals, the axes helper."""
-import ctypes
 import os
 
 import numpy as np
@@ -132,13 +131,13 @@ REFUSED = (
     [(spp.spp_rotary_table, TABLE, c) for c in (
         dict(n_axes=0), dict(n_axes=5), dict(axis_of=[0] * 7), dict(axis_of=[0] * 12), dict(axis_of=[0] * 72),
         dict(axis_of=[]), dict(axis_of=[3] + [0] * 7), dict(axis_of=[-1] + [0] * 7), dict(T=-1), dict(T=1 << 30),
-        dict(pos_dev=0), dict(inv_freq_dev=0), dict(table_dev=0), dict(table_dev=GOOD + 4), dict(pos_stride=4),
+        dict(pos_dev=0), dict(pos_dev=GOOD + 2), dict(inv_freq_dev=0), dict(inv_freq_dev=GOOD + 1), dict(table_dev=0), dict(table_dev=GOOD + 4), dict(pos_stride=4),
         dict(pos_stride=-5), dict(pos_stride=1 << 60))]
     + [(spp.spp_kv4_store, STORE, c) for c in (
         dict(cache_dev=0), dict(cache_dev=GOOD + 8), dict(dtype=2), dict(dtype=-1), dict(q_dev=0), dict(q_out_dev=0),
         dict(q_dev=GOOD + 8), dict(q_stride=511), dict(q_stride=504), dict(q_stride=-512), dict(q_stride=1 << 62),
         dict(k_dev=0), dict(v_dev=0), dict(k_dev=GOOD + 2), dict(k_stride=120), dict(v_stride=132), dict(table_dev=0),
-        dict(table_dev=GOOD + 4), dict(n_freq=0), dict(n_freq=12), dict(n_freq=40), dict(n_freq=-8), dict(slots_dev=0),
+        dict(table_dev=GOOD + 4), dict(n_freq=0), dict(n_freq=12), dict(n_freq=40), dict(n_freq=-8), dict(slots_dev=0), dict(slots_dev=GOOD + 4),
         dict(T=-1), dict(T=1 << 30), dict(q_out_dev=GOOD + 16), dict(q_out_dev=GOOD + 1024),
         dict(q_out_dev=GOOD, q_out_stride=1024))]
     + [(spp.spp_kv4_load, LOAD, c) for c in (
@@ -150,7 +149,8 @@ REFUSED = (
         dict(pages_stride=1 << 27), dict(pages_stride=1 << 62), dict(n_seq=-1), dict(n_tokens=-1), dict(n_tokens=1 << 30), dict(max_q=0),
         dict(max_kv=-1), dict(max_q=1 << 29), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
         dict(scale=float("inf")), dict(scale=1e-60), dict(causal=2), dict(out_dev=0), dict(out_dev=GOOD + 512), dict(out_stride=1024, out_dev=GOOD),
-        dict(workspace_dev=0), dict(workspace_dev=GOOD * 4 + 8), dict(workspace_bytes=0))]
+        dict(workspace_dev=0), dict(workspace_dev=GOOD * 4 + 8), dict(workspace_bytes=0, max_kv=4096), dict(workspace_bytes=16384, max_kv=4096),
+        dict(kv_len_dev=GOOD + 2), dict(pages_dev=GOOD + 1), dict(q_start_dev=GOOD + 2))]
 )
 
 
@@ -175,7 +175,30 @@ def test_calls_with_nothing_to_do():
 
 
 def test_workspace_grows_with_the_work_and_needs_no_device():
-    d = spp.make_attn_desc(32, 4, 128, 64, 100)
-    small, large = spp.spp_kv4_attend_workspace(d, 1, 1, 100), spp.spp_kv4_attend_workspace(d, 1, 1, 100000)
-    assert 0 < small <= large < (1 << 28)
-    assert ctypes.c_size_t(large).value == large
+    sizes = [1, 2, 3, 7, 16, 17, 64, 300, 5000]
+    for heads, kv_heads, dim in ((32, 4, 128), (8, 8, 64), (16, 1, 128)):
+        d = spp.make_attn_desc(heads, kv_heads, dim, 64, 100)
+        for n in sizes:
+            for q in sizes:
+                for kv in (0, 200, 1000, 100000):
+                    need = spp.spp_kv4_attend_workspace(d, n, q, kv)
+                    assert 0 < need < (1 << 27)
+                    # never less for more
+                    assert need >= spp.spp_kv4_attend_workspace(d, max(1, n // 2), max(1, q // 3), kv // 2)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_a_workspace_is_enough_for_every_smaller_call(dtype):
+    """A call whose workspace is too small says so before anything else is found wrong with the device."""
+    rng = np.random.default_rng(0)
+    for _ in range(400):
+        kv_heads = int(rng.integers(1, 9))
+        d = spp.make_attn_desc(kv_heads * int(rng.integers(1, 9)), kv_heads, int(rng.choice([64, 128])), 16, 4)
+        n, q, kv = (int(np.exp(rng.uniform(0, np.log(m)))) for m in (2000, 600, 200000))
+        need = spp.spp_kv4_attend_workspace(d, n, q, kv)
+        small = [max(1, int(v * f)) for v, f in zip((n, q, kv), rng.uniform(0, 1, size=3))]
+        row = d.n_heads * d.head_dim
+        with pytest.raises(spp.SppError) as e:
+            spp.spp_kv4_attend(d, GOOD, dtype, GOOD, row, GOOD, GOOD, GOOD, 1, small[0], 1, small[1], small[2], True, 0.1,
+                               GOOD * 64, row, GOOD * 4, need)
+        assert "workspace" not in str(e.value), (d.n_heads, kv_heads, n, q, kv, small)

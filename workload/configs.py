@@ -67,6 +67,18 @@ class MoEConfig:
     # layer's update of the residual stream relative to the stream itself.
     router_rank: int = 0
     update_scale: float = 1.0
+    # attention in front of every layer (attn_heads > 0; without has_proj): query
+    # and key/value heads of head_dim elements over a 4-bit cache of kv_tokens
+    # tokens a sequence in pages of kv_page, rotary positions over as many axes
+    # as rotary_sections has entries (frequencies of each)
+    attn_heads: int = 0
+    attn_kv_heads: int = 1
+    head_dim: int = 128
+    kv_page: int = 64
+    kv_tokens: int = 4096
+    rotary_sections: Tuple[int, ...] = (24, 20, 20)
+    rotary_interleaved: bool = True
+    rotary_theta: float = 1e6
 
     @property
     def elem_bytes(self) -> int:

@@ -24,6 +24,8 @@ checkpoints; neither is available, so synthetic stand-ins take their place):
 * 4-bit experts (codec "q4"): codes q = clip(round(N(0, 2.5^2)), -8, 7) + 8
   and per-block fp16 scales w_std/2.5 * U(0.75, 1.25), drawn directly (the
   codec is the workload's weight format; nothing is quantised here);
+* attention (attn_heads > 0): W_qkv and W_o like the projection, rotary
+  frequencies theta^(-i/F);
 * layer-0 hidden states: an AR(1) sequence per batch element,
   h_0 = e_0, h_t = rho h_{t-1} + sigma e_t with e_t ~ N(0, I), built in fp64 and
   stored in the config dtype.
@@ -49,6 +51,8 @@ KIND_Q4_CODES = 12
 KIND_Q4_SCALES = 13
 KIND_SHARED_Q4_CODES = 14
 KIND_SHARED_Q4_SCALES = 15
+KIND_QKV = 16
+KIND_ATTN_OUT = 17
 
 
 def _rng(cfg: MoEConfig, kind: int, layer: int, index: int = 0) -> np.random.Generator:
@@ -129,6 +133,19 @@ def shared_expert_weights(cfg: MoEConfig, layer: int, j: int):
 def proj_weight(cfg: MoEConfig, layer: int) -> np.ndarray:
     """Dense stand-in projection of a layer (in place of attention), [D, D]."""
     return _normal_weights(cfg, KIND_PROJ, layer, 0, (cfg.D, cfg.D))
+
+
+def attention_weights(cfg: MoEConfig, layer: int):
+    """(W_qkv [(heads + 2 kv_heads) head_dim, D], W_o [D, heads head_dim]) of a layer's attention."""
+    q, kv = cfg.attn_heads * cfg.head_dim, cfg.attn_kv_heads * cfg.head_dim
+    return (_normal_weights(cfg, KIND_QKV, layer, 0, (q + 2 * kv, cfg.D)),
+            _normal_weights(cfg, KIND_ATTN_OUT, layer, 0, (cfg.D, q)))
+
+
+def rotary_frequencies(cfg: MoEConfig) -> np.ndarray:
+    """theta^(-i/F), i < F, fp32."""
+    F = sum(cfg.rotary_sections)
+    return (cfg.rotary_theta ** (-np.arange(F) / max(F, 1))).astype(np.float32)
 
 
 def _stored_values(cfg: MoEConfig, a: np.ndarray) -> np.ndarray:
