@@ -373,6 +373,48 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int p, int b, int
   return at;
 }
 
+// What a workgroup works on: rows row0 .. last of a sequence's key/value head,
+// and of its tiles [begin, end), one of `parts` parts.
+struct Spot {
+  Seq seq;
+  int b, h, rt, split, parts, row0, last, begin, end;
+  size_t part;  // index of its partial rows
+};
+
+// False: nothing to do (the whole workgroup alike).  rows: rows per workgroup.
+__device__ __forceinline__ bool find_spot(const AttendArgs& a, int rows, int lane, Spot& s) {
+  int p = 0, each = 1 << 30;
+  s.split = 0;
+  if (a.units > 0) {
+    const int plane = static_cast<int>(blockIdx.x) % a.planes;
+    p = static_cast<int>(blockIdx.x) / a.planes;
+    s.h = plane % a.Hkv, s.rt = plane / a.Hkv;
+    const Place at = place_of(a, p, -1, lane);
+    if (at.b < 0) return false;
+    s.b = at.b, s.split = p - at.base, each = at.each;
+  } else {
+    // the row tiles of one sequence and head are a multiple of 8 workgroups
+    // apart, which brings them to one XCD and the cached rows into its L2; the
+    // rows that see most go first
+    const int heads = a.n_seq * a.Hkv, step = a.row_tiles > 1 ? (heads + 7) / 8 * 8 : heads;
+    const int bh = static_cast<int>(blockIdx.x) % step;
+    if (bh >= heads) return false;
+    s.rt = a.row_tiles - 1 - static_cast<int>(blockIdx.x) / step;
+    s.b = bh / a.Hkv, s.h = bh - s.b * a.Hkv;
+  }
+  s.seq = sequence(a, s.b);
+  const int nrows = s.seq.nq * a.G;
+  s.row0 = s.rt * rows;
+  if (s.row0 >= nrows) return false;
+  s.last = min(s.row0 + rows, nrows) - 1;
+  const int tiles = (s.seq.limit(a, s.last) + kTile - 1) / kTile;
+  s.parts = max(1, static_cast<int>((static_cast<uint32_t>(tiles) + each - 1) / static_cast<uint32_t>(each)));
+  if (s.split >= s.parts) return false;
+  s.begin = s.split * each, s.end = min(tiles, s.begin + each);
+  s.part = static_cast<size_t>(s.rt * a.Hkv + s.h) * (a.units + a.n_seq) + p;
+  return true;
+}
+
 // Two floats (8-byte aligned) written and read at agent scope
 __device__ __forceinline__ void put2(float* p, float x, float y) {
   const uint64_t v = static_cast<uint64_t>(__float_as_uint(y)) << 32 | __float_as_uint(x);
@@ -491,6 +533,71 @@ __device__ __forceinline__ void value_frags(const uint32_t* w, const float* sc, 
   if constexpr (B + 1 < D / 32) value_frags<D, B + 1>(w, sc, frag);
 }
 
+// The B operand of K Q^T for one row: step j covers elements g*D/4 + 8j ..
+template <typename T, int D, int NS>
+__device__ __forceinline__ void load_query(const AttendArgs& a, const Seq& seq, int h, int row, int g,
+                                           u32x4 (&qf)[NS][D / 32]) {
+  const int tok = row / a.G, hq = h * a.G + row - tok * a.G;
+  const T* qp = reinterpret_cast<const T*>(a.q) + static_cast<int64_t>(seq.q0 + tok) * a.q_stride + hq * D + g * (D / 4);
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j) {
+    if constexpr (NS == 1) {
+      qf[0][j] = *reinterpret_cast<const u32x4*>(qp + 8 * j);
+    } else {
+      float f[8];
+      load8(qp + 8 * j, f);
+      u32x4 terms[NS];
+      split8<NS>(f, terms);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) qf[s][j] = terms[s];
+    }
+  }
+}
+
+// A tile's scores (masked ones -inf) to the probabilities of the value
+// product, relative to the running maximum m; l and o follow where it moves.
+template <int D, int R, int NS>
+__device__ __forceinline__ void probabilities(const f32x4 (&s)[R][2], float scale_log2, float (&m)[R], f32x4 (&l)[R],
+                                              f32x4 (&o)[R][D / 16], u32x4 (&pf)[R][NS]) {
+  const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+  float top[R];
+  bool moves = false;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    top[r] = s[r][0][0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) top[r] = fmaxf(top[r], s[r][k / 4][k % 4]);
+    top[r] *= scale_log2;
+    moves |= top[r] > m[r] + 8.f;
+  }
+  // The running maximum moves only when a score passes it by 2^8: the
+  // probabilities stay below 2^8, far from fp32's range, and most steps
+  // neither reduce across lanes nor rescale.
+  if (__any(moves)) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      top[r] = fmaxf(top[r], __shfl_xor(top[r], 16));
+      top[r] = fmaxf(top[r], __shfl_xor(top[r], 32));
+      const float now = top[r] > m[r] + 8.f ? top[r] : m[r];  // a row's bits do not depend on the rows beside it
+      const float alpha = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[r] - now);
+      m[r] = now;
+      l[r] *= alpha;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) o[r][n] *= alpha;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float ref = m[r] == -INFINITY ? 0.f : m[r];  // nothing seen yet: every power is 0
+    float p[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(fmaf(s[r][k / 4][k % 4], scale_log2, -ref));
+    split8<NS>(p, pf[r]);
+#pragma unroll
+    for (int k = 0; k < NS; ++k) l[r] = mfma(ones, pf[r][NS - 1 - k], l[r]);
+  }
+}
+
 template <typename T>
 __device__ __forceinline__ T* out_row(const AttendArgs& a, const Seq& seq, int h, int row, int d) {
   const int tok = row / a.G, hq = h * a.G + row - tok * a.G;
@@ -528,7 +635,7 @@ __device__ __forceinline__ void store_n(T* p, const float* y) {
 // Workgroups per compute unit (waves per SIMD) that the registers of a variant
 // leave without spilling.
 constexpr int resident(bool f32, int d, int R) {
-  const int w = R == 1 ? 4 : (R == 2 ? 2 : 1);
+  const int w = R == 1 ? 4 : 2;
   return f32 && d == 128 && w > 1 ? w / 2 : w;
 }
 
@@ -581,35 +688,13 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
-  int b, h, rt, p = 0, split = 0, each = 1 << 30;
-  if (a.units > 0) {
-    const int plane = static_cast<int>(blockIdx.x) % a.planes;
-    p = static_cast<int>(blockIdx.x) / a.planes;
-    h = plane % a.Hkv, rt = plane / a.Hkv;
-    const Place at = place_of(a, p, -1, lane);
-    if (at.b < 0) return;
-    b = at.b, split = p - at.base, each = at.each;
-  } else {
-    // the row tiles of one sequence and head are a multiple of 8 workgroups
-    // apart, which brings them to one XCD and the cached rows into its L2; the
-    // rows that see most go first
-    const int heads = a.n_seq * a.Hkv, step = a.row_tiles > 1 ? (heads + 7) / 8 * 8 : heads;
-    const int bh = static_cast<int>(blockIdx.x) % step;
-    if (bh >= heads) return;
-    rt = a.row_tiles - 1 - static_cast<int>(blockIdx.x) / step;
-    b = bh / a.Hkv, h = bh - b * a.Hkv;
-  }
-  const Seq seq = sequence(a, b);
-  const int nrows = seq.nq * a.G, row0 = rt * kRows;
-  if (row0 >= nrows) return;
-  const int last = min(row0 + kRows, nrows) - 1;
+  Spot at;
+  if (!find_spot(a, kRows, lane, at)) return;
+  const Seq& seq = at.seq;
+  const int h = at.h, row0 = at.row0, last = at.last, parts = at.parts, begin = at.begin, end = at.end;
   const int lim_min = seq.limit(a, row0), lim_max = seq.limit(a, last);
-  const int tiles = (lim_max + kTile - 1) / kTile;
-  const int parts = max(1, static_cast<int>((static_cast<uint32_t>(tiles) + each - 1) / static_cast<uint32_t>(each)));
-  if (split >= parts) return;
-  const int begin = split * each, end = min(tiles, begin + each);
 
-  const int32_t* pages = a.pages + static_cast<int64_t>(b) * a.pages_stride;
+  const int32_t* pages = a.pages + static_cast<int64_t>(at.b) * a.pages_stride;
   const uint8_t* head = a.cache.base + static_cast<uint64_t>(h) * a.cache.head_bytes;
   // two steps ahead the page ids, one step ahead the codes and scales
   int tile = begin + wave;
@@ -618,31 +703,15 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
   if (tile < end) load_tile<D>(a, head, pid, tile * kTile, c, g, next);
   pid = page_ids(a, pages, (tile + W) * kTile, c, g);
 
-  // queries: the B operand of K Q^T; step j covers elements g*D/4 + 8j ..
   u32x4 qf[R][NS][KW];
   int limit[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = min(row0 + r * 16 + c, last);  // rows past the last repeat it and are not stored
     limit[r] = seq.limit(a, row);
-    const int tok = row / a.G, hq = h * a.G + row - tok * a.G;
-    const T* qp = reinterpret_cast<const T*>(a.q) + static_cast<int64_t>(seq.q0 + tok) * a.q_stride + hq * D + g * (D / 4);
-#pragma unroll
-    for (int j = 0; j < KW; ++j) {
-      if constexpr (NS == 1) {
-        qf[r][0][j] = *reinterpret_cast<const u32x4*>(qp + 8 * j);
-      } else {
-        float f[8];
-        load8(qp + 8 * j, f);
-        u32x4 terms[NS];
-        split8<NS>(f, terms);
-#pragma unroll
-        for (int s = 0; s < NS; ++s) qf[r][s][j] = terms[s];
-      }
-    }
+    load_query<T, D, NS>(a, seq, h, row, g, qf[r]);
   }
 
-  const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
   f32x4 o[R][NT], l[R];  // l: every element the sum of its row's probabilities, as rounded for the product
   float m[R];
 #pragma unroll
@@ -690,43 +759,8 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
           for (int e = 0; e < 4; ++e)
             if (t0 + 8 * g + 4 * i + e >= limit[r]) s[r][i][e] = -INFINITY;
     }
-    float top[R];
-    bool moves = false;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      top[r] = s[r][0][0];
-#pragma unroll
-      for (int k = 1; k < 8; ++k) top[r] = fmaxf(top[r], s[r][k / 4][k % 4]);
-      top[r] *= a.scale_log2;
-      moves |= top[r] > m[r] + 8.f;
-    }
-    // The running maximum moves only when a score passes it by 2^8: the
-    // probabilities stay below 2^8, far from fp32's range, and most steps
-    // neither reduce across lanes nor rescale.
-    if (__any(moves)) {
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        top[r] = fmaxf(top[r], __shfl_xor(top[r], 16));
-        top[r] = fmaxf(top[r], __shfl_xor(top[r], 32));
-        const float now = top[r] > m[r] + 8.f ? top[r] : m[r];  // a row's bits do not depend on the rows beside it
-        const float alpha = m[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[r] - now);
-        m[r] = now;
-        l[r] *= alpha;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) o[r][n] *= alpha;
-      }
-    }
     u32x4 pf[R][NS];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const float ref = m[r] == -INFINITY ? 0.f : m[r];  // nothing seen yet: every power is 0
-      float p[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(fmaf(s[r][k / 4][k % 4], a.scale_log2, -ref));
-      split8<NS>(p, pf[r]);
-#pragma unroll
-      for (int k = 0; k < NS; ++k) l[r] = mfma(ones, pf[r][NS - 1 - k], l[r]);
-    }
+    probabilities<D, R, NS>(s, a.scale_log2, m, l, o, pf);
 
     float sc[8];
 #pragma unroll
@@ -773,8 +807,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
 
   // the waves' sums join: weights 2^(m_w - max m)
   const size_t part_floats = static_cast<size_t>(kRows) * (D + 2);  // [rows][D] sums, then [rows] maximum, sum
-  float* plane_parts = a.part + static_cast<size_t>(rt * a.Hkv + h) * (a.units + a.n_seq) * part_floats;
-  float* part = plane_parts + static_cast<size_t>(p) * part_floats;
+  float* part = a.part + at.part * part_floats;
   constexpr int kPer = 16 * D / (64 * W), kThr = D / kPer;  // elements per thread, threads per row
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -792,7 +825,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
     __syncthreads();
     const int rr = threadIdx.x / kThr, e0 = (threadIdx.x % kThr) * kPer;
     const int row = row0 + r * 16 + rr;
-    if (row >= nrows) continue;
+    if (row > last) continue;
     float top = s_m[0][rr];
 #pragma unroll
     for (int w = 1; w < W; ++w) top = fmaxf(top, s_m[w][rr]);
@@ -808,16 +841,16 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
       for (int k = 0; k < kPer; ++k) y[k] += f * s_o[w][rr][e0 + k];
     }
     if (parts > 1) {
-      const int at = r * 16 + rr;
-      float* to = part + at * D + e0;
+      const int ri = r * 16 + rr;
+      float* to = part + ri * D + e0;
       if (a.join_apart) {
 #pragma unroll
         for (int k = 0; k < kPer; k += 4) *reinterpret_cast<f32x4*>(to + k) = f32x4{y[k], y[k + 1], y[k + 2], y[k + 3]};
-        if (e0 == 0) *reinterpret_cast<float2*>(part + kRows * D + 2 * at) = make_float2(top, sum);
+        if (e0 == 0) *reinterpret_cast<float2*>(part + kRows * D + 2 * ri) = make_float2(top, sum);
       } else {
 #pragma unroll
         for (int k = 0; k < kPer; k += 2) put2(to + k, y[k], y[k + 1]);
-        if (e0 == 0) put2(part + kRows * D + 2 * at, top, sum);
+        if (e0 == 0) put2(part + kRows * D + 2 * ri, top, sum);
       }
       continue;
     }
@@ -833,7 +866,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
-    unsigned* count = a.count + static_cast<size_t>(rt * a.Hkv + h) * a.n_seq + b;
+    unsigned* count = a.count + static_cast<size_t>(at.rt * a.Hkv + h) * a.n_seq + at.b;
     const unsigned before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (before + 1 >= static_cast<unsigned>(parts)) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     s_done = before + 1;
@@ -841,20 +874,20 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
   __syncthreads();
   const unsigned done = __builtin_amdgcn_readfirstlane(s_done);
   if (done < static_cast<unsigned>(parts)) return;
-  const float* all = part - static_cast<size_t>(split) * part_floats;
+  const float* all = part - static_cast<size_t>(at.split) * part_floats;
   constexpr int kCols = D / 4, kSlots = 64 * W / kCols;  // a slot of threads takes a row of a group of parts
   const int slot = threadIdx.x / kCols, col = threadIdx.x % kCols, rows = last - row0 + 1;
   const int groups = max(1, kSlots / rows);
   float* s_y = &s_o[0][0][0];  // [kSlots][D]
   float *s_sum = &s_l[0][0], *s_top = &s_m[0][0];
   static_assert(sizeof(s_o) >= sizeof(float) * kSlots * D && sizeof(s_l) >= sizeof(float) * kSlots, "join buffers");
-  for (int at = groups > 1 ? slot % rows : slot, grp = groups > 1 ? slot / rows : 0; at < rows; at += kSlots) {
+  for (int ri = groups > 1 ? slot % rows : slot, grp = groups > 1 ? slot / rows : 0; ri < rows; ri += kSlots) {
     Joined<4> j;
     if (grp < groups)
       j.template take<8>(parts, grp, groups, [&](int k, float2& ml, float* v) {
         const float* from = all + k * part_floats;
-        ml = get2(from + kRows * D + 2 * at);
-        const float2 lo = get2(from + at * D + 4 * col), hi = get2(from + at * D + 4 * col + 2);
+        ml = get2(from + kRows * D + 2 * ri);
+        const float2 lo = get2(from + ri * D + 4 * col), hi = get2(from + ri * D + 4 * col + 2);
         v[0] = lo.x, v[1] = lo.y, v[2] = hi.x, v[3] = hi.y;
       });
     if (groups > 1) {
@@ -872,22 +905,223 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
       j = whole;
     }
     // a count beyond the parts: the workspace was not zero, and nothing is known of the parts
-    finish<T, 4>(a, seq, h, row0 + at, D, 4 * col, done > static_cast<unsigned>(parts) ? NAN : j.sum, j.y);
+    finish<T, 4>(a, seq, h, row0 + ri, D, 4 * col, done > static_cast<unsigned>(parts) ? NAN : j.sum, j.y);
   }
 }
 
-// Joins the parts of one row: one workgroup per (row, head and sequence).  A
-// wave takes every W-th part, its loads all in flight at once, since this
-// kernel is bound by their latency; then the waves' sums join.
-constexpr int kJoinWaves = 16, kJoinBatch = 16;
+// Many rows (a prompt's tokens): 16 R rows a wave, 8 waves a workgroup.  The
+// waves form the operands of a step's two tiles together, each its share of
+// the codes, straight in the order in which lanes read them from LDS; then
+// every wave multiplies them with its own rows.  Two buffers, one barrier a
+// step: while one step is multiplied, the next one's codes are on their way.
+constexpr int kRowWaves = 8;
+
+template <int D>
+struct RawStep {
+  uint32_t k[D / 64];  // the lane's words of one token's key codes
+  uint32_t ks;
+  uint32_t v[8];       // one byte of each of 8 tokens' value codes
+  u32x2 vs;
+};
+
 template <typename T, int D, int R>
-__global__ __launch_bounds__(64 * kJoinWaves) void kv4_join_kernel(AttendArgs a) {
-  constexpr int kRows = 16 * R, kPer = D / 64, W = kJoinWaves;
+__global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(AttendArgs a) {
+  constexpr int W = kRowWaves;
+  constexpr int NS = std::is_same<T, float>::value ? 3 : 1;
+  constexpr int KW = D / 32, NT = D / 16;
+  constexpr int kRows = 16 * R * W;
+  __shared__ u32x4 s_k[2][2][2 * KW][64];  // buffer, tile, (half of the tile's tokens, step over elements), lane
+  __shared__ u32x4 s_v[2][2][NT][64];
+  __shared__ int s_poisoned[D / 32];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  Spot at;
+  if (!find_spot(a, kRows, lane, at)) return;
+  const Seq& seq = at.seq;
+  if (threadIdx.x < D / 32) s_poisoned[threadIdx.x] = INT32_MAX;
+  const int lim_all = seq.limit(a, at.last);
+  const int row0 = at.row0 + wave * 16 * R, last = min(row0 + 16 * R - 1, at.last);
+  const bool mine = row0 <= at.last;
+  const int lim_min = mine ? seq.limit(a, row0) : 0, lim_max = mine ? seq.limit(a, last) : 0;
+
+  const int32_t* pages = a.pages + static_cast<int64_t>(at.b) * a.pages_stride;
+  const uint8_t* head = a.cache.base + static_cast<uint64_t>(at.h) * a.cache.head_bytes;
+  // this wave's share of a step: of tile wave / 4 the keys of half (wave / 2) % 2, every second pair of their words,
+  // and the values' byte wave % 4
+  const int share = wave >> 2, half = (wave >> 1) & 1, part_k = wave & 1, byte_v = wave & 3;
+  const auto load = [&](Pids pid, int t0, RawStep<D>& x) {
+    const int page = a.cache.page;
+    const bool kbad = static_cast<uint32_t>(pid.k) >= static_cast<uint32_t>(a.cache.n_pages);
+    const bool vbad = static_cast<uint32_t>(pid.v) >= static_cast<uint32_t>(a.cache.n_pages);
+    const uint8_t* kb = head + static_cast<uint64_t>(kbad ? 0 : pid.k) * a.cache.page_bytes;
+    const uint8_t* vb = head + static_cast<uint64_t>(vbad ? 0 : pid.v) * a.cache.page_bytes;
+    const int ko = (t0 + (c >> 2) * 8 + (c & 3) + 4 * half) & (page - 1), vo = (t0 + g * 8) & (page - 1);
+    const uint8_t* kp = kb + Block<D>::codes(page, 0, ko) + g * (D / 8) + part_k * (D / 16);
+    if constexpr (D == 128) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(kp);
+      x.k[0] = w[0], x.k[1] = w[1];
+    } else {
+      x.k[0] = *reinterpret_cast<const uint32_t*>(kp);
+    }
+    const uint32_t byte = kb[Block<D>::scales(page, 0, g * (D / 4) / 32, ko)];
+    x.ks = kbad ? static_cast<uint32_t>(kNanByte) : byte;
+    if (byte_v < D / 32) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x.v[j] = vb[Block<D>::codes(page, 1, vo + j) + c * (D / 32) + byte_v];
+      x.vs = *reinterpret_cast<const u32x2*>(vb + Block<D>::scales(page, 1, c * (D / 16) / 32, vo));
+    }
+  };
+  // Values that are not finite go in as zeros, whoever sees them, and rows that
+  // see one of a block's get their NaN at the end: the first such token is
+  // enough to know, since a row sees all tokens up to its limit.
+  int poisoned = INT32_MAX;
+  const auto form = [&](const RawStep<D>& x, int t0, int buf) {
+    const float ks = scale_of(x.ks);
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) s_k[buf][share][half * KW + part_k * (D / 64) + j][lane] = cvt8(x.k[j], ks);
+    if (byte_v < D / 32) {
+      uint32_t v[8];
+#pragma unroll
+      for (int j = 7; j >= 0; --j) {
+        const uint32_t byte = (x.vs[j / 4] >> (8 * (j % 4))) & 255u;
+        const bool special = byte > kMaxByte;
+        const int token = t0 + 8 * g + j;
+        if (special && token < lim_all) poisoned = min(poisoned, token);
+        v[j] = cvt2<0>(special ? 0u : x.v[j], scale_of(special ? 127u : byte));
+      }
+      u32x4 lo, hi;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        lo[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x05040100u);
+        hi[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x07060302u);
+      }
+      s_v[buf][share][2 * byte_v][lane] = lo;
+      s_v[buf][share][2 * byte_v + 1][lane] = hi;
+    }
+  };
+
+  RawStep<D> raw;
+  int tile = at.begin;
+  const auto ids = [&](int step_tile) { return page_ids(a, pages, (step_tile + share) * kTile, c, g); };
+  load(ids(tile), (tile + share) * kTile, raw);
+  Pids pid = ids(tile + 2);
+
+  u32x4 qf[R][NS][KW];
+  int limit[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = min(row0 + r * 16 + c, at.last);
+    limit[r] = seq.limit(a, row);
+    load_query<T, D, NS>(a, seq, at.h, row, g, qf[r]);
+  }
+  f32x4 o[R][NT], l[R];
+  float m[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = -INFINITY;
+    l[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < NT; ++n) o[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  form(raw, (tile + share) * kTile, 0);
+  if (tile + 2 < at.end) {
+    load(pid, (tile + 2 + share) * kTile, raw);
+    pid = ids(tile + 4);
+  }
+  __syncthreads();
+  for (int buf = 0; tile < at.end; tile += 2, buf ^= 1) {
+#pragma unroll
+    for (int i2 = 0; i2 < 2; ++i2) {
+      const int t0 = (tile + i2) * kTile;
+      if (t0 >= lim_max) break;  // nothing of it is seen by this wave's rows
+      f32x4 s[R][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < KW; ++j) {
+          const u32x4 kf = s_k[buf][i2][i * KW + j][lane];
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int n = 0; n < NS; ++n) s[r][i] = mfma(kf, qf[r][NS - 1 - n][j], s[r][i]);
+        }
+      }
+      if (t0 + kTile > lim_min) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (t0 + 8 * g + 4 * i + e >= limit[r]) s[r][i][e] = -INFINITY;
+      }
+      u32x4 pf[R][NS];
+      probabilities<D, R, NS>(s, a.scale_log2, m, l, o, pf);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const u32x4 vf = s_v[buf][i2][n][lane];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int k = 0; k < NS; ++k) o[r][n] = mfma(vf, pf[r][NS - 1 - k], o[r][n]);
+      }
+    }
+    if (tile + 2 < at.end) {
+      form(raw, (tile + 2 + share) * kTile, buf ^ 1);
+      if (tile + 4 < at.end) {
+        load(pid, (tile + 4 + share) * kTile, raw);
+        pid = ids(tile + 6);
+      }
+    }
+    __syncthreads();
+  }
+
+  // this lane's sums are of block g (D = 128) or g / 2
+  if (poisoned != INT32_MAX) atomicMin(&s_poisoned[c * (D / 16) / 32], poisoned);
+  __syncthreads();
+  const int first = s_poisoned[g * (D / 4) / 32];
+  constexpr size_t kPartFloats = static_cast<size_t>(kRows) * (D + 2);
+  float* part = a.part + at.part * kPartFloats;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int row = row0 + r * 16 + c, ri = row - at.row0;
+    if (row > at.last) continue;
+    const float sum = l[r][0];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {  // A row 4g + e is elements (4g + e) * NT + n
+      const int e0 = (4 * g + e) * NT;
+      float y[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) y[n] = first < limit[r] ? NAN : o[r][n][e];
+      if (at.parts > 1) {
+#pragma unroll
+        for (int n = 0; n < NT; n += 4)
+          *reinterpret_cast<f32x4*>(part + ri * D + e0 + n) = f32x4{y[n], y[n + 1], y[n + 2], y[n + 3]};
+      } else {
+        finish<T, NT>(a, seq, at.h, row, D, e0, sum, y);
+      }
+    }
+    if (at.parts > 1 && g == 0) *reinterpret_cast<float2*>(part + kRows * D + 2 * ri) = make_float2(m[r], sum);
+  }
+}
+
+// Joins the parts of rows.  W = 16: a workgroup of 16 waves per (row, head and
+// sequence), for many parts: a wave takes every 16th, and the waves' sums join.
+// W = 1: a wave per row, four rows a workgroup.  Bound by the latency of the
+// reads, so a wave has several parts' in flight at once.
+template <typename T, int D, int kRows, int W>
+__global__ __launch_bounds__(64 * (W == 1 ? 4 : W)) void kv4_join_kernel(AttendArgs a) {
+  constexpr int kPer = D / 64, kBatch = W == 1 ? 8 : 16;
   __shared__ float s_y[W][D], s_sum[W], s_m[W];
   const int heads = a.n_seq * a.Hkv;
-  const int bh = static_cast<int>(blockIdx.x) % heads, row = static_cast<int>(blockIdx.x) / heads;
-  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bh = static_cast<int>(blockIdx.x) % heads;
+  const int row = W == 1 ? static_cast<int>(blockIdx.x) / heads * 4 + wave : static_cast<int>(blockIdx.x) / heads;
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
   const Place at = place_of(a, 0, b, lane);
   const Seq seq = sequence(a, b);
   const int nrows = seq.nq * a.G;
@@ -899,24 +1133,27 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv4_join_kernel(AttendArgs a)
   constexpr size_t kStride = static_cast<size_t>(kRows) * (D + 2);
   const float* part = a.part + (static_cast<size_t>(rt * a.Hkv + h) * (a.units + a.n_seq) + at.base) * kStride;
   Joined<kPer> j;
-  j.template take<kJoinBatch>(parts, wave, W, [&](int k, float2& ml, float* v) {
+  j.template take<kBatch>(parts, W == 1 ? 0 : wave, W, [&](int k, float2& ml, float* v) {
     const float* from = part + k * kStride;
     ml = *reinterpret_cast<const float2*>(from + kRows * D + 2 * ri);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) v[i] = from[ri * D + lane * kPer + i];
   });
-  if (lane == 0) s_sum[wave] = j.sum, s_m[wave] = j.top;
+  if constexpr (W > 1) {
+    if (lane == 0) s_sum[wave] = j.sum, s_m[wave] = j.top;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) s_y[wave][lane * kPer + k] = j.y[k];
-  __syncthreads();
-  if (wave != 0) return;
-  Joined<kPer> whole;
-  whole.template take<W>(W, 0, 1, [&](int k, float2& ml, float* v) {
-    ml = make_float2(s_m[k], s_sum[k]);
+    for (int k = 0; k < kPer; ++k) s_y[wave][lane * kPer + k] = j.y[k];
+    __syncthreads();
+    if (wave != 0) return;
+    Joined<kPer> whole;
+    whole.template take<W>(W, 0, 1, [&](int k, float2& ml, float* v) {
+      ml = make_float2(s_m[k], s_sum[k]);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = s_y[k][lane * kPer + i];
-  });
-  finish<T, kPer>(a, seq, h, row, D, lane * kPer, whole.sum, whole.y);
+      for (int i = 0; i < kPer; ++i) v[i] = s_y[k][lane * kPer + i];
+    });
+    j = whole;
+  }
+  finish<T, kPer>(a, seq, h, row, D, lane * kPer, j.sum, j.y);
 }
 
 // ------------------------------------------------------------------ host side
@@ -1002,42 +1239,52 @@ void launch_load(const LoadArgs& a, int d, unsigned grid, hipStream_t st) {
 // and about how many parts a plane's cached tokens make.  Goes by the caller's
 // bounds alone, so that the workspace can be sized without a device.
 struct Cut {
-  int R, row_tiles, planes, units;
+  int form;  // 0: 16 rows, 1: 32 rows, whose waves share the tokens out; 2: kv4_attend_rows_kernel
+  int rows;  // rows per workgroup
+  int row_tiles, planes, units;
   bool join_apart;
 };
 
 constexpr int kCUs = 256;
 constexpr int kMinTiles = 2 * kWaves;
 constexpr int kFusedParts = 32;
+constexpr int kFewRows = 32;
 
 // The counters stand at the workspace's start and take the same room in every
 // call, so that no call's partial rows come to lie where another one counts.
 constexpr int kMaxItems = 4 * kCUs * 4;
 constexpr size_t kCountBytes = kMaxItems * sizeof(unsigned);
 
-// Sixteens of rows a workgroup takes of a sequence's `rows`
-int rows_per_group(bool f32, int d, int64_t rows) { return rows <= 16 ? 1 : (rows <= 32 || (f32 && d == 128) ? 2 : 4); }
+// Rows of a wave of kv4_attend_rows_kernel, in sixteens, by the registers of fp32's three terms
+constexpr int rows_r(bool f32, int d) { return f32 && d == 128 ? 1 : 2; }
+
+int form_of(int64_t rows) { return rows <= 16 ? 0 : (rows <= kFewRows ? 1 : 2); }
+
+int group_rows(bool f32, int d, int form) { return form == 2 ? 16 * kRowWaves * rows_r(f32, d) : 16 << form; }
+
+// Workgroups that fill the device
+int fill(bool f32, int d, int form) { return form == 2 ? kCUs : kCUs * resident(f32, d, 1 << form); }
 
 // Row tiles, over all sequences and heads, below which tokens are split
-int split_below(bool f32, int d, int R) { return std::min((R == 4 ? 2 : 4) * kCUs * resident(f32, d, R), kMaxItems); }
+int split_below(bool f32, int d, int form) { return form == 2 ? kCUs : std::min(4 * fill(f32, d, form), kMaxItems); }
 
 Cut cut_of(const spp_attn_desc* d, bool f32, int32_t n_seq, int32_t max_q, int32_t max_kv) {
   Cut c{};
   const int64_t rows = static_cast<int64_t>(max_q) * (d->n_heads / d->n_kv_heads);
-  c.R = rows_per_group(f32, d->head_dim, rows);
-  c.row_tiles = static_cast<int>((rows + 16 * c.R - 1) / (16 * c.R));
+  c.form = form_of(rows);
+  c.rows = group_rows(f32, d->head_dim, c.form);
+  c.row_tiles = static_cast<int>((rows + c.rows - 1) / c.rows);
   c.planes = d->n_kv_heads * c.row_tiles;
   const int64_t items = static_cast<int64_t>(n_seq) * c.planes;
-  const int fit = resident(f32, d->head_dim, c.R);
   const int64_t tiles = (static_cast<int64_t>(max_kv) + kTile - 1) / kTile;
-  if (items == 0 || tiles <= kMinTiles || items >= split_below(f32, d->head_dim, c.R)) return c;
-  c.units = static_cast<int>(std::max<int64_t>(1, kCUs * fit / c.planes - n_seq / 2));
-  c.join_apart = std::min<int64_t>(c.units / n_seq, tiles / kMinTiles) >= kFusedParts;
+  if (items == 0 || tiles <= kMinTiles || items >= split_below(f32, d->head_dim, c.form)) return c;
+  c.units = std::max(1, fill(f32, d->head_dim, c.form) / c.planes - n_seq / 2);
+  c.join_apart = c.form == 2 || std::min<int64_t>(c.units / n_seq, tiles / kMinTiles) >= kFusedParts;
   return c;
 }
 
 size_t part_bytes(const Cut& c, int32_t n_seq, int d) {
-  return c.units > 0 ? static_cast<size_t>(c.planes) * (c.units + n_seq) * (16 * c.R) * (d + 2) * sizeof(float) : 0;
+  return c.units > 0 ? static_cast<size_t>(c.planes) * (c.units + n_seq) * c.rows * (d + 2) * sizeof(float) : 0;
 }
 
 template <typename T, int D>
@@ -1047,18 +1294,18 @@ void launch_attend_d(const AttendArgs& a, const Cut& c, int64_t rows, hipStream_
   const dim3 grid(c.units > 0 ? static_cast<unsigned>(c.units + a.n_seq) * static_cast<unsigned>(c.planes)
                               : static_cast<unsigned>(c.row_tiles > 1 ? (heads + 7) / 8 * 8 : heads) *
                                     static_cast<unsigned>(c.row_tiles));
-  const dim3 join(static_cast<unsigned>(heads) * static_cast<unsigned>(rows));
-  const auto run = [&](auto r) {
-    constexpr int R = decltype(r)::value;
-    hipLaunchKernelGGL((kv4_attend_kernel<T, D, R>), grid, dim3(64 * kWaves), 0, st, a);
-    if (c.join_apart) hipLaunchKernelGGL((kv4_join_kernel<T, D, R>), join, dim3(64 * kJoinWaves), 0, st, a);
+  const auto run = [&](auto kernel, auto joining, int waves, int rows_each, int join_waves) {
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, st, a);
+    const dim3 join(static_cast<unsigned>(heads) * static_cast<unsigned>((rows + rows_each - 1) / rows_each));
+    if (c.join_apart) hipLaunchKernelGGL(joining, join, dim3(64 * join_waves), 0, st, a);
   };
-  if (c.R == 1)
-    run(std::integral_constant<int, 1>());
-  else if (c.R == 2)
-    run(std::integral_constant<int, 2>());
-  else if constexpr (!(f32 && D == 128))
-    run(std::integral_constant<int, 4>());
+  constexpr int kR = rows_r(f32, D);
+  if (c.form == 0)
+    run(kv4_attend_kernel<T, D, 1>, kv4_join_kernel<T, D, 16, 16>, kWaves, 1, 16);
+  else if (c.form == 1)
+    run(kv4_attend_kernel<T, D, 2>, kv4_join_kernel<T, D, 32, 16>, kWaves, 1, 16);
+  else
+    run(kv4_attend_rows_kernel<T, D, kR>, kv4_join_kernel<T, D, 16 * kRowWaves * kR, 1>, kRowWaves, 4, 4);
 }
 
 template <typename T>
@@ -1206,13 +1453,12 @@ extern "C" size_t spp_kv4_attend_workspace(const spp_attn_desc* desc, int32_t n_
   const int64_t rows = static_cast<int64_t>(max_q) * (desc->n_heads / desc->n_kv_heads);
   if ((static_cast<int64_t>(max_kv) + kTile - 1) / kTile <= kMinTiles) return most;
   for (bool f32 : {false, true})
-    for (int R : {1, 2, 4}) {
-      if (R > rows_per_group(f32, desc->head_dim, rows)) continue;
-      const bool longest = R == rows_per_group(f32, desc->head_dim, kMaxUnits);
-      const int64_t row_tiles = longest ? (rows + 16 * R - 1) / (16 * R) : 1;
-      const int64_t items = std::min<int64_t>(n_seq * desc->n_kv_heads * row_tiles, split_below(f32, desc->head_dim, R) - 1);
-      const int64_t parts = std::max<int64_t>(kCUs * resident(f32, desc->head_dim, R), items) + items;
-      most = std::max(most, kCountBytes + static_cast<size_t>(parts) * (16 * R) * (desc->head_dim + 2) * sizeof(float));
+    for (int form = 0; form <= form_of(rows); ++form) {
+      const int d = desc->head_dim, each = group_rows(f32, d, form);
+      const int64_t row_tiles = form == 2 ? (rows + each - 1) / each : 1;
+      const int64_t items = std::min<int64_t>(n_seq * desc->n_kv_heads * row_tiles, split_below(f32, d, form) - 1);
+      const int64_t parts = std::max<int64_t>(fill(f32, d, form), items) + items;
+      most = std::max(most, kCountBytes + static_cast<size_t>(parts) * each * (d + 2) * sizeof(float));
     }
   return most;
 }
