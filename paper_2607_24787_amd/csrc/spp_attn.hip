@@ -48,6 +48,17 @@ struct Block {
 
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// Byte j of 8 as a scale for cvt2, for which only the exponent field counts
+__device__ __forceinline__ float scale_byte(u32x2 w, int j) {
+  return __uint_as_float(j % 4 == 3 ? w[j / 4] >> 1 : w[j / 4] << (23 - 8 * (j % 4)));
+}
+
+// Whether a byte of w is kMaxByte or more (its upper six bits are ones)
+__device__ __forceinline__ bool high_byte(uint32_t w) {
+  const uint32_t u = ~w & 0xfcfcfcfcu;
+  return ((u - 0x01010101u) & ~u & 0x80808080u) != 0;
+}
+
 // Two codes of byte SEL of w to bf16, times the power of two in `scale`'s
 // exponent field (its other bits do not count; exponent 255 gives NaN).
 template <int SEL>
@@ -554,12 +565,11 @@ __device__ __forceinline__ void load_query(const AttendArgs& a, const Seq& seq, 
   }
 }
 
-// A tile's scores (masked ones -inf) to the probabilities of the value
-// product, relative to the running maximum m; l and o follow where it moves.
-template <int D, int R, int NS>
-__device__ __forceinline__ void probabilities(const f32x4 (&s)[R][2], float scale_log2, float (&m)[R], f32x4 (&l)[R],
-                                              f32x4 (&o)[R][D / 16], u32x4 (&pf)[R][NS]) {
-  const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+// The running maximum m over a tile's scores (masked ones -inf) too; l and o
+// follow where it moves.
+template <int D, int R>
+__device__ __forceinline__ void follow_maximum(const f32x4 (&s)[R][2], float scale_log2, float (&m)[R], f32x4 (&l)[R],
+                                               f32x4 (&o)[R][D / 16]) {
   float top[R];
   bool moves = false;
 #pragma unroll
@@ -586,6 +596,14 @@ __device__ __forceinline__ void probabilities(const f32x4 (&s)[R][2], float scal
       for (int n = 0; n < D / 16; ++n) o[r][n] *= alpha;
     }
   }
+}
+
+// A tile's scores to the probabilities of the value product, relative to the
+// maximum; l sums them as they are rounded for it.
+template <int R, int NS>
+__device__ __forceinline__ void probabilities(const f32x4 (&s)[R][2], float scale_log2, const float (&m)[R],
+                                              f32x4 (&l)[R], u32x4 (&pf)[R][NS]) {
+  const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const float ref = m[r] == -INFINITY ? 0.f : m[r];  // nothing seen yet: every power is 0
@@ -759,15 +777,13 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
           for (int e = 0; e < 4; ++e)
             if (t0 + 8 * g + 4 * i + e >= limit[r]) s[r][i][e] = -INFINITY;
     }
+    follow_maximum<D, R>(s, a.scale_log2, m, l, o);
     u32x4 pf[R][NS];
-    probabilities<D, R, NS>(s, a.scale_log2, m, l, o, pf);
+    probabilities<R, NS>(s, a.scale_log2, m, l, pf);
 
     float sc[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t w = t.vs[j / 4];
-      sc[j] = __uint_as_float(j % 4 == 3 ? w >> 1 : w << (23 - 8 * (j % 4)));  // only the exponent field counts
-    }
+    for (int j = 0; j < 8; ++j) sc[j] = scale_byte(t.vs, j);
     if (masked) {
       // Zero times a value that is not finite is NaN, so none goes into the
       // product of a tile with masked places: what no row sees may hold
@@ -912,15 +928,20 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
 // Many rows (a prompt's tokens): 16 R rows a wave, 8 waves a workgroup.  The
 // waves form the operands of a step's two tiles together, each its share of
 // the codes, straight in the order in which lanes read them from LDS; then
-// every wave multiplies them with its own rows.  Two buffers, one barrier a
-// step: while one step is multiplied, the next one's codes are on their way.
+// every wave multiplies them with its own rows.  One barrier a step: while one
+// step is multiplied, the codes of the next ones are on their way.  A tile's
+// scores are multiplied while the tile before it goes through the softmax, so
+// that the matrix cores and the vector units have work at the same time; the
+// keys are therefore formed two steps ahead, the values one.
 constexpr int kRowWaves = 8;
 
 template <int D>
-struct RawStep {
-  uint32_t k[D / 64];  // the lane's words of one token's key codes
+struct RawKeys {
+  uint32_t k[D / 64];  // the lane's words of one token's codes
   uint32_t ks;
-  uint32_t v[8];       // one byte of each of 8 tokens' value codes
+};
+struct RawValues {
+  uint32_t v[8];  // one byte of each of 8 tokens' codes
   u32x2 vs;
 };
 
@@ -930,7 +951,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
   constexpr int NS = std::is_same<T, float>::value ? 3 : 1;
   constexpr int KW = D / 32, NT = D / 16;
   constexpr int kRows = 16 * R * W;
-  __shared__ u32x4 s_k[2][2][2 * KW][64];  // buffer, tile, (half of the tile's tokens, step over elements), lane
+  __shared__ u32x4 s_k[3][2][2 * KW][64];  // buffer, tile, (half of the tile's tokens, step over elements), lane
   __shared__ u32x4 s_v[2][2][NT][64];
   __shared__ int s_poisoned[D / 32];
 
@@ -950,62 +971,79 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
   // this wave's share of a step: of tile wave / 4 the keys of half (wave / 2) % 2, every second pair of their words,
   // and the values' byte wave % 4
   const int share = wave >> 2, half = (wave >> 1) & 1, part_k = wave & 1, byte_v = wave & 3;
-  const auto load = [&](Pids pid, int t0, RawStep<D>& x) {
+  const auto load_keys = [&](int pid, int t0, RawKeys<D>& x) {
     const int page = a.cache.page;
-    const bool kbad = static_cast<uint32_t>(pid.k) >= static_cast<uint32_t>(a.cache.n_pages);
-    const bool vbad = static_cast<uint32_t>(pid.v) >= static_cast<uint32_t>(a.cache.n_pages);
-    const uint8_t* kb = head + static_cast<uint64_t>(kbad ? 0 : pid.k) * a.cache.page_bytes;
-    const uint8_t* vb = head + static_cast<uint64_t>(vbad ? 0 : pid.v) * a.cache.page_bytes;
-    const int ko = (t0 + (c >> 2) * 8 + (c & 3) + 4 * half) & (page - 1), vo = (t0 + g * 8) & (page - 1);
-    const uint8_t* kp = kb + Block<D>::codes(page, 0, ko) + g * (D / 8) + part_k * (D / 16);
+    const bool none = static_cast<uint32_t>(pid) >= static_cast<uint32_t>(a.cache.n_pages);
+    const uint8_t* kb = head + static_cast<uint64_t>(none ? 0 : pid) * a.cache.page_bytes;
+    const int off = (t0 + (c >> 2) * 8 + (c & 3) + 4 * half) & (page - 1);
+    const uint8_t* kp = kb + Block<D>::codes(page, 0, off) + g * (D / 8) + part_k * (D / 16);
     if constexpr (D == 128) {
       const u32x2 w = *reinterpret_cast<const u32x2*>(kp);
       x.k[0] = w[0], x.k[1] = w[1];
     } else {
       x.k[0] = *reinterpret_cast<const uint32_t*>(kp);
     }
-    const uint32_t byte = kb[Block<D>::scales(page, 0, g * (D / 4) / 32, ko)];
-    x.ks = kbad ? static_cast<uint32_t>(kNanByte) : byte;
-    if (byte_v < D / 32) {
+    const uint32_t byte = kb[Block<D>::scales(page, 0, g * (D / 4) / 32, off)];
+    x.ks = none ? static_cast<uint32_t>(kNanByte) : byte;
+  };
+  const auto load_values = [&](int pid, int t0, RawValues& x) {
+    if (byte_v >= D / 32) return;
+    const int page = a.cache.page;
+    const bool none = static_cast<uint32_t>(pid) >= static_cast<uint32_t>(a.cache.n_pages);
+    const uint8_t* vb = head + static_cast<uint64_t>(none ? 0 : pid) * a.cache.page_bytes;
+    const int off = (t0 + g * 8) & (page - 1);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x.v[j] = vb[Block<D>::codes(page, 1, vo + j) + c * (D / 32) + byte_v];
-      x.vs = *reinterpret_cast<const u32x2*>(vb + Block<D>::scales(page, 1, c * (D / 16) / 32, vo));
-    }
+    for (int j = 0; j < 8; ++j) x.v[j] = vb[Block<D>::codes(page, 1, off + j) + c * (D / 32) + byte_v];
+    x.vs = *reinterpret_cast<const u32x2*>(vb + Block<D>::scales(page, 1, c * (D / 16) / 32, off));
+  };
+  const auto form_keys = [&](const RawKeys<D>& x, int buf) {
+    const float ks = scale_of(x.ks);
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) s_k[buf][share][half * KW + part_k * (D / 64) + j][lane] = cvt8(x.k[j], ks);
   };
   // Values that are not finite go in as zeros, whoever sees them, and rows that
   // see one of a block's get their NaN at the end: the first such token is
   // enough to know, since a row sees all tokens up to its limit.
   int poisoned = INT32_MAX;
-  const auto form = [&](const RawStep<D>& x, int t0, int buf) {
-    const float ks = scale_of(x.ks);
+  const auto form_values = [&](const RawValues& x, int t0, int buf) {
+    if (byte_v >= D / 32) return;
+    uint32_t codes[8], v[8];
+    u32x2 vs = x.vs;
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) s_k[buf][share][half * KW + part_k * (D / 64) + j][lane] = cvt8(x.k[j], ks);
-    if (byte_v < D / 32) {
-      uint32_t v[8];
+    for (int j = 0; j < 8; ++j) codes[j] = x.v[j];
+    if (__any(high_byte(vs[0]) | high_byte(vs[1]))) {
 #pragma unroll
       for (int j = 7; j >= 0; --j) {
-        const uint32_t byte = (x.vs[j / 4] >> (8 * (j % 4))) & 255u;
-        const bool special = byte > kMaxByte;
         const int token = t0 + 8 * g + j;
-        if (special && token < lim_all) poisoned = min(poisoned, token);
-        v[j] = cvt2<0>(special ? 0u : x.v[j], scale_of(special ? 127u : byte));
+        if (((vs[j / 4] >> (8 * (j % 4))) & 255u) <= kMaxByte) continue;
+        if (token < lim_all) poisoned = min(poisoned, token);
+        codes[j] = 0u;
+        vs[j / 4] &= ~(128u << (8 * (j % 4)));
       }
-      u32x4 lo, hi;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        lo[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x05040100u);
-        hi[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x07060302u);
-      }
-      s_v[buf][share][2 * byte_v][lane] = lo;
-      s_v[buf][share][2 * byte_v + 1][lane] = hi;
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = cvt2<0>(codes[j], scale_byte(vs, j));
+    u32x4 lo, hi;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      lo[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x05040100u);
+      hi[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x07060302u);
+    }
+    s_v[buf][share][2 * byte_v][lane] = lo;
+    s_v[buf][share][2 * byte_v + 1][lane] = hi;
   };
 
-  RawStep<D> raw;
+  // where this wave's share of the step at `tile` starts, and the pages there
+  const auto start = [&](int tile) { return (tile + share) * kTile; };
+  const auto ids = [&](int tile) { return page_ids(a, pages, start(tile), c, g); };
   int tile = at.begin;
-  const auto ids = [&](int step_tile) { return page_ids(a, pages, (step_tile + share) * kTile, c, g); };
-  load(ids(tile), (tile + share) * kTile, raw);
-  Pids pid = ids(tile + 2);
+  RawKeys<D> rk, rk1;
+  RawValues rv;
+  Pids id = ids(tile), id1 = ids(tile + 2);
+  load_keys(id.k, start(tile), rk);
+  load_values(id.v, start(tile), rv);
+  load_keys(id1.k, start(tile + 2), rk1);
+  const Pids id2 = ids(tile + 4);
 
   u32x4 qf[R][NS][KW];
   int limit[R];
@@ -1025,58 +1063,134 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
     for (int n = 0; n < NT; ++n) o[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  form(raw, (tile + share) * kTile, 0);
-  if (tile + 2 < at.end) {
-    load(pid, (tile + 2 + share) * kTile, raw);
-    pid = ids(tile + 4);
-  }
+  form_keys(rk, 0);
+  form_values(rv, start(tile), 0);
+  form_keys(rk1, 1);
+  load_values(id1.v, start(tile + 2), rv);
+  load_keys(id2.k, start(tile + 4), rk);
+  id = id2;
+  id1 = ids(tile + 6);  // the next step's keys and the values behind them: read a step before they are needed
   __syncthreads();
-  for (int buf = 0; tile < at.end; tile += 2, buf ^= 1) {
+
+  const auto scores = [&](int buf, int i2, f32x4 (&s)[R][2]) {
 #pragma unroll
-    for (int i2 = 0; i2 < 2; ++i2) {
-      const int t0 = (tile + i2) * kTile;
-      if (t0 >= lim_max) break;  // nothing of it is seen by this wave's rows
-      f32x4 s[R][2];
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int r = 0; r < R; ++r) s[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < KW; ++j) {
-          const u32x4 kf = s_k[buf][i2][i * KW + j][lane];
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int n = 0; n < NS; ++n) s[r][i] = mfma(kf, qf[r][NS - 1 - n][j], s[r][i]);
-        }
-      }
-      if (t0 + kTile > lim_min) {
+      for (int j = 0; j < KW; ++j) {
+        const u32x4 kf = s_k[buf][i2][i * KW + j][lane];
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (t0 + 8 * g + 4 * i + e >= limit[r]) s[r][i][e] = -INFINITY;
-      }
-      u32x4 pf[R][NS];
-      probabilities<D, R, NS>(s, a.scale_log2, m, l, o, pf);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const u32x4 vf = s_v[buf][i2][n][lane];
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-          for (int k = 0; k < NS; ++k) o[r][n] = mfma(vf, pf[r][NS - 1 - k], o[r][n]);
+          for (int n = 0; n < NS; ++n) s[r][i] = mfma(kf, qf[r][NS - 1 - n][j], s[r][i]);
       }
     }
+  };
+  const auto hide = [&](int t0, f32x4 (&s)[R][2]) {
+    if (t0 + kTile > lim_min) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (t0 + 8 * g + 4 * i + e >= limit[r]) s[r][i][e] = -INFINITY;
+    }
+  };
+  // a wave has work as long as its rows see something of a tile
+  const auto seen = [&](int tile) { return tile < at.end && tile * kTile < lim_max; };
+  bool live = seen(tile);
+  f32x4 s[R][2], s2[R][2];  // by turns: the tile that is in the softmax, and the next one's
+  if (live) {
+    scores(0, 0, s);
+    hide(tile * kTile, s);
+    follow_maximum<D, R>(s, a.scale_log2, m, l, o);
+  }
+  // The operands' reads stand half a tile or more before their products, so
+  // that the waves, which are in step behind a barrier, do not all wait for LDS
+  // at once.  kh: the first half of the keys of the scores to come.
+  constexpr int QF = 2 * KW, kHalf = QF / 2, kEach = 8 * R / QF;  // kEach: powers behind each operand's products
+  u32x4 kh[kHalf];
+  const auto key = [&](int buf, int i2, int q) { return s_k[buf][i2][q % 2 * KW + q / 2][lane]; };  // halves by turns
+  const auto step = [&](int now, int kbuf, int vbuf, int i2, int after, f32x4 (&s)[R][2], f32x4 (&ahead)[R][2]) {
+    if (!live) return;
+    u32x4 kl[kHalf], vf[NT];
+#pragma unroll
+    for (int q = 0; q < kHalf; ++q) kl[q] = key(kbuf, 1 - i2, kHalf + q);
+    float ref[R], p[R][8];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      ref[r] = m[r] == -INFINITY ? 0.f : m[r];  // nothing seen yet: every power is 0
+#pragma unroll
+      for (int i = 0; i < 2; ++i) ahead[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < QF; ++q) {
+      const u32x4 kf = q < kHalf ? kh[q] : kl[q - kHalf];
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int n = 0; n < NS; ++n) ahead[r][q % 2] = mfma(kf, qf[r][NS - 1 - n][q / 2], ahead[r][q % 2]);
+#pragma unroll
+      for (int x = 0; x < kEach; ++x) {
+        const int at = q * kEach + x, r = at / 8, k = at % 8;
+        p[r][k] = __builtin_amdgcn_exp2f(fmaf(s[r][k / 4][k % 4], a.scale_log2, -ref[r]));
+        asm volatile("" : "+v"(p[r][k]));  // here, not where it is used
+      }
+      if (q == kHalf - 1) {
+#pragma unroll
+        for (int n = 0; n < NT / 2; ++n) vf[n] = s_v[vbuf][i2][n][lane];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int n = NT / 2; n < NT; ++n) vf[n] = s_v[vbuf][i2][n][lane];
+    u32x4 pf[R][NS];
+#pragma unroll
+    for (int r = 0; r < R; ++r) split8<NS>(p[r], pf[r]);
+    live = seen(now + 1);
+    if (live) hide((now + 1) * kTile, ahead);
+    const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int k = 0; k < NS; ++k) l[r] = mfma(ones, pf[r][NS - 1 - k], l[r]);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (n == NT / 2) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < kHalf; ++q) kh[q] = key(after, i2, q);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int k = 0; k < NS; ++k) o[r][n] = mfma(vf[n], pf[r][NS - 1 - k], o[r][n]);
+    }
+    if (live) follow_maximum<D, R>(ahead, a.scale_log2, m, l, o);
+  };
+  int kbuf = 0, knext = 1, kfree = 2;
+#pragma unroll
+  for (int q = 0; q < kHalf; ++q) kh[q] = key(kbuf, 1, q);
+  for (int vbuf = 0; tile < at.end; tile += 2, vbuf ^= 1) {
+    // the scores to come: tile 1 of this step, then tile 0 of the next, whose tile 1 follows
+    step(tile, kbuf, vbuf, 0, knext, s, s2);
+    step(tile + 1, knext, vbuf, 1, knext, s2, s);
     if (tile + 2 < at.end) {
-      form(raw, (tile + 2 + share) * kTile, buf ^ 1);
+      form_values(rv, start(tile + 2), vbuf ^ 1);
       if (tile + 4 < at.end) {
-        load(pid, (tile + 4 + share) * kTile, raw);
-        pid = ids(tile + 6);
+        form_keys(rk, kfree);
+        load_values(id.v, start(tile + 4), rv);
+        load_keys(id1.k, start(tile + 6), rk);
+        id = id1;
+        id1 = ids(tile + 8);
       }
     }
+    const int used = kbuf;
+    kbuf = knext, knext = kfree, kfree = used;
     __syncthreads();
   }
 
