@@ -29,7 +29,7 @@ constexpr int kMaxByte = 252;  // scale 2^125: 6 * 2^125 is the largest that is 
 
 struct Cache {
   const uint8_t* base;
-  uint64_t page_bytes;  // all heads of a page
+  uint32_t page_bytes;  // all heads of a page
   uint32_t head_bytes;  // one head of a page
   int page, shift;      // tokens per page and its logarithm
   int n_pages;
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(StoreArgs a) {
   const uint32_t w = quantise8(y, &byte);
   if (static_cast<uint64_t>(slot) >= static_cast<uint64_t>(a.cache.n_pages) << a.cache.shift) return;
   const int off = static_cast<int>(slot) & (a.cache.page - 1);
-  uint8_t* blk = const_cast<uint8_t*>(a.cache.base) + static_cast<uint64_t>(slot >> a.cache.shift) * a.cache.page_bytes +
+  uint8_t* blk = const_cast<uint8_t*>(a.cache.base) + static_cast<uint64_t>(slot >> a.cache.shift) * static_cast<uint64_t>(a.cache.page_bytes) +
                  static_cast<uint64_t>(h) * a.cache.head_bytes;
   *reinterpret_cast<uint32_t*>(blk + Block<D>::codes(a.cache.page, kind - 1, off) + e0 / 2) = w;
   if (e0 % 32 == 0) blk[Block<D>::scales(a.cache.page, kind - 1, e0 / 32, off)] = static_cast<uint8_t>(byte);
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(LoadArgs a) {
   const int64_t slot = a.slots[t];
   if (static_cast<uint64_t>(slot) >= static_cast<uint64_t>(a.cache.n_pages) << a.cache.shift) return;
   const int off = static_cast<int>(slot) & (a.cache.page - 1);
-  const uint8_t* blk = a.cache.base + static_cast<uint64_t>(slot >> a.cache.shift) * a.cache.page_bytes +
+  const uint8_t* blk = a.cache.base + static_cast<uint64_t>(slot >> a.cache.shift) * static_cast<uint64_t>(a.cache.page_bytes) +
                        static_cast<uint64_t>(h) * a.cache.head_bytes;
   const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + Block<D>::codes(a.cache.page, kv, off) + e0 / 2);
   const uint32_t byte = blk[Block<D>::scales(a.cache.page, kv, e0 / 32, off)];
@@ -480,48 +480,71 @@ struct Pids {
   int k, v;
 };
 
-__device__ __forceinline__ Pids page_ids(const AttendArgs& a, const int32_t* pages, int t0, int c, int g) {
-  const int ik = (t0 + (c >> 2) * 8) >> a.cache.shift, iv = (t0 + g * 8) >> a.cache.shift;
+__device__ __forceinline__ Pids page_ids(const AttendArgs& a, const int32_t* pages, int t0, int k, int v) {
+  const int ik = (t0 + k) >> a.cache.shift, iv = (t0 + v) >> a.cache.shift, room = static_cast<int>(a.pages_stride);
   Pids p;
-  p.k = ik < a.pages_stride ? pages[ik] : -1;
-  p.v = iv < a.pages_stride ? pages[iv] : -1;
+  p.k = ik < room ? pages[ik] : -1;
+  p.v = iv < room ? pages[iv] : -1;
   return p;
 }
 
+// A tile starts at a multiple of 32 tokens, so that a lane's place in a page is
+// the tile's, alike for all lanes, plus its own: where a lane reads is one
+// address for its own part, formed once, and a page and a tile added to it.
+__device__ __forceinline__ const uint8_t* in_page(const Cache& c, const uint8_t* own, int pid, uint32_t tile_bytes) {
+  return own + static_cast<uint64_t>(static_cast<uint32_t>(pid)) * c.page_bytes + tile_bytes;
+}
+
+__device__ __forceinline__ bool no_page(const Cache& c, int pid) {
+  return static_cast<uint32_t>(pid) >= static_cast<uint32_t>(c.n_pages);
+}
+
+// A lane's key tokens 8 (c/4) + c%4 (and 4 on), its value tokens from 8g
+__device__ __forceinline__ int key_token(int c) { return (c >> 2) * 8 + (c & 3); }
+
 template <int D>
-__device__ __forceinline__ void load_tile(const AttendArgs& a, const uint8_t* head, Pids pid, int t0, int c, int g,
-                                          Tile<D>& t) {
-  const int page = a.cache.page;
-  const bool kbad = static_cast<uint32_t>(pid.k) >= static_cast<uint32_t>(a.cache.n_pages);
-  const bool vbad = static_cast<uint32_t>(pid.v) >= static_cast<uint32_t>(a.cache.n_pages);
+struct TileLane {
+  const uint8_t *k, *ks, *v, *vs;
+
+  __device__ __forceinline__ TileLane(const Cache& cache, const uint8_t* head, int c, int g) {
+    const int page = cache.page, kt = key_token(c) & (page - 1), vt = (8 * g) & (page - 1);
+    k = head + Block<D>::codes(page, 0, kt) + g * (D / 8);
+    ks = head + Block<D>::scales(page, 0, g * (D / 4) / 32, kt);
+    v = head + Block<D>::codes(page, 1, vt) + c * (D / 32);
+    vs = head + Block<D>::scales(page, 1, c * (D / 16) / 32, vt);
+  }
+};
+
+template <int D>
+__device__ __forceinline__ void load_tile(const Cache& cache, const TileLane<D>& own, Pids pid, int t0, Tile<D>& t) {
   // a page that is none: its keys are NaN, which makes NaN of every row that
   // sees them; page 0 stands in for the loads
-  const uint8_t* kb = head + static_cast<uint64_t>(kbad ? 0 : pid.k) * a.cache.page_bytes;
-  const uint8_t* vb = head + static_cast<uint64_t>(vbad ? 0 : pid.v) * a.cache.page_bytes;
-  const int ko = (t0 + (c >> 2) * 8 + (c & 3)) & (page - 1), vo = (t0 + g * 8) & (page - 1);
+  const bool kbad = no_page(cache, pid.k);
+  const int kp = kbad ? 0 : pid.k, vp = no_page(cache, pid.v) ? 0 : pid.v;
+  const uint32_t u = static_cast<uint32_t>(t0 & (cache.page - 1));
+  const uint8_t *k = in_page(cache, own.k, kp, u * (D / 2)), *ks = in_page(cache, own.ks, kp, u);
+  const uint8_t *v = in_page(cache, own.v, vp, u * (D / 2)), *vs = in_page(cache, own.vs, vp, u);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const uint8_t* p = kb + Block<D>::codes(page, 0, ko + 4 * i) + g * (D / 8);
     if constexpr (D == 128) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+      const u32x4 w = *reinterpret_cast<const u32x4*>(k + 4 * i * (D / 2));
 #pragma unroll
       for (int j = 0; j < 4; ++j) t.k[i][j] = w[j];
     } else {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+      const u32x2 w = *reinterpret_cast<const u32x2*>(k + 4 * i * (D / 2));
       t.k[i][0] = w[0], t.k[i][1] = w[1];
     }
-    const uint32_t byte = kb[Block<D>::scales(page, 0, g * (D / 4) / 32, ko + 4 * i)];
+    const uint32_t byte = ks[4 * i];
     t.ks[i] = kbad ? static_cast<uint32_t>(kNanByte) : byte;
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const uint8_t* p = vb + Block<D>::codes(page, 1, vo + j) + c * (D / 32);
     if constexpr (D == 128)
-      t.v[j] = *reinterpret_cast<const uint32_t*>(p);
+      t.v[j] = *reinterpret_cast<const uint32_t*>(v + j * (D / 2));
     else
-      t.v[j] = *reinterpret_cast<const uint16_t*>(p);
+      t.v[j] = *reinterpret_cast<const uint16_t*>(v + j * (D / 2));
   }
-  t.vs = *reinterpret_cast<const u32x2*>(vb + Block<D>::scales(page, 1, c * (D / 16) / 32, vo));
+  t.vs = *reinterpret_cast<const u32x2*>(vs);
 }
 
 // O += V^T P^T over a tile: product n takes element c * D/16 + n of every
@@ -716,10 +739,11 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
   const uint8_t* head = a.cache.base + static_cast<uint64_t>(h) * a.cache.head_bytes;
   // two steps ahead the page ids, one step ahead the codes and scales
   int tile = begin + wave;
-  Pids pid = page_ids(a, pages, tile * kTile, c, g);
+  const TileLane<D> own(a.cache, head, c, g);
+  Pids pid = page_ids(a, pages, tile * kTile, key_token(c), 8 * g);
   Tile<D> next;
-  if (tile < end) load_tile<D>(a, head, pid, tile * kTile, c, g, next);
-  pid = page_ids(a, pages, (tile + W) * kTile, c, g);
+  if (tile < end) load_tile<D>(a.cache, own, pid, tile * kTile, next);
+  pid = page_ids(a, pages, (tile + W) * kTile, key_token(c), 8 * g);
 
   u32x4 qf[R][NS][KW];
   int limit[R];
@@ -744,8 +768,8 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
     const int t0 = tile * kTile;
     Tile<D> t = next;
     if (tile + W < end) {
-      load_tile<D>(a, head, pid, t0 + W * kTile, c, g, next);
-      pid = page_ids(a, pages, t0 + 2 * W * kTile, c, g);
+      load_tile<D>(a.cache, own, pid, t0 + W * kTile, next);
+      pid = page_ids(a, pages, t0 + 2 * W * kTile, key_token(c), 8 * g);
     }
     const bool masked = t0 + kTile > lim_min;
     __builtin_amdgcn_sched_barrier(0);
@@ -935,14 +959,23 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
 // keys are therefore formed two steps ahead, the values one.
 constexpr int kRowWaves = 8;
 
+// Two tokens' codes as words of the value operands: fn(n, word) for element n
+template <int D, int B = 0, typename Fn>
+__device__ __forceinline__ void join_pairs(const uint32_t (&codes)[2], float s0, float s1, Fn fn) {
+  const uint32_t x = cvt2<B>(codes[0], s0), y = cvt2<B>(codes[1], s1);
+  fn(2 * B, __builtin_amdgcn_perm(y, x, 0x05040100u));
+  fn(2 * B + 1, __builtin_amdgcn_perm(y, x, 0x07060302u));
+  if constexpr (B + 1 < D / 32) join_pairs<D, B + 1>(codes, s0, s1, fn);
+}
+
 template <int D>
 struct RawKeys {
   uint32_t k[D / 64];  // the lane's words of one token's codes
   uint32_t ks;
 };
 struct RawValues {
-  uint32_t v[8];  // one byte of each of 8 tokens' codes
-  u32x2 vs;
+  uint32_t v[2];  // codes of two tokens (D = 64: 16 bits each)
+  uint32_t vs;    // their scale bytes
 };
 
 template <typename T, int D, int R>
@@ -968,33 +1001,40 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
 
   const int32_t* pages = a.pages + static_cast<int64_t>(at.b) * a.pages_stride;
   const uint8_t* head = a.cache.base + static_cast<uint64_t>(at.h) * a.cache.head_bytes;
-  // this wave's share of a step: of tile wave / 4 the keys of half (wave / 2) % 2, every second pair of their words,
-  // and the values' byte wave % 4
-  const int share = wave >> 2, half = (wave >> 1) & 1, part_k = wave & 1, byte_v = wave & 3;
+  // this wave's share of a step: of tile wave / 4 the keys of half (wave / 2) % 2,
+  // every second pair of their words, and the value tokens 8g + 2 (wave % 4) and
+  // the next, which are one word of each operand
+  const int share = wave >> 2, half = (wave >> 1) & 1, part_k = wave & 1, pair = wave & 3;
+  const int kt = key_token(c) + 4 * half, vt = 8 * g + 2 * pair, kin = kt & (a.cache.page - 1), vin = vt & (a.cache.page - 1);
+  const uint8_t* own_k = head + Block<D>::codes(a.cache.page, 0, kin) + g * (D / 8) + part_k * (D / 16);
+  const uint8_t* own_ks = head + Block<D>::scales(a.cache.page, 0, g * (D / 4) / 32, kin);
+  const uint8_t* own_v = head + Block<D>::codes(a.cache.page, 1, vin) + c * (D / 32);
+  const uint8_t* own_vs = head + Block<D>::scales(a.cache.page, 1, c * (D / 16) / 32, vin);
   const auto load_keys = [&](int pid, int t0, RawKeys<D>& x) {
-    const int page = a.cache.page;
-    const bool none = static_cast<uint32_t>(pid) >= static_cast<uint32_t>(a.cache.n_pages);
-    const uint8_t* kb = head + static_cast<uint64_t>(none ? 0 : pid) * a.cache.page_bytes;
-    const int off = (t0 + (c >> 2) * 8 + (c & 3) + 4 * half) & (page - 1);
-    const uint8_t* kp = kb + Block<D>::codes(page, 0, off) + g * (D / 8) + part_k * (D / 16);
+    const bool none = no_page(a.cache, pid);
+    const uint32_t u = static_cast<uint32_t>(t0 & (a.cache.page - 1));
+    const uint8_t* k = in_page(a.cache, own_k, none ? 0 : pid, u * (D / 2));
     if constexpr (D == 128) {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(kp);
+      const u32x2 w = *reinterpret_cast<const u32x2*>(k);
       x.k[0] = w[0], x.k[1] = w[1];
     } else {
-      x.k[0] = *reinterpret_cast<const uint32_t*>(kp);
+      x.k[0] = *reinterpret_cast<const uint32_t*>(k);
     }
-    const uint32_t byte = kb[Block<D>::scales(page, 0, g * (D / 4) / 32, off)];
+    const uint32_t byte = *in_page(a.cache, own_ks, none ? 0 : pid, u);
     x.ks = none ? static_cast<uint32_t>(kNanByte) : byte;
   };
   const auto load_values = [&](int pid, int t0, RawValues& x) {
-    if (byte_v >= D / 32) return;
-    const int page = a.cache.page;
-    const bool none = static_cast<uint32_t>(pid) >= static_cast<uint32_t>(a.cache.n_pages);
-    const uint8_t* vb = head + static_cast<uint64_t>(none ? 0 : pid) * a.cache.page_bytes;
-    const int off = (t0 + g * 8) & (page - 1);
+    const int p = no_page(a.cache, pid) ? 0 : pid;
+    const uint32_t u = static_cast<uint32_t>(t0 & (a.cache.page - 1));
+    const uint8_t* v = in_page(a.cache, own_v, p, u * (D / 2));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x.v[j] = vb[Block<D>::codes(page, 1, off + j) + c * (D / 32) + byte_v];
-    x.vs = *reinterpret_cast<const u32x2*>(vb + Block<D>::scales(page, 1, c * (D / 16) / 32, off));
+    for (int j = 0; j < 2; ++j) {
+      if constexpr (D == 128)
+        x.v[j] = *reinterpret_cast<const uint32_t*>(v + j * (D / 2));
+      else
+        x.v[j] = *reinterpret_cast<const uint16_t*>(v + j * (D / 2));
+    }
+    x.vs = *reinterpret_cast<const uint16_t*>(in_page(a.cache, own_vs, p, u));
   };
   const auto form_keys = [&](const RawKeys<D>& x, int buf) {
     const float ks = scale_of(x.ks);
@@ -1006,36 +1046,24 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
   // enough to know, since a row sees all tokens up to its limit.
   int poisoned = INT32_MAX;
   const auto form_values = [&](const RawValues& x, int t0, int buf) {
-    if (byte_v >= D / 32) return;
-    uint32_t codes[8], v[8];
-    u32x2 vs = x.vs;
+    uint32_t codes[2] = {x.v[0], x.v[1]}, scales = x.vs;
+    if (__any(high_byte(scales))) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) codes[j] = x.v[j];
-    if (__any(high_byte(vs[0]) | high_byte(vs[1]))) {
-#pragma unroll
-      for (int j = 7; j >= 0; --j) {
-        const int token = t0 + 8 * g + j;
-        if (((vs[j / 4] >> (8 * (j % 4))) & 255u) <= kMaxByte) continue;
+      for (int j = 1; j >= 0; --j) {
+        const int token = t0 + vt + j;
+        if (((scales >> (8 * j)) & 255u) <= kMaxByte) continue;
         if (token < lim_all) poisoned = min(poisoned, token);
         codes[j] = 0u;
-        vs[j / 4] &= ~(128u << (8 * (j % 4)));
+        scales &= ~(128u << (8 * j));
       }
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = cvt2<0>(codes[j], scale_byte(vs, j));
-    u32x4 lo, hi;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      lo[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x05040100u);
-      hi[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x07060302u);
-    }
-    s_v[buf][share][2 * byte_v][lane] = lo;
-    s_v[buf][share][2 * byte_v + 1][lane] = hi;
+    uint32_t* to = reinterpret_cast<uint32_t*>(&s_v[buf][share][0][lane]) + pair;
+    join_pairs<D>(codes, scale_of(scales & 255u), scale_of(scales >> 8), [&](int n, uint32_t w) { to[n * 64 * 4] = w; });
   };
 
   // where this wave's share of the step at `tile` starts, and the pages there
   const auto start = [&](int tile) { return (tile + share) * kTile; };
-  const auto ids = [&](int tile) { return page_ids(a, pages, start(tile), c, g); };
+  const auto ids = [&](int tile) { return page_ids(a, pages, start(tile), kt, vt); };
   int tile = at.begin;
   RawKeys<D> rk, rk1;
   RawValues rv;
@@ -1292,7 +1320,7 @@ Cache cache_of(const spp_attn_desc* d, const void* base) {
   Cache c;
   c.base = static_cast<const uint8_t*>(base);
   c.head_bytes = static_cast<uint32_t>(d->page * (d->head_dim + d->head_dim / 16));
-  c.page_bytes = static_cast<uint64_t>(c.head_bytes) * static_cast<uint64_t>(d->n_kv_heads);
+  c.page_bytes = c.head_bytes * static_cast<uint32_t>(d->n_kv_heads);  // at most 2^10 heads of 256 tokens: 36 MB
   c.page = d->page;
   c.shift = __builtin_ctz(static_cast<unsigned>(d->page));
   c.n_pages = d->n_pages;
