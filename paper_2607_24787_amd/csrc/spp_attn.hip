@@ -91,6 +91,19 @@ __device__ __forceinline__ void load8(const T* p, float* f) {
   }
 }
 
+// The same 8 elements past the caches (streams that nothing here reads again)
+template <typename T>
+__device__ __forceinline__ void stream8(T* p, const float* f) {
+  if constexpr (std::is_same<T, float>::value) {
+    __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4*>(p));
+    __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4*>(p) + 1);
+  } else {
+    __builtin_nontemporal_store(
+        u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])},
+        reinterpret_cast<u32x4*>(p));
+  }
+}
+
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float* f) {
   if constexpr (std::is_same<T, float>::value) {
@@ -154,6 +167,7 @@ struct StoreArgs {
   const int64_t* slots;
   int Hq, Hkv, F;  // Hq = 0: no queries
   int T;
+  int stream_q;    // the queries are more than the L2 caches hold
 };
 
 // Codes (one word) and scale byte of this lane's 8 elements of a block of 32,
@@ -223,7 +237,11 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(StoreArgs a) {
     for (int i = 0; i < 8; ++i) y[i] = turn(y[i], z[i], c[i], s[i], first);
   }
   if (kind == 0) {
-    store8(reinterpret_cast<T*>(a.q_out) + static_cast<int64_t>(t) * a.q_out_stride + h * D + e0, y);
+    T* to = reinterpret_cast<T*>(a.q_out) + static_cast<int64_t>(t) * a.q_out_stride + h * D + e0;
+    if (a.stream_q)
+      stream8(to, y);
+    else
+      store8(to, y);
     return;
   }
   uint32_t byte;
@@ -267,14 +285,10 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(LoadArgs a) {
   T* out = kv ? reinterpret_cast<T*>(a.v) + static_cast<int64_t>(t) * a.v_stride
               : reinterpret_cast<T*>(a.k) + static_cast<int64_t>(t) * a.k_stride;
   out += h * D + e0;
-  if constexpr (std::is_same<T, float>::value) {
-    float f[8];
+  float f[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[2 * i] = bf16_lo(b[i]), f[2 * i + 1] = bf16_hi(b[i]);
-    store8(out, f);
-  } else {
-    *reinterpret_cast<u32x4*>(out) = b;
-  }
+  for (int i = 0; i < 4; ++i) f[2 * i] = bf16_lo(b[i]), f[2 * i + 1] = bf16_hi(b[i]);
+  stream8(out, f);
 }
 
 // ------------------------------------------------------------------- attention
@@ -1390,7 +1404,7 @@ struct Cut {
 constexpr int kCUs = 256;
 constexpr int kMinTiles = 2 * kWaves;
 constexpr int kFusedParts = 32;
-constexpr int kFewRows = 32;
+constexpr int kPairRows = 32, kFewRows = 208, kFewHeads = 32;
 
 // The counters stand at the workspace's start and take the same room in every
 // call, so that no call's partial rows come to lie where another one counts.
@@ -1400,7 +1414,17 @@ constexpr size_t kCountBytes = kMaxItems * sizeof(unsigned);
 // Rows of a wave of kv4_attend_rows_kernel, in sixteens, by the registers of fp32's three terms
 constexpr int rows_r(bool f32, int d) { return f32 && d == 128 ? 1 : 2; }
 
-int form_of(int64_t rows) { return rows <= 16 ? 0 : (rows <= kFewRows ? 1 : 2); }
+// kv4_attend_rows_kernel takes 256 rows (128 for fp32 heads of 128) whether they
+// are there or not, but needs fewer parts to fill the device.  Measured in us,
+// 8 heads per key/value head of 128, tokens cut over the waves / rows over them:
+// 48 sequences over 6,000 tokens of 64 rows each 79 / 157, of 192 rows 187 /
+// 222; one sequence of 64 rows 26 / 18, of 192 rows 25 / 25; six sequences of
+// 64 rows 34 / 29, of 128 rows 34 / 35; of 24 rows 20 / 16 and 26 / 25, but over
+// 1,000 tokens 12.7 / 14.0.
+int form_of(int64_t rows, int64_t heads) {
+  if (rows <= 16) return 0;
+  return rows <= kPairRows || (rows <= kFewRows && heads > kFewHeads) ? 1 : 2;
+}
 
 int group_rows(bool f32, int d, int form) { return form == 2 ? 16 * kRowWaves * rows_r(f32, d) : 16 << form; }
 
@@ -1413,7 +1437,7 @@ int split_below(bool f32, int d, int form) { return form == 2 ? kCUs : std::min(
 Cut cut_of(const spp_attn_desc* d, bool f32, int32_t n_seq, int32_t max_q, int32_t max_kv) {
   Cut c{};
   const int64_t rows = static_cast<int64_t>(max_q) * (d->n_heads / d->n_kv_heads);
-  c.form = form_of(rows);
+  c.form = form_of(rows, static_cast<int64_t>(n_seq) * d->n_kv_heads);
   c.rows = group_rows(f32, d->head_dim, c.form);
   c.row_tiles = static_cast<int>((rows + c.rows - 1) / c.rows);
   c.planes = d->n_kv_heads * c.row_tiles;
@@ -1532,6 +1556,8 @@ extern "C" spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int3
   a.Hq = Hq;
   a.Hkv = desc->n_kv_heads;
   a.F = n_freq;
+  // 8,192 tokens of 32 + 2 * 4 heads: 33.2 us so, 36.5 with ordinary stores
+  a.stream_q = static_cast<int64_t>(T) * Hq * d * elem > (int64_t{32} << 20);
   a.T = T;
   const int per = 256 / (d / 8);
   const int64_t units = static_cast<int64_t>(T) * (Hq + 2 * desc->n_kv_heads);
@@ -1595,9 +1621,9 @@ extern "C" size_t spp_kv4_attend_workspace(const spp_attn_desc* desc, int32_t n_
   const int64_t rows = static_cast<int64_t>(max_q) * (desc->n_heads / desc->n_kv_heads);
   if ((static_cast<int64_t>(max_kv) + kTile - 1) / kTile <= kMinTiles) return most;
   for (bool f32 : {false, true})
-    for (int form = 0; form <= form_of(rows); ++form) {
+    for (int form = 0; form <= (rows <= 16 ? 0 : (rows <= kPairRows ? 1 : 2)); ++form) {
       const int d = desc->head_dim, each = group_rows(f32, d, form);
-      const int64_t row_tiles = form == 2 ? (rows + each - 1) / each : 1;
+      const int64_t row_tiles = ((form == 2 ? rows : std::min<int64_t>(rows, kFewRows)) + each - 1) / each;
       const int64_t items = std::min<int64_t>(n_seq * desc->n_kv_heads * row_tiles, split_below(f32, d, form) - 1);
       const int64_t parts = std::max<int64_t>(fill(f32, d, form), items) + items;
       most = std::max(most, kCountBytes + static_cast<size_t>(parts) * each * (d + 2) * sizeof(float));

@@ -307,6 +307,55 @@ def test_prompts(torch, d, dtype, page):
     s.check(s.run())
 
 
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "f32"), (128, "f32"), (64, "bf16")])
+@pytest.mark.parametrize("nq,heads,kv_heads,seqs", [(3, 24, 2, 3), (9, 8, 1, 2), (9, 16, 4, 9), (40, 8, 2, 1), (33, 8, 1, 3)])
+def test_every_way_of_cutting_the_work(torch, d, dtype, nq, heads, kv_heads, seqs):
+    """Row counts on both sides of each rule, over lengths that are cut into parts, with page tables of pages of 16."""
+    kv = [700, 333, 290, 512, 64, 31, 1, 600, 0][:seqs]
+    s = Setup([nq] * seqs, kv, heads, kv_heads, d, 16, dtype, seed=nq + seqs)
+    for causal in (True, False):
+        s.check(s.run(causal=causal), causal=causal)
+
+
+@pytest.mark.parametrize("seqs,kv_heads", [(65, 1), (200, 2), (300, 4), (1100, 4)])
+def test_many_sequences(torch, seqs, kv_heads):
+    """More sequences than a wave has lanes, most short, a few long; up to where nothing is split."""
+    rng = np.random.default_rng(seqs)
+    kv = rng.integers(0, 40, size=seqs)
+    kv[rng.integers(0, seqs, size=3)] = [900, 400, 700]
+    kv[-1] = 333
+    s = Setup([1] * seqs, kv.tolist(), kv_heads * 2, kv_heads, 64, 16, "bf16", seed=seqs, extra_rows=0)
+    s.check(s.run(null_start=True))
+    nq = rng.integers(0, 4, size=seqs)
+    if seqs < 1000:
+        s = Setup(nq.tolist(), kv.tolist(), kv_heads * 2, kv_heads, 64, 32, "f32", seed=seqs)
+        s.check(s.run())
+
+
+@pytest.mark.parametrize("T,H", [(1100, 128), (16500, 16)])
+def test_store_of_many_queries(torch, T, H):
+    """Queries of more than 32 MB go past the caches: the plain form's values all the same."""
+    rng = np.random.default_rng(T)
+    from paper_2607_24787_amd import spp
+    d = 128
+    rows = torch.randn((T, (H + 2) * d), device="cuda").bfloat16()
+    if T * H * d * 2 <= 32 << 20:
+        rows = rows.float()
+    code = spp.DTYPE_BF16 if rows.dtype == torch.bfloat16 else spp.DTYPE_F32
+    assert T * H * d * rows.element_size() > 32 << 20
+    desc = spp.make_attn_desc(H, 1, d, 16, -(-T // 16))
+    cache = torch.zeros(spp.spp_kv4_cache_bytes(desc), dtype=torch.uint8, device="cuda")
+    table = _dev(oa.rotary_table(rng.integers(0, 9000, size=(1, T)), [0] * 64, 1e4 ** (-np.arange(64) / 64)).astype(np.float32))
+    out = torch.empty((T, H * d), device="cuda", dtype=rows.dtype)
+    slots = torch.arange(T, device="cuda")
+    at, size, wide = rows.data_ptr(), rows.element_size(), (H + 2) * d
+    spp.spp_kv4_store(desc, cache.data_ptr(), code, at, wide, out.data_ptr(), H * d, at + H * d * size, wide,
+                      at + (H + 1) * d * size, wide, table.data_ptr(), 64, slots.data_ptr(), T, _stream())
+    torch.cuda.synchronize()
+    want = torch.from_numpy(oa.rotate(_host(rows)[:, :H * d].reshape(T, H, d), _host(table))).to(rows.dtype)
+    assert torch.equal(out.cpu().reshape(T, H, d), want)
+
+
 @pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "f32")])
 @pytest.mark.parametrize("nq", [1, 3])
 def test_long_sequences(torch, d, dtype, nq):
@@ -324,17 +373,21 @@ def test_hints_do_not_change_what_is_right(torch):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
-def test_what_is_not_finite_reaches_only_rows_that_see_it(torch, dtype, d):
+@pytest.mark.parametrize("nq", [40, 15, 4])
+def test_what_is_not_finite_reaches_only_rows_that_see_it(torch, dtype, d, nq):
     """Key and value blocks of NaN and of scales beyond the format's in the middle of a causal chunk: rows before are
     as without it, rows from there on are NaN (a value block: its elements)."""
-    s = Setup([40, 6, 1], [90, 6, 70], 4, 2, d, 16, dtype, seed=5)
-    where = [(0, 77, 1, 1, 255), (0, 60, 0, 0, 255), (1, 3, 1, 0, 255), (2, 69, 1, 1, 255)]
+    s = Setup([nq, 6, 1], [90, 6, 70], 4, 2, d, 16, dtype, seed=5)    # many rows, 30 of them, a few
+    where = [(0, 88, 1, 1, 255), (0, 87, 0, 0, 255), (1, 3, 1, 0, 255), (2, 69, 1, 1, 255)]
+    if nq > 20:
+        where += [(0, 77, 1, 1, 255), (0, 60, 0, 0, 255)]
     for b, t, head, kv, byte in where:
         slot = int(s.pages[b, t // 16]) * 16 + t % 16
         p, _, places = s.cache._places(kv, slot)
         s.cache.raw[p, head, places[0]] = byte
     want = s.check(s.run())
-    assert np.isnan(want).any() and not np.isnan(want[:10]).any()
+    first = nq - (90 - min(t for b, t, *_ in where if b == 0))     # the first query that sees one
+    assert np.isnan(want[first:nq]).any() and not np.isnan(want[:first]).any()
 
 
 def test_queries_that_are_not_finite(torch):
