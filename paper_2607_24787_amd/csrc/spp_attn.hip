@@ -326,26 +326,34 @@ struct Seq {
   }
 };
 
-__device__ __forceinline__ Seq sequence(const AttendArgs& a, int b) {
+// A sequence's numbers as they stand in memory
+struct RawSeq {
+  int len = 0, first = 0, end = 0;
+};
+
+__device__ __forceinline__ RawSeq raw_sequence(const AttendArgs& a, int b) {
+  RawSeq r;
+  if (b >= a.n_seq) return r;
+  r.len = a.kv_len[b];
+  r.first = a.q_start ? a.q_start[b] : b;
+  r.end = a.q_start ? a.q_start[b + 1] : b + 1;
+  return r;
+}
+
+__device__ __forceinline__ Seq sequence(const AttendArgs& a, RawSeq r) {
   Seq s;
-  if (a.q_start) {
-    s.q0 = min(max(a.q_start[b], 0), a.n_tokens);
-    s.nq = min(max(a.q_start[b + 1], s.q0), a.n_tokens) - s.q0;
-  } else {
-    s.q0 = b;
-    s.nq = 1;
-  }
+  s.q0 = min(max(r.first, 0), a.n_tokens);
+  s.nq = min(max(r.end, s.q0), a.n_tokens) - s.q0;
   const int64_t room = a.pages_stride * a.cache.page;
-  s.len = max(a.kv_len[b], 0);
+  s.len = max(r.len, 0);
   s.overlong = s.len > room;
   if (s.overlong) s.len = static_cast<int>(room);
   return s;
 }
 
-__device__ __forceinline__ int tiles_of(const AttendArgs& a, int i) {
-  if (i >= a.n_seq) return 0;
-  const int64_t len = min(static_cast<int64_t>(max(a.kv_len[i], 0)), a.pages_stride * a.cache.page);
-  return static_cast<int>((len + kTile - 1) / kTile);
+__device__ __forceinline__ uint32_t tiles_of(const AttendArgs& a, RawSeq r) {
+  const int64_t len = min(static_cast<int64_t>(max(r.len, 0)), a.pages_stride * a.cache.page);
+  return static_cast<uint32_t>((len + kTile - 1) / kTile);
 }
 
 // Inclusive sums over the wave's lanes (all of them active)
@@ -363,6 +371,7 @@ __device__ __forceinline__ int wave_scan(int x) {
 // part p - base.
 struct Place {
   int b, base, each;
+  Seq seq;
 };
 
 // A plane's parts are equal pieces of all its sequences' tiles, at most
@@ -371,26 +380,32 @@ struct Place {
 // finds its part by itself, from the lengths on the device: a scan over 64
 // sequences at a time.  b >= 0: the place of that sequence's first part instead.
 __device__ __forceinline__ Place place_of(const AttendArgs& a, int p, int b, int lane) {
-  const int mine = tiles_of(a, lane);
+  const RawSeq mine = raw_sequence(a, lane);
   const uint32_t up = (1u << a.sum_shift) - 1u;  // sums in units of 2^sum_shift tiles fit 31 bits
-  uint32_t total = (static_cast<uint32_t>(mine) + up) >> a.sum_shift;
-  for (int i = 64 + lane; i - lane < a.n_seq; i += 64) total += (static_cast<uint32_t>(tiles_of(a, i)) + up) >> a.sum_shift;
+  uint32_t total = (tiles_of(a, mine) + up) >> a.sum_shift;
+  for (int i = 64 + lane; i - lane < a.n_seq; i += 64) total += (tiles_of(a, raw_sequence(a, i)) + up) >> a.sum_shift;
   total = __builtin_amdgcn_readlane(wave_scan(static_cast<int>(total)), 63);
-  uint32_t each = ((total + static_cast<uint32_t>(a.units) - 1) / static_cast<uint32_t>(a.units)) << a.sum_shift;
-  each = (max(each, static_cast<uint32_t>(a.min_tiles)) + kWaves - 1) / kWaves * kWaves;  // whole steps of a workgroup
+  uint32_t each = min((total + static_cast<uint32_t>(a.units) - 1) / static_cast<uint32_t>(a.units), 1u << (30 - a.sum_shift));
+  each = max(each << a.sum_shift, static_cast<uint32_t>(a.min_tiles));
+  each = (each + kWaves - 1) / kWaves * kWaves;  // whole steps of a workgroup
   Place at;
   at.b = -1;
   at.base = 0;
-  at.each = static_cast<int>(min(each, 1u << 30));
+  at.each = static_cast<int>(each);
   for (int i0 = 0; i0 < a.n_seq; i0 += 64) {
-    const int t = i0 == 0 ? mine : tiles_of(a, i0 + lane);
-    const int n = i0 + lane < a.n_seq ? max(1, static_cast<int>((static_cast<uint32_t>(t) + at.each - 1) / static_cast<uint32_t>(at.each))) : 0;
+    const RawSeq r = i0 == 0 ? mine : raw_sequence(a, i0 + lane);
+    const int n = i0 + lane < a.n_seq ? max(1, static_cast<int>((tiles_of(a, r) + each - 1) / each)) : 0;
     const int sum = wave_scan(n);
     const uint64_t past = __ballot(b < 0 ? at.base + sum > p : i0 + lane == b);
     if (past) {
       const int l = __builtin_ctzll(past);
       at.b = i0 + l;
       at.base += __builtin_amdgcn_readlane(sum - n, l);
+      RawSeq found;
+      found.len = __builtin_amdgcn_readlane(r.len, l);
+      found.first = __builtin_amdgcn_readlane(r.first, l);
+      found.end = __builtin_amdgcn_readlane(r.end, l);
+      at.seq = sequence(a, found);
       return at;
     }
     at.base += __builtin_amdgcn_readlane(sum, 63);
@@ -417,6 +432,7 @@ __device__ __forceinline__ bool find_spot(const AttendArgs& a, int rows, int lan
     const Place at = place_of(a, p, -1, lane);
     if (at.b < 0) return false;
     s.b = at.b, s.split = p - at.base, each = at.each;
+    s.seq = at.seq;
   } else {
     // the row tiles of one sequence and head are a multiple of 8 workgroups
     // apart, which brings them to one XCD and the cached rows into its L2; the
@@ -426,8 +442,8 @@ __device__ __forceinline__ bool find_spot(const AttendArgs& a, int rows, int lan
     if (bh >= heads) return false;
     s.rt = a.row_tiles - 1 - static_cast<int>(blockIdx.x) / step;
     s.b = bh / a.Hkv, s.h = bh - s.b * a.Hkv;
+    s.seq = sequence(a, raw_sequence(a, s.b));
   }
-  s.seq = sequence(a, s.b);
   const int nrows = s.seq.nq * a.G;
   s.row0 = s.rt * rows;
   if (s.row0 >= nrows) return false;
@@ -1279,7 +1295,7 @@ __global__ __launch_bounds__(64 * (W == 1 ? 4 : W)) void kv4_join_kernel(AttendA
   const int row = W == 1 ? static_cast<int>(blockIdx.x) / heads * 4 + wave : static_cast<int>(blockIdx.x) / heads;
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;
   const Place at = place_of(a, 0, b, lane);
-  const Seq seq = sequence(a, b);
+  const Seq& seq = at.seq;
   const int nrows = seq.nq * a.G;
   if (row >= nrows) return;
   const int rt = row / kRows, ri = row - rt * kRows;

@@ -329,7 +329,7 @@ def spp_rotary_table(pos_dev: int, pos_stride: int, n_axes: int, axis_of, inv_fr
     """cos and sin of the T tokens' angles into table_dev (fp32 [T, 2, len(axis_of)]); axis_of: the axis of each
     frequency (host ints)."""
     a = np.ascontiguousarray(axis_of, dtype=np.int32)
-    _check(lib().spp_rotary_table(pos_dev, pos_stride, n_axes, a.ctypes.data, inv_freq_dev, a.size, T, table_dev, stream))
+    _check(lib().spp_rotary_table(pos_dev, pos_stride, n_axes, a.__array_interface__["data"][0], inv_freq_dev, a.size, T, table_dev, stream))
 
 
 def rotary_axes(sections, interleaved: bool):
