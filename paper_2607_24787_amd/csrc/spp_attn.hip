@@ -1075,14 +1075,14 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
   // see one of a block's get their NaN at the end: the first such token is
   // enough to know, since a row sees all tokens up to its limit.
   int poisoned = INT32_MAX;
-  const auto form_values = [&](const RawValues& x, int t0, int buf) {
+  const auto form_values = [&](const RawValues& x, int t0, int buf, int lim) {
     uint32_t codes[2] = {x.v[0], x.v[1]}, scales = x.vs;
     if (__any(high_byte(scales))) {
 #pragma unroll
       for (int j = 1; j >= 0; --j) {
         const int token = t0 + vt + j;
         if (((scales >> (8 * j)) & 255u) <= kMaxByte) continue;
-        if (token < lim_all) poisoned = min(poisoned, token);
+        if (token < lim) poisoned = min(poisoned, token);
         codes[j] = 0u;
         scales &= ~(128u << (8 * j));
       }
@@ -1122,7 +1122,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
   }
 
   form_keys(rk, 0);
-  form_values(rv, start(tile), 0);
+  form_values(rv, start(tile), 0, at.begin < at.end ? lim_all : 0);
   form_keys(rk1, 1);
   load_values(id1.v, start(tile + 2), rv);
   load_keys(id2.k, start(tile + 4), rk);
@@ -1171,8 +1171,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
   constexpr int QF = 2 * KW, kHalf = QF / 2, kEach = 8 * R / QF;  // kEach: powers behind each operand's products
   u32x4 kh[kHalf];
   const auto key = [&](int buf, int i2, int q) { return s_k[buf][i2][q % 2 * KW + q / 2][lane]; };  // halves by turns
-  const auto step = [&](int now, int kbuf, int vbuf, int i2, int after, f32x4 (&s)[R][2], f32x4 (&ahead)[R][2]) {
-    if (!live) return;
+  const auto step = [&](int now, int kbuf, int vbuf, int i2, int after, f32x4 (&s)[R][2], f32x4 (&ahead)[R][2],
+                        const auto& form) {
+    if (!live) return form();
     u32x4 kl[kHalf], vf[NT];
 #pragma unroll
     for (int q = 0; q < kHalf; ++q) kl[q] = key(kbuf, 1 - i2, kHalf + q);
@@ -1210,6 +1211,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
     for (int r = 0; r < R; ++r) split8<NS>(p[r], pf[r]);
     live = seen(now + 1);
     if (live) hide((now + 1) * kTile, ahead);
+    form();  // vector work beside the products below
     const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -1234,19 +1236,18 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
 #pragma unroll
   for (int q = 0; q < kHalf; ++q) kh[q] = key(kbuf, 1, q);
   for (int vbuf = 0; tile < at.end; tile += 2, vbuf ^= 1) {
-    // the scores to come: tile 1 of this step, then tile 0 of the next, whose tile 1 follows
-    step(tile, kbuf, vbuf, 0, knext, s, s2);
-    step(tile + 1, knext, vbuf, 1, knext, s2, s);
-    if (tile + 2 < at.end) {
-      form_values(rv, start(tile + 2), vbuf ^ 1);
-      if (tile + 4 < at.end) {
-        form_keys(rk, kfree);
-        load_values(id.v, start(tile + 4), rv);
-        load_keys(id1.k, start(tile + 6), rk);
-        id = id1;
-        id1 = ids(tile + 8);
-      }
-    }
+    // the scores to come: tile 1 of this step, then tile 0 of the next, whose tile 1 follows; behind the last step
+    // what is formed and read is of no use, and of the cache all the same
+    step(tile, kbuf, vbuf, 0, knext, s, s2, [&] {
+      form_keys(rk, kfree);
+      load_keys(id1.k, start(tile + 6), rk);
+    });
+    step(tile + 1, knext, vbuf, 1, knext, s2, s, [&] {
+      form_values(rv, start(tile + 2), vbuf ^ 1, tile + 2 < at.end ? lim_all : 0);
+      load_values(id.v, start(tile + 4), rv);
+      id = id1;
+      id1 = ids(tile + 8);
+    });
     const int used = kbuf;
     kbuf = knext, knext = kfree, kfree = used;
     __syncthreads();
