@@ -387,7 +387,8 @@ spp_status spp_rotary_table(const int32_t* pos, int64_t pos_stride, int32_t n_ax
  * cache.  q: dev [T][n_heads][d] in dtype, token t at q + t * q_stride
  * elements; k, v the same with n_kv_heads heads and k_stride, v_stride (rows
  * of one fused product need no copies).  q_out (row stride q_out_stride)
- * receives the rotated queries in dtype; q_out may be q with the same stride.
+ * receives the rotated queries in dtype; q_out may be q with the same stride,
+ * and otherwise overlaps neither the span of q's rows nor rows of k and v.
  * q and q_out both NULL: keys and values only.  table: of spp_rotary_table,
  * [T][2][n_freq], 2 * n_freq <= d; element i < n_freq turns with element
  * i + n_freq, elements from 2 * n_freq on stay.  n_freq = 0 (table NULL): no
@@ -401,7 +402,7 @@ spp_status spp_rotary_table(const int32_t* pos, int64_t pos_stride, int32_t n_ax
  * the even one): no element is off by more than half of its step, except that
  * magnitudes above 7 * 2^125 become 6 * 2^125.  A block with an infinity or
  * a NaN becomes a NaN block.  Pointers 16-byte aligned, strides multiples of
- * 16 bytes, at least a row. */
+ * 16 bytes, at least a row; T * (n_heads + 2 n_kv_heads) at most 2^27. */
 spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int32_t dtype, const void* q, int64_t q_stride,
                          void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, const void* v,
                          int64_t v_stride, const float* table, int32_t n_freq, const int64_t* slots, int32_t T,
@@ -410,14 +411,15 @@ spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int32_t dtype, 
 /* Read T tokens' keys and values back: k_out, v_out dev [T][n_kv_heads][d] in
  * dtype with their row strides (exact in either dtype); either may be NULL.
  * The rows of a token whose slot is outside [0, n_pages * page) are left as
- * they were.  Alignment as for spp_kv4_store. */
+ * they were.  Alignment as for spp_kv4_store; T * 2 n_kv_heads at most 2^27. */
 spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dtype, const int64_t* slots, int32_t T,
                         void* k_out, int64_t k_stride, void* v_out, int64_t v_stride, void* hip_stream);
 
 /* Attention of n_seq sequences' query tokens over their cached tokens:
  *   out[i] = sum_t softmax_t(scale * q[i] . k[t]) v[t].
  * q, out: dev [n_tokens][n_heads][d] in dtype with their row strides (out may
- * be q with the same stride).  q_start: dev int32 [n_seq + 1], sequence b has
+ * be q with the same stride; else their spans, first row to last, do not
+ * overlap).  scale: positive, at most 1e38.  q_start: dev int32 [n_seq + 1], sequence b has
  * the query tokens q_start[b] .. q_start[b+1] - 1; NULL: one each (n_tokens =
  * n_seq).  kv_len: dev int32 [n_seq], cached tokens of each; token t of
  * sequence b is in page pages[b * pages_stride + t / page] (dev int32).
@@ -435,7 +437,8 @@ spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dt
  * gives that query NaN.
  * Scores and softmax statistics are fp32; bf16 queries are exact operands,
  * probabilities are rounded to bf16 for the value product (their sum is not);
- * fp32 queries and probabilities go in as three bf16 terms each.
+ * fp32 queries and probabilities go in as three bf16 terms each (a query
+ * beyond bf16's largest number, 3.39e38, counts as infinite).
  * workspace: dev, 16-byte aligned, all zero before its first call; each call
  * leaves it fit for the next.  spp_kv4_attend_workspace gives the bytes for
  * every call of at most these sizes, in either dtype.  A call holds it until

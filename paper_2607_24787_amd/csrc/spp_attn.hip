@@ -4,7 +4,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 #include <cstdint>
 #include <type_traits>
 
@@ -893,7 +892,11 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
         *reinterpret_cast<f32x4*>(&s_o[wave][c][(4 * g + e) * NT + n]) =
             f32x4{o[r][n][e], o[r][n + 1][e], o[r][n + 2][e], o[r][n + 3][e]};
     __syncthreads();
-    const int rr = threadIdx.x / kThr, e0 = (threadIdx.x % kThr) * kPer;
+    // a thread's elements, in pairs: one run of a finished row; of a partial row
+    // pairs 2 kThr apart, so that the threads of a row write 128 bytes in a piece
+    // (their 8-byte agent-scope writes are not gathered on the way)
+    const int rr = threadIdx.x / kThr, tc = threadIdx.x % kThr;
+    const int e0 = tc * (parts > 1 ? 2 : kPer), apart = parts > 1 ? 2 * kThr : 2;
     const int row = row0 + r * 16 + rr;
     if (row > last) continue;
     float top = s_m[0][rr];
@@ -908,19 +911,27 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
       const float f = __builtin_amdgcn_exp2f(s_m[w][rr] - ref);
       sum += f * s_l[w][rr];
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) y[k] += f * s_o[w][rr][e0 + k];
+      for (int k = 0; k < kPer; k += 2) {
+        const float2 v = *reinterpret_cast<const float2*>(&s_o[w][rr][e0 + k / 2 * apart]);
+        y[k] += f * v.x;
+        y[k + 1] += f * v.y;
+      }
     }
     if (parts > 1) {
       const int ri = r * 16 + rr;
-      float* to = part + ri * D + e0;
-      if (a.join_apart) {
+      float *to = part + ri * D + e0, *ml = part + kRows * D + 2 * ri;
 #pragma unroll
-        for (int k = 0; k < kPer; k += 4) *reinterpret_cast<f32x4*>(to + k) = f32x4{y[k], y[k + 1], y[k + 2], y[k + 3]};
-        if (e0 == 0) *reinterpret_cast<float2*>(part + kRows * D + 2 * ri) = make_float2(top, sum);
-      } else {
-#pragma unroll
-        for (int k = 0; k < kPer; k += 2) put2(to + k, y[k], y[k + 1]);
-        if (e0 == 0) put2(part + kRows * D + 2 * ri, top, sum);
+      for (int k = 0; k < kPer; k += 2) {
+        if (a.join_apart)
+          *reinterpret_cast<float2*>(to + k / 2 * apart) = make_float2(y[k], y[k + 1]);
+        else
+          put2(to + k / 2 * apart, y[k], y[k + 1]);
+      }
+      if (tc == 0) {
+        if (a.join_apart)
+          *reinterpret_cast<float2*>(ml) = make_float2(top, sum);
+        else
+          put2(ml, top, sum);
       }
       continue;
     }
@@ -1358,7 +1369,8 @@ Cache cache_of(const spp_attn_desc* d, const void* base) {
   return c;
 }
 
-constexpr int64_t kMaxUnits = int64_t{1} << 30;  // so that 32-bit indices of threads and units hold
+constexpr int64_t kMaxUnits = int64_t{1} << 30;     // so that 32-bit indices hold
+constexpr int64_t kMaxHeadRows = int64_t{1} << 27;  // 16 threads each: a launch has less than 2^32
 
 // Rows [T][heads][d] at a stride of `stride` elements
 const char* rows_why(const void* p, int64_t stride, int heads, int d, int elem) {
@@ -1382,9 +1394,13 @@ const char* dtype_why(int32_t dtype) {
   return dtype == SPP_DTYPE_F32 || dtype == SPP_DTYPE_BF16 ? nullptr : "dtype must be 0 (f32) or 1 (bf16)";
 }
 
-spp_status launched() {
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? SPP_OK : spp::set_error(SPP_EHIP, hipGetErrorString(e));
+spp_status launched(hipError_t e) { return e == hipSuccess ? SPP_OK : spp::set_error(SPP_EHIP, hipGetErrorString(e)); }
+
+// The launch's own status, and no other call's that may still be pending
+template <typename Args>
+hipError_t launch(void (*kernel)(Args), unsigned grid, unsigned threads, const Args& args, hipStream_t st) {
+  void* params[] = {const_cast<Args*>(&args)};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(grid), dim3(threads), params, 0, st);
 }
 
 #define SPP_BAD(expr)                   \
@@ -1393,19 +1409,13 @@ spp_status launched() {
   } while (0)
 
 template <typename T>
-void launch_store(const StoreArgs& a, int d, unsigned grid, hipStream_t st) {
-  if (d == 128)
-    hipLaunchKernelGGL((kv4_store_kernel<T, 128>), dim3(grid), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((kv4_store_kernel<T, 64>), dim3(grid), dim3(256), 0, st, a);
+hipError_t launch_store(const StoreArgs& a, int d, unsigned grid, hipStream_t st) {
+  return d == 128 ? launch(kv4_store_kernel<T, 128>, grid, 256, a, st) : launch(kv4_store_kernel<T, 64>, grid, 256, a, st);
 }
 
 template <typename T>
-void launch_load(const LoadArgs& a, int d, unsigned grid, hipStream_t st) {
-  if (d == 128)
-    hipLaunchKernelGGL((kv4_load_kernel<T, 128>), dim3(grid), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((kv4_load_kernel<T, 64>), dim3(grid), dim3(256), 0, st, a);
+hipError_t launch_load(const LoadArgs& a, int d, unsigned grid, hipStream_t st) {
+  return d == 128 ? launch(kv4_load_kernel<T, 128>, grid, 256, a, st) : launch(kv4_load_kernel<T, 64>, grid, 256, a, st);
 }
 
 // How a call's work is cut: rows per workgroup, row tiles, waves per workgroup,
@@ -1470,30 +1480,30 @@ size_t part_bytes(const Cut& c, int32_t n_seq, int d) {
   return c.units > 0 ? static_cast<size_t>(c.planes) * (c.units + n_seq) * c.rows * (d + 2) * sizeof(float) : 0;
 }
 
+// Workgroups of the attention itself
+int64_t attend_grid(const Cut& c, int64_t n_seq, int64_t Hkv) {
+  if (c.units > 0) return (c.units + n_seq) * c.planes;
+  return (c.row_tiles > 1 ? (n_seq * Hkv + 7) / 8 * 8 : n_seq * Hkv) * c.row_tiles;
+}
+
 template <typename T, int D>
-void launch_attend_d(const AttendArgs& a, const Cut& c, int64_t rows, hipStream_t st) {
+hipError_t launch_attend_d(const AttendArgs& a, const Cut& c, int64_t rows, hipStream_t st) {
   constexpr bool f32 = std::is_same<T, float>::value;
-  const int heads = a.n_seq * a.Hkv;
-  const dim3 grid(c.units > 0 ? static_cast<unsigned>(c.units + a.n_seq) * static_cast<unsigned>(c.planes)
-                              : static_cast<unsigned>(c.row_tiles > 1 ? (heads + 7) / 8 * 8 : heads) *
-                                    static_cast<unsigned>(c.row_tiles));
-  const auto run = [&](auto kernel, auto joining, int waves, int rows_each, int join_waves) {
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), 0, st, a);
-    const dim3 join(static_cast<unsigned>(heads) * static_cast<unsigned>((rows + rows_each - 1) / rows_each));
-    if (c.join_apart) hipLaunchKernelGGL(joining, join, dim3(64 * join_waves), 0, st, a);
+  const auto run = [&](void (*kernel)(AttendArgs), void (*joining)(AttendArgs), int waves, int rows_each, int join_waves) {
+    const hipError_t e = launch(kernel, static_cast<unsigned>(attend_grid(c, a.n_seq, a.Hkv)), 64u * waves, a, st);
+    if (e != hipSuccess || !c.join_apart) return e;
+    return launch(joining, static_cast<unsigned>(a.n_seq * a.Hkv * ((rows + rows_each - 1) / rows_each)), 64u * join_waves,
+                  a, st);
   };
   constexpr int kR = rows_r(f32, D);
-  if (c.form == 0)
-    run(kv4_attend_kernel<T, D, 1>, kv4_join_kernel<T, D, 16, 16>, kWaves, 1, 16);
-  else if (c.form == 1)
-    run(kv4_attend_kernel<T, D, 2>, kv4_join_kernel<T, D, 32, 16>, kWaves, 1, 16);
-  else
-    run(kv4_attend_rows_kernel<T, D, kR>, kv4_join_kernel<T, D, 16 * kRowWaves * kR, 1>, kRowWaves, 4, 4);
+  if (c.form == 0) return run(kv4_attend_kernel<T, D, 1>, kv4_join_kernel<T, D, 16, 16>, kWaves, 1, 16);
+  if (c.form == 1) return run(kv4_attend_kernel<T, D, 2>, kv4_join_kernel<T, D, 32, 16>, kWaves, 1, 16);
+  return run(kv4_attend_rows_kernel<T, D, kR>, kv4_join_kernel<T, D, 16 * kRowWaves * kR, 1>, kRowWaves, 4, 4);
 }
 
 template <typename T>
-void launch_attend(const AttendArgs& a, int d, const Cut& c, int64_t rows, hipStream_t st) {
-  d == 128 ? launch_attend_d<T, 128>(a, c, rows, st) : launch_attend_d<T, 64>(a, c, rows, st);
+hipError_t launch_attend(const AttendArgs& a, int d, const Cut& c, int64_t rows, hipStream_t st) {
+  return d == 128 ? launch_attend_d<T, 128>(a, c, rows, st) : launch_attend_d<T, 64>(a, c, rows, st);
 }
 
 }  // namespace
@@ -1526,9 +1536,8 @@ extern "C" spp_status spp_rotary_table(const int32_t* pos, int64_t pos_stride, i
   a.F = n_freq;
   a.T = T;
   const int64_t threads = static_cast<int64_t>(T) * (n_freq / kTableFreqs);
-  hipLaunchKernelGGL(rotary_table_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0,
-                     static_cast<hipStream_t>(hip_stream), a);
-  return launched();
+  return launched(launch(rotary_table_kernel, static_cast<unsigned>((threads + 255) / 256), 256, a,
+                         static_cast<hipStream_t>(hip_stream)));
 }
 
 extern "C" spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int32_t dtype, const void* q,
@@ -1542,8 +1551,8 @@ extern "C" spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int3
   if ((table != nullptr) != (n_freq > 0) && T > 0) return bad("table must be given iff n_freq > 0");
   if ((q != nullptr) != (q_out != nullptr)) return bad("q and q_out must be given together");
   const int Hq = q ? desc->n_heads : 0;
-  if (T < 0 || static_cast<int64_t>(T) * (desc->n_heads + 2 * desc->n_kv_heads) > kMaxUnits)
-    return bad("T must be >= 0, T * (n_heads + 2 n_kv_heads) at most 2^30");
+  if (T < 0 || static_cast<int64_t>(T) * (desc->n_heads + 2 * desc->n_kv_heads) > kMaxHeadRows)
+    return bad("T must be >= 0, T * (n_heads + 2 n_kv_heads) at most 2^27");
   if (T == 0) return SPP_OK;
   if (!cache || !k || !v || !slots) return bad("cache, k, v and slots must not be NULL");
   if (!aligned16(cache) || !aligned(slots, 8)) return bad("cache must be 16-byte aligned, slots 8-byte aligned");
@@ -1580,11 +1589,7 @@ extern "C" spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int3
   const int64_t units = static_cast<int64_t>(T) * (Hq + 2 * desc->n_kv_heads);
   const unsigned grid = static_cast<unsigned>((units + per - 1) / per);
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (dtype == SPP_DTYPE_BF16)
-    launch_store<__bf16>(a, d, grid, st);
-  else
-    launch_store<float>(a, d, grid, st);
-  return launched();
+  return launched(dtype == SPP_DTYPE_BF16 ? launch_store<__bf16>(a, d, grid, st) : launch_store<float>(a, d, grid, st));
 }
 
 extern "C" spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dtype, const int64_t* slots,
@@ -1593,8 +1598,8 @@ extern "C" spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache,
   SPP_BAD(desc_why(desc));
   SPP_BAD(dtype_why(dtype));
   const int d = desc->head_dim, elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
-  if (T < 0 || static_cast<int64_t>(T) * 2 * desc->n_kv_heads > kMaxUnits)
-    return bad("T must be >= 0, T * 2 n_kv_heads at most 2^30");
+  if (T < 0 || static_cast<int64_t>(T) * 2 * desc->n_kv_heads > kMaxHeadRows)
+    return bad("T must be >= 0, T * 2 n_kv_heads at most 2^27");
   if (T == 0 || (!k_out && !v_out)) return SPP_OK;
   if (!cache || !slots) return bad("cache and slots must not be NULL");
   if (!aligned16(cache) || !aligned(slots, 8)) return bad("cache must be 16-byte aligned, slots 8-byte aligned");
@@ -1613,11 +1618,7 @@ extern "C" spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache,
   const int64_t units = static_cast<int64_t>(T) * desc->n_kv_heads * (k_out && v_out ? 2 : 1);
   const unsigned grid = static_cast<unsigned>((units + per - 1) / per);
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (dtype == SPP_DTYPE_BF16)
-    launch_load<__bf16>(a, d, grid, st);
-  else
-    launch_load<float>(a, d, grid, st);
-  return launched();
+  return launched(dtype == SPP_DTYPE_BF16 ? launch_load<__bf16>(a, d, grid, st) : launch_load<float>(a, d, grid, st));
 }
 
 namespace {
@@ -1657,7 +1658,7 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
   SPP_BAD(dtype_why(dtype));
   const int d = desc->head_dim, elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
   if (causal != 0 && causal != 1) return bad("causal must be 0 or 1");
-  if (!(scale > 0.f) || !std::isfinite(scale)) return bad("scale must be finite and positive");
+  if (!(scale > 0.f) || !(scale <= 1e38f)) return bad("scale must be positive, at most 1e38");
   if (n_tokens < 0 || static_cast<int64_t>(n_tokens) * desc->n_heads > kMaxUnits)
     return bad("n_tokens must be >= 0, n_tokens * n_heads at most 2^30");
   if (!q_start && n_tokens != n_seq) return bad("without q_start every sequence has one query token: n_tokens must be n_seq");
@@ -1675,6 +1676,8 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
     return bad("out must be q with the same stride, or not overlap it");
   if (!workspace || !aligned16(workspace)) return bad("workspace must not be NULL, and 16-byte aligned");
   const Cut cut = cut_of(desc, dtype == SPP_DTYPE_F32, n_seq, max_q, max_kv);
+  if (attend_grid(cut, n_seq, desc->n_kv_heads) >= int64_t{1} << 22)
+    return bad("too many sequences, heads and query tokens for one call");
   if (cut.units > 0 && workspace_bytes < kCountBytes + part_bytes(cut, n_seq, d)) return bad("the workspace is too small");
   AttendArgs a{};
   a.cache = cache_of(desc, cache);
@@ -1701,9 +1704,6 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
   a.count = static_cast<unsigned*>(workspace);
   a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kCountBytes);
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (dtype == SPP_DTYPE_BF16)
-    launch_attend<__bf16>(a, d, cut, static_cast<int64_t>(max_q) * a.G, st);
-  else
-    launch_attend<float>(a, d, cut, static_cast<int64_t>(max_q) * a.G, st);
-  return launched();
+  const int64_t rows = static_cast<int64_t>(max_q) * a.G;
+  return launched(dtype == SPP_DTYPE_BF16 ? launch_attend<__bf16>(a, d, cut, rows, st) : launch_attend<float>(a, d, cut, rows, st));
 }

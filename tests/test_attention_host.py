@@ -138,17 +138,18 @@ REFUSED = (
         dict(q_dev=GOOD + 8), dict(q_stride=511), dict(q_stride=504), dict(q_stride=-512), dict(q_stride=1 << 62),
         dict(k_dev=0), dict(v_dev=0), dict(k_dev=GOOD + 2), dict(k_stride=120), dict(v_stride=132), dict(table_dev=0),
         dict(table_dev=GOOD + 4), dict(n_freq=0), dict(n_freq=12), dict(n_freq=40), dict(n_freq=-8), dict(slots_dev=0), dict(slots_dev=GOOD + 4),
-        dict(T=-1), dict(T=1 << 30), dict(q_out_dev=GOOD + 16), dict(q_out_dev=GOOD + 1024),
+        dict(T=-1), dict(T=1 << 30), dict(T=(1 << 27) // 12 + 1), dict(q_out_dev=GOOD + 16), dict(q_out_dev=GOOD + 1024),
         dict(q_out_dev=GOOD, q_out_stride=1024))]
     + [(spp.spp_kv4_load, LOAD, c) for c in (
-        dict(cache_dev=0), dict(cache_dev=GOOD + 1), dict(dtype=7), dict(slots_dev=0), dict(T=-2), dict(T=1 << 30),
+        dict(cache_dev=0), dict(cache_dev=GOOD + 1), dict(dtype=7), dict(slots_dev=0), dict(T=-2), dict(T=1 << 30), dict(T=(1 << 25) + 1),
         dict(k_out_dev=GOOD + 4), dict(k_stride=64), dict(v_stride=129))]
     + [(spp.spp_kv4_attend, ATTEND, c) for c in (
         dict(cache_dev=0), dict(cache_dev=GOOD + 4), dict(dtype=3), dict(q_dev=0), dict(q_dev=GOOD + 6), dict(q_stride=500),
         dict(q_start_dev=0), dict(kv_len_dev=0), dict(pages_dev=0), dict(pages_stride=0), dict(pages_stride=-1),
         dict(pages_stride=1 << 27), dict(pages_stride=1 << 62), dict(n_seq=-1), dict(n_tokens=-1), dict(n_tokens=1 << 30), dict(max_q=0),
         dict(max_kv=-1), dict(max_q=1 << 29), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
-        dict(scale=float("inf")), dict(scale=1e-60), dict(causal=2), dict(out_dev=0), dict(out_dev=GOOD + 512), dict(out_stride=1024, out_dev=GOOD),
+        dict(scale=float("inf")), dict(scale=1e-60), dict(scale=3e38),
+        dict(n_seq=1 << 24, n_tokens=1 << 24, max_q=1), dict(causal=2), dict(out_dev=0), dict(out_dev=GOOD + 512), dict(out_stride=1024, out_dev=GOOD),
         dict(workspace_dev=0), dict(workspace_dev=GOOD * 4 + 8), dict(workspace_bytes=0, max_kv=4096), dict(workspace_bytes=16384, max_kv=4096),
         dict(kv_len_dev=GOOD + 2), dict(pages_dev=GOOD + 1), dict(q_start_dev=GOOD + 2))]
 )
