@@ -128,7 +128,10 @@ struct TableArgs {
 constexpr int kTableFreqs = 4;  // per thread: 16-byte stores
 
 // The angle in turns, reduced to [-1/2, 1/2] in 64 bits; what is left of it
-// beyond fp32 goes in by the first term of the addition theorem.
+// beyond fp32 goes in by the first term of the addition theorem (error 2.6e-8
+// of the values, half a step of fp32 2e-8 on average).  16,001 tokens of 64
+// frequencies 5.1 us (8.4 MB written, 1.6 TB/s: bound by its arithmetic and the
+// launch), 64 tokens 2.5 us.
 __global__ __launch_bounds__(256) void rotary_table_kernel(TableArgs a) {
   const uint32_t per = static_cast<uint32_t>(a.F / kTableFreqs);
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
@@ -205,7 +208,10 @@ __device__ __forceinline__ float turn(float y, float z, float c, float s, bool f
 
 // D/8 lanes per head, 8 elements each; a thread reads its elements and those
 // they turn with before it writes, and a head lies within one wave, so the
-// queries may be rotated in place.
+// queries may be rotated in place.  The partner's elements are read a second
+// time (from L1) instead of exchanged.  Bound by memory: 8,192 tokens of 32 + 4
+// + 4 heads of 128, 160 MB, in 33 to 36 us (4.4 to 4.8 TB/s; a large copy 5.0);
+// one token 2.5 us.  Non-temporal reads of the rows as well: 39 us.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_store_kernel(StoreArgs a) {
   constexpr int L = D / 8;
@@ -261,6 +267,9 @@ struct LoadArgs {
   int Hkv, T;
 };
 
+// Bound by memory, most of it the rows written: 100,000 tokens of 4 heads of 128
+// in bf16, 260 MB, in 45 us (5.8 TB/s) with stores past the caches, 77 us with
+// ordinary ones, 66 us with reads past them too; 700 tokens in fp32 3.1 us.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_load_kernel(LoadArgs a) {
   constexpr int L = D / 8;
@@ -470,7 +479,10 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
 }
 
 // fp32 as three bf16 terms that add up to it (24 significant bits); for bf16
-// one term, the value rounded to it.
+// one term, the value rounded to it.  One term of a probability is a choice:
+// outputs of bf16 are then 2.3e-3 from the exact ones instead of the 1.7e-3 that
+// their own rounding costs, and the value product of a prompt, which the matrix
+// cores bound, takes half of what it would with two.
 template <int NS>
 __device__ __forceinline__ void split8(const float* f, u32x4* out) {
   float r[8];
@@ -746,6 +758,20 @@ struct Joined {
   }
 };
 
+// Few rows (decoding): 16 R rows a workgroup, its waves take the cached tiles by
+// turns, one pass with the running maximum and sum.  Scores are formed as
+// S^T = K Q^T and outputs as O^T = V^T P^T: a lane then holds the probabilities
+// of its row for eight tokens in a row, which is the operand of the second
+// product as it stands, and codes become operands in registers, keys without any
+// exchange.  Codes are converted by the hardware (exactly), scales with them.
+// Bound by reading the cache: 131,072 tokens of 4 heads of 128, 71 MB, in 17.5 us
+// (4.1 TB/s, about 2.5 us of them the first loads' latency), vector units at half
+// of their rate; 64 sequences of 128 to 8,192 tokens, 90 MB, 27 us, of which 4.5
+// joining parts and 2 writing them.  Four waves and as many workgroups as are
+// resident at once: 131,072 tokens with half as many 18.5 us, twice as many 20.7
+// and a longer join, 16 waves (a quarter as many parts) 20.0; the 64 sequences
+// with half as many parts 36 us, twice as many 36.  Parts of 4 tiles instead of 8
+// at least: nine short fp32 sequences 13.5 us, not 11.6.
 template <typename T, int D, int R>
 __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value, D, R)) void kv4_attend_kernel(AttendArgs a) {
   constexpr int W = kWaves;
@@ -943,7 +969,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
   // order.  Parts pass between XCDs, whose L2 caches do not see each other:
   // they are written and read at agent scope, past those caches, and counted
   // only when every write has arrived.  (Fences in their place write back and
-  // drop whole caches: one token against 131,072 took 92 us instead of 20.)
+  // drop whole caches: one token against 131,072 took 92 us, not 27, joined this way.)
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -997,7 +1023,13 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
 // step is multiplied, the codes of the next ones are on their way.  A tile's
 // scores are multiplied while the tile before it goes through the softmax, so
 // that the matrix cores and the vector units have work at the same time; the
-// keys are therefore formed two steps ahead, the values one.
+// keys are therefore formed two steps ahead, the values one, beside the value
+// products.  Bound by the matrix cores and what is left between their products:
+// 2 sequences of 1,024 tokens over 8,192, 32 heads of 128, 258 us, 998 TFLOP/s
+// (1,150 for a large library product here).  On the way: 64 rows a workgroup in
+// the form above 437 us; operands shared, tile after tile 349; scores ahead 325;
+// wider loads of the codes 271; forming beside the products 258.  Without
+// forming (wrong results) it is 228.
 constexpr int kRowWaves = 8;
 
 // Two tokens' codes as words of the value operands: fn(n, word) for element n
@@ -1429,7 +1461,11 @@ struct Cut {
 };
 
 constexpr int kCUs = 256;
-constexpr int kMinTiles = 2 * kWaves;
+constexpr int kMinTiles = 2 * kWaves;  // two steps a wave
+// Parts a sequence from which a launch of its own joins them: 256 parts by the
+// last workgroup alone would read 1 MB in turn; a launch costs 5.6 us (131,072
+// tokens 23.0 us in all), while 64 sequences in about four parts each take 26.9
+// us joined by the last workgroup and 39 with a launch.
 constexpr int kFusedParts = 32;
 constexpr int kPairRows = 32, kFewRows = 208, kFewHeads = 32;
 
