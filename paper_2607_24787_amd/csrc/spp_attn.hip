@@ -478,11 +478,8 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// fp32 as three bf16 terms that add up to it (24 significant bits); for bf16
-// one term, the value rounded to it.  One term of a probability is a choice:
-// outputs of bf16 are then 2.3e-3 from the exact ones instead of the 1.7e-3 that
-// their own rounding costs, and the value product of a prompt, which the matrix
-// cores bound, takes half of what it would with two.
+// fp32 as NS bf16 terms: three add up to it (24 significant bits), two hold 16
+// bits of it, one is the value rounded to it.
 template <int NS>
 __device__ __forceinline__ void split8(const float* f, u32x4* out) {
   float r[8];
@@ -631,8 +628,8 @@ __device__ __forceinline__ void load_query(const AttendArgs& a, const Seq& seq, 
 
 // The running maximum m over a tile's scores (masked ones -inf) too; l and o
 // follow where it moves.
-template <int D, int R>
-__device__ __forceinline__ void follow_maximum(const f32x4 (&s)[R][2], float scale_log2, float (&m)[R], f32x4 (&l)[R],
+template <int D, int R, typename Sum>
+__device__ __forceinline__ void follow_maximum(const f32x4 (&s)[R][2], float scale_log2, float (&m)[R], Sum (&l)[R],
                                                f32x4 (&o)[R][D / 16]) {
   float top[R];
   bool moves = false;
@@ -663,20 +660,18 @@ __device__ __forceinline__ void follow_maximum(const f32x4 (&s)[R][2], float sca
 }
 
 // A tile's scores to the probabilities of the value product, relative to the
-// maximum; l sums them as they are rounded for it.
+// maximum; l sums this lane's eight.
 template <int R, int NS>
 __device__ __forceinline__ void probabilities(const f32x4 (&s)[R][2], float scale_log2, const float (&m)[R],
-                                              f32x4 (&l)[R], u32x4 (&pf)[R][NS]) {
-  const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+                                              float (&l)[R], u32x4 (&pf)[R][NS]) {
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const float ref = m[r] == -INFINITY ? 0.f : m[r];  // nothing seen yet: every power is 0
     float p[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(fmaf(s[r][k / 4][k % 4], scale_log2, -ref));
+    l[r] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     split8<NS>(p, pf[r]);
-#pragma unroll
-    for (int k = 0; k < NS; ++k) l[r] = mfma(ones, pf[r][NS - 1 - k], l[r]);
   }
 }
 
@@ -775,7 +770,11 @@ struct Joined {
 template <typename T, int D, int R>
 __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value, D, R)) void kv4_attend_kernel(AttendArgs a) {
   constexpr int W = kWaves;
-  constexpr int NS = std::is_same<T, float>::value ? 3 : 1;  // bf16 terms of a query and of a probability
+  constexpr int NS = std::is_same<T, float>::value ? 3 : 1;  // bf16 terms of a query
+  // and of a probability: two lose 2^-16 of it, so that a bf16 output is off by
+  // its own rounding alone.  One would lose as much as that rounding: 131,072
+  // tokens 23.1 us in all instead of 24.0, 64 ragged sequences 26.9, not 27.8.
+  constexpr int NP = std::is_same<T, float>::value ? 3 : 2;
   constexpr int KW = D / 32, NT = D / 16;
   constexpr int kRows = 16 * R, kPad = 4;
   __shared__ float s_o[W][16][D + kPad];
@@ -809,12 +808,12 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
     load_query<T, D, NS>(a, seq, h, row, g, qf[r]);
   }
 
-  f32x4 o[R][NT], l[R];  // l: every element the sum of its row's probabilities, as rounded for the product
-  float m[R];
+  f32x4 o[R][NT];
+  float m[R], l[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = -INFINITY;
-    l[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    l[r] = 0.f;
 #pragma unroll
     for (int n = 0; n < NT; ++n) o[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -857,8 +856,8 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
             if (t0 + 8 * g + 4 * i + e >= limit[r]) s[r][i][e] = -INFINITY;
     }
     follow_maximum<D, R>(s, a.scale_log2, m, l, o);
-    u32x4 pf[R][NS];
-    probabilities<R, NS>(s, a.scale_log2, m, l, pf);
+    u32x4 pf[R][NP];
+    probabilities<R, NP>(s, a.scale_log2, m, l, pf);
 
     float sc[8];
 #pragma unroll
@@ -896,9 +895,14 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int k = 0; k < NS; ++k) o[r][n] = mfma(vf, pf[r][NS - 1 - k], o[r][n]);
+        for (int k = 0; k < NP; ++k) o[r][n] = mfma(vf, pf[r][NP - 1 - k], o[r][n]);
     });
   }
+
+  // rows are divided by the head count again below: the reciprocal from above
+  // would take a register through the loop
+  AttendArgs again = a;
+  asm volatile("" : "+s"(again.G));
 
   // the waves' sums join: weights 2^(m_w - max m)
   const size_t part_floats = static_cast<size_t>(kRows) * (D + 2);  // [rows][D] sums, then [rows] maximum, sum
@@ -907,9 +911,11 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (r > 0) __syncthreads();
+    l[r] += __shfl_xor(l[r], 16);
+    l[r] += __shfl_xor(l[r], 32);
     if (g == 0) {
       s_m[wave][c] = m[r];
-      s_l[wave][c] = l[r][0];
+      s_l[wave][c] = l[r];
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)  // A row 4g + e is elements (4g + e) * NT + n
@@ -961,7 +967,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
       }
       continue;
     }
-    finish<T, kPer>(a, seq, h, row, D, e0, sum, y);
+    finish<T, kPer>(again, seq, h, row, D, e0, sum, y);
   }
   if (parts == 1 || a.join_apart) return;
 
@@ -1012,7 +1018,7 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
       j = whole;
     }
     // a count beyond the parts: the workspace was not zero, and nothing is known of the parts
-    finish<T, 4>(a, seq, h, row0 + ri, D, 4 * col, done > static_cast<unsigned>(parts) ? NAN : j.sum, j.y);
+    finish<T, 4>(again, seq, h, row0 + ri, D, 4 * col, done > static_cast<unsigned>(parts) ? NAN : j.sum, j.y);
   }
 }
 
@@ -1054,6 +1060,9 @@ struct RawValues {
 template <typename T, int D, int R>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(AttendArgs a) {
   constexpr int W = kRowWaves;
+  // bf16 terms of a query and of a probability.  One term of a probability is a
+  // choice: bf16 outputs are then 2.3e-3 from the exact ones instead of the 1.7e-3
+  // that their own rounding costs, but two terms make 347 us of the 258 above.
   constexpr int NS = std::is_same<T, float>::value ? 3 : 1;
   constexpr int KW = D / 32, NT = D / 16;
   constexpr int kRows = 16 * R * W;
