@@ -309,6 +309,7 @@ struct AttendArgs {
   const int32_t *q_start, *kv_len, *pages;
   int64_t pages_stride;
   int n_seq, n_tokens, Hkv, G;  // G: query heads per key/value head
+  int max_rows;  // of a sequence's key/value head: max_q query tokens times G
   int causal;
   int planes, row_tiles;  // a plane: one key/value head and row tile (Hkv * row_tiles of them)
   int units;              // about the parts that a plane's cached tokens are cut into; 0: a part is a whole sequence
@@ -452,7 +453,7 @@ __device__ __forceinline__ bool find_spot(const AttendArgs& a, int rows, int lan
     s.b = bh / a.Hkv, s.h = bh - s.b * a.Hkv;
     s.seq = sequence(a, raw_sequence(a, s.b));
   }
-  const int nrows = s.seq.nq * a.G;
+  const int nrows = min(s.seq.nq * a.G, a.max_rows);
   s.row0 = s.rt * rows;
   if (s.row0 >= nrows) return false;
   s.last = min(s.row0 + rows, nrows) - 1;
@@ -1349,7 +1350,7 @@ __global__ __launch_bounds__(64 * (W == 1 ? 4 : W)) void kv4_join_kernel(AttendA
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;
   const Place at = place_of(a, 0, b, lane);
   const Seq& seq = at.seq;
-  const int nrows = seq.nq * a.G;
+  const int nrows = min(seq.nq * a.G, a.max_rows);
   if (row >= nrows) return;
   const int rt = row / kRows, ri = row - rt * kRows;
   const int tiles = (seq.limit(a, min((rt + 1) * kRows, nrows) - 1) + kTile - 1) / kTile;
@@ -1738,6 +1739,8 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
   a.n_tokens = n_tokens;
   a.Hkv = desc->n_kv_heads;
   a.G = desc->n_heads / desc->n_kv_heads;
+  const int64_t rows = static_cast<int64_t>(max_q) * a.G;
+  a.max_rows = static_cast<int>(rows);  // at most 2^30
   a.causal = causal;
   a.scale_log2 = scale * 1.44269504088896340736f;
   a.planes = cut.planes;
@@ -1749,6 +1752,5 @@ extern "C" spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cach
   a.count = static_cast<unsigned*>(workspace);
   a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kCountBytes);
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const int64_t rows = static_cast<int64_t>(max_q) * a.G;
   return launched(dtype == SPP_DTYPE_BF16 ? launch_attend<__bf16>(a, d, cut, rows, st) : launch_attend<float>(a, d, cut, rows, st));
 }

@@ -28,3 +28,24 @@ def test_few_rows_keep_sixteen_bits_of_a_probability(torch, heads, kv_heads, d, 
     bound = rel * spread + U16 * np.abs(want) * (1 + rel) + (6 * n + 1) * 2.0 ** -126
     off = np.abs(got - want)
     assert np.all(off <= bound), np.max(off / bound)
+
+
+# ----------------------------------------------------------------------- max_q
+
+@pytest.mark.parametrize("max_kv", [0, 700, 100000])    # whole; parts joined by the last workgroup; by a launch
+@pytest.mark.parametrize("heads,kv_heads,d,dtype,max_q,nq", [
+    (8, 1, 128, "bf16", 1, [3, 1]), (4, 2, 64, "f32", 3, [8, 9]), (24, 1, 128, "bf16", 1, [2, 4]), (6, 1, 64, "f32", 5, [6, 2]),
+    (8, 1, 128, "bf16", 5, [9, 41]), (2, 1, 64, "f32", 50, [51, 300]), (8, 8, 128, "f32", 37, [40, 36]), (8, 8, 64, "bf16", 2, [10, 1])])
+def test_tokens_past_max_q_stay_as_they_were(torch, heads, kv_heads, d, dtype, max_q, nq, max_kv):
+    """Of each sequence the first max_q queries, at the places that all its queries give them."""
+    s = Setup(nq, [700, 333], heads, kv_heads, d, 32, dtype, seed=22)
+    within = np.concatenate([np.arange(n) < max_q for n in s.nq] + [np.zeros(s.T - sum(s.nq), dtype=bool)])
+    beyond = torch.from_numpy(~within).cuda()
+    out = s.run(max_q=max_q, max_kv=max_kv)
+    assert bool((out[beyond] == 7.0).all())
+    whole = s.run()
+    out[beyond] = whole[beyond]
+    s.check(out)
+    both = s.q.clone()                      # in place: those stay queries
+    s.run(q=both, out=both, max_q=max_q, max_kv=max_kv)
+    assert torch.equal(both[beyond], s.q[beyond])
