@@ -113,9 +113,8 @@ def attend(cache, q, q_start, kv_len, pages, causal, scale, out):
     spread, reach = np.zeros(out.shape), np.zeros(out.shape[:2])
     G = q.shape[1] // cache.h
     for b, n in enumerate(kv_len):
-        n = max(int(n), 0)
-        room = len(pages[b]) * cache.page
-        overlong, n = n > room, min(n, room)
+        whole = max(int(n), 0)
+        n = min(whole, len(pages[b]) * cache.page)
         nq = q_start[b + 1] - q_start[b]
         k, v = np.full((n, cache.h, cache.d), np.nan), np.full((n, cache.h, cache.d), np.nan)
         for t in range(n):
@@ -125,7 +124,7 @@ def attend(cache, q, q_start, kv_len, pages, causal, scale, out):
                 k[t], v[t] = cache.read(0, slot), cache.read(1, slot)
         for j in range(nq):
             i = q_start[b] + j
-            seen = max(0, n - nq + j + 1) if causal else n
+            seen = whole - nq + j + 1 if causal else whole
             out[i] = 0.0
             if seen <= 0:
                 continue
@@ -135,7 +134,7 @@ def attend(cache, q, q_start, kv_len, pages, causal, scale, out):
                 with np.errstate(all="ignore"):
                     p = np.exp(z - np.max(z))
                     p = p / np.sum(p)
-                    out[i, h] = np.nan if overlong else p @ vv
+                    out[i, h] = np.nan if whole > n else p @ vv
                     spread[i, h] = p @ np.abs(vv)
                     reach[i, h] = scale * np.max(np.abs(kk) @ np.abs(q[i, h]))
     return out, spread, reach

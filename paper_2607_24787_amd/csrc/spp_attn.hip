@@ -327,11 +327,12 @@ constexpr int kTile = 32;  // cached tokens per step: one 16x16x32 product over 
 // The rows of a sequence's key/value head are its query tokens times the G
 // heads that share it, token-major: row r is token r / G, head r % G.
 struct Seq {
-  int q0, nq;     // first query token, count
-  int len;        // cached tokens (at most what the page table row names)
-  bool overlong;  // it has more than that
+  int q0, nq;  // first query token, count
+  int len;     // cached tokens that the page table row has a place for
+  int first;   // tokens that query 0 sees, by the whole length (causal; below 0: the next ones see none either)
+  bool overlong;  // there are more than the row has a place for
   __device__ __forceinline__ int limit(const AttendArgs& a, int row) const {
-    return a.causal ? max(0, len - nq + row / a.G + 1) : len;
+    return a.causal ? min(max(0, first + row / a.G), len) : len;
   }
 };
 
@@ -353,10 +354,10 @@ __device__ __forceinline__ Seq sequence(const AttendArgs& a, RawSeq r) {
   Seq s;
   s.q0 = min(max(r.first, 0), a.n_tokens);
   s.nq = min(max(r.end, s.q0), a.n_tokens) - s.q0;
-  const int64_t room = a.pages_stride * a.cache.page;
-  s.len = max(r.len, 0);
-  s.overlong = s.len > room;
-  if (s.overlong) s.len = static_cast<int>(room);
+  const int whole = max(r.len, 0);
+  s.len = static_cast<int>(min(static_cast<int64_t>(whole), a.pages_stride * a.cache.page));
+  s.first = whole - s.nq + 1;
+  s.overlong = whole > s.len;
   return s;
 }
 

@@ -49,3 +49,22 @@ def test_tokens_past_max_q_stay_as_they_were(torch, heads, kv_heads, d, dtype, m
     both = s.q.clone()                      # in place: those stay queries
     s.run(q=both, out=both, max_q=max_q, max_kv=max_kv)
     assert torch.equal(both[beyond], s.q[beyond])
+
+
+# ---------------------------------------------- lengths beyond the page table row
+
+@pytest.mark.parametrize("max_kv", [0, 100000])
+@pytest.mark.parametrize("nq,room,over,heads,kv_heads,d,dtype", [
+    (16, 1, 14, 4, 2, 64, "bf16"), (20, 1, 2, 2, 2, 64, "bf16"), (20, 1, 3, 3, 3, 128, "f32"), (40, 2, 4, 2, 1, 128, "bf16"),
+    (50, 2, 700, 3, 1, 64, "f32"), (400, 20, 9, 1, 1, 64, "bf16")])
+def test_queries_of_a_sequence_longer_than_its_pages(torch, nq, room, over, heads, kv_heads, d, dtype, max_kv):
+    """room pages of 16 tokens, `over` tokens more: queries that see a token give NaN, also those that would see none if the
+    sequence ended with its pages; queries before the first token give zeros."""
+    s = Setup([nq, 3], [room * 16, 10], heads, kv_heads, d, 16, dtype, seed=23)
+    s.wide, s.pages = room, np.ascontiguousarray(s.pages[:, :room])
+    n = room * 16 + over
+    got = s.run(kv_len=[n, 10], max_kv=max_kv)
+    want = s.check(got, kv_len=[n, 10])
+    first = max(0, nq - n)
+    assert (want[:first] == 0).all() and np.isnan(want[first:nq]).all() and not np.isnan(want[nq:]).any()
+    s.check(s.run(kv_len=[n, 10], causal=False, max_kv=max_kv), causal=False, kv_len=[n, 10])
