@@ -127,9 +127,11 @@ struct TableArgs {
 
 constexpr int kTableFreqs = 4;  // per thread: 16-byte stores
 
-// The angle in turns, reduced to [-1/2, 1/2] in 64 bits; what is left of it
-// beyond fp32 goes in by the first term of the addition theorem (error 2.6e-8
-// of the values, half a step of fp32 2e-8 on average).  16,001 tokens of 64
+// The angle in turns, reduced to [-1/2, 1/2] in 64 bits: its product with 1 / (2
+// pi) is not rounded before the whole turns are off it (rounded, it would cost
+// 3e-7 of a value at the largest positions, five steps of fp32).  What is left
+// beyond fp32 goes in by the first term of the addition theorem (error 2.6e-8 of
+// the values, half a step of fp32 2e-8 on average).  16,001 tokens of 64
 // frequencies 5.1 us (8.4 MB written, 1.6 TB/s: bound by its arithmetic and the
 // launch), 64 tokens 2.5 us.
 __global__ __launch_bounds__(256) void rotary_table_kernel(TableArgs a) {
@@ -144,8 +146,9 @@ __global__ __launch_bounds__(256) void rotary_table_kernel(TableArgs a) {
     const int f = f0 + k;
     const int axis = static_cast<int>(a.axes[f / 16] >> (2 * (f % 16))) & 3;
     const double angle = static_cast<double>(a.pos[axis * a.pos_stride + t]) * static_cast<double>(a.inv_freq[f]);
-    double turns = angle * 0.15915494309189533577;
-    turns -= rint(turns);
+    constexpr double kPerTurn = 0.15915494309189533577, kRest = -9.839338337591243e-18;  // 1 / (2 pi) in two terms
+    const double whole = rint(angle * kPerTurn);
+    const double turns = fma(angle, kRest, fma(angle, kPerTurn, -whole));
     const double half = 2.0 * turns;  // in units of pi
     const float hi = static_cast<float>(half);
     const float lo = static_cast<float>((half - static_cast<double>(hi)) * 3.14159265358979323846);

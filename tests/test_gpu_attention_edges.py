@@ -68,3 +68,22 @@ def test_queries_of_a_sequence_longer_than_its_pages(torch, nq, room, over, head
     first = max(0, nq - n)
     assert (want[:first] == 0).all() and np.isnan(want[first:nq]).all() and not np.isnan(want[nq:]).any()
     s.check(s.run(kv_len=[n, 10], causal=False, max_kv=max_kv), causal=False, kv_len=[n, 10])
+
+
+# ------------------------------------------------------------------ far positions
+
+def test_rotary_table_at_the_ends_of_the_positions(torch):
+    """The angle's reduction leaves 4 units of 2^-24 (as near positions have) up to the largest position, and for
+    frequencies above 1."""
+    from paper_2607_24787_amd import spp
+    rng = np.random.default_rng(24)
+    T, F = 2000, 16
+    pos = rng.integers(-(1 << 31), (1 << 31) - 1, size=(2, T)).astype(np.int32)
+    pos[:, :2] = [[(1 << 31) - 1, -(1 << 31)]] * 2
+    freq = np.concatenate([rng.uniform(0.1, 1, size=F - 4), [1.0, 2.0, 7.3, 50.0]]).astype(np.float32)
+    axis_of = np.arange(F) % 2
+    table = torch.empty((T, 2, F), device="cuda")
+    p, f = _dev(pos), _dev(freq)
+    spp.spp_rotary_table(p.data_ptr(), T, 2, axis_of, f.data_ptr(), T, table.data_ptr(), _stream())
+    torch.cuda.synchronize()
+    assert np.max(np.abs(_host(table) - oa.rotary_table(pos, axis_of, freq))) <= 4 * U32
