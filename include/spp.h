@@ -387,8 +387,8 @@ spp_status spp_rotary_table(const int32_t* pos, int64_t pos_stride, int32_t n_ax
  * cache.  q: dev [T][n_heads][d] in dtype, token t at q + t * q_stride
  * elements; k, v the same with n_kv_heads heads and k_stride, v_stride (rows
  * of one fused product need no copies).  q_out (row stride q_out_stride)
- * receives the rotated queries in dtype; q_out may be q with the same stride,
- * and otherwise overlaps neither the span of q's rows nor rows of k and v.
+ * receives the rotated queries in dtype; it overlaps no row of k or v, and is q
+ * with the same stride or does not overlap the span of q's rows (EINVAL).
  * q and q_out both NULL: keys and values only.  table: of spp_rotary_table,
  * [T][2][n_freq], 2 * n_freq <= d; element i < n_freq turns with element
  * i + n_freq, elements from 2 * n_freq on stay.  n_freq = 0 (table NULL): no

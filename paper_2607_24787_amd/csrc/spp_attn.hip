@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <type_traits>
+#include <utility>
 
 #include "spp.h"
 #include "spp_internal.h"
@@ -1436,6 +1437,26 @@ bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
   return x < y + nb && y < x + na;
 }
 
+// Whether T rows of na bytes, sa bytes apart, and T rows of nb bytes, sb apart,
+// have a byte in common (a stride is at least its row).  Rows of one fused
+// product lie between each other without.
+bool rows_overlap(const void* a, int64_t sa, int64_t na, const void* b, int64_t sb, int64_t nb, int64_t T) {
+  const int64_t span_a = (T - 1) * sa + na, span_b = (T - 1) * sb + nb;
+  if (!overlap(a, static_cast<uint64_t>(span_a), b, static_cast<uint64_t>(span_b))) return false;
+  const int64_t off = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
+  const auto below = [](int64_t x, int64_t y) { return x / y - (x % y < 0); };  // floor(x / y)
+  // rows of a from the first that ends past row u of b to the last that starts before its end
+  const auto meets = [&](int64_t u) {
+    const int64_t at = off + u * sb;
+    return std::max<int64_t>(0, below(at - na, sa) + 1) <= std::min<int64_t>(T - 1, below(at + nb - 1, sa));
+  };
+  // with one stride all of b's rows lie alike to a's: its first and last are the ones that meet the most
+  if (sa == sb) return meets(0) || meets(T - 1);
+  for (int64_t u = 0; u < T; ++u)
+    if (meets(u)) return true;
+  return false;
+}
+
 const char* dtype_why(int32_t dtype) {
   return dtype == SPP_DTYPE_F32 || dtype == SPP_DTYPE_BF16 ? nullptr : "dtype must be 0 (f32) or 1 (bf16)";
 }
@@ -1616,6 +1637,11 @@ extern "C" spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int3
     const uint64_t out_bytes = extent(q_out_stride, T, desc->n_heads, d, elem);
     if (!same && overlap(q, extent(q_stride, T, desc->n_heads, d, elem), q_out, out_bytes))
       return bad("q_out must be q with the same stride, or not overlap it");
+    const int64_t kv_bytes = static_cast<int64_t>(desc->n_kv_heads) * d * elem;
+    for (const auto& [rows, stride] : {std::pair{k, k_stride}, std::pair{v, v_stride}})
+      if (rows_overlap(q_out, q_out_stride * elem, static_cast<int64_t>(desc->n_heads) * d * elem, rows, stride * elem,
+                       kv_bytes, T))
+        return bad("q_out must not overlap rows of k or v");
   }
   StoreArgs a{};
   a.cache = cache_of(desc, cache);

@@ -203,3 +203,42 @@ def test_a_workspace_is_enough_for_every_smaller_call(dtype):
             spp.spp_kv4_attend(d, GOOD, dtype, GOOD, row, GOOD, GOOD, GOOD, 1, small[0], 1, small[1], small[2], True, 0.1,
                                GOOD * 64, row, GOOD * 4, need)
         assert "workspace" not in str(e.value), (d.n_heads, kv_heads, n, q, kv, small)
+
+
+# ------------------------------------------------------- outputs that overlap rows
+
+ROW, KV = 8 * 64 * 2, 2 * 64 * 2       # bytes of DESC's query rows, of its key or value rows (bf16)
+WIDE = ROW + 2 * KV                    # one fused row: queries, keys, values
+
+
+def _fused(**change):
+    """A call on rows of one fused product, in elements."""
+    return dict(STORE, q_dev=GOOD, q_stride=WIDE // 2, q_out_dev=GOOD, q_out_stride=WIDE // 2, k_dev=GOOD + ROW,
+                k_stride=WIDE // 2, v_dev=GOOD + ROW + KV, v_stride=WIDE // 2, T=5, **change)
+
+
+def _not_refused(call):
+    with pytest.raises(spp.SppError) as e:    # what is left is that there is no device
+        call()
+    assert e.value.status == spp.SPP_EHIP
+
+
+@pytest.mark.parametrize("change", [
+    dict(k_dev=GOOD), dict(v_dev=GOOD + ROW - 16), dict(k_dev=GOOD + WIDE - 16), dict(v_dev=GOOD + 4 * WIDE),
+    dict(k_dev=GOOD - WIDE + ROW - 16),
+    # rotated queries beside the fused rows, keys where they go
+    dict(q_out_dev=2 * GOOD, q_out_stride=ROW // 2, k_dev=2 * GOOD + 3 * ROW, k_stride=KV // 2),
+    dict(q_out_dev=2 * GOOD, q_out_stride=ROW // 2, v_dev=2 * GOOD - 4 * WIDE - KV + 16),
+    dict(q_out_dev=2 * GOOD, q_out_stride=2 * WIDE // 2, k_dev=2 * GOOD + WIDE, k_stride=WIDE // 2)])
+def test_rotated_queries_over_keys_or_values_are_refused(change):
+    _refused(lambda: spp.spp_kv4_store(**{**_fused(), **change}))
+
+
+@pytest.mark.parametrize("change", [
+    {}, dict(v_dev=GOOD + ROW), dict(k_dev=GOOD + 5 * WIDE), dict(k_dev=GOOD - 5 * WIDE + ROW),
+    dict(q_out_dev=2 * GOOD, q_out_stride=ROW // 2, v_dev=2 * GOOD - 4 * WIDE - KV),
+    # between the rows: at the same stride, and at twice the stride
+    dict(q_dev=4 * GOOD, q_out_dev=2 * GOOD + WIDE, k_dev=2 * GOOD + ROW),
+    dict(q_dev=4 * GOOD, q_out_dev=2 * GOOD, k_dev=2 * GOOD + ROW, k_stride=WIDE)])
+def test_rotated_queries_beside_keys_and_values_are_taken(change):
+    _not_refused(lambda: spp.spp_kv4_store(**{**_fused(), **change}))
