@@ -409,7 +409,8 @@ spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int32_t dtype, 
                          void* hip_stream);
 
 /* Read T tokens' keys and values back: k_out, v_out dev [T][n_kv_heads][d] in
- * dtype with their row strides (exact in either dtype); either may be NULL.
+ * dtype with their row strides (exact in either dtype), no row of one over one
+ * of the other; either may be NULL.
  * The rows of a token whose slot is outside [0, n_pages * page) are left as
  * they were.  Alignment as for spp_kv4_store; T * 2 n_kv_heads at most 2^27. */
 spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dtype, const int64_t* slots, int32_t T,

@@ -1681,6 +1681,9 @@ extern "C" spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache,
   if (!aligned16(cache) || !aligned(slots, 8)) return bad("cache must be 16-byte aligned, slots 8-byte aligned");
   if (k_out) SPP_BAD(rows_why(k_out, k_stride, desc->n_kv_heads, d, elem));
   if (v_out) SPP_BAD(rows_why(v_out, v_stride, desc->n_kv_heads, d, elem));
+  const int64_t row_bytes = static_cast<int64_t>(desc->n_kv_heads) * d * elem;
+  if (k_out && v_out && rows_overlap(k_out, k_stride * elem, row_bytes, v_out, v_stride * elem, row_bytes, T))
+    return bad("k_out must not overlap rows of v_out");
   LoadArgs a{};
   a.cache = cache_of(desc, cache);
   a.slots = slots;

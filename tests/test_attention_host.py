@@ -242,3 +242,11 @@ def test_rotated_queries_over_keys_or_values_are_refused(change):
     dict(q_dev=4 * GOOD, q_out_dev=2 * GOOD, k_dev=2 * GOOD + ROW, k_stride=WIDE)])
 def test_rotated_queries_beside_keys_and_values_are_taken(change):
     _not_refused(lambda: spp.spp_kv4_store(**{**_fused(), **change}))
+
+
+def test_read_back_keys_over_values_are_refused():
+    rows = dict(LOAD, T=4, k_stride=256, v_stride=256)
+    for v in (GOOD, GOOD + 128, GOOD + 3 * 512, GOOD + 512 - 16, GOOD - 3 * 512 + 240):
+        _refused(lambda: spp.spp_kv4_load(**{**rows, "v_out_dev": v}))
+    for v in (GOOD + 256, GOOD - 256, GOOD + 4 * 512, GOOD - 3 * 512 - 256):
+        _not_refused(lambda: spp.spp_kv4_load(**{**rows, "v_out_dev": v}))
