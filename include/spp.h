@@ -478,8 +478,10 @@ spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cache, int32_t 
  * slots (dev int64 [B], where each token's key and value go), kv_len (dev int32
  * [B], the sequences' lengths with this token), pages as for spp_kv4_attend.
  * The arrays are read by the step's layer calls on the compute stream: they
- * stay as they are until that work is done.  A layer call without a step of
- * its B is refused (ESTATE). */
+ * stay as they are until that work is done.  A step serves one call of each
+ * layer: a layer call without a step of its B that has not served the layer
+ * yet is refused (ESTATE; it would write the last token's place again).  A step
+ * that is refused leaves the one before it as it is. */
 spp_status spp_set_attention(spp_ctx* ctx, const spp_attn_desc* desc, int32_t n_axes, const int32_t* axis_of,
                              const float* inv_freq, int32_t n_freq, int32_t max_kv);
 spp_status spp_bind_attention(spp_ctx* ctx, int32_t l, const void* w_qkv, const void* w_o, void* cache);

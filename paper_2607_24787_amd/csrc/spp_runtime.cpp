@@ -69,6 +69,7 @@ struct LayerState {
   const void* shared = nullptr;
   const void *w_qkv = nullptr, *w_o = nullptr;  // attention (spp_bind_attention)
   void* kv_cache = nullptr;
+  uint64_t attn_step = 0;  // the attention step that served this layer (Attention::step; 0: none)
   const uint8_t* host_store = nullptr;
   const uint8_t* host_store_dev = nullptr;  // its device-visible address (read by the copy kernel)
   uint8_t* slots = nullptr;
@@ -101,7 +102,8 @@ struct Attention {
   void* out = nullptr;     // [max_batch, n_heads head_dim]
   void* workspace = nullptr;
   size_t workspace_bytes = 0;
-  int32_t B = 0;  // tokens of the step that was set; 0: none
+  uint64_t step = 0;  // number of the step that was set; 0: none
+  int32_t B = 0;      // its tokens
   const int64_t* slots = nullptr;
   const int32_t *kv_len = nullptr, *pages = nullptr;
   int64_t pages_stride = 0;
@@ -1142,7 +1144,8 @@ spp_status layer_begin(spp_ctx* c, int32_t l, const void* h_in, void* h_out, int
   if (M_max < -1) return fail(SPP_EINVAL, "M_max must be >= -1");
   LayerState& ls = c->layers[l];
   if (c->attn.on && !ls.kv_cache) return fail(SPP_ESTATE, "the layer's attention is not bound");
-  if (c->attn.on && c->attn.B != B) return fail(SPP_ESTATE, "no attention step was set for this batch");
+  if (c->attn.on && (c->attn.B != B || ls.attn_step == c->attn.step))
+    return fail(SPP_ESTATE, "no attention step was set for this call of the layer");
   Flight& fl = *out;
   fl.l = l;
   fl.B = B;
@@ -1173,6 +1176,7 @@ spp_status layer_begin(spp_ctx* c, int32_t l, const void* h_in, void* h_out, int
     SPP_HIP(spp::launch_proj(pa, dt, c->compute));
   } else if (c->attn.on) {
     if (spp_status s = attention_prologue(c, ls, h_in, B)) return s;
+    ls.attn_step = c->attn.step;
   }
   fl.seq = next_router_seq(c);
   fl.set = next_rec_set(c);
@@ -1248,6 +1252,13 @@ spp_status layer_begin(spp_ctx* c, int32_t l, const void* h_in, void* h_out, int
   return SPP_OK;
 }
 
+// Give up a call whose launches are enqueued but whose host side will not run:
+// its attention step serves the layer again (the same rows of the cache).
+void layer_drop(spp_ctx* c, Flight& fl) {
+  if (c->timing) c->free_sets.push_back(fl.ts);
+  c->layers[fl.l].attn_step = 0;
+}
+
 // The host side of a layer call: its routing, the slot decisions (with the
 // copies, the FFN and the combine where the layer was not device-routed), the
 // prefetch for layer l+1, and the outputs.
@@ -1264,7 +1275,7 @@ spp_status layer_finish(spp_ctx* c, Flight& fl, int32_t* topk_out, float* gate_o
   const bool split_ok = c->ffn_overlap && !c->grouped && B == 1;
   if (spp_status e = wait_router(c, fl.seq, fl.set, 0, B)) {
     c->clock = tau - 1;
-    if (c->timing) c->free_sets.push_back(ts);
+    layer_drop(c, fl);
     return e;
   }
   const auto t_routed = std::chrono::steady_clock::now();
@@ -1286,7 +1297,7 @@ spp_status layer_finish(spp_ctx* c, Flight& fl, int32_t* topk_out, float* gate_o
                               "needs the batched bf16 path";
     if (bad != SPP_OK) {
       c->clock = tau - 1;
-      if (c->timing) c->free_sets.push_back(ts);
+      layer_drop(c, fl);
       return fail(bad, msg);
     }
   }
@@ -1469,11 +1480,6 @@ spp_status layer_finish(spp_ctx* c, Flight& fl, int32_t* topk_out, float* gate_o
   c->stats.waited += st.waited;
   if (st_out) *st_out = st;
   return SPP_OK;
-}
-
-// Give up a call whose launches are enqueued but whose host side will not run.
-void layer_drop(spp_ctx* c, Flight& fl) {
-  if (c->timing) c->free_sets.push_back(fl.ts);
 }
 
 }  // namespace
@@ -1670,6 +1676,7 @@ spp_status spp_attention_step(spp_ctx* c, int32_t B, const int32_t* pos, int64_t
     if (spp_status s = spp_rotary_table(pos, pos_stride, at.n_axes, at.axis_of, at.inv_freq, at.n_freq, B, at.table,
                                         c->compute))
       return s;
+  at.step += 1;
   at.B = B;
   at.slots = slots;
   at.kv_len = kv_len;
