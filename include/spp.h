@@ -469,7 +469,7 @@ spp_status spp_kv4_attend(const spp_attn_desc* desc, const void* cache, int32_t 
  * n_freq as for spp_rotary_table, inv_freq kept; n_freq 0: no rotation) and
  * about how many tokens a sequence comes to (a hint).  n_heads * head_dim at
  * most 4096 (bf16) or 2048 (fp32).  Allocates the context's buffers; ESTATE if
- * it was set before.
+ * it was set before, or after a layer call.
  * spp_bind_attention, for every layer: w_qkv dev [(n_heads + 2 n_kv_heads) *
  * head_dim][D] (queries, keys, values), w_o dev [D][n_heads * head_dim], cache
  * dev spp_kv4_cache_bytes bytes, all 16-byte aligned.

@@ -126,6 +126,7 @@ struct spp_ctx {
   std::vector<LayerState> layers;
   float* u_dev = nullptr;      // [maxB, D] prologue output
   Attention attn;
+  bool layer_called = false;   // what is set before the first layer call can be set no more
   float* x_dev = nullptr;      // [maxB, D] router input
   float* zbuf = nullptr;       // [maxB, n + r]
   uint64_t* ztag = nullptr;    // [n + r] batch-1 router values tagged with their launch's seq (zero: none yet)
@@ -1162,6 +1163,7 @@ spp_status layer_begin(spp_ctx* c, int32_t l, const void* h_in, void* h_out, int
   c->device_routed += fl.routed ? 1 : 0;
   if (fl.routed)
     if (spp_status s = upload_slot_table(c, ls)) return s;
+  c->layer_called = true;
   fl.tau = ++c->clock;
   const int dt = d.dtype;
   TimingSet& ts = fl.ts;
@@ -1620,6 +1622,7 @@ spp_status spp_set_attention(spp_ctx* c, const spp_attn_desc* desc, int32_t n_ax
     if (axis_of[i] < 0 || axis_of[i] >= n_axes) return fail(SPP_EINVAL, "axis_of names an axis outside [0, n_axes)");
   if (max_kv < 1) return fail(SPP_EINVAL, "max_kv must be >= 1");
   if (c->attn.on) return fail(SPP_ESTATE, "the context's attention is already set");
+  if (c->layer_called) return fail(SPP_ESTATE, "the context's attention is set before its first layer call");
   Attention at;
   at.desc = *desc;
   at.n_axes = n_axes;

@@ -55,3 +55,21 @@ def test_a_step_serves_one_call_of_each_layer(stack_of, name):
             st.layer(l, l % 2, 1 - l % 2, 0)
     finally:
         st.close()
+
+
+def test_attention_is_set_before_the_first_layer_call(stack_of):
+    from paper_2607_24787_amd import spp
+    from workload import gen
+    st = stack_of(SMALL.with_(attn_heads=0))
+    try:
+        desc = spp.make_attn_desc(4, 2, 64, 16, 4)
+        h0 = gen.hidden_states(st.cfg, tokens=1)
+        _refused(spp.SPP_EINVAL, st.step, h0[0], -2)                 # a refused call is none
+        st.step(h0[0], 0)
+        out = st.download(st.hbuf[st.last_buf])
+        _refused(spp.SPP_ESTATE, spp.spp_set_attention, st.ctx, desc, 1, [], 0, 10)
+        st.reset()
+        st.step(h0[0], 0)                                            # and the context goes on without
+        assert np.array_equal(st.download(st.hbuf[st.last_buf]), out)
+    finally:
+        st.close()
