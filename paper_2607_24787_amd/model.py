@@ -77,8 +77,18 @@ class PagedAttention:
                 self.pos[:, :B] = torch.from_numpy(np.ascontiguousarray(positions, dtype=np.int32)).to(self.pos.device)
             self.kv_len[:B] += 1
         self.length[:B] += 1
-        spp.spp_attention_step(self.stack.ctx, B, self.pos.data_ptr(), cfg.batch, self.slots.data_ptr(),
-                               self.kv_len.data_ptr(), self.pages.data_ptr(), self.per_seq)
+        try:
+            spp.spp_attention_step(self.stack.ctx, B, self.pos.data_ptr(), cfg.batch, self.slots.data_ptr(),
+                                   self.kv_len.data_ptr(), self.pages.data_ptr(), self.per_seq)
+        except spp.SppError:
+            self.take_back(B)
+            raise
+
+    def take_back(self, B: int):
+        """Undo next_token(B) after a step that was refused or did not reach its end: the next token takes the same places."""
+        with self.stack.torch.cuda.stream(self.stack.stream):
+            self.kv_len[:B] -= 1
+        self.length[:B] -= 1
 
 
 class OffloadedMoEStack:
@@ -181,6 +191,10 @@ class OffloadedMoEStack:
         if self.attention:
             self.attention.next_token(self.cfg.batch if B is None else B)
 
+    def _take_back(self, B: Optional[int]):
+        if self.attention:
+            self.attention.take_back(self.cfg.batch if B is None else B)
+
     def _to_storage(self, v):
         from workload.gen import f32_to_bf16_bits
         v = np.asarray(v, dtype=np.float32)
@@ -215,9 +229,13 @@ class OffloadedMoEStack:
         self._next_token(B)
         out = []
         src = 0
-        for l in range(self.cfg.L):
-            out.append(self.layer(l, src, 1 - src, M_max, B))
-            src = 1 - src
+        try:
+            for l in range(self.cfg.L):
+                out.append(self.layer(l, src, 1 - src, M_max, B))
+                src = 1 - src
+        except spp.SppError:
+            self._take_back(B)
+            raise
         self.last_buf = src
         return out
 
@@ -228,10 +246,14 @@ class OffloadedMoEStack:
         out = []
         src_ptr = h_in_ptr
         dst = 0
-        for l in range(self.cfg.L):
-            out.append(spp.moe_layer_forward(self.ctx, l, src_ptr, self.hbuf[dst].data_ptr(), B, self.cfg.K, M_max))
-            src_ptr = self.hbuf[dst].data_ptr()
-            dst = 1 - dst
+        try:
+            for l in range(self.cfg.L):
+                out.append(spp.moe_layer_forward(self.ctx, l, src_ptr, self.hbuf[dst].data_ptr(), B, self.cfg.K, M_max))
+                src_ptr = self.hbuf[dst].data_ptr()
+                dst = 1 - dst
+        except spp.SppError:
+            self._take_back(B)
+            raise
         self.last_buf = 1 - dst
         return out
 
@@ -241,8 +263,12 @@ class OffloadedMoEStack:
         (topk, gates, stats) like step_from."""
         B = self.cfg.batch if B is None else B
         self._next_token(B)
-        topk, gates, stats = spp.spp_decode_step(self.ctx, self.cfg.L, h_in_ptr, self.hbuf[0].data_ptr(),
-                                                 self.hbuf[1].data_ptr(), B, self.cfg.K, M_max)
+        try:
+            topk, gates, stats = spp.spp_decode_step(self.ctx, self.cfg.L, h_in_ptr, self.hbuf[0].data_ptr(),
+                                                     self.hbuf[1].data_ptr(), B, self.cfg.K, M_max)
+        except spp.SppError:
+            self._take_back(B)
+            raise
         self.last_buf = 0
         return [(topk[l], gates[l], stats[l]) for l in range(self.cfg.L)]
 

@@ -73,3 +73,35 @@ def test_attention_is_set_before_the_first_layer_call(stack_of):
         assert np.array_equal(st.download(st.hbuf[st.last_buf]), out)
     finally:
         st.close()
+
+
+@pytest.mark.parametrize("how", ["step", "step_from", "decode_step_from"])
+def test_a_refused_step_leaves_the_sequences_as_they_were(stack_of, how):
+    """A step that a layer refuses, and one that is refused before: the next one writes the places they would have."""
+    import torch
+    from paper_2607_24787_amd import spp
+    from workload import gen
+    cfg = CASES["bf16_b1"]
+    a, b = stack_of(cfg), stack_of(cfg)
+    try:
+        h0 = gen.hidden_states(cfg, tokens=18)
+
+        def run(st, t, M_max, B=None):
+            src = torch.from_numpy(np.ascontiguousarray(h0[t]).view(np.uint8).reshape(-1).copy()).to(st.device)
+            call = getattr(st, how)
+            return call(h0[t], M_max, B) if how == "step" else call(src.data_ptr(), M_max, B)
+
+        for t in range(18):
+            before = _state(a)
+            _refused(spp.SPP_EINVAL, run, a, t, -2)
+            assert _state(a) == before
+            if t % 5 == 0:
+                _refused(spp.SPP_EINVAL, run, a, t, 0, cfg.batch + 1)     # the step itself is refused
+                assert _state(a) == before
+            run(a, t, 1)
+            run(b, t, 1)
+            assert np.array_equal(a.download(a.hbuf[a.last_buf]), b.download(b.hbuf[b.last_buf])), t
+        assert _state(a) == _state(b)
+    finally:
+        a.close()
+        b.close()
