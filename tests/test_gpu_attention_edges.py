@@ -87,3 +87,37 @@ def test_rotary_table_at_the_ends_of_the_positions(torch):
     spp.spp_rotary_table(p.data_ptr(), T, 2, axis_of, f.data_ptr(), T, table.data_ptr(), _stream())
     torch.cuda.synchronize()
     assert np.max(np.abs(_host(table) - oa.rotary_table(pos, axis_of, freq))) <= 4 * U32
+
+
+# ------------------------------------------------- many steps of one workgroup
+
+LONG = [(1, 4, 1, 64, "f32"), (3, 5, 1, 128, "f32"), (2, 8, 1, 128, "bf16"), (5, 3, 1, 64, "bf16"),          # 16 rows
+        (3, 8, 1, 128, "bf16"), (3, 8, 1, 64, "f32"), (4, 6, 1, 128, "f32"), (9, 3, 1, 64, "bf16"),          # 32
+        (150, 2, 1, 128, "bf16"), (150, 2, 1, 64, "f32"), (70, 2, 1, 128, "f32"), (300, 1, 1, 64, "bf16")]   # shared operands
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("nq,heads,kv_heads,d,dtype", LONG)
+def test_long_runs_of_one_workgroup(torch, nq, heads, kv_heads, d, dtype, causal):
+    """A hint of no cached tokens leaves every sequence in one part: 22 to 47 tiles of 32 tokens a workgroup, on shuffled
+    pages of 16."""
+    s = Setup([nq, nq, 2], [1500, 701, 930], heads, kv_heads, d, 16, dtype, seed=25)
+    s.check(s.run(causal=causal, max_kv=0), causal=causal)
+
+
+@pytest.mark.parametrize("max_kv", [0, 1500])
+@pytest.mark.parametrize("nq,heads,kv_heads,d,dtype", LONG)
+def test_what_is_not_finite_late_in_a_long_run(torch, nq, heads, kv_heads, d, dtype, max_kv):
+    """A missing page, a NaN key block and a NaN value block past a workgroup's eighth tile reach the rows that see them, and
+    no other."""
+    s = Setup([nq, nq, nq], [1500, 701, 930], heads, kv_heads, d, 16, dtype, seed=26)
+    s.pages[0, 93] = -1                                                    # tokens 1,488 .. 1,499
+    for b, t, kv in ((1, 700 - nq // 2, 0), (2, 929 - nq // 3, 1)):
+        slot = int(s.pages[b, t // 16]) * 16 + t % 16
+        p, _, places = s.cache._places(kv, slot)
+        s.cache.raw[p, 0, places[1 if d == 128 else 0]] = 255
+    want = s.check(s.run(max_kv=max_kv))
+    assert np.isnan(want[nq - 1]).all() and np.isnan(want[2 * nq - 1]).all() and np.isnan(want[3 * nq - 1]).any()
+    assert not np.isnan(want[2 * nq:3 * nq]).all()
+    if nq > 12:
+        assert not np.isnan(want[0]).any() and not np.isnan(want[nq]).any()
