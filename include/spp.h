@@ -420,10 +420,12 @@ spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dt
  *   out[i] = sum_t softmax_t(scale * q[i] . k[t]) v[t].
  * q, out: dev [n_tokens][n_heads][d] in dtype with their row strides (out may
  * be q with the same stride; else their spans, first row to last, do not
- * overlap).  scale: positive, at most 1e38.  q_start: dev int32 [n_seq + 1], sequence b has
- * the query tokens q_start[b] .. q_start[b+1] - 1; NULL: one each (n_tokens =
- * n_seq).  kv_len: dev int32 [n_seq], cached tokens of each; token t of
- * sequence b is in page pages[b * pages_stride + t / page] (dev int32).
+ * overlap).  scale: positive, at most 1e38.  q_start: dev int32 [n_seq + 1],
+ * sequence b has the query tokens q_start[b] .. q_start[b+1] - 1 (entries count
+ * as the nearest of 0 .. n_tokens; where they fall back, a row of two sequences
+ * holds no certain result); NULL: one each (n_tokens = n_seq).  kv_len: dev
+ * int32 [n_seq], cached tokens of each; token t of sequence b is in page
+ * pages[b * pages_stride + t / page] (dev int32).
  * causal = 1: the queries are the sequence's last tokens, query j of n sees
  * cached tokens t <= kv_len - n + j; 0: every query sees all of them.  A
  * query that sees no token gives zeros.  Rows of no sequence are left as they
@@ -442,7 +444,9 @@ spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dt
  * at most 208 with n_seq * n_kv_heads above 32.  In calls of more rows they are
  * rounded to bf16, and divided by the fp32 sum of them as rounded.  fp32 queries
  * and probabilities go in as three bf16 terms each (a query beyond bf16's
- * largest number, 3.39e38, counts as infinite).
+ * largest number, 3.39e38, counts as infinite).  Sums of values are fp32 and up
+ * to 2^8 for each token seen before they are divided: values near the format's
+ * largest, beyond 2^120 over the tokens seen, may give infinities.
  * Sizes: n_seq * max_q * n_heads and n_tokens * n_heads at most 2^30, and fewer
  * than 2^22 workgroups, which take 16 to 256 rows (query tokens times the heads
  * of a key/value head) of one sequence and key/value head each.

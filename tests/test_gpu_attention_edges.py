@@ -121,3 +121,27 @@ def test_what_is_not_finite_late_in_a_long_run(torch, nq, heads, kv_heads, d, dt
     assert not np.isnan(want[2 * nq:3 * nq]).all()
     if nq > 12:
         assert not np.isnan(want[0]).any() and not np.isnan(want[nq]).any()
+
+
+# ------------------------------------------------------------------- one workspace
+
+def test_one_workspace_serves_calls_of_every_shape(torch):
+    """Calls of changing head counts, types, lengths and row counts on one workspace, cleared once: the bits of a workspace of
+    their own, whatever the calls before have left in it.  Up to 1,024 rows a token."""
+    rng = np.random.default_rng(27)
+    ws = torch.zeros((1 << 26) + 64, dtype=torch.uint8, device="cuda")
+    for heads, kv_heads, d, dtype, seqs, nq in [(8, 1, 128, "bf16", 5, 1), (64, 1, 64, "f32", 3, 1), (32, 4, 128, "bf16", 20, 1),
+                                                (6, 3, 64, "bf16", 4, 7), (1024, 1, 64, "bf16", 1, 1), (8, 1, 128, "bf16", 1, 1),
+                                                (40, 1, 128, "f32", 2, 2), (4, 2, 64, "f32", 9, 40), (8, 1, 128, "bf16", 5, 1)]:
+        kv = [900] + rng.integers(0, 900, size=seqs - 1).tolist()
+        s = Setup([nq] * seqs, kv, heads, kv_heads, d, 32, dtype, seed=seqs)
+        for max_kv in (900, 100000):
+            own = s.run(max_kv=max_kv)
+            s.check(own)
+            from paper_2607_24787_amd import spp
+            size = spp.spp_kv4_attend_workspace(s.desc, seqs, nq, max_kv)
+            shared = ws[:size + 64]
+            guard = ws[size:size + 64].clone()
+            ws[size:size + 64] = 255                 # what run() looks for behind a workspace
+            assert torch.equal(s.run(max_kv=max_kv, ws=shared), own)
+            ws[size:size + 64] = guard
