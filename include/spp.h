@@ -439,14 +439,14 @@ spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dt
  * page), or with a page id outside [0, n_pages) among those a query sees,
  * gives that query NaN.
  * Scores and softmax statistics are fp32; bf16 queries are exact operands.
- * Their probabilities go into the value product as two bf16 terms (16 bits) in
- * calls of few rows: max_q times the heads of a key/value head at most 32, or
- * at most 208 with n_seq * n_kv_heads above 32.  In calls of more rows they are
- * rounded to bf16, and divided by the fp32 sum of them as rounded.  fp32 queries
- * and probabilities go in as three bf16 terms each (a query beyond bf16's
- * largest number, 3.39e38, counts as infinite).  Sums of values are fp32 and up
- * to 2^8 for each token seen before they are divided: values near the format's
- * largest, beyond 2^120 over the tokens seen, may give infinities.
+ * Where max_q times the heads of a key/value head is at most 16, their
+ * probabilities go into the value product as two bf16 terms (16 bits); in calls
+ * of more rows they are rounded to bf16, and divided by the fp32 sum of them as
+ * rounded.  fp32 queries and probabilities go in as three bf16 terms each (a
+ * query beyond bf16's largest number, 3.39e38, counts as infinite).  Sums of
+ * values are fp32 and up to 2^8 for each token seen before they are divided:
+ * values near the format's largest, beyond 2^120 over the tokens seen, may give
+ * infinities.
  * Sizes: n_seq * max_q * n_heads and n_tokens * n_heads at most 2^30, and fewer
  * than 2^22 workgroups, which take 16 to 256 rows (query tokens times the heads
  * of a key/value head) of one sequence and key/value head each.

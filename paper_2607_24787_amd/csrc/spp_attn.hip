@@ -666,18 +666,22 @@ __device__ __forceinline__ void follow_maximum(const f32x4 (&s)[R][2], float sca
 }
 
 // A tile's scores to the probabilities of the value product, relative to the
-// maximum; l sums this lane's eight.
-template <int R, int NS>
+// maximum.  One term (f32x4 sums): l sums the row's as rounded, so that what the
+// rounding does to all of them alike is divided out.  More: l sums this lane's
+// eight as they are.
+template <int R, int NP, typename Sum>
 __device__ __forceinline__ void probabilities(const f32x4 (&s)[R][2], float scale_log2, const float (&m)[R],
-                                              float (&l)[R], u32x4 (&pf)[R][NS]) {
+                                              Sum (&l)[R], u32x4 (&pf)[R][NP]) {
+  const u32x4 ones = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const float ref = m[r] == -INFINITY ? 0.f : m[r];  // nothing seen yet: every power is 0
     float p[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) p[k] = __builtin_amdgcn_exp2f(fmaf(s[r][k / 4][k % 4], scale_log2, -ref));
-    l[r] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-    split8<NS>(p, pf[r]);
+    if constexpr (NP > 1) l[r] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    split8<NP>(p, pf[r]);
+    if constexpr (NP == 1) l[r] = mfma(ones, pf[r][0], l[r]);
   }
 }
 
@@ -778,9 +782,13 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
   constexpr int W = kWaves;
   constexpr int NS = std::is_same<T, float>::value ? 3 : 1;  // bf16 terms of a query
   // and of a probability: two lose 2^-16 of it, so that a bf16 output is off by
-  // its own rounding alone.  One would lose as much as that rounding: 131,072
-  // tokens 23.1 us in all instead of 24.0, 64 ragged sequences 26.9, not 27.8.
-  constexpr int NP = std::is_same<T, float>::value ? 3 : 2;
+  // its own rounding alone (1.6e-3; with one term 2.3e-3).  One token over
+  // 131,072 takes 24.0 us with two and 23.1 with one, 64 ragged sequences 27.8
+  // and 26.9.  32 rows a workgroup keep one: their products and vector work bound
+  // them, and two terms would make 60 us of 53 (48 sequences of 32 rows over
+  // 6,000 tokens) and 93 of 78 (64 rows).
+  constexpr int NP = std::is_same<T, float>::value ? 3 : (R == 1 ? 2 : 1);
+  using Sum = typename std::conditional<NP == 1, f32x4, float>::type;
   constexpr int KW = D / 32, NT = D / 16;
   constexpr int kRows = 16 * R, kPad = 4;
   __shared__ float s_o[W][16][D + kPad];
@@ -815,11 +823,12 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
   }
 
   f32x4 o[R][NT];
-  float m[R], l[R];
+  Sum l[R];
+  float m[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = -INFINITY;
-    l[r] = 0.f;
+    l[r] = Sum{};
 #pragma unroll
     for (int n = 0; n < NT; ++n) o[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -917,11 +926,16 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (r > 0) __syncthreads();
-    l[r] += __shfl_xor(l[r], 16);
-    l[r] += __shfl_xor(l[r], 32);
+    float whole;  // the row's sum of this wave's probabilities
+    if constexpr (NP == 1) {
+      whole = l[r][0];
+    } else {
+      whole = l[r] + __shfl_xor(l[r], 16);
+      whole += __shfl_xor(whole, 32);
+    }
     if (g == 0) {
       s_m[wave][c] = m[r];
-      s_l[wave][c] = l[r];
+      s_l[wave][c] = whole;
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)  // A row 4g + e is elements (4g + e) * NT + n
