@@ -173,7 +173,6 @@ struct StoreArgs {
   const int64_t* slots;
   int Hq, Hkv, F;  // Hq = 0: no queries
   int T;
-  int stream_q;    // the queries are more than the L2 caches hold
 };
 
 // Codes (one word) and scale byte of this lane's 8 elements of a block of 32,
@@ -214,8 +213,10 @@ __device__ __forceinline__ float turn(float y, float z, float c, float s, bool f
 // they turn with before it writes, and a head lies within one wave, so the
 // queries may be rotated in place.  The partner's elements are read a second
 // time (from L1) instead of exchanged.  Bound by memory: 8,192 tokens of 32 + 4
-// + 4 heads of 128, 160 MB, in 33 to 36 us (4.4 to 4.8 TB/s; a large copy 5.0);
-// one token 2.5 us.  Non-temporal reads of the rows as well: 39 us.
+// + 4 heads of 128, 160 MB (170 by the counters), in 36.4 us (4.7 TB/s; a large
+// copy 5.0); one token 2.5 us.  Queries written past the caches would take 4 us
+// off that, but what reads them next then waits for memory: 8,192 tokens with a
+// reader behind them 57.6 us so, 59.9 past the caches; 16,384 tokens 113, 111.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_store_kernel(StoreArgs a) {
   constexpr int L = D / 8;
@@ -247,10 +248,7 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(StoreArgs a) {
   }
   if (kind == 0) {
     T* to = reinterpret_cast<T*>(a.q_out) + static_cast<int64_t>(t) * a.q_out_stride + h * D + e0;
-    if (a.stream_q)
-      stream8(to, y);
-    else
-      store8(to, y);
+    store8(to, y);
     return;
   }
   uint32_t byte;
@@ -1672,8 +1670,6 @@ extern "C" spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int3
   a.Hq = Hq;
   a.Hkv = desc->n_kv_heads;
   a.F = n_freq;
-  // 8,192 tokens of 32 + 2 * 4 heads: 33.2 us so, 36.5 with ordinary stores
-  a.stream_q = static_cast<int64_t>(T) * Hq * d * elem > (int64_t{32} << 20);
   a.T = T;
   const int per = 256 / (d / 8);
   const int64_t units = static_cast<int64_t>(T) * (Hq + 2 * desc->n_kv_heads);
