@@ -133,8 +133,9 @@ constexpr int kTableFreqs = 4;  // per thread: 16-byte stores
 // 3e-7 of a value at the largest positions, five steps of fp32).  What is left
 // beyond fp32 goes in by the first term of the addition theorem (error 2.6e-8 of
 // the values, half a step of fp32 2e-8 on average).  16,001 tokens of 64
-// frequencies 5.1 us (8.4 MB written, 1.6 TB/s: bound by its arithmetic and the
-// launch), 64 tokens 2.5 us.
+// frequencies 5.2 us (8.2 MB written), 64 tokens 2.5 us: a launch and one round of
+// waves, which are all resident at once; a wave of the 16,001 tokens' lives 2.5
+// us, half of it waiting for its positions and frequencies.
 __global__ __launch_bounds__(256) void rotary_table_kernel(TableArgs a) {
   const uint32_t per = static_cast<uint32_t>(a.F / kTableFreqs);
   const uint32_t i = blockIdx.x * 256u + threadIdx.x;
@@ -271,7 +272,9 @@ struct LoadArgs {
 
 // Bound by memory, most of it the rows written: 100,000 tokens of 4 heads of 128
 // in bf16, 260 MB, in 45 us (5.8 TB/s) with stores past the caches, 77 us with
-// ordinary ones, 66 us with reads past them too; 700 tokens in fp32 3.1 us.
+// ordinary ones, 66 us with reads past them too; 700 tokens in fp32 3.1 us.  With
+// a reader of the rows behind it: 16,000 tokens 19.4 us past the caches, 18.8
+// with ordinary stores, 100,000 tokens 124 and 125, 64,000 in fp32 134 and 151.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_load_kernel(LoadArgs a) {
   constexpr int L = D / 8;
@@ -767,14 +770,17 @@ struct Joined {
 // of its row for eight tokens in a row, which is the operand of the second
 // product as it stands, and codes become operands in registers, keys without any
 // exchange.  Codes are converted by the hardware (exactly), scales with them.
-// Bound by reading the cache: 131,072 tokens of 4 heads of 128, 71 MB, in 17.5 us
-// (4.1 TB/s, about 2.5 us of them the first loads' latency), vector units at half
-// of their rate; 64 sequences of 128 to 8,192 tokens, 90 MB, 27 us, of which 4.5
-// joining parts and 2 writing them.  Four waves and as many workgroups as are
-// resident at once: 131,072 tokens with half as many 18.5 us, twice as many 20.7
+// Bound by reading the cache, with the conversions' vector work close behind:
+// 131,072 tokens of 4 heads of 128, 71 MB, in 20.6 us from memory (3.5 TB/s, about
+// 2.5 us of them the first loads' latency) and 18.9 where the last-level cache
+// still holds a part; vector instructions issue for 0.65 of the waves' time, and a
+// wave waits for loads for 0.43 of its own.  64 sequences of 128 to 8,192 tokens,
+// 90 MB, 28.9 us (31 from memory), of which 4.5 joining parts and 2 writing them.
+// Four waves and as many workgroups as are resident at once; with one term of a
+// probability (see NP), 17.5 us: half as many workgroups 18.5, twice as many 20.7
 // and a longer join, 16 waves (a quarter as many parts) 20.0; the 64 sequences
-// with half as many parts 36 us, twice as many 36.  Parts of 4 tiles instead of 8
-// at least: nine short fp32 sequences 13.5 us, not 11.6.
+// with half as many parts 36 us, twice as many 36, not 27.  Parts of 4 tiles
+// instead of 8 at least: nine short fp32 sequences 13.5 us, not 11.6.
 template <typename T, int D, int R>
 __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value, D, R)) void kv4_attend_kernel(AttendArgs a) {
   constexpr int W = kWaves;
@@ -1048,12 +1054,14 @@ __global__ __launch_bounds__(64 * kWaves, resident(std::is_same<T, float>::value
 // scores are multiplied while the tile before it goes through the softmax, so
 // that the matrix cores and the vector units have work at the same time; the
 // keys are therefore formed two steps ahead, the values one, beside the value
-// products.  Bound by the matrix cores and what is left between their products:
-// 2 sequences of 1,024 tokens over 8,192, 32 heads of 128, 258 us, 998 TFLOP/s
-// (1,150 for a large library product here).  On the way: 64 rows a workgroup in
-// the form above 437 us; operands shared, tile after tile 349; scores ahead 325;
-// wider loads of the codes 271; forming beside the products 258.  Without
-// forming (wrong results) it is 228.
+// products.  2 sequences of 1,024 tokens over 8,192, 32 heads of 128, 256 us,
+// 1,007 TFLOP/s (1,140 for a large library product here).  The matrix units are
+// busy for 0.46 of that, other vector instructions issue for 0.36, and the two
+// waves of a SIMD overlap the two only in part; a wave waits for LDS, loads and
+// the barrier for 0.29 of its time.  On the way: 64 rows a workgroup in the form
+// above 437 us; operands shared, tile after tile 349; scores ahead 325; wider
+// loads of the codes 271; forming beside the products 258.  Without forming (wrong
+// results) it is 228.
 constexpr int kRowWaves = 8;
 
 // Two tokens' codes as words of the value operands: fn(n, word) for element n
@@ -1080,7 +1088,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void kv4_attend_rows_kernel(Atte
   constexpr int W = kRowWaves;
   // bf16 terms of a query and of a probability.  One term of a probability is a
   // choice: bf16 outputs are then 2.3e-3 from the exact ones instead of the 1.7e-3
-  // that their own rounding costs, but two terms make 347 us of the 258 above.
+  // that their own rounding costs, but two terms make 347 us of the 256 above.
   constexpr int NS = std::is_same<T, float>::value ? 3 : 1;
   constexpr int KW = D / 32, NT = D / 16;
   constexpr int kRows = 16 * R * W;
@@ -1510,9 +1518,9 @@ struct Cut {
 constexpr int kCUs = 256;
 constexpr int kMinTiles = 2 * kWaves;  // two steps a wave
 // Parts a sequence from which a launch of its own joins them: 256 parts by the
-// last workgroup alone would read 1 MB in turn; a launch costs 5.6 us (131,072
-// tokens 23.0 us in all), while 64 sequences in about four parts each take 26.9
-// us joined by the last workgroup and 39 with a launch.
+// last workgroup alone would read 1 MB in turn (131,072 tokens 51.9 us in all, 24.0
+// with a launch of 5.8), while 64 sequences in about four parts each take 27.8 us
+// joined by the last workgroup and 44.9 with a launch.
 constexpr int kFusedParts = 32;
 constexpr int kPairRows = 32, kFewRows = 208, kFewHeads = 32;
 
@@ -1527,8 +1535,8 @@ constexpr int rows_r(bool f32, int d) { return f32 && d == 128 ? 1 : 2; }
 // kv4_attend_rows_kernel takes 256 rows (128 for fp32 heads of 128) whether they
 // are there or not, but needs fewer parts to fill the device.  Measured in us,
 // 8 heads per key/value head of 128, tokens cut over the waves / rows over them:
-// 48 sequences over 6,000 tokens of 64 rows each 79 / 157, of 192 rows 187 /
-// 222; one sequence of 64 rows 26 / 18, of 192 rows 25 / 25; six sequences of
+// 48 sequences over 6,000 tokens of 64 rows each 78 / 146, of 192 rows 176 /
+// 212; one sequence of 64 rows 26 / 18, of 192 rows 25 / 25; six sequences of
 // 64 rows 34 / 29, of 128 rows 34 / 35; of 24 rows 20 / 16 and 26 / 25, but over
 // 1,000 tokens 12.7 / 14.0.
 int form_of(int64_t rows, int64_t heads) {
