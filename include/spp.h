@@ -444,9 +444,8 @@ spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache, int32_t dt
  * of more rows they are rounded to bf16, and divided by the fp32 sum of them as
  * rounded.  fp32 queries and probabilities go in as three bf16 terms each (a
  * query beyond bf16's largest number, 3.39e38, counts as infinite).  Sums of
- * values are fp32 and up to 2^8 for each token seen before they are divided:
- * values near the format's largest, beyond 2^120 over the tokens seen, may give
- * infinities.
+ * probabilities times values are fp32, each probability up to 2^8 before the
+ * division: values beyond 2^120 over the tokens seen may give infinities.
  * Sizes: n_seq * max_q * n_heads and n_tokens * n_heads at most 2^30, and fewer
  * than 2^22 workgroups, which take 16 to 256 rows (query tokens times the heads
  * of a key/value head) of one sequence and key/value head each.
