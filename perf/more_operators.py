@@ -322,7 +322,7 @@ def _own(s):
         return out
     pair, place = s["pair"].data_ptr(), s["place"].data_ptr()
     spp.spp_expert_sort(topk, T, K, n, s["start"].data_ptr(), pair, place, space.data_ptr(), space.numel(), stream)
-    spp.spp_expert_gather(code, x, D, pair, T, K, D, s["rows"].data_ptr(), D, stream)
+    spp.spp_expert_gather(code, x, D, place, T, K, D, s["rows"].data_ptr(), D, stream)
     spp.spp_expert_combine(code, s["y"].data_ptr(), D, place, gates, T, K, D, x, D, out.data_ptr(), D, stream)
     got = {k: s[k] for k in ("start", "pair", "place", "rows", "out")}
     if c["grad"]:
