@@ -9,21 +9,12 @@
 #include <utility>
 
 #include "spp.h"
+#include "spp_fp4.h"
 #include "spp_internal.h"
 
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kMaxFreq = 64;
-constexpr uint32_t kExpMask = 0x7f800000u;
-constexpr int kNanByte = 255;
-constexpr int kMinByte = 2;    // scale 2^-125: every nonzero value of a block stays a normal number
-constexpr int kMaxByte = 252;  // scale 2^125: 6 * 2^125 is the largest that is finite in bf16 and fp32
 
 // ------------------------------------------------------------------ the cache
 
@@ -46,8 +37,6 @@ struct Block {
   }
 };
 
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
-
 // Byte j of 8 as a scale for cvt2, for which only the exponent field counts
 __device__ __forceinline__ float scale_byte(u32x2 w, int j) {
   return __uint_as_float(j % 4 == 3 ? w[j / 4] >> 1 : w[j / 4] << (23 - 8 * (j % 4)));
@@ -57,62 +46,6 @@ __device__ __forceinline__ float scale_byte(u32x2 w, int j) {
 __device__ __forceinline__ bool high_byte(uint32_t w) {
   const uint32_t u = ~w & 0xfcfcfcfcu;
   return ((u - 0x01010101u) & ~u & 0x80808080u) != 0;
-}
-
-// Two codes of byte SEL of w to bf16, times the power of two in `scale`'s
-// exponent field (its other bits do not count; exponent 255 gives NaN).
-template <int SEL>
-__device__ __forceinline__ uint32_t cvt2(uint32_t w, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
-}
-
-// 8 codes to 8 bf16, in order
-__device__ __forceinline__ u32x4 cvt8(uint32_t w, float scale) {
-  return u32x4{cvt2<0>(w, scale), cvt2<1>(w, scale), cvt2<2>(w, scale), cvt2<3>(w, scale)};
-}
-
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
-}
-
-// 8 consecutive elements of a row (16-byte aligned)
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* f) {
-  if constexpr (std::is_same<T, float>::value) {
-    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = a[i], f[4 + i] = b[i];
-  } else {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[2 * i] = bf16_lo(a[i]), f[2 * i + 1] = bf16_hi(a[i]);
-  }
-}
-
-// The same 8 elements past the caches (streams that nothing here reads again)
-template <typename T>
-__device__ __forceinline__ void stream8(T* p, const float* f) {
-  if constexpr (std::is_same<T, float>::value) {
-    __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4*>(p));
-    __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4*>(p) + 1);
-  } else {
-    __builtin_nontemporal_store(
-        u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])},
-        reinterpret_cast<u32x4*>(p));
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float* f) {
-  if constexpr (std::is_same<T, float>::value) {
-    reinterpret_cast<f32x4*>(p)[0] = f32x4{f[0], f[1], f[2], f[3]};
-    reinterpret_cast<f32x4*>(p)[1] = f32x4{f[4], f[5], f[6], f[7]};
-  } else {
-    *reinterpret_cast<u32x4*>(p) =
-        u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
-  }
 }
 
 // --------------------------------------------------------------- rotary table
@@ -175,32 +108,6 @@ struct StoreArgs {
   int Hq, Hkv, F;  // Hq = 0: no queries
   int T;
 };
-
-// Codes (one word) and scale byte of this lane's 8 elements of a block of 32,
-// which lanes 4j .. 4j+3 hold together.
-__device__ __forceinline__ uint32_t quantise8(const float* y, uint32_t* byte) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(y[i]) & 0x7fffffffu);  // ordered as the magnitudes are; NaN above infinity
-  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
-  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
-  if (top >= kExpMask) {
-    *byte = kNanByte;
-    return 0u;
-  }
-  // top = 1.m * 2^(E-127) <= 7 * 2^e = 1.75 * 2^(e+2)
-  const int E = static_cast<int>(top >> 23);
-  int s = (top & 0x7fffffu) <= 0x600000u ? E - 2 : E - 1;
-  s = min(max(s, kMinByte), kMaxByte);
-  const float scale = scale_of(static_cast<uint32_t>(s));
-  *byte = static_cast<uint32_t>(s);
-  uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], scale, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], scale, 3);
-  return w;
-}
 
 // Each product and the sum rounded, not contracted: what is quantised next is
 // then the same number wherever it is formed.
@@ -1409,11 +1316,6 @@ __global__ __launch_bounds__(64 * (W == 1 ? 4 : W)) void kv4_join_kernel(AttendA
 
 // ------------------------------------------------------------------ host side
 
-bool aligned(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-spp_status bad(const char* why) { return spp::set_error(SPP_EINVAL, why); }
-
 const char* desc_why(const spp_attn_desc* d) {
   if (!d) return "desc is NULL";
   if (d->n_kv_heads < 1 || d->n_heads < 1 || d->n_heads > 1024 || d->n_heads % d->n_kv_heads != 0)
@@ -1452,11 +1354,6 @@ uint64_t extent(int64_t stride, int64_t T, int heads, int d, int elem) {
   return static_cast<uint64_t>((T - 1) * stride + static_cast<int64_t>(heads) * d) * static_cast<uint64_t>(elem);
 }
 
-bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
-}
-
 // Whether T rows of na bytes, sa bytes apart, and T rows of nb bytes, sb apart,
 // have a byte in common (a stride is at least its row).  Rows of one fused
 // product lie between each other without.
@@ -1476,24 +1373,6 @@ bool rows_overlap(const void* a, int64_t sa, int64_t na, const void* b, int64_t 
     if (meets(u)) return true;
   return false;
 }
-
-const char* dtype_why(int32_t dtype) {
-  return dtype == SPP_DTYPE_F32 || dtype == SPP_DTYPE_BF16 ? nullptr : "dtype must be 0 (f32) or 1 (bf16)";
-}
-
-spp_status launched(hipError_t e) { return e == hipSuccess ? SPP_OK : spp::set_error(SPP_EHIP, hipGetErrorString(e)); }
-
-// The launch's own status, and no other call's that may still be pending
-template <typename Args>
-hipError_t launch(void (*kernel)(Args), unsigned grid, unsigned threads, const Args& args, hipStream_t st) {
-  void* params[] = {const_cast<Args*>(&args)};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(grid), dim3(threads), params, 0, st);
-}
-
-#define SPP_BAD(expr)                   \
-  do {                                  \
-    if (const char* w_ = (expr)) return bad(w_); \
-  } while (0)
 
 template <typename T>
 hipError_t launch_store(const StoreArgs& a, int d, unsigned grid, hipStream_t st) {
