@@ -491,6 +491,124 @@ spp_status spp_bind_attention(spp_ctx* ctx, int32_t l, const void* w_qkv, const 
 spp_status spp_attention_step(spp_ctx* ctx, int32_t B, const int32_t* pos, int64_t pos_stride, const int64_t* slots,
                               const int32_t* kv_len, const int32_t* pages, int64_t pages_stride);
 
+/* ------------------------- matrices in 4 bits, and tokens to their experts
+ *
+ * The weights of an MoE layer's products in the 4-bit format of the key/value
+ * cache, for any number of tokens, and the tokens' way to their experts and
+ * back.  Operators on explicit device pointers, as the attention's above: no
+ * context, no allocation, no host wait, work enqueued on hip_stream of the
+ * current device, fit for capture into a graph; a call with nothing to do
+ * returns SPP_OK; EINVAL before anything is enqueued.
+ *
+ * Matrix: rows x cols elements, cols a multiple of 32, at most 2^17.  codes:
+ * dev [rows][cols/2], byte j of a row holds elements 2j (low nibble) and 2j+1;
+ * scales: dev [rows][cols/32], one byte for 32 elements.  An element is its
+ * code's value times 2^(scale - 127), both as in the cache; scale 255 makes
+ * the block NaN.  codes 16-byte aligned; rows at most 2^31 - 1, and
+ * rows * cols at most 2^40. */
+typedef struct {
+  void* codes;
+  void* scales;
+  int64_t rows;
+  int32_t cols;
+} spp_mx4_matrix;
+
+enum { SPP_ACT_BF16 = 0, SPP_ACT_MX4 = 1 };
+
+/* x (dev [rows][cols] in dtype, row stride x_stride elements) into q: a block
+ * of 32 takes the smallest scale with no magnitude above 7 * 2^(s-127),
+ * 2 <= s <= 252, and each element the nearest code (ties to the even one;
+ * magnitudes above 7 * 2^125 become 6 * 2^125); a block with an infinity or a
+ * NaN becomes a NaN block.  Rows 16-byte aligned, strides multiples of 16
+ * bytes.  No array may overlap another. */
+spp_status spp_mx4_quantize(int32_t dtype, const void* x, int64_t x_stride, const spp_mx4_matrix* q, void* hip_stream);
+/* The values of q into out (dev [rows][cols] in dtype), exact in either dtype
+ * for every scale from 2 to 252. */
+spp_status spp_mx4_load(const spp_mx4_matrix* q, int32_t dtype, void* out, int64_t out_stride, void* hip_stream);
+
+/* out[i][j] = sum_k x[i][k] W_g[j][k] for the rows i of group g: w holds
+ * `groups` (1 to 1024) matrices of N = w->rows / groups rows one after the
+ * other (N at most 2^20), and group g has the rows start[g] .. start[g+1] - 1
+ * of the M rows of x (dev int32 [groups + 1]; entries count as the nearest of
+ * 0 .. M, and where they fall back, rows hold no certain result); start NULL:
+ * one group of all rows.  Rows of no group are left as they were.
+ * x: dev bf16 [M][w->cols], 16-byte aligned rows (stride x_stride elements, a
+ * multiple of 8); out: dev [M][N] in dtype, row stride out_stride, no
+ * alignment beyond an element's.  M at most 2^24.  out overlaps no input.
+ * Products are exact; sums are fp32, in an order that depends on the sizes M,
+ * N, K and groups and on a group's rows alone, so a repeated call gives the
+ * same bits.  A NaN block makes its outputs NaN. */
+spp_status spp_mx4_matmul(const spp_mx4_matrix* w, int32_t groups, const int32_t* start, const void* x,
+                          int64_t x_stride, int32_t M, int32_t dtype, void* out, int64_t out_stride,
+                          void* hip_stream);
+/* The same with x in 4 bits too: x->rows = M, x->cols = w->cols. */
+spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups, const int32_t* start, const spp_mx4_matrix* x,
+                              int32_t M, int32_t dtype, void* out, int64_t out_stride, void* hip_stream);
+
+/* The routed experts of T tokens, from experts in 4 bits that are in HBM:
+ *   out[t] = [residual[t] +] sum_k gates[t][k] D_e (silu(G_e x[t]) * (U_e x[t])), e = topk[t][k].
+ * gate_up: n * 2I rows of D columns, expert e's rows first its I rows of G,
+ * then its I rows of U; down: n * D rows of I columns.  D and I multiples of
+ * 32.  x, residual (or NULL), out: dev bf16 [T][D] with their row strides
+ * (multiples of 8, pointers 16-byte aligned; out may be residual with the same
+ * stride, else overlaps no input); topk: dev int32 [T][K]; gates: dev fp32
+ * [T][K].  An id outside 0 .. n-1 adds nothing; an id may occur twice.
+ * act SPP_ACT_BF16: the SwiGLU's result is rounded to bf16 between the
+ * products.  SPP_ACT_MX4: x and the SwiGLU's result (in fp32) are brought into
+ * 4 bits as by spp_mx4_quantize, and both sides of each product are 4-bit.
+ * Sums are fp32; the results of each expert are kept in fp32 or, in calls of
+ * many tokens, rounded to bf16 before the gates' sum.
+ * n at most 1024, K at most 64, T * K at most 2^24.
+ * workspace: dev, 16-byte aligned, spp_mx4_experts_workspace bytes for every
+ * call of at most T tokens (with either act); its contents do not matter, and
+ * are undefined afterwards.  A call holds it until the stream has passed it:
+ * calls (and captured graphs) that may run at the same time need one each. */
+size_t spp_mx4_experts_workspace(int32_t n, int32_t D, int32_t I, int32_t T, int32_t K);
+spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_mx4_matrix* down, int32_t n, int32_t act,
+                           const void* x, int64_t x_stride, const int32_t* topk, const float* gates, int32_t T,
+                           int32_t K, const void* residual, int64_t residual_stride, void* out, int64_t out_stride,
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The pairs p = t * K + k of T tokens and their K experts, sorted by expert:
+ * pair[i] is the pair at place i, place[p] its place; pairs of an expert stay
+ * in their order, expert e has the places start[e] .. start[e+1] - 1.  topk:
+ * dev int32 [T][K]; start: dev int32 [n + 1]; pair, place: dev int32 [T * K].
+ * A pair whose id is outside 0 .. n-1 has no place (place[p] = -1); the last
+ * places then have no pair (pair[i] = -1).  n at most 1024, T * K at most 2^24.
+ * workspace: as for spp_mx4_experts, spp_expert_sort_workspace bytes for every
+ * call of at most T tokens. */
+size_t spp_expert_sort_workspace(int32_t T, int32_t K, int32_t n);
+spp_status spp_expert_sort(const int32_t* topk, int32_t T, int32_t K, int32_t n, int32_t* start, int32_t* pair,
+                           int32_t* place, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* rows[place[t * K + k]] = x[t]: the tokens' rows, in the experts' order.  x:
+ * dev [T][D], rows: dev [T * K][D], both in dtype with their row strides; rows
+ * 16-byte aligned, a row and the strides multiples of 16 bytes (the same for
+ * the calls below).  place: of spp_expert_sort, or any other int32 [T * K]: an
+ * entry outside 0 .. T*K-1 takes no row, rows that no entry names are left as
+ * they were, and a row that two entries name holds either one's.  The gradient
+ * of x is spp_expert_combine of the rows' gradients, without weights. */
+spp_status spp_expert_gather(int32_t dtype, const void* x, int64_t x_stride, const int32_t* place, int32_t T, int32_t K,
+                             int32_t D, void* rows, int64_t rows_stride, void* hip_stream);
+/* out[t] = [residual[t] +] sum_k weights[t][k] rows[place[t * K + k]], sums in
+ * fp32 in the order of k, the residual last; weights: dev fp32 [T][K], or
+ * NULL: 1; an entry of place outside 0 .. T*K-1 adds nothing.  out may be
+ * residual with the same stride; else it overlaps no input. */
+spp_status spp_expert_combine(int32_t dtype, const void* rows, int64_t rows_stride, const int32_t* place,
+                              const float* weights, int32_t T, int32_t K, int32_t D, const void* residual,
+                              int64_t residual_stride, void* out, int64_t out_stride, void* hip_stream);
+/* The gradients of that sum: d_rows[place[t * K + k]] = weights[t][k] d_out[t],
+ * d_weights[t][k] = <d_out[t], rows[place[t * K + k]]> (fp32 sums).  d_rows
+ * and d_weights may each be NULL; rows may be NULL without d_weights; weights
+ * NULL: 1.  d_rows may be rows with the same stride.  A pair without a place
+ * gets d_weights 0, rows that no pair names are left as they were; a row that
+ * two pairs name holds either one's (and d_rows must then not be rows).  The
+ * residual's gradient is d_out itself. */
+spp_status spp_expert_combine_grad(int32_t dtype, const void* d_out, int64_t d_out_stride, const void* rows,
+                                   int64_t rows_stride, const int32_t* place, const float* weights, int32_t T,
+                                   int32_t K, int32_t D, void* d_rows, int64_t d_rows_stride, float* d_weights,
+                                   void* hip_stream);
+
 /* ------------------------------------------------------ inspection / runs */
 
 /* Slot table of layer l: experts_out host int32 [S] (-1 = EMPTY), stamps_out

@@ -1,5 +1,5 @@
 // Internal interface between the runtime (spp_runtime.cpp) and the gfx950
-// kernels (spp_kernels.hip).  Not part of the public ABI.
+// kernels, and between the operators' files.  Not part of the public ABI.
 #pragma once
 
 #include <hip/hip_runtime_api.h>
@@ -206,5 +206,24 @@ hipError_t launch_read_probe(const FfnArgs& a, int grid, uint32_t* sink, hipStre
 // or 4 units per wave and pass), as many as keep the grid near 256 workgroups.
 int ffn_grid_q4(int nunits, int I, int* upw, int* upp);
 size_t ffn_max_grid();
+
+// Pairs sorted by expert (spp_expert_sort), and the workspace's bytes.
+size_t expert_sort_bytes(int64_t P, int32_t n);
+hipError_t launch_expert_sort(const int32_t* topk, int64_t P, int32_t n, int32_t* start, int32_t* pair, int32_t* place,
+                              void* workspace, hipStream_t st);
+// spp_expert_combine; place NULL: pair p's row is row p, for ids[p] in [0, n);
+// fp32_rows: rows in fp32 for bf16 outputs, with weights.
+struct ExpertSum {
+  const void* rows;
+  int64_t rows_stride;
+  const int32_t *place, *ids;
+  const float* weights;
+  int32_t n, dtype, fp32_rows, T, K, D;
+  const void* residual;
+  int64_t residual_stride;
+  void* out;
+  int64_t out_stride;
+};
+hipError_t launch_expert_combine(const ExpertSum& c, hipStream_t st);
 
 }  // namespace spp

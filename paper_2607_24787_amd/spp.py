@@ -22,6 +22,7 @@ LAYOUT_UNITS, LAYOUT_TILED, LAYOUT_Q4_UNITS = 0, 1, 2
 CODEC_PLAIN, CODEC_Q4 = 0, 1
 PREFETCH_ADAPTER, PREFETCH_PREV_TOKEN = 0, 1
 COPY_KERNEL, COPY_SDMA, COPY_SPLIT = 0, 1, 2
+ACT_BF16, ACT_MX4 = 0, 1
 
 
 class SppError(RuntimeError):
@@ -37,6 +38,10 @@ class ModelDesc(ctypes.Structure):
 
 class AttnDesc(ctypes.Structure):
     _fields_ = [(f, c_int32) for f in ("n_heads", "n_kv_heads", "head_dim", "page", "n_pages")]
+
+
+class Mx4Matrix(ctypes.Structure):
+    _fields_ = [("codes", c_void_p), ("scales", c_void_p), ("rows", c_int64), ("cols", c_int32)]
 
 
 class LayerStats(ctypes.Structure):
@@ -102,6 +107,25 @@ _SIGS = {
     "spp_set_attention": (c_int32, [c_void_p, POINTER(AttnDesc), c_int32, POINTER(c_int32), c_void_p, c_int32, c_int32]),
     "spp_bind_attention": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
     "spp_attention_step": (c_int32, [c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64]),
+    "spp_mx4_quantize": (c_int32, [c_int32, c_void_p, c_int64, POINTER(Mx4Matrix), c_void_p]),
+    "spp_mx4_load": (c_int32, [POINTER(Mx4Matrix), c_int32, c_void_p, c_int64, c_void_p]),
+    "spp_mx4_matmul": (c_int32, [POINTER(Mx4Matrix), c_int32, c_void_p, c_void_p, c_int64, c_int32, c_int32, c_void_p,
+                                 c_int64, c_void_p]),
+    "spp_mx4_matmul_mx4": (c_int32, [POINTER(Mx4Matrix), c_int32, c_void_p, POINTER(Mx4Matrix), c_int32, c_int32,
+                                     c_void_p, c_int64, c_void_p]),
+    "spp_mx4_experts_workspace": (c_size_t, [c_int32, c_int32, c_int32, c_int32, c_int32]),
+    "spp_mx4_experts": (c_int32, [POINTER(Mx4Matrix), POINTER(Mx4Matrix), c_int32, c_int32, c_void_p, c_int64, c_void_p,
+                                  c_void_p, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_size_t,
+                                  c_void_p]),
+    "spp_expert_sort_workspace": (c_size_t, [c_int32, c_int32, c_int32]),
+    "spp_expert_sort": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
+                                  c_void_p]),
+    "spp_expert_gather": (c_int32, [c_int32, c_void_p, c_int64, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int64,
+                                    c_void_p]),
+    "spp_expert_combine": (c_int32, [c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p,
+                                     c_int64, c_void_p, c_int64, c_void_p]),
+    "spp_expert_combine_grad": (c_int32, [c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_int32,
+                                          c_int32, c_int32, c_void_p, c_int64, c_void_p, c_void_p]),
     "spp_get_slot_table": (c_int32, [c_void_p, c_int32, POINTER(c_int32), POINTER(c_int64)]),
     "spp_set_slot_table": (c_int32, [c_void_p, c_int32, POINTER(c_int32), POINTER(c_int64)]),
     "spp_get_clock": (c_int32, [c_void_p, POINTER(c_int64)]),
@@ -397,6 +421,85 @@ def spp_attention_step(ctx, B: int, pos_dev: int, pos_stride: int, slots_dev: in
     """The positions, slots, lengths and pages (device) of the next decode step's B tokens."""
     _check(lib().spp_attention_step(c_void_p(ctx), B, pos_dev, pos_stride, slots_dev, kv_len_dev, pages_dev,
                                     pages_stride))
+
+
+# ------------------------- matrices in 4 bits, and tokens to their experts
+
+def make_mx4(codes_dev: int, scales_dev: int, rows: int, cols: int) -> Mx4Matrix:
+    return Mx4Matrix(codes_dev or None, scales_dev or None, rows, cols)
+
+
+def spp_mx4_quantize(dtype: int, x_dev: int, x_stride: int, q: Mx4Matrix, stream: int = 0):
+    """Rows of x into the codes and scales of q."""
+    _check(lib().spp_mx4_quantize(dtype, x_dev, x_stride, byref(q), stream))
+
+
+def spp_mx4_load(q: Mx4Matrix, dtype: int, out_dev: int, out_stride: int, stream: int = 0):
+    """The values of q, in dtype."""
+    _check(lib().spp_mx4_load(byref(q), dtype, out_dev, out_stride, stream))
+
+
+def spp_mx4_matmul(w: Mx4Matrix, groups: int, start_dev: int, x_dev: int, x_stride: int, M: int, dtype: int, out_dev: int,
+                   out_stride: int, stream: int = 0):
+    """out = x W^T, group by group; x bf16."""
+    _check(lib().spp_mx4_matmul(byref(w), groups, start_dev, x_dev, x_stride, M, dtype, out_dev, out_stride, stream))
+
+
+def spp_mx4_matmul_mx4(w: Mx4Matrix, groups: int, start_dev: int, x: Mx4Matrix, M: int, dtype: int, out_dev: int,
+                       out_stride: int, stream: int = 0):
+    """out = x W^T, group by group; x in 4 bits."""
+    _check(lib().spp_mx4_matmul_mx4(byref(w), groups, start_dev, byref(x), M, dtype, out_dev, out_stride, stream))
+
+
+def spp_mx4_experts_workspace(n: int, D: int, I: int, T: int, K: int) -> int:
+    size = int(lib().spp_mx4_experts_workspace(n, D, I, T, K))
+    if size == 0:
+        raise SppError(SPP_EINVAL, spp_last_error())
+    return size
+
+
+def spp_mx4_experts(gate_up: Mx4Matrix, down: Mx4Matrix, n: int, act: int, x_dev: int, x_stride: int, topk_dev: int,
+                    gates_dev: int, T: int, K: int, residual_dev: int, residual_stride: int, out_dev: int,
+                    out_stride: int, workspace_dev: int, workspace_bytes: int, stream: int = 0):
+    """The routed experts' FFN of T tokens, experts in 4 bits; residual_dev 0: none."""
+    _check(lib().spp_mx4_experts(byref(gate_up), byref(down), n, act, x_dev, x_stride, topk_dev, gates_dev, T, K,
+                                 residual_dev, residual_stride, out_dev, out_stride, workspace_dev, workspace_bytes,
+                                 stream))
+
+
+def spp_expert_sort_workspace(T: int, K: int, n: int) -> int:
+    size = int(lib().spp_expert_sort_workspace(T, K, n))
+    if size == 0:
+        raise SppError(SPP_EINVAL, spp_last_error())
+    return size
+
+
+def spp_expert_sort(topk_dev: int, T: int, K: int, n: int, start_dev: int, pair_dev: int, place_dev: int,
+                    workspace_dev: int, workspace_bytes: int, stream: int = 0):
+    """The pairs (token, expert) sorted by expert: start [n + 1], pair and its inverse place [T * K]."""
+    _check(lib().spp_expert_sort(topk_dev, T, K, n, start_dev, pair_dev, place_dev, workspace_dev, workspace_bytes,
+                                 stream))
+
+
+def spp_expert_gather(dtype: int, x_dev: int, x_stride: int, place_dev: int, T: int, K: int, D: int, rows_dev: int,
+                      rows_stride: int, stream: int = 0):
+    """Each token's row to its pairs' places."""
+    _check(lib().spp_expert_gather(dtype, x_dev, x_stride, place_dev, T, K, D, rows_dev, rows_stride, stream))
+
+
+def spp_expert_combine(dtype: int, rows_dev: int, rows_stride: int, place_dev: int, weights_dev: int, T: int, K: int,
+                       D: int, residual_dev: int, residual_stride: int, out_dev: int, out_stride: int, stream: int = 0):
+    """Each token's rows summed with its weights (0: all 1), and residual (0: none)."""
+    _check(lib().spp_expert_combine(dtype, rows_dev, rows_stride, place_dev, weights_dev, T, K, D, residual_dev,
+                                    residual_stride, out_dev, out_stride, stream))
+
+
+def spp_expert_combine_grad(dtype: int, d_out_dev: int, d_out_stride: int, rows_dev: int, rows_stride: int,
+                            place_dev: int, weights_dev: int, T: int, K: int, D: int, d_rows_dev: int,
+                            d_rows_stride: int, d_weights_dev: int, stream: int = 0):
+    """The gradients of spp_expert_combine's rows and weights; either may be 0."""
+    _check(lib().spp_expert_combine_grad(dtype, d_out_dev, d_out_stride, rows_dev, rows_stride, place_dev, weights_dev,
+                                         T, K, D, d_rows_dev, d_rows_stride, d_weights_dev, stream))
 
 
 def spp_last_error() -> str:
