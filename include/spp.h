@@ -534,7 +534,8 @@ spp_status spp_mx4_load(const spp_mx4_matrix* q, int32_t dtype, void* out, int64
  * one group of all rows.  Rows of no group are left as they were.
  * x: dev bf16 [M][w->cols], 16-byte aligned rows (stride x_stride elements, a
  * multiple of 8); out: dev [M][N] in dtype, row stride out_stride, no
- * alignment beyond an element's.  M at most 2^24.  out overlaps no input.
+ * alignment beyond an element's.  M at most 2^24, M * N at most 2^36.  out
+ * overlaps no input.
  * Products are exact; sums are fp32, in an order that depends on the sizes M,
  * N, K and groups and on a group's rows alone, so a repeated call gives the
  * same bits.  A NaN block makes its outputs NaN. */
@@ -558,7 +559,8 @@ spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups, const int
  * 4 bits as by spp_mx4_quantize, and both sides of each product are 4-bit.
  * Sums are fp32; the results of each expert are kept in fp32 or, in calls of
  * many tokens, rounded to bf16 before the gates' sum.
- * n at most 1024, K at most 64, T * K at most 2^24.
+ * n at most 1024, K at most 64, T * K at most 2^24, T * K times D or I at most
+ * 2^36.
  * workspace: dev, 16-byte aligned, spp_mx4_experts_workspace bytes for every
  * call of at most T tokens (with either act); its contents do not matter, and
  * are undefined afterwards.  A call holds it until the stream has passed it:

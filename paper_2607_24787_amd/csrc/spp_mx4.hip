@@ -79,6 +79,7 @@ struct ProductArgs {
   const void* x;
   int64_t x_stride;               // bytes
   const uint8_t* x_scales;        // kXCodes: [rows][nb]
+  int64_t x_blocks;               // of all rows of x
   const int32_t* start;
   int M, groups;
   const int32_t* ids;             // kRowsIds: [M]
@@ -87,6 +88,9 @@ struct ProductArgs {
   int by_pair;                    // kRowsIds: blockIdx.y is a pair, and the first with its id takes the group
   void* out;
   int64_t out_stride;             // elements
+  uint8_t* out_scales;            // SwiGLU results in 4 bits
+  int columns;                    // workgroups over a group's outputs
+  int wide_out;                   // rows of out are 16-byte aligned
 };
 
 // Scale bytes [at, at + 4) as one word, of `total` bytes; those past the end do
@@ -300,6 +304,316 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
   }
 }
 
+// -------------------------------------------------------- products of many rows
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kTileThreads = 256;
+constexpr int kTileWaves = kTileThreads / 64;
+constexpr int kTileRows = 64 * kTileWaves;  // weight rows of a workgroup
+constexpr int kXcds = 8;
+
+__device__ const u32x4 kZeros = {0, 0, 0, 0};
+
+// 16 bytes from global memory to `to` + 16 * lane of LDS
+__device__ __forceinline__ void to_lds(const uint8_t* from, uint8_t* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
+                                   (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
+}
+
+// Where 16-byte piece c of a row of `pieces` goes: 8 neighbouring rows' pieces c
+// spread over the banks.
+template <int kPieces>
+__device__ __forceinline__ int swizzled(int row, int c) {
+  return c ^ ((row / (8 / kPieces)) % kPieces);
+}
+
+// Scale bytes of kBlocks blocks of a row from block b on, in bounds; 1 past the
+// row's end
+template <int kBlocks>
+__device__ __forceinline__ uint32_t row_scales(const uint8_t* p, int64_t row, int b, int nb, int64_t total) {
+  uint32_t w = scales4(p, row * nb + b, total);
+#pragma unroll
+  for (int j = 1; j < kBlocks; ++j)
+    if (b + j >= nb) w = (w & ~(255u << (8 * j))) | static_cast<uint32_t>(kOne) << (8 * j);
+  return w;
+}
+
+template <int SEL>
+__device__ __forceinline__ f32x16 mfma_mx4_32(u32x4 w, uint32_t w_scales, u32x4 x, uint32_t x_scales, f32x16 c) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(w), wide(x), c, 4, 4, SEL, static_cast<int>(w_scales), SEL,
+                                                         static_cast<int>(x_scales));
+}
+
+// Row tile `tile` of kTile rows over all groups' rows, group after group: its
+// group, first row and rows.  Every wave finds it by itself.
+struct Tile {
+  int group, first, count;
+};
+
+template <int kTile>
+__device__ __forceinline__ int tiles_of(const ProductArgs& a, int g, int* first, int* count) {
+  *first = min(max(a.start[g], 0), a.M);
+  *count = max(min(max(a.start[g + 1], 0), a.M) - *first, 0);
+  return (*count + kTile - 1) / kTile;
+}
+
+template <int kTile>
+__device__ __forceinline__ int total_tiles(const ProductArgs& a, int* before) {
+  const int lane = threadIdx.x & 63;
+  const int per = (a.groups + 63) / 64;
+  int sum = 0;
+  for (int j = 0; j < per; ++j) {
+    const int g = lane * per + j;
+    int first, count;
+    if (g < a.groups) sum += tiles_of<kTile>(a, g, &first, &count);
+  }
+  int incl = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(incl, d);
+    if (lane >= d) incl += o;
+  }
+  *before = incl - sum;
+  return __shfl(incl, 63);
+}
+
+template <int kTile>
+__device__ __forceinline__ Tile find_tile(const ProductArgs& a, int before, int tile) {
+  const int lane = threadIdx.x & 63;
+  const int per = (a.groups + 63) / 64;
+  int group = -1, first = 0, count = 0;
+  for (int j = 0; j < per; ++j) {
+    const int g = lane * per + j;
+    if (g >= a.groups) break;
+    int f, c;
+    const int t = tiles_of<kTile>(a, g, &f, &c);
+    if (tile >= before && tile < before + t) {
+      group = g;
+      first = f + (tile - before) * kTile;
+      count = min(c - (tile - before) * kTile, kTile);
+    }
+    before += t;
+  }
+  const int from = max(__ffsll(static_cast<long long>(__ballot(group >= 0))) - 1, 0);
+  return Tile{__shfl(group, from), __shfl(first, from), __shfl(count, from)};
+}
+
+// A workgroup takes 256 weight rows (128 outputs of both matrices for SwiGLU)
+// and 32 * CT rows of one group; K goes through LDS in two buffers.  A wave
+// takes 64 of the weight rows and all rows of x.
+template <int X, bool kSwiglu, typename Out, int CT>
+__global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a) {
+  constexpr int KB = X == kXCodes ? 2 : 1;  // blocks of a lane and stage
+  constexpr int BL = 2 * KB;                // blocks of a row and stage
+  constexpr int AC = BL, BC = X == kXCodes ? BL : 4 * BL;  // 16-byte pieces of a row
+  constexpr int TM = 32 * CT;
+  constexpr int kA = kTileRows * AC * 16, kB = TM * BC * 16;
+  __shared__ __attribute__((aligned(16))) uint8_t s_a[2][kA];
+  __shared__ __attribute__((aligned(16))) uint8_t s_b[2][kB];
+  __shared__ uint32_t s_sa[2][kTileRows];
+  __shared__ uint32_t s_sb[2][TM];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
+
+  // the tile: workgroups of one XCD take neighbouring ones
+  int before = 0;
+  const int64_t total = static_cast<int64_t>(a.start ? total_tiles<TM>(a, &before) : (a.M + TM - 1) / TM) * a.columns;
+  const int64_t each = (total + kXcds - 1) / kXcds, at = blockIdx.x / kXcds;
+  const int64_t logical = blockIdx.x % kXcds * each + at;
+  if (at >= each || logical >= total) return;
+  const int tile = static_cast<int>(logical / a.columns), column = static_cast<int>(logical - static_cast<int64_t>(tile) * a.columns);
+  Tile t{0, tile * TM, min(a.M - tile * TM, TM)};
+  if (a.start) t = find_tile<TM>(a, before, tile);
+  if (t.count < 1) return;
+
+  // what this lane loads: rows' addresses, at the piece that goes to its place
+  const uint8_t* pa[AC];
+  int ca[AC];
+#pragma unroll
+  for (int i = 0; i < AC; ++i) {
+    const int idx = (i * kTileWaves + wave) * 64 + lane, r = idx / AC;
+    ca[i] = swizzled<AC>(r, idx % AC);
+    const int rho = r & 31, up = (r >> 5) & 1, w = r >> 6;
+    const int hh = (rho >> 2) & 1, j = 4 * (rho >> 3) + (rho & 3);
+    const int f = kSwiglu ? column * (kTileRows / 2) + w * 32 + 16 * hh + j : column * kTileRows + w * 64 + 32 * hh + 16 * up + j;
+    const int64_t row = kSwiglu ? (static_cast<int64_t>(t.group) * 2 + up) * a.N + min(f, a.N - 1)
+                                : static_cast<int64_t>(t.group) * a.N + min(f, a.N - 1);
+    pa[i] = a.codes + row * a.nb * 16;
+  }
+  constexpr int BI = (TM * BC + kTileThreads - 1) / kTileThreads;
+  const uint8_t* pb[BI];
+  int cb[BI];
+#pragma unroll
+  for (int i = 0; i < BI; ++i) {
+    const int idx = (i * kTileWaves + wave) * 64 + lane, r = min(idx / BC, TM - 1);
+    cb[i] = swizzled<BC>(r, idx % BC);
+    const int p = t.first + min(r, t.count - 1);
+    const int64_t row = (a.pair ? a.pair[p] : p) / a.xdiv;
+    pb[i] = static_cast<const uint8_t*>(a.x) + row * a.x_stride;
+  }
+  int64_t scale_row, x_row = 0;
+  {
+    const int rho = tid & 31, up = (tid >> 5) & 1, w = tid >> 6;
+    const int hh = (rho >> 2) & 1, j = 4 * (rho >> 3) + (rho & 3);
+    const int f = kSwiglu ? column * (kTileRows / 2) + w * 32 + 16 * hh + j : column * kTileRows + w * 64 + 32 * hh + 16 * up + j;
+    scale_row = kSwiglu ? (static_cast<int64_t>(t.group) * 2 + up) * a.N + min(f, a.N - 1)
+                        : static_cast<int64_t>(t.group) * a.N + min(f, a.N - 1);
+    if (X == kXCodes && tid < TM) {
+      const int p = t.first + min(tid, t.count - 1);
+      x_row = (a.pair ? a.pair[p] : p) / a.xdiv;
+    }
+  }
+  uint32_t wa = 0, wb = 0;
+  const auto issue = [&](int st, int buf) {
+    const int b0 = st * BL;
+#pragma unroll
+    for (int i = 0; i < AC; ++i)
+      to_lds(pa[i] + static_cast<int64_t>(b0 + ca[i] < a.nb ? b0 + ca[i] : 0) * 16, s_a[buf] + (i * kTileWaves + wave) * 1024);
+#pragma unroll
+    for (int i = 0; i < BI; ++i) {
+      if (BI * kTileThreads != TM * BC && (i * kTileWaves + wave) * 64 >= TM * BC) break;
+      const int block = X == kXCodes ? b0 + cb[i] : b0 + cb[i] / 4;
+      const uint8_t* from = pb[i] + (static_cast<int64_t>(b0) * (BC / BL) + cb[i]) * 16;
+      to_lds(block < a.nb ? from : reinterpret_cast<const uint8_t*>(&kZeros), s_b[buf] + (i * kTileWaves + wave) * 1024);
+    }
+    wa = row_scales<BL>(a.scales, scale_row, b0, a.nb, a.blocks);
+    if (X == kXCodes && tid < TM) wb = row_scales<BL>(a.x_scales, x_row, b0, a.nb, a.x_blocks);
+  };
+  const auto put_scales = [&](int buf) {
+    s_sa[buf][tid] = wa;
+    if (X == kXCodes && tid < TM) s_sb[buf][tid] = wb;
+  };
+
+  f32x16 acc[2][CT];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[i][c][j] = 0.f;
+
+  const int stages = (a.nb + BL - 1) / BL;
+  issue(0, 0);
+  put_scales(0);
+  __syncthreads();
+  for (int st = 0; st < stages; ++st) {
+    const int buf = st & 1;
+    if (st + 1 < stages) issue(st + 1, buf ^ 1);
+    const auto read_a = [&](int i, int c) {
+      const int r = wave * 64 + i * 32 + l32;
+      return *reinterpret_cast<const u32x4*>(s_a[buf] + (r * AC + swizzled<AC>(r, c)) * 16);
+    };
+    const auto read_b = [&](int i, int c) {
+      const int r = i * 32 + l32;
+      return *reinterpret_cast<const u32x4*>(s_b[buf] + (r * BC + swizzled<BC>(r, c)) * 16);
+    };
+    if constexpr (X == kXCodes) {
+      uint32_t sa[2], sb[CT];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) sa[i] = s_sa[buf][wave * 64 + i * 32 + l32] >> (8 * KB * half);
+#pragma unroll
+      for (int i = 0; i < CT; ++i) sb[i] = s_sb[buf][i * 32 + l32] >> (8 * KB * half);
+      u32x4 va[2], vb[CT];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) va[i] = read_a(i, half * KB);
+#pragma unroll
+      for (int i = 0; i < CT; ++i) vb[i] = read_b(i, half * KB);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[i][c] = mfma_mx4_32<0>(va[i], sa[i], vb[c], sb[c], acc[i][c]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) va[i] = read_a(i, half * KB + 1);
+#pragma unroll
+      for (int i = 0; i < CT; ++i) vb[i] = read_b(i, half * KB + 1);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[i][c] = mfma_mx4_32<1>(va[i], sa[i], vb[c], sb[c], acc[i][c]);
+    } else {
+      u32x4 va[2];
+      float sa[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        va[i] = read_a(i, half);
+        sa[i] = scale_of((s_sa[buf][wave * 64 + i * 32 + l32] >> (8 * half)) & 255u);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        u32x4 vb[CT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) vb[c] = read_b(c, half * 4 + q);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const bf16x8 w = __builtin_bit_cast(bf16x8, cvt8(va[i][q], sa[i]));
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+            acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, vb[c]), acc[i][c], 0, 0, 0);
+        }
+      }
+    }
+    if (st + 1 < stages) put_scales(buf ^ 1);
+    __syncthreads();
+  }
+
+  // a lane holds 32 neighbouring outputs of a row (16 of both for SwiGLU)
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int r = c * 32 + l32;
+    const int64_t row = t.first + r;
+    const bool ok = r < t.count;
+    if constexpr (kSwiglu) {
+      const int f = column * (kTileRows / 2) + wave * 32 + 16 * half;
+      float y[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) y[j] = swiglu(acc[0][c][j], acc[1][c][j]);
+      if constexpr (X == kXCodes) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(y[j]) & 0x7fffffffu);
+        top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32)));
+        const uint32_t byte = byte_of(top);
+        const float scale = scale_of(byte);
+        u32x2 w;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t v = 0;
+          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k], y[8 * k + 1], scale, 0);
+          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k + 2], y[8 * k + 3], scale, 1);
+          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k + 4], y[8 * k + 5], scale, 2);
+          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k + 6], y[8 * k + 7], scale, 3);
+          w[k] = byte == kNanByte ? 0u : v;
+        }
+        if (ok && f < a.N) {
+          *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.out) + (row * a.N + f) / 2) = w;
+          if (half == 0) a.out_scales[(row * a.N + f) / 32] = static_cast<uint8_t>(byte);
+        }
+      } else if (ok && f < a.N) {
+        __bf16* out = static_cast<__bf16*>(a.out) + row * a.N + f;
+        store8(out, y);
+        store8(out + 8, y + 8);
+      }
+    } else {
+      const int f = column * kTileRows + wave * 64 + 32 * half;
+      if (!ok || f >= a.N) continue;
+      Out* out = static_cast<Out*>(a.out) + row * a.out_stride + f;
+      if (a.wide_out && f + 32 <= a.N) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = acc[k / 2][c][8 * (k % 2) + j];
+          store8(out + 8 * k, y);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (f + j < a.N) out[j] = static_cast<Out>(acc[j / 16][c][j % 16]);
+      }
+    }
+  }
+}
+
 // ------------------------------------------------------------------ host side
 
 const char* rows_why(const void* p, int64_t stride, int64_t row, int elem) {
@@ -343,6 +657,7 @@ hipError_t launch2(void (*kernel)(ProductArgs), unsigned x, unsigned y, unsigned
 
 constexpr int kMaxM = 1 << 24;
 constexpr int kMaxN = 1 << 20;
+constexpr int64_t kMaxOutputs = int64_t{1} << 36;  // below 2^24 workgroups in every form
 
 const char* product_why(const spp_mx4_matrix* w, int32_t groups, const int32_t* start, int32_t M, int32_t dtype,
                         const void* out, int64_t out_stride) {
@@ -354,8 +669,9 @@ const char* product_why(const spp_mx4_matrix* w, int32_t groups, const int32_t* 
   if (!start && groups != 1) return "start must not be NULL with more than one group";
   if (!aligned(start, 4)) return "start must be aligned to its elements";
   if (M < 0 || M > kMaxM) return "M must be in [0, 2^24]";
-  if (M == 0) return nullptr;
   const int64_t N = w->rows / groups;
+  if (M * N > kMaxOutputs) return "M times a group's rows of weights must be at most 2^36";
+  if (M == 0) return nullptr;
   if (!out || !aligned(out, dtype == SPP_DTYPE_BF16 ? 2 : 4)) return "out must not be NULL, and aligned to its elements";
   if (out_stride < N || out_stride > int64_t{1} << 30) return "out's stride must be at least a row, at most 2^30 elements";
   const uint64_t bytes = span(M, out_stride, N, dtype == SPP_DTYPE_BF16 ? 2 : 4);
@@ -383,8 +699,36 @@ ProductArgs product_of(const spp_mx4_matrix& w, int32_t groups, const int32_t* s
 
 unsigned tiles16(int N) { return static_cast<unsigned>((N + 15) / 16); }
 
+template <int X, bool kSwiglu, typename Out, int CT>
+hipError_t launch_tile(ProductArgs a, hipStream_t st) {
+  a.columns = (a.N + (kSwiglu ? kTileRows / 2 : kTileRows) - 1) / (kSwiglu ? kTileRows / 2 : kTileRows);
+  a.wide_out = aligned16(a.out) && a.out_stride * static_cast<int64_t>(sizeof(Out)) % 16 == 0;
+  // groups with a last tile of their own: at most one a group, and one a row
+  const int64_t tiles = a.M / (32 * CT) + std::min(a.groups, a.M);
+  const int64_t grid = (tiles * a.columns + kXcds - 1) / kXcds * kXcds;
+  return launch(mx4_tile_kernel<X, kSwiglu, Out, CT>, static_cast<unsigned>(grid), kTileThreads, a, st);
+}
+
+// Rows of x that a workgroup of the tiled products takes, by the mean of a
+// group's; 0: few rows
+constexpr int kFewRows = 20;
+int tile_rows(int64_t M, int groups) {
+  const int64_t mean = M / groups;
+  return mean >= 96 ? 128 : mean >= 48 ? 64 : mean >= kFewRows ? 32 : 0;
+}
+
+template <int X, bool kSwiglu, typename Out>
+hipError_t launch_tiles(const ProductArgs& a, int rows, hipStream_t st) {
+  return rows == 128  ? launch_tile<X, kSwiglu, Out, 4>(a, st)
+         : rows == 64 ? launch_tile<X, kSwiglu, Out, 2>(a, st)
+                      : launch_tile<X, kSwiglu, Out, 1>(a, st);
+}
+
 template <int X>
 hipError_t launch_product(const ProductArgs& a, int32_t dtype, hipStream_t st) {
+  const int rows = tile_rows(a.M, a.groups);
+  if (rows > 0)
+    return dtype == SPP_DTYPE_BF16 ? launch_tiles<X, false, __bf16>(a, rows, st) : launch_tiles<X, false, float>(a, rows, st);
   const auto kernel = dtype == SPP_DTYPE_BF16 ? mx4_few_kernel<X, false, __bf16, kRowsStart>
                                               : mx4_few_kernel<X, false, float, kRowsStart>;
   return launch2(kernel, tiles16(a.N), static_cast<unsigned>(a.groups), kFewThreads, a, st);
@@ -392,16 +736,37 @@ hipError_t launch_product(const ProductArgs& a, int32_t dtype, hipStream_t st) {
 
 // The parts of a workspace of the experts' call
 struct Space {
-  size_t h, y, bytes;
+  size_t h, y, start, pair, place, sort, xq, xq_scales, h_scales, bytes;
 };
 
 size_t up256(size_t n) { return (n + 255) & ~size_t{255}; }
 
-Space space_of(int64_t P, int32_t D, int32_t I) {
+// Few rows an expert: h and y in fp32 at the pairs' own places.  Many: sorted, in
+// bf16 or 4 bits.
+Space few_space(int64_t P, int32_t D, int32_t I) {
   Space s{};
-  s.h = 0;
   s.y = up256(static_cast<size_t>(P) * I * 4);
   s.bytes = s.y + up256(static_cast<size_t>(P) * D * 4);
+  return s;
+}
+
+Space tile_space(int64_t T, int64_t P, int32_t n, int32_t D, int32_t I) {
+  Space s{};
+  size_t at = up256(static_cast<size_t>(P) * I * 2);
+  const auto take = [&](size_t bytes) {
+    const size_t from = at;
+    at += up256(bytes);
+    return from;
+  };
+  s.h_scales = take(static_cast<size_t>(P) * I / 32);
+  s.y = take(static_cast<size_t>(P) * D * 2);
+  s.start = take((static_cast<size_t>(n) + 1) * 4);
+  s.pair = take(static_cast<size_t>(P) * 4);
+  s.place = take(static_cast<size_t>(P) * 4);
+  s.sort = take(spp::expert_sort_bytes(P, n));
+  s.xq = take(static_cast<size_t>(T) * D / 2);
+  s.xq_scales = take(static_cast<size_t>(T) * D / 32);
+  s.bytes = at;
   return s;
 }
 
@@ -411,6 +776,7 @@ const char* experts_why(int32_t n, int32_t D, int32_t I, int32_t T, int32_t K) {
   if (T < 0 || static_cast<int64_t>(T) * K > kMaxM) return "T must be >= 0, and T * K at most 2^24";
   if (D < 32 || D % 32 != 0 || D > 1 << 17 || I < 32 || I % 32 != 0 || I > 1 << 17)
     return "D and I must be multiples of 32, at most 2^17";
+  if (static_cast<int64_t>(T) * K * std::max(D, I) > kMaxOutputs) return "T * K times D or I must be at most 2^36";
   return nullptr;
 }
 
@@ -482,12 +848,15 @@ extern "C" spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups
   a.x = x->codes;
   a.x_stride = x->cols / 2;
   a.x_scales = static_cast<const uint8_t*>(x->scales);
+  a.x_blocks = x->rows * (x->cols / 32);
   return launched(launch_product<kXCodes>(a, dtype, static_cast<hipStream_t>(hip_stream)));
 }
 
 extern "C" size_t spp_mx4_experts_workspace(int32_t n, int32_t D, int32_t I, int32_t T, int32_t K) {
   if (const char* w = experts_why(n, D, I, T, K)) return bad(w), 0;
-  return std::max<size_t>(16, space_of(static_cast<int64_t>(T) * K, D, I).bytes);
+  // every smaller call: the largest of few rows, and this one
+  const int64_t P = static_cast<int64_t>(T) * K, few = std::min<int64_t>(P, int64_t{kFewRows} * n);
+  return std::max(few_space(few, D, I).bytes, tile_rows(P, n) > 0 ? tile_space(T, P, n, D, I).bytes : size_t{16});
 }
 
 extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_mx4_matrix* down, int32_t n, int32_t act,
@@ -517,12 +886,65 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
         overlap(residual, span(T, residual_stride, D, 2), out, out_bytes))
       return bad("out must be residual with the same stride, or not overlap it");
   }
-  const Space s = space_of(P, D, I);
+  const bool mx4 = act == SPP_ACT_MX4;
+  const int rows = tile_rows(P, n);
+  const Space s = rows > 0 ? tile_space(T, P, n, D, I) : few_space(P, D, I);
   if (!workspace || !aligned16(workspace)) return bad("workspace must not be NULL, and 16-byte aligned");
   if (workspace_bytes < s.bytes) return bad("the workspace is too small");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   uint8_t* space = static_cast<uint8_t*>(workspace);
-  const bool mx4 = act == SPP_ACT_MX4;
+
+  spp::ExpertSum c{};
+  c.rows = space + s.y;
+  c.rows_stride = D;
+  c.weights = gates;
+  c.dtype = SPP_DTYPE_BF16;
+  c.T = T;
+  c.K = K;
+  c.D = D;
+  c.residual = residual;
+  c.residual_stride = residual_stride;
+  c.out = out;
+  c.out_stride = out_stride;
+
+  if (rows > 0) {
+    int32_t* start = reinterpret_cast<int32_t*>(space + s.start);
+    int32_t* pair = reinterpret_cast<int32_t*>(space + s.pair);
+    int32_t* place = reinterpret_cast<int32_t*>(space + s.place);
+    hipError_t e = spp::launch_expert_sort(topk, P, n, start, pair, place, space + s.sort, st);
+    if (e != hipSuccess) return launched(e);
+    if (mx4) {
+      RowsQ q{};
+      q.x = x;
+      q.x_stride = x_stride;
+      q.codes = space + s.xq;
+      q.scales = space + s.xq_scales;
+      q.per_row = D / 8;
+      q.words = static_cast<int64_t>(T) * q.per_row;
+      e = launch(mx4_quantize_kernel<__bf16>, quant_grid(q.words), kQuantThreads, q, st);
+      if (e != hipSuccess) return launched(e);
+    }
+    ProductArgs a = product_of(*gate_up, n, start, static_cast<int32_t>(P), space, I);
+    a.N = I;
+    a.pair = pair;
+    a.xdiv = K;
+    a.x = mx4 ? static_cast<const void*>(space + s.xq) : x;
+    a.x_stride = mx4 ? D / 2 : x_stride * 2;
+    a.x_scales = space + s.xq_scales;
+    a.x_blocks = static_cast<int64_t>(T) * a.nb;
+    a.out_scales = space + s.h_scales;
+    e = mx4 ? launch_tiles<kXCodes, true, __bf16>(a, rows, st) : launch_tiles<kXBf16, true, __bf16>(a, rows, st);
+    if (e != hipSuccess) return launched(e);
+    ProductArgs d = product_of(*down, n, start, static_cast<int32_t>(P), space + s.y, D);
+    d.x = space;
+    d.x_stride = mx4 ? I / 2 : static_cast<int64_t>(I) * 2;
+    d.x_scales = space + s.h_scales;
+    d.x_blocks = P * d.nb;
+    e = mx4 ? launch_tiles<kXCodes, false, __bf16>(d, rows, st) : launch_tiles<kXBf16, false, __bf16>(d, rows, st);
+    if (e != hipSuccess) return launched(e);
+    c.place = place;
+    return launched(spp::launch_expert_combine(c, st));
+  }
 
   ProductArgs a = product_of(*gate_up, n, nullptr, static_cast<int32_t>(P), space + s.h, I);
   a.N = I;
@@ -544,20 +966,8 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
   e = launch2(mx4 ? mx4_few_kernel<kXQuantF32, false, float, kRowsIds> : mx4_few_kernel<kXBf16, false, float, kRowsIds>,
               tiles16(D), groups, kFewThreads, d, st);
   if (e != hipSuccess) return launched(e);
-  spp::ExpertSum c{};
-  c.rows = space + s.y;
-  c.rows_stride = D;
   c.ids = topk;
-  c.weights = gates;
   c.n = n;
-  c.dtype = SPP_DTYPE_BF16;
   c.fp32_rows = 1;
-  c.T = T;
-  c.K = K;
-  c.D = D;
-  c.residual = residual;
-  c.residual_stride = residual_stride;
-  c.out = out;
-  c.out_stride = out_stride;
   return launched(spp::launch_expert_combine(c, st));
 }

@@ -118,7 +118,7 @@ REFUSED = (
         dict(out_dev=6 * GOOD + 1), dict(out_stride=9), dict(out_stride=-10), dict(out_stride=1 << 31), dict(x_dev=0),
         dict(x_dev=5 * GOOD + 4), dict(x_stride=56), dict(x_stride=70), dict(x_stride=1 << 40), dict(out_dev=5 * GOOD),
         dict(out_dev=GOOD + 30 * 32 - 2), dict(out_dev=3 * GOOD + 2), dict(out_dev=7 * GOOD), dict(dtype=0, out_dev=6 * GOOD + 2),
-        dict(w=mx4(rows=0)), dict(w=mx4(rows=(1 << 20) + 1), groups=1, out_stride=1 << 21))]
+        dict(w=mx4(rows=0)), dict(w=mx4(rows=1 << 16), groups=1, M=(1 << 20) + 1, out_stride=1 << 16), dict(w=mx4(rows=(1 << 20) + 1), groups=1, out_stride=1 << 21))]
     + [(spp.spp_mx4_matmul_mx4, MATMUL4, c) for c in (
         dict(groups=7), dict(M=8), dict(x=mx4(rows=9, cols=32)), dict(x=mx4(rows=10)), dict(dtype=2), dict(out_dev=0),
         dict(out_stride=9), dict(out_dev=5 * GOOD + 16), dict(out_dev=8 * GOOD))]
@@ -202,7 +202,7 @@ def test_workspaces_never_shrink_with_more_tokens():
                  (0, 1, 4096, 8191, 8192, 12287, 12288, 100000, 262143, 262144, 262145, 300000, 1 << 20, 1 << 24)]
         assert all(s > 0 for s in sorts) and sorts == sorted(sorts)
     for bad in ((0, 64, 64, 1, 1), (1025, 64, 64, 1, 1), (4, 48, 64, 1, 1), (4, 64, 40, 1, 1), (4, 64, 64, -1, 1), (4, 64, 64, 1, 0),
-                (4, 64, 64, 1, 65), (4, 64, 64, 1 << 20, 32)):
+                (4, 64, 64, 1, 65), (4, 1 << 14, 64, (1 << 19) + 1, 8), (4, 64, 64, 1 << 20, 32)):
         _refused(spp.spp_mx4_experts_workspace, *bad)
     for bad in ((-1, 1, 4), (1, 0, 4), (1 << 24, 2, 4), (4, 4, 0), (4, 4, 1025)):
         _refused(spp.spp_expert_sort_workspace, *bad)
