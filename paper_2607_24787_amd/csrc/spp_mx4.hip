@@ -328,16 +328,30 @@ __device__ __forceinline__ int swizzled(int row, int c) {
   return c ^ ((row / (8 / kPieces)) % kPieces);
 }
 
-// Scale bytes of kBlocks blocks of a row from block b on, in bounds; 1 past the
-// row's end
-template <int kBlocks>
-__device__ __forceinline__ uint32_t row_scales(const uint8_t* p, int64_t row, int b, int nb, int64_t total) {
-  uint32_t w = scales4(p, row * nb + b, total);
+// A row's scale bytes, four blocks at a time, read whole and in bounds: near the
+// end of all scales (at least four) the word starts earlier.
+struct ScaleRow {
+  const uint8_t* p;
+  int last;  // the last block at which a word may start
+  __device__ __forceinline__ ScaleRow(const uint8_t* scales, int64_t row, int nb, int64_t total) {
+    p = scales + row * nb;
+    last = static_cast<int>(min(total - 4 - row * nb, int64_t{1} << 20));
+  }
+  __device__ __forceinline__ uint32_t load(int b) const {
+    uint32_t w;
+    __builtin_memcpy(&w, p + min(b, last), 4);
+    return w;
+  }
+  // kBlocks bytes from block b on of what load(b) gave; 1 past the row's end
+  template <int kBlocks>
+  __device__ __forceinline__ uint32_t bytes(uint32_t w, int b, int nb) const {
+    w >>= 8 * (b - min(b, last));
 #pragma unroll
-  for (int j = 1; j < kBlocks; ++j)
-    if (b + j >= nb) w = (w & ~(255u << (8 * j))) | static_cast<uint32_t>(kOne) << (8 * j);
-  return w;
-}
+    for (int j = 1; j < kBlocks; ++j)
+      if (b + j >= nb) w = (w & ~(255u << (8 * j))) | static_cast<uint32_t>(kOne) << (8 * j);
+    return w;
+  }
+};
 
 template <int SEL>
 __device__ __forceinline__ f32x16 mfma_mx4_32(u32x4 w, uint32_t w_scales, u32x4 x, uint32_t x_scales, f32x16 c) {
@@ -399,9 +413,22 @@ __device__ __forceinline__ Tile find_tile(const ProductArgs& a, int before, int 
   return Tile{__shfl(group, from), __shfl(first, from), __shfl(count, from)};
 }
 
+constexpr int kBuffers = 3;
+
+// Waits until at most kLeft of this wave's loads are on their way
+template <int kLeft>
+__device__ __forceinline__ void wait_loads() {
+  // vmcnt in bits 3:0 and 15:14; the other counters' bits all ones: not waited for
+  __builtin_amdgcn_s_waitcnt((kLeft & 15) | 0x0f70 | (kLeft >> 4) << 14);
+}
+
+// A barrier for LDS reads and writes that leaves loads into LDS on their way:
+// __syncthreads() would wait for them.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // A workgroup takes 256 weight rows (128 outputs of both matrices for SwiGLU)
-// and 32 * CT rows of one group; K goes through LDS in two buffers.  A wave
-// takes 64 of the weight rows and all rows of x.
+// and 32 * CT rows of one group; K goes through LDS in three buffers, loaded two
+// stages ahead.  A wave takes 64 of the weight rows and all rows of x.
 template <int X, bool kSwiglu, typename Out, int CT>
 __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a) {
   constexpr int KB = X == kXCodes ? 2 : 1;  // blocks of a lane and stage
@@ -409,10 +436,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   constexpr int AC = BL, BC = X == kXCodes ? BL : 4 * BL;  // 16-byte pieces of a row
   constexpr int TM = 32 * CT;
   constexpr int kA = kTileRows * AC * 16, kB = TM * BC * 16;
-  __shared__ __attribute__((aligned(16))) uint8_t s_a[2][kA];
-  __shared__ __attribute__((aligned(16))) uint8_t s_b[2][kB];
-  __shared__ uint32_t s_sa[2][kTileRows];
-  __shared__ uint32_t s_sb[2][TM];
+  // an array for each buffer: the compiler then sees that reads of one need not
+  // wait for loads into another
+  __shared__ __attribute__((aligned(16))) uint8_t s_a0[kA], s_a1[kA], s_a2[kA];
+  __shared__ __attribute__((aligned(16))) uint8_t s_b0[kB], s_b1[kB], s_b2[kB];
+  __shared__ uint32_t s_sa[kBuffers][kTileRows];
+  __shared__ uint32_t s_sb[X == kXCodes ? kBuffers : 1][kTileThreads];
+  const auto a_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_a0 : buf == 1 ? s_a1 : s_a2; };
+  const auto b_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_b0 : buf == 1 ? s_b1 : s_b2; };
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
 
   // the tile: workgroups of one XCD take neighbouring ones
@@ -458,30 +489,33 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     const int f = kSwiglu ? column * (kTileRows / 2) + w * 32 + 16 * hh + j : column * kTileRows + w * 64 + 32 * hh + 16 * up + j;
     scale_row = kSwiglu ? (static_cast<int64_t>(t.group) * 2 + up) * a.N + min(f, a.N - 1)
                         : static_cast<int64_t>(t.group) * a.N + min(f, a.N - 1);
-    if (X == kXCodes && tid < TM) {
+    if (X == kXCodes) {
       const int p = t.first + min(tid, t.count - 1);
       x_row = (a.pair ? a.pair[p] : p) / a.xdiv;
     }
   }
-  uint32_t wa = 0, wb = 0;
-  const auto issue = [&](int st, int buf) {
+  const ScaleRow scale_a(a.scales, scale_row, a.nb, a.blocks), scale_b(a.x_scales, x_row, a.nb, a.x_blocks);
+  // of the next two stages
+  uint32_t wa[2] = {0, 0}, wb[2] = {0, 0};
+  constexpr int kStageLoads = AC + (TM * BC) / kTileThreads + (X == kXCodes ? 2 : 1);  // of a wave, at least
+  const auto issue = [&](int st, auto buf, uint32_t& sa, uint32_t& sb) {
     const int b0 = st * BL;
+    sa = scale_a.load(b0);
+    if (X == kXCodes) sb = scale_b.load(b0);
 #pragma unroll
     for (int i = 0; i < AC; ++i)
-      to_lds(pa[i] + static_cast<int64_t>(b0 + ca[i] < a.nb ? b0 + ca[i] : 0) * 16, s_a[buf] + (i * kTileWaves + wave) * 1024);
+      to_lds(pa[i] + static_cast<int64_t>(b0 + ca[i] < a.nb ? b0 + ca[i] : 0) * 16, a_of(buf) + (i * kTileWaves + wave) * 1024);
 #pragma unroll
     for (int i = 0; i < BI; ++i) {
       if (BI * kTileThreads != TM * BC && (i * kTileWaves + wave) * 64 >= TM * BC) break;
       const int block = X == kXCodes ? b0 + cb[i] : b0 + cb[i] / 4;
       const uint8_t* from = pb[i] + (static_cast<int64_t>(b0) * (BC / BL) + cb[i]) * 16;
-      to_lds(block < a.nb ? from : reinterpret_cast<const uint8_t*>(&kZeros), s_b[buf] + (i * kTileWaves + wave) * 1024);
+      to_lds(block < a.nb ? from : reinterpret_cast<const uint8_t*>(&kZeros), b_of(buf) + (i * kTileWaves + wave) * 1024);
     }
-    wa = row_scales<BL>(a.scales, scale_row, b0, a.nb, a.blocks);
-    if (X == kXCodes && tid < TM) wb = row_scales<BL>(a.x_scales, x_row, b0, a.nb, a.x_blocks);
   };
-  const auto put_scales = [&](int buf) {
-    s_sa[buf][tid] = wa;
-    if (X == kXCodes && tid < TM) s_sb[buf][tid] = wb;
+  const auto put_scales = [&](int st, int buf, uint32_t sa, uint32_t sb) {
+    s_sa[buf][tid] = scale_a.bytes<BL>(sa, st * BL, a.nb);
+    if (X == kXCodes) s_sb[buf][tid] = scale_b.bytes<BL>(sb, st * BL, a.nb);
   };
 
   f32x16 acc[2][CT];
@@ -493,19 +527,28 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
       for (int j = 0; j < 16; ++j) acc[i][c][j] = 0.f;
 
   const int stages = (a.nb + BL - 1) / BL;
-  issue(0, 0);
-  put_scales(0);
-  __syncthreads();
-  for (int st = 0; st < stages; ++st) {
-    const int buf = st & 1;
-    if (st + 1 < stages) issue(st + 1, buf ^ 1);
+  using Buf0 = std::integral_constant<int, 0>;
+  using Buf1 = std::integral_constant<int, 1>;
+  using Buf2 = std::integral_constant<int, 2>;
+  issue(0, Buf0{}, wa[0], wb[0]);
+  if (stages > 1) issue(1, Buf1{}, wa[1], wb[1]);
+  if (stages > 1)
+    wait_loads<kStageLoads>();
+  else
+    wait_loads<0>();
+  put_scales(0, 0, wa[0], wb[0]);
+  lds_barrier();
+  const auto step = [&](int st, auto buf) {
+    constexpr int kNext = (buf + 1) % kBuffers, kAfter = (buf + 2) % kBuffers;
+    wa[0] = wa[1], wb[0] = wb[1];
+    if (st + 2 < stages) issue(st + 2, std::integral_constant<int, kAfter>{}, wa[1], wb[1]);
     const auto read_a = [&](int i, int c) {
       const int r = wave * 64 + i * 32 + l32;
-      return *reinterpret_cast<const u32x4*>(s_a[buf] + (r * AC + swizzled<AC>(r, c)) * 16);
+      return *reinterpret_cast<const u32x4*>(a_of(buf) + (r * AC + swizzled<AC>(r, c)) * 16);
     };
     const auto read_b = [&](int i, int c) {
       const int r = i * 32 + l32;
-      return *reinterpret_cast<const u32x4*>(s_b[buf] + (r * BC + swizzled<BC>(r, c)) * 16);
+      return *reinterpret_cast<const u32x4*>(b_of(buf) + (r * BC + swizzled<BC>(r, c)) * 16);
     };
     if constexpr (X == kXCodes) {
       uint32_t sa[2], sb[CT];
@@ -552,8 +595,18 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
         }
       }
     }
-    if (st + 1 < stages) put_scales(buf ^ 1);
-    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);  // the products go before the wait
+    if (st + 2 < stages)
+      wait_loads<kStageLoads>();
+    else
+      wait_loads<0>();
+    if (st + 1 < stages) put_scales(st + 1, kNext, wa[0], wb[0]);
+    lds_barrier();
+  };
+  for (int st = 0; st < stages; st += kBuffers) {
+    step(st, Buf0{});
+    if (st + 1 < stages) step(st + 1, Buf1{});
+    if (st + 2 < stages) step(st + 2, Buf2{});
   }
 
   // a lane holds 32 neighbouring outputs of a row (16 of both for SwiGLU)
@@ -727,7 +780,7 @@ hipError_t launch_tiles(const ProductArgs& a, int rows, hipStream_t st) {
 template <int X>
 hipError_t launch_product(const ProductArgs& a, int32_t dtype, hipStream_t st) {
   const int rows = tile_rows(a.M, a.groups);
-  if (rows > 0)
+  if (rows > 0 && a.blocks >= 4)  // fewer scales than a word: the few rows' kernel alone reads them byte by byte
     return dtype == SPP_DTYPE_BF16 ? launch_tiles<X, false, __bf16>(a, rows, st) : launch_tiles<X, false, float>(a, rows, st);
   const auto kernel = dtype == SPP_DTYPE_BF16 ? mx4_few_kernel<X, false, __bf16, kRowsStart>
                                               : mx4_few_kernel<X, false, float, kRowsStart>;
