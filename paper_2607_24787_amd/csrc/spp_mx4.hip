@@ -420,6 +420,7 @@ template <int kLeft>
 __device__ __forceinline__ void wait_loads() {
   // vmcnt in bits 3:0 and 15:14; the other counters' bits all ones: not waited for
   __builtin_amdgcn_s_waitcnt((kLeft & 15) | 0x0f70 | (kLeft >> 4) << 14);
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // A barrier for LDS reads and writes that leaves loads into LDS on their way:
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   __shared__ uint32_t s_sb[X == kXCodes ? kBuffers : 1][kTileThreads];
   const auto a_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_a0 : buf == 1 ? s_a1 : s_a2; };
   const auto b_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_b0 : buf == 1 ? s_b1 : s_b2; };
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, l32 = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
 
   // the tile: workgroups of one XCD take neighbouring ones
   int before = 0;
@@ -457,20 +458,28 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   if (a.start) t = find_tile<TM>(a, before, tile);
   if (t.count < 1) return;
 
-  // what this lane loads: rows' addresses, at the piece that goes to its place
-  const uint8_t* pa[AC];
+  // what this lane loads: rows' addresses, at the piece that goes to its place.
+  // Weight rows lie in one window (two for SwiGLU: a load's rows in one of them).
+  const int64_t first_row = (static_cast<int64_t>(t.group) * (kSwiglu ? 2 : 1)) * a.N;
+  const auto weight_row = [&](int r, int* up) {  // LDS row r's, in its window
+    const int rho = r & 31, w = r >> 6, hh = (rho >> 2) & 1, j = 4 * (rho >> 3) + (rho & 3);
+    *up = (r >> 5) & 1;
+    const int f = kSwiglu ? column * (kTileRows / 2) + w * 32 + 16 * hh + j : column * kTileRows + w * 64 + 32 * hh + 16 * *up + j;
+    return min(f, a.N - 1);
+  };
+  const int window = column * (kSwiglu ? kTileRows / 2 : kTileRows);
+  uint32_t pa[AC];  // bytes from the window's start
   int ca[AC];
 #pragma unroll
   for (int i = 0; i < AC; ++i) {
     const int idx = (i * kTileWaves + wave) * 64 + lane, r = idx / AC;
     ca[i] = swizzled<AC>(r, idx % AC);
-    const int rho = r & 31, up = (r >> 5) & 1, w = r >> 6;
-    const int hh = (rho >> 2) & 1, j = 4 * (rho >> 3) + (rho & 3);
-    const int f = kSwiglu ? column * (kTileRows / 2) + w * 32 + 16 * hh + j : column * kTileRows + w * 64 + 32 * hh + 16 * up + j;
-    const int64_t row = kSwiglu ? (static_cast<int64_t>(t.group) * 2 + up) * a.N + min(f, a.N - 1)
-                                : static_cast<int64_t>(t.group) * a.N + min(f, a.N - 1);
-    pa[i] = a.codes + row * a.nb * 16;
+    int up;
+    pa[i] = static_cast<uint32_t>(weight_row(r, &up) - window) * static_cast<uint32_t>(a.nb) * 16;
   }
+  const uint8_t* base[2];
+  base[0] = a.codes + (first_row + window) * a.nb * 16;
+  base[1] = kSwiglu ? base[0] + static_cast<int64_t>(a.N) * a.nb * 16 : base[0];
   constexpr int BI = (TM * BC + kTileThreads - 1) / kTileThreads;
   const uint8_t* pb[BI];
   int cb[BI];
@@ -484,27 +493,25 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   }
   int64_t scale_row, x_row = 0;
   {
-    const int rho = tid & 31, up = (tid >> 5) & 1, w = tid >> 6;
-    const int hh = (rho >> 2) & 1, j = 4 * (rho >> 3) + (rho & 3);
-    const int f = kSwiglu ? column * (kTileRows / 2) + w * 32 + 16 * hh + j : column * kTileRows + w * 64 + 32 * hh + 16 * up + j;
-    scale_row = kSwiglu ? (static_cast<int64_t>(t.group) * 2 + up) * a.N + min(f, a.N - 1)
-                        : static_cast<int64_t>(t.group) * a.N + min(f, a.N - 1);
+    int up;
+    const int r = weight_row(tid, &up);
+    scale_row = first_row + (kSwiglu && up ? a.N : 0) + r;
     if (X == kXCodes) {
       const int p = t.first + min(tid, t.count - 1);
       x_row = (a.pair ? a.pair[p] : p) / a.xdiv;
     }
   }
   const ScaleRow scale_a(a.scales, scale_row, a.nb, a.blocks), scale_b(a.x_scales, x_row, a.nb, a.x_blocks);
-  // of the next two stages
-  uint32_t wa[2] = {0, 0}, wb[2] = {0, 0};
+  uint32_t wa[kBuffers] = {}, wb[kBuffers] = {};  // of the stages on their way, by buffer
   constexpr int kStageLoads = AC + (TM * BC) / kTileThreads + (X == kXCodes ? 2 : 1);  // of a wave, at least
-  const auto issue = [&](int st, auto buf, uint32_t& sa, uint32_t& sb) {
+  const auto issue = [&](int st, auto buf) {
     const int b0 = st * BL;
-    sa = scale_a.load(b0);
-    if (X == kXCodes) sb = scale_b.load(b0);
+    wa[buf] = scale_a.load(b0);
+    if (X == kXCodes) wb[buf] = scale_b.load(b0);
 #pragma unroll
     for (int i = 0; i < AC; ++i)
-      to_lds(pa[i] + static_cast<int64_t>(b0 + ca[i] < a.nb ? b0 + ca[i] : 0) * 16, a_of(buf) + (i * kTileWaves + wave) * 1024);
+      to_lds(base[((i * kTileWaves + wave) * (64 / AC) >> 5) & 1] + (pa[i] + (b0 + ca[i] < a.nb ? b0 + ca[i] : 0) * 16),
+             a_of(buf) + (i * kTileWaves + wave) * 1024);
 #pragma unroll
     for (int i = 0; i < BI; ++i) {
       if (BI * kTileThreads != TM * BC && (i * kTileWaves + wave) * 64 >= TM * BC) break;
@@ -514,6 +521,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     }
   };
   const auto put_scales = [&](int st, int buf, uint32_t sa, uint32_t sb) {
+    asm volatile("" : "+v"(sa), "+v"(sb));  // not before the wait
     s_sa[buf][tid] = scale_a.bytes<BL>(sa, st * BL, a.nb);
     if (X == kXCodes) s_sb[buf][tid] = scale_b.bytes<BL>(sb, st * BL, a.nb);
   };
@@ -530,45 +538,52 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   using Buf0 = std::integral_constant<int, 0>;
   using Buf1 = std::integral_constant<int, 1>;
   using Buf2 = std::integral_constant<int, 2>;
-  issue(0, Buf0{}, wa[0], wb[0]);
-  if (stages > 1) issue(1, Buf1{}, wa[1], wb[1]);
-  if (stages > 1)
+  issue(0, Buf0{});
+  if (stages > 1) {
+    issue(1, Buf1{});
     wait_loads<kStageLoads>();
-  else
+  } else {
     wait_loads<0>();
+  }
   put_scales(0, 0, wa[0], wb[0]);
   lds_barrier();
-  const auto step = [&](int st, auto buf) {
-    constexpr int kNext = (buf + 1) % kBuffers, kAfter = (buf + 2) % kBuffers;
-    wa[0] = wa[1], wb[0] = wb[1];
-    if (st + 2 < stages) issue(st + 2, std::integral_constant<int, kAfter>{}, wa[1], wb[1]);
+  // where this lane reads: its row's first piece, and the others by exclusive or
+  // with their number; its row's scales of its half.  Hidden from the compiler,
+  // which would keep an address of its own for every read of every buffer.
+  uint32_t at_a = (l32 * AC + swizzled<AC>(l32, half * KB)) * 16 + wave * 64 * AC * 16;
+  uint32_t at_b = (l32 * BC + swizzled<BC>(l32, half * (BC / 2))) * 16;
+  uint32_t at_sa = (wave * 64 + l32) * 4 + half * KB, at_sb = l32 * 4 + half * KB;
+  const auto products = [&](const uint8_t* in_a, const uint8_t* in_b, const uint32_t* in_sa, const uint32_t* in_sb) {
+    asm volatile("" : "+v"(at_a), "+v"(at_b), "+v"(at_sa), "+v"(at_sb));
     const auto read_a = [&](int i, int c) {
-      const int r = wave * 64 + i * 32 + l32;
-      return *reinterpret_cast<const u32x4*>(a_of(buf) + (r * AC + swizzled<AC>(r, c)) * 16);
+      return *reinterpret_cast<const u32x4*>(in_a + (at_a ^ (c << 4)) + i * 32 * AC * 16);
     };
     const auto read_b = [&](int i, int c) {
-      const int r = i * 32 + l32;
-      return *reinterpret_cast<const u32x4*>(b_of(buf) + (r * BC + swizzled<BC>(r, c)) * 16);
+      return *reinterpret_cast<const u32x4*>(in_b + (at_b ^ (c << 4)) + i * 32 * BC * 16);
+    };
+    const auto scale = [&](const uint32_t* in, uint32_t at, int i) -> uint32_t {
+      const uint8_t* p = reinterpret_cast<const uint8_t*>(in) + at + i * 128;
+      return KB == 2 ? *reinterpret_cast<const uint16_t*>(p) : *p;
     };
     if constexpr (X == kXCodes) {
       uint32_t sa[2], sb[CT];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) sa[i] = s_sa[buf][wave * 64 + i * 32 + l32] >> (8 * KB * half);
+      for (int i = 0; i < 2; ++i) sa[i] = scale(in_sa, at_sa, i);
 #pragma unroll
-      for (int i = 0; i < CT; ++i) sb[i] = s_sb[buf][i * 32 + l32] >> (8 * KB * half);
+      for (int i = 0; i < CT; ++i) sb[i] = scale(in_sb, at_sb, i);
       u32x4 va[2], vb[CT];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) va[i] = read_a(i, half * KB);
+      for (int i = 0; i < 2; ++i) va[i] = read_a(i, 0);
 #pragma unroll
-      for (int i = 0; i < CT; ++i) vb[i] = read_b(i, half * KB);
+      for (int i = 0; i < CT; ++i) vb[i] = read_b(i, 0);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[i][c] = mfma_mx4_32<0>(va[i], sa[i], vb[c], sb[c], acc[i][c]);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) va[i] = read_a(i, half * KB + 1);
+      for (int i = 0; i < 2; ++i) va[i] = read_a(i, 1);
 #pragma unroll
-      for (int i = 0; i < CT; ++i) vb[i] = read_b(i, half * KB + 1);
+      for (int i = 0; i < CT; ++i) vb[i] = read_b(i, 1);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -578,14 +593,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
       float sa[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        va[i] = read_a(i, half);
-        sa[i] = scale_of((s_sa[buf][wave * 64 + i * 32 + l32] >> (8 * half)) & 255u);
+        va[i] = read_a(i, 0);
+        sa[i] = scale_of(scale(in_sa, at_sa, i));
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         u32x4 vb[CT];
 #pragma unroll
-        for (int c = 0; c < CT; ++c) vb[c] = read_b(c, half * 4 + q);
+        for (int c = 0; c < CT; ++c) vb[c] = read_b(c, q);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const bf16x8 w = __builtin_bit_cast(bf16x8, cvt8(va[i][q], sa[i]));
@@ -595,19 +610,30 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
         }
       }
     }
-    __builtin_amdgcn_sched_barrier(0);  // the products go before the wait
-    if (st + 2 < stages)
+    __builtin_amdgcn_sched_barrier(0);  // the products go before what follows
+  };
+  const auto step = [&](int st, auto buf, bool load) {
+    constexpr int kNext = (buf + 1) % kBuffers, kAfter = (buf + 2) % kBuffers;
+    if (load) issue(st + 2, std::integral_constant<int, kAfter>{});
+    products(a_of(buf), b_of(buf), s_sa[buf], s_sb[X == kXCodes ? buf : 0]);
+    if (load)
       wait_loads<kStageLoads>();
     else
       wait_loads<0>();
-    if (st + 1 < stages) put_scales(st + 1, kNext, wa[0], wb[0]);
+    put_scales(st + 1, kNext, wa[kNext], wb[kNext]);
     lds_barrier();
   };
-  for (int st = 0; st < stages; st += kBuffers) {
-    step(st, Buf0{});
-    if (st + 1 < stages) step(st + 1, Buf1{});
-    if (st + 2 < stages) step(st + 2, Buf2{});
+  int st = 0;
+  for (; st + 4 < stages; st += kBuffers) {
+    step(st, Buf0{}, true);
+    step(st + 1, Buf1{}, true);
+    step(st + 2, Buf2{}, true);
   }
+  // one to four are left
+  step(st, Buf0{}, st + 2 < stages);
+  if (st + 1 < stages) step(st + 1, Buf1{}, st + 3 < stages);
+  if (st + 2 < stages) step(st + 2, Buf2{}, false);
+  if (st + 3 < stages) step(st + 3, Buf0{}, false);
 
   // a lane holds 32 neighbouring outputs of a row (16 of both for SwiGLU)
 #pragma unroll
