@@ -178,65 +178,99 @@ __device__ __forceinline__ uint32_t byte_or_one(uint32_t w, int s, bool ok) { re
 
 constexpr int kFewThreads = 256;
 constexpr int kFewWaves = kFewThreads / 64;
-constexpr int kStep = 4;  // blocks of a lane whose loads are in flight together
-
-// The sums of one wave's share of K for 16 weight rows (times kTiles) and 16
-// rows of x.  Lane l holds weight row and row of x l % 16; lanes 16g .. 16g+15
-// of wave w own blocks (4w + g) * per and on, of both: what the matrix
-// instruction sums over goes by lane and place, whatever the blocks' order in K.
-template <int X, int kTiles>
-__device__ __forceinline__ void few_sums(const ProductArgs& a, const int64_t* row, int64_t x_row, bool x_ok, int b0, int b1,
-                                         int per, f32x4* acc) {
-  for (int s0 = 0; s0 < per; s0 += kStep) {
-    u32x4 w[kTiles][kStep];
-    uint32_t ws[kTiles];
+// Up to kStep blocks of a lane, of kTiles weight rows: codes and scale bytes.
+// Lane l holds weight row and row of x l % 16.  Which blocks a lane takes is
+// free as long as both operands agree: the matrix instruction's sum goes by lane
+// and place, whatever the blocks' order in K.  Here a lane's blocks follow one
+// another, so that its loads share cache lines and its scales a word.
+template <int kTiles, int kStep>
+struct WeightBlocks {
+  u32x4 codes[kTiles][kStep];
+  uint32_t scales[kTiles];
+  // blocks b .. b + kStep - 1, those from b1 on not used
+  __device__ __forceinline__ void load(const ProductArgs& a, const int64_t* row, int b, int b1) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      ws[t] = scales4(a.scales, row[t] * a.nb + min(b0 + s0, a.nb - 1), a.blocks);
+      scales[t] = scales4(a.scales, row[t] * a.nb + min(b, a.nb - 1), a.blocks);
 #pragma unroll
-      for (int s = 0; s < kStep; ++s) {
-        const int b = b0 + s0 + s;
-        w[t][s] = reinterpret_cast<const u32x4*>(a.codes)[row[t] * a.nb + (b < b1 ? b : 0)];
-      }
+      for (int s = 0; s < kStep; ++s)
+        codes[t][s] = reinterpret_cast<const u32x4*>(a.codes)[row[t] * a.nb + (b + s < b1 ? b + s : 0)];
     }
+  }
+  template <int X>
+  __device__ __forceinline__ void products(const ProductArgs& a, int64_t x_row, bool x_ok, int b, int b1, f32x4* acc) const {
 #pragma unroll
     for (int s = 0; s < kStep; ++s) {
-      const bool ok = b0 + s0 + s < b1;
+      const bool ok = b + s < b1;
       u32x4 v[4];
       uint32_t byte;
-      x_block<X>(a, x_row, b0 + s0 + s, ok && x_ok, v, &byte);
+      x_block<X>(a, x_row, b + s, ok && x_ok, v, &byte);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
-        const uint32_t wb = byte_or_one(ws[t], s, ok);
+        const uint32_t wb = byte_or_one(scales[t], s, ok);
         if constexpr (X == kXBf16) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) acc[t] = mfma_bf16(cvt8(w[t][s][q], scale_of(wb)), v[q], acc[t]);
+          for (int q = 0; q < 4; ++q) acc[t] = mfma_bf16(cvt8(codes[t][s][q], scale_of(wb)), v[q], acc[t]);
         } else {
-          acc[t] = mfma_mx4<0>(w[t][s], wb, v[0], byte, acc[t]);
+          acc[t] = mfma_mx4<0>(codes[t][s], wb, v[0], byte, acc[t]);
         }
       }
     }
   }
+};
+
+constexpr int kIds = 8;
+
+// Ids of 64 * kIds pairs from p0 on, by lanes
+struct Ids {
+  int id[kIds];
+  __device__ __forceinline__ void load(const ProductArgs& a, int p0) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < kIds; ++j) id[j] = a.ids[min(p0 + 64 * j + lane, a.M - 1)];
+  }
+};
+
+// The pairs with id `group` whose place among them is in [r0, r0 + 16), by one
+// wave; returns how many there are in all.  ids: the first pairs'.  first: the
+// first of all.
+__device__ __forceinline__ int find_pairs(const ProductArgs& a, Ids ids, int group, int r0, int* row, int* first) {
+  const int lane = threadIdx.x & 63;
+  int seen = 0;
+  *first = a.M;
+  for (int p0 = 0; p0 < a.M; p0 += 64 * kIds) {
+    if (p0 > 0) ids.load(a, p0);
+#pragma unroll
+    for (int j = 0; j < kIds; ++j) {
+      const int p = p0 + 64 * j + lane;
+      const bool mine = p < a.M && ids.id[j] == group;
+      const uint64_t m = __ballot(mine);
+      const int at = seen + __popcll(m & ((uint64_t{1} << lane) - 1)) - r0;
+      if (mine && at >= 0 && at < 16) row[at] = p;
+      if (seen == 0 && m) *first = p0 + 64 * j + __ffsll(static_cast<long long>(m)) - 1;
+      seen += __popcll(m);
+    }
+  }
+  return seen;
 }
 
-// A workgroup takes 16 outputs (of both matrices for SwiGLU) of one group for
-// 16 of its rows at a time; its waves share K.
-template <int X, bool kSwiglu, typename Out, int kRows>
+// A workgroup takes 16 * NT outputs (of both matrices for SwiGLU) of one group
+// for 16 of its rows at a time; its waves share K, kStep blocks of a lane at a
+// time.  The first weights are on their way before the rows are known; the ids
+// that tell them go before the weights, since loads return in order.
+template <int X, bool kSwiglu, int NT, int kStep, typename Out, int kRows>
 __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
-  constexpr int kTiles = kSwiglu ? 2 : 1;
+  constexpr int kTiles = kSwiglu ? 2 * NT : NT;
   __shared__ f32x4 s_part[kFewWaves][kTiles][64];
-  __shared__ int s_row[16];
-  __shared__ int s_count;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, l16 = lane & 15;
+  __shared__ int s_rows[kFewWaves][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, l16 = lane & 15;
+  int* s_row = s_rows[wave];
   int group = blockIdx.y, begin = 0, count = 0;
+  Ids ids;
   if constexpr (kRows == kRowsIds) {
-    if (a.by_pair) {
-      group = a.ids[blockIdx.y];
-      if (static_cast<unsigned>(group) >= static_cast<unsigned>(a.groups)) return;
-      bool earlier = false;
-      for (int p = lane; p < static_cast<int>(blockIdx.y); p += 64) earlier |= a.ids[p] == group;
-      if (__ballot(earlier)) return;
-    }
+    ids.load(a, 0);
+    if (a.by_pair) group = a.ids[blockIdx.y];
+    if (static_cast<unsigned>(group) >= static_cast<unsigned>(a.groups)) return;
   } else {
     count = a.M;
     if (a.start) {
@@ -247,61 +281,111 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
   }
   const int per = (a.nb + 4 * kFewWaves - 1) / (4 * kFewWaves);
   const int b0 = (wave * 4 + g) * per, b1 = min(b0 + per, a.nb);
-  const int f0 = blockIdx.x * 16;
+  const int f0 = blockIdx.x * 16 * NT;
   int64_t row[kTiles];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t)
-    row[t] = (static_cast<int64_t>(group) * kTiles + t) * a.N + min(f0 + l16, a.N - 1);
+    row[t] = (static_cast<int64_t>(group) * (kSwiglu ? 2 : 1) + t / NT) * a.N + min(f0 + 16 * (t % NT) + l16, a.N - 1);
+  WeightBlocks<kTiles, kStep> w;
+  w.load(a, row, b0, b1);
   for (int r0 = 0;; r0 += 16) {
     if constexpr (kRows == kRowsIds) {
-      if (wave == 0) {
-        int seen = 0;
-        for (int p0 = 0; p0 < a.M; p0 += 64) {
-          const bool mine = p0 + lane < a.M && a.ids[p0 + lane] == group;
-          const uint64_t m = __ballot(mine);
-          const int at = seen + __popcll(m & ((uint64_t{1} << lane) - 1)) - r0;
-          if (mine && at >= 0 && at < 16) s_row[at] = p0 + lane;
-          seen += __popcll(m);
-        }
-        if (lane == 0) s_count = seen;
-      }
-      __syncthreads();
-      count = s_count;
-      if (r0 >= count) return;
-    } else {
-      if (tid < 16) s_row[tid] = begin + min(r0 + tid, count - 1);
-      __syncthreads();
+      int first;
+      count = find_pairs(a, ids, group, r0, s_row, &first);
+      if (r0 >= count || (a.by_pair && first != static_cast<int>(blockIdx.y))) return;
+      __builtin_amdgcn_wave_barrier();
     }
     const bool x_ok = r0 + l16 < count;
     int64_t x_row = 0;
-    if (x_ok) {
-      const int i = s_row[l16];
-      const int p = a.pair ? a.pair[i] : i;
-      x_row = p / a.xdiv;
-    }
+    if (x_ok) x_row = kRows == kRowsIds ? s_row[l16] / a.xdiv : begin + r0 + l16;
     f32x4 acc[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    few_sums<X, kTiles>(a, row, x_row, x_ok, b0, b1, per, acc);
+    for (int s0 = 0; s0 < per; s0 += kStep) {
+      if (s0 > 0 || (r0 > 0 && per > kStep)) w.load(a, row, b0 + s0, b1);
+      w.template products<X>(a, x_row, x_ok, b0 + s0, b1, acc);
+    }
     // outputs 4g .. 4g+3 of row l16
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) s_part[wave][t][l16 * 4 + g] = acc[t];
     __syncthreads();
-    const int i = tid >> 4, f = f0 + (tid & 15);
-    float v[kTiles];
+    for (int j = tid; j < 64 * NT; j += kFewThreads) {
+      const int i = j / (4 * NT), q = j % (4 * NT), t = q / 4, at = i * 4 + q % 4;  // row i, four outputs
+      f32x4 y = s_part[0][t][at];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      v[t] = 0.f;
-      for (int w = 0; w < kFewWaves; ++w) v[t] += reinterpret_cast<const float*>(s_part[w][t])[tid];
-    }
-    if (r0 + i < count && f < a.N) {
-      float y = v[0];
-      if constexpr (kSwiglu) y = swiglu(v[0], v[1]);
-      static_cast<Out*>(a.out)[s_row[i] * a.out_stride + f] = static_cast<Out>(y);
+      for (int v = 1; v < kFewWaves; ++v) y += s_part[v][t][at];
+      if constexpr (kSwiglu) {
+        f32x4 u = s_part[0][NT + t][at];
+#pragma unroll
+        for (int v = 1; v < kFewWaves; ++v) u += s_part[v][NT + t][at];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
+      }
+      const int f = f0 + 4 * q;
+      if (r0 + i >= count || f >= a.N) continue;
+      const int64_t to = kRows == kRowsIds ? s_row[i] : begin + r0 + i;
+      Out* out = static_cast<Out*>(a.out) + to * a.out_stride + f;
+      if (a.wide_out && f + 4 <= a.N) {
+        if constexpr (std::is_same<Out, float>::value)
+          *reinterpret_cast<f32x4*>(out) = y;
+        else
+          *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (f + e < a.N) out[e] = static_cast<Out>(y[e]);
+      }
     }
     if (r0 + 16 >= count) return;
     __syncthreads();
   }
+}
+
+// The second product of one or a few tokens with the gates' sum, one launch for
+// both: a workgroup takes 16 outputs of token blockIdx.y, its waves its experts
+// (and shares of K where there are fewer experts than waves).
+struct LastArgs {
+  ProductArgs p;  // x: the SwiGLU's results, row t * K + k; ids
+  const float* gates;
+  const void* residual;
+  int64_t residual_stride;
+  int K;
+};
+
+constexpr int kLastThreads = 512;
+constexpr int kLastWaves = kLastThreads / 64;
+
+template <int X>
+__global__ __launch_bounds__(kLastThreads) void mx4_last_kernel(LastArgs a) {
+  __shared__ f32x4 s_part[kLastWaves][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, l16 = lane & 15;
+  const int parts = a.K >= kLastWaves ? 1 : kLastWaves / a.K;
+  const int per = (a.p.nb + 4 * parts - 1) / (4 * parts);
+  const int f0 = blockIdx.x * 16, token = blockIdx.y;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int i = wave; i < a.K * parts; i += kLastWaves) {
+    const int pair = token * a.K + i / parts, e = a.p.ids[pair];
+    if (static_cast<unsigned>(e) >= static_cast<unsigned>(a.p.groups)) continue;
+    const float gate = a.gates[pair];
+    const int b0 = (i % parts * 4 + g) * per, b1 = min(b0 + per, a.p.nb);
+    const int64_t row = static_cast<int64_t>(e) * a.p.N + min(f0 + l16, a.p.N - 1);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    constexpr int kStep = 3;
+    WeightBlocks<1, kStep> w;
+    for (int s0 = 0; s0 < per; s0 += kStep) {
+      w.load(a.p, &row, b0 + s0, b1);
+      w.template products<X>(a.p, pair, l16 == 0, b0 + s0, b1, &acc);
+    }
+    sum += gate * acc;
+  }
+  if (l16 == 0) s_part[wave][g] = sum;
+  __syncthreads();
+  if (tid >= 16 || f0 + tid >= a.p.N) return;
+  float y = 0.f;
+#pragma unroll
+  for (int w = 0; w < kLastWaves; ++w) y += reinterpret_cast<const float*>(s_part[w])[tid];
+  if (a.residual) y += static_cast<float>(static_cast<const __bf16*>(a.residual)[token * a.residual_stride + f0 + tid]);
+  static_cast<__bf16*>(a.p.out)[token * a.p.out_stride + f0 + tid] = static_cast<__bf16>(y);
 }
 
 // -------------------------------------------------------- products of many rows
@@ -734,6 +818,7 @@ hipError_t launch2(void (*kernel)(ProductArgs), unsigned x, unsigned y, unsigned
   return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(x, y), dim3(threads), params, 0, st);
 }
 
+constexpr int kLastTokens = 2;  // at most, of mx4_last_kernel
 constexpr int kMaxM = 1 << 24;
 constexpr int kMaxN = 1 << 20;
 constexpr int64_t kMaxOutputs = int64_t{1} << 36;  // below 2^24 workgroups in every form
@@ -776,12 +861,49 @@ ProductArgs product_of(const spp_mx4_matrix& w, int32_t groups, const int32_t* s
   return a;
 }
 
-unsigned tiles16(int N) { return static_cast<unsigned>((N + 15) / 16); }
+bool wide_rows(const void* out, int64_t stride, size_t elem) {
+  return aligned16(out) && stride * static_cast<int64_t>(elem) % 16 == 0;
+}
+
+// Blocks of a lane at a time: the fewest that are loaded in vain, then the most
+int few_step(int per) {
+  int best = 4;
+  for (int s = 3; s > 1; --s)
+    if ((per + s - 1) / s * s < (per + best - 1) / best * best) best = s;
+  return best;
+}
+
+// Sixteens of outputs a workgroup of few rows takes: as many as leave four
+// workgroups to a compute unit, and a lane about 8 loads at once
+int few_outputs(const ProductArgs& a, int64_t groups, bool swiglu, int step) {
+  for (int nt = swiglu ? 2 : 4; nt > 1; nt /= 2)
+    if (nt * (swiglu ? 2 : 1) * step <= 8 && groups * ((a.N + 16 * nt - 1) / (16 * nt)) >= 1024) return nt;
+  return 1;
+}
+
+template <int X, bool kSwiglu, int NT, typename Out, int kRows>
+hipError_t launch_few(const ProductArgs& a, int64_t groups, int step, hipStream_t st) {
+  const auto kernel = step == 4   ? mx4_few_kernel<X, kSwiglu, NT, 4, Out, kRows>
+                      : step == 3 ? mx4_few_kernel<X, kSwiglu, NT, 3, Out, kRows>
+                                  : mx4_few_kernel<X, kSwiglu, NT, 2, Out, kRows>;
+  return launch2(kernel, static_cast<unsigned>((a.N + 16 * NT - 1) / (16 * NT)), static_cast<unsigned>(groups), kFewThreads,
+                 a, st);
+}
+
+template <int X, bool kSwiglu, typename Out, int kRows>
+hipError_t launch_few(ProductArgs a, int64_t groups, hipStream_t st) {
+  a.wide_out = wide_rows(a.out, a.out_stride, sizeof(Out));
+  const int step = few_step((a.nb + 4 * kFewWaves - 1) / (4 * kFewWaves)), nt = few_outputs(a, groups, kSwiglu, step);
+  if constexpr (!kSwiglu)
+    if (nt == 4) return launch_few<X, kSwiglu, 4, Out, kRows>(a, groups, step, st);
+  return nt == 2 ? launch_few<X, kSwiglu, 2, Out, kRows>(a, groups, step, st)
+                 : launch_few<X, kSwiglu, 1, Out, kRows>(a, groups, step, st);
+}
 
 template <int X, bool kSwiglu, typename Out, int CT>
 hipError_t launch_tile(ProductArgs a, hipStream_t st) {
   a.columns = (a.N + (kSwiglu ? kTileRows / 2 : kTileRows) - 1) / (kSwiglu ? kTileRows / 2 : kTileRows);
-  a.wide_out = aligned16(a.out) && a.out_stride * static_cast<int64_t>(sizeof(Out)) % 16 == 0;
+  a.wide_out = wide_rows(a.out, a.out_stride, sizeof(Out));
   // groups with a last tile of their own: at most one a group, and one a row
   const int64_t tiles = a.M / (32 * CT) + std::min(a.groups, a.M);
   const int64_t grid = (tiles * a.columns + kXcds - 1) / kXcds * kXcds;
@@ -808,9 +930,8 @@ hipError_t launch_product(const ProductArgs& a, int32_t dtype, hipStream_t st) {
   const int rows = tile_rows(a.M, a.groups);
   if (rows > 0 && a.blocks >= 4)  // fewer scales than a word: the few rows' kernel alone reads them byte by byte
     return dtype == SPP_DTYPE_BF16 ? launch_tiles<X, false, __bf16>(a, rows, st) : launch_tiles<X, false, float>(a, rows, st);
-  const auto kernel = dtype == SPP_DTYPE_BF16 ? mx4_few_kernel<X, false, __bf16, kRowsStart>
-                                              : mx4_few_kernel<X, false, float, kRowsStart>;
-  return launch2(kernel, tiles16(a.N), static_cast<unsigned>(a.groups), kFewThreads, a, st);
+  return dtype == SPP_DTYPE_BF16 ? launch_few<X, false, __bf16, kRowsStart>(a, a.groups, st)
+                                 : launch_few<X, false, float, kRowsStart>(a, a.groups, st);
 }
 
 // The parts of a workspace of the experts' call
@@ -1032,18 +1153,31 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
   a.ids = topk;
   a.xdiv = K;
   a.by_pair = P < n;
-  const unsigned groups = static_cast<unsigned>(std::min<int64_t>(P, n));
-  hipError_t e = launch2(mx4 ? mx4_few_kernel<kXQuantBf16, true, float, kRowsIds>
-                             : mx4_few_kernel<kXBf16, true, __bf16, kRowsIds>,
-                         tiles16(I), groups, kFewThreads, a, st);
+  const int64_t groups = std::min<int64_t>(P, n);
+  hipError_t e = mx4 ? launch_few<kXQuantBf16, true, float, kRowsIds>(a, groups, st)
+                     : launch_few<kXBf16, true, __bf16, kRowsIds>(a, groups, st);
   if (e != hipSuccess) return launched(e);
   ProductArgs d = product_of(*down, n, nullptr, static_cast<int32_t>(P), space + s.y, D);
   d.x = space + s.h;
   d.x_stride = static_cast<int64_t>(I) * (mx4 ? 4 : 2);
   d.ids = topk;
   d.by_pair = P < n;
-  e = launch2(mx4 ? mx4_few_kernel<kXQuantF32, false, float, kRowsIds> : mx4_few_kernel<kXBf16, false, float, kRowsIds>,
-              tiles16(D), groups, kFewThreads, d, st);
+  if (T <= kLastTokens) {
+    LastArgs l{};
+    l.p = d;
+    l.p.out = out;
+    l.p.out_stride = out_stride;
+    l.gates = gates;
+    l.residual = residual;
+    l.residual_stride = residual_stride;
+    l.K = K;
+    void* params[] = {&l};
+    const void* kernel = reinterpret_cast<const void*>(mx4 ? mx4_last_kernel<kXQuantF32> : mx4_last_kernel<kXBf16>);
+    return launched(hipLaunchKernel(kernel, dim3(static_cast<unsigned>((D + 15) / 16), static_cast<unsigned>(T)),
+                                    dim3(kLastThreads), params, 0, st));
+  }
+  e = mx4 ? launch_few<kXQuantF32, false, float, kRowsIds>(d, groups, st)
+          : launch_few<kXBf16, false, float, kRowsIds>(d, groups, st);
   if (e != hipSuccess) return launched(e);
   c.ids = topk;
   c.n = n;
