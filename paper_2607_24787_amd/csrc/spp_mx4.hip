@@ -85,6 +85,7 @@ struct ProductArgs {
   const int32_t* ids;             // kRowsIds: [M]
   const int32_t* pair;            // row i of a group is row pair[i] / xdiv of x (NULL: i / xdiv)
   int xdiv;
+  int run;                        // few rows: tiles of a workgroup
   int by_pair;                    // kRowsIds: blockIdx.y is a pair, and the first with its id takes the group
   void* out;
   int64_t out_stride;             // elements
@@ -93,20 +94,30 @@ struct ProductArgs {
   int wide_out;                   // rows of out are 16-byte aligned
 };
 
-// Scale bytes [at, at + 4) as one word, of `total` bytes; those past the end do
-// not count.
-__device__ __forceinline__ uint32_t scales4(const uint8_t* p, int64_t at, int64_t total) {
-  if (total < 4) {
-    uint32_t w = 0;
-    for (int j = 0; j < 4; ++j)
-      if (at + j < total) w |= static_cast<uint32_t>(p[at + j]) << (8 * j);
+// A row's scale bytes, four blocks at a time, read whole and in bounds: near the
+// end of all scales (at least four) the word starts earlier.
+struct ScaleRow {
+  const uint8_t* p;
+  int last;  // the last block at which a word may start
+  __device__ __forceinline__ ScaleRow(const uint8_t* scales, int64_t row, int nb, int64_t total) {
+    p = scales + row * nb;
+    last = static_cast<int>(min(total - 4 - row * nb, int64_t{1} << 20));
+  }
+  __device__ __forceinline__ uint32_t load(int b) const {
+    uint32_t w;
+    __builtin_memcpy(&w, p + min(b, last), 4);
     return w;
   }
-  const int64_t o = min(at, total - 4);
-  uint32_t w;
-  __builtin_memcpy(&w, p + o, 4);
-  return w >> (8 * static_cast<int>(at - o));
-}
+  // kBlocks bytes from block b on of what load(b) gave; 1 past the row's end
+  template <int kBlocks>
+  __device__ __forceinline__ uint32_t bytes(uint32_t w, int b, int nb) const {
+    w >>= 8 * (b - min(b, last));
+#pragma unroll
+    for (int j = 1; j < kBlocks; ++j)
+      if (b + j >= nb) w = (w & ~(255u << (8 * j))) | static_cast<uint32_t>(kOne) << (8 * j);
+    return w;
+  }
+};
 
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -137,33 +148,42 @@ __device__ __forceinline__ i32x8 wide(u32x4 c) {
   return i32x8{static_cast<int>(c[0]), static_cast<int>(c[1]), static_cast<int>(c[2]), static_cast<int>(c[3]), 0, 0, 0, 0};
 }
 
-// Block b of row x (or nothing): bf16 rows as four operands of 8 elements, rows
-// in 4 bits as codes in v[0] with their scale byte
-template <int X>
-__device__ __forceinline__ void x_block(const ProductArgs& a, int64_t row, int b, bool ok, u32x4* v, uint32_t* byte) {
-  *byte = kOne;
+// A barrier for LDS reads and writes that leaves loads into LDS on their way:
+// __syncthreads() would wait for them.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// kStep blocks of a row of x: bf16 rows as four operands of 8 elements each, rows
+// in 4 bits as codes with their scale byte
+template <int X, int kStep>
+struct XBlocks {
+  static constexpr int kParts = X == kXBf16 ? 4 : 1;
+  u32x4 v[kStep][kParts];
+  uint32_t byte[kStep];
+  // blocks b .. b + kStep - 1, zeros from b1 on, or for no row
+  __device__ __forceinline__ void load(const ProductArgs& a, int64_t row, bool have, int b, int b1) {
+    const uint8_t* p = static_cast<const uint8_t*>(a.x) + row * a.x_stride;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) v[q] = u32x4{0, 0, 0, 0};
-  if (!ok) return;
-  const uint8_t* p = static_cast<const uint8_t*>(a.x) + row * a.x_stride;
-  if constexpr (X == kXCodes) {
-    v[0] = reinterpret_cast<const u32x4*>(p)[b];
-    *byte = a.x_scales[row * a.nb + b];
-  } else if constexpr (X == kXQuantF32) {
-    float y[32];
+    for (int s = 0; s < kStep; ++s) {
+      byte[s] = kOne;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) load8(reinterpret_cast<const float*>(p) + 32 * b + 8 * q, y + 8 * q);
-    v[0] = quantise32(y, byte);
-  } else if constexpr (X == kXQuantBf16) {
-    float y[32];
+      for (int q = 0; q < kParts; ++q) v[s][q] = u32x4{0, 0, 0, 0};
+      if (!have || b + s >= b1) continue;
+      if constexpr (X == kXCodes) {
+        v[s][0] = reinterpret_cast<const u32x4*>(p)[b + s];
+        byte[s] = a.x_scales[row * a.nb + b + s];
+      } else if constexpr (X == kXBf16) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) load8(reinterpret_cast<const __bf16*>(p) + 32 * b + 8 * q, y + 8 * q);
-    v[0] = quantise32(y, byte);
-  } else {
+        for (int q = 0; q < 4; ++q) v[s][q] = reinterpret_cast<const u32x4*>(p)[4 * (b + s) + q];
+      } else {
+        using T = typename std::conditional<X == kXQuantF32, float, __bf16>::type;
+        float y[32];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = reinterpret_cast<const u32x4*>(p)[4 * b + q];
+        for (int q = 0; q < 4; ++q) load8(reinterpret_cast<const T*>(p) + 32 * (b + s) + 8 * q, y + 8 * q);
+        v[s][0] = quantise32(y, &byte[s]);
+      }
+    }
   }
-}
+};
 
 template <int SEL>
 __device__ __forceinline__ f32x4 mfma_mx4(u32x4 w, uint32_t w_scales, u32x4 x, uint32_t x_byte, f32x4 c) {
@@ -173,46 +193,51 @@ __device__ __forceinline__ f32x4 mfma_mx4(u32x4 w, uint32_t w_scales, u32x4 x, u
 
 __device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + expf(-g)) * u; }
 
-// Byte s of w, or 1's
-__device__ __forceinline__ uint32_t byte_or_one(uint32_t w, int s, bool ok) { return ok ? (w >> (8 * s)) & 255u : kOne; }
-
 constexpr int kFewThreads = 256;
 constexpr int kFewWaves = kFewThreads / 64;
 // Up to kStep blocks of a lane, of kTiles weight rows: codes and scale bytes.
 // Lane l holds weight row and row of x l % 16.  Which blocks a lane takes is
 // free as long as both operands agree: the matrix instruction's sum goes by lane
 // and place, whatever the blocks' order in K.  Here a lane's blocks follow one
-// another, so that its loads share cache lines and its scales a word.
-template <int kTiles, int kStep>
+// another, so that its loads share cache lines and its scales a word.  kTiny:
+// fewer scales than a word's in all.
+template <int kTiles, int kStep, bool kTiny>
 struct WeightBlocks {
   u32x4 codes[kTiles][kStep];
   uint32_t scales[kTiles];
+  int shift[kTiles];
   // blocks b .. b + kStep - 1, those from b1 on not used
   __device__ __forceinline__ void load(const ProductArgs& a, const int64_t* row, int b, int b1) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      scales[t] = scales4(a.scales, row[t] * a.nb + min(b, a.nb - 1), a.blocks);
+      const int first = min(b, a.nb - 1);
+      if constexpr (kTiny) {
+        const uint8_t* p = a.scales + row[t] * a.nb;
+        scales[t] = 0, shift[t] = 0;
+        for (int s = 0; s < 4 && first + s < a.nb; ++s) scales[t] |= static_cast<uint32_t>(p[first + s]) << (8 * s);
+      } else {
+        const ScaleRow r(a.scales, row[t], a.nb, a.blocks);
+        scales[t] = r.load(first);
+        shift[t] = 8 * (first - min(first, r.last));
+      }
 #pragma unroll
       for (int s = 0; s < kStep; ++s)
         codes[t][s] = reinterpret_cast<const u32x4*>(a.codes)[row[t] * a.nb + (b + s < b1 ? b + s : 0)];
     }
   }
   template <int X>
-  __device__ __forceinline__ void products(const ProductArgs& a, int64_t x_row, bool x_ok, int b, int b1, f32x4* acc) const {
+  __device__ __forceinline__ void products(const XBlocks<X, kStep>& x, int b, int b1, f32x4* acc) const {
 #pragma unroll
-    for (int s = 0; s < kStep; ++s) {
-      const bool ok = b + s < b1;
-      u32x4 v[4];
-      uint32_t byte;
-      x_block<X>(a, x_row, b + s, ok && x_ok, v, &byte);
+    for (int t = 0; t < kTiles; ++t) {
+      const uint32_t word = scales[t] >> shift[t];
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        const uint32_t wb = byte_or_one(scales[t], s, ok);
+      for (int s = 0; s < kStep; ++s) {
+        const uint32_t byte = b + s < b1 ? (word >> (8 * s)) & 255u : kOne;
         if constexpr (X == kXBf16) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) acc[t] = mfma_bf16(cvt8(codes[t][s][q], scale_of(wb)), v[q], acc[t]);
+          for (int q = 0; q < 4; ++q) acc[t] = mfma_bf16(cvt8(codes[t][s][q], scale_of(byte)), x.v[s][q], acc[t]);
         } else {
-          acc[t] = mfma_mx4<0>(codes[t][s], wb, v[0], byte, acc[t]);
+          acc[t] = mfma_mx4<0>(codes[t][s], byte, x.v[s][0], x.byte[s], acc[t]);
         }
       }
     }
@@ -254,14 +279,16 @@ __device__ __forceinline__ int find_pairs(const ProductArgs& a, Ids ids, int gro
   return seen;
 }
 
-// A workgroup takes 16 * NT outputs (of both matrices for SwiGLU) of one group
-// for 16 of its rows at a time; its waves share K, kStep blocks of a lane at a
-// time.  The first weights are on their way before the rows are known; the ids
-// that tell them go before the weights, since loads return in order.
-template <int X, bool kSwiglu, int NT, int kStep, typename Out, int kRows>
+// A workgroup takes a.run tiles of 16 * NT outputs (of both matrices for SwiGLU)
+// of one group, for 16 of its rows at a time; its waves share K, kStep blocks of
+// a lane at a time.  A tile's weights are on their way while the one before is
+// multiplied, the first one's before the rows are known; the ids that tell them
+// go before the weights, since loads return in order.  kHold: K is one step, and
+// x stays in registers over the tiles.
+template <int X, bool kSwiglu, int NT, int kStep, bool kHold, bool kTiny, typename Out, int kRows>
 __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
   constexpr int kTiles = kSwiglu ? 2 * NT : NT;
-  __shared__ f32x4 s_part[kFewWaves][kTiles][64];
+  __shared__ f32x4 s_part[2][kFewWaves][kTiles][64];
   __shared__ int s_rows[kFewWaves][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, l16 = lane & 15;
   int* s_row = s_rows[wave];
@@ -281,13 +308,18 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
   }
   const int per = (a.nb + 4 * kFewWaves - 1) / (4 * kFewWaves);
   const int b0 = (wave * 4 + g) * per, b1 = min(b0 + per, a.nb);
-  const int f0 = blockIdx.x * 16 * NT;
-  int64_t row[kTiles];
+  const int tiles = (a.N + 16 * NT - 1) / (16 * NT);
+  const int from = static_cast<int>(blockIdx.x) * a.run, to = min(from + a.run, tiles);
+  const int64_t first_row = static_cast<int64_t>(group) * (kSwiglu ? 2 : 1) * a.N;
+  using Weights = WeightBlocks<kTiles, kStep, kTiny>;
+  const auto load = [&](Weights& w, int tile, int s0) {
+    int64_t row[kTiles];
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t)
-    row[t] = (static_cast<int64_t>(group) * (kSwiglu ? 2 : 1) + t / NT) * a.N + min(f0 + 16 * (t % NT) + l16, a.N - 1);
-  WeightBlocks<kTiles, kStep> w;
-  w.load(a, row, b0, b1);
+    for (int t = 0; t < kTiles; ++t) row[t] = first_row + t / NT * a.N + min((tile * NT + t % NT) * 16 + l16, a.N - 1);
+    w.load(a, row, b0 + s0, b1);
+  };
+  Weights even, odd;
+  load(even, from, 0);
   for (int r0 = 0;; r0 += 16) {
     if constexpr (kRows == kRowsIds) {
       int first;
@@ -298,46 +330,62 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
     const bool x_ok = r0 + l16 < count;
     int64_t x_row = 0;
     if (x_ok) x_row = kRows == kRowsIds ? s_row[l16] / a.xdiv : begin + r0 + l16;
-    f32x4 acc[kTiles];
+    XBlocks<X, kStep> x;
+    if (kHold) x.load(a, x_row, x_ok, b0, b1);
+    const auto take = [&](Weights& w, Weights& next, int tile) {
+      if (tile + 1 < to) load(next, tile + 1, 0);
+      f32x4 acc[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < per; s0 += kStep) {
-      if (s0 > 0 || (r0 > 0 && per > kStep)) w.load(a, row, b0 + s0, b1);
-      w.template products<X>(a, x_row, x_ok, b0 + s0, b1, acc);
-    }
-    // outputs 4g .. 4g+3 of row l16
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) s_part[wave][t][l16 * 4 + g] = acc[t];
-    __syncthreads();
-    for (int j = tid; j < 64 * NT; j += kFewThreads) {
-      const int i = j / (4 * NT), q = j % (4 * NT), t = q / 4, at = i * 4 + q % 4;  // row i, four outputs
-      f32x4 y = s_part[0][t][at];
-#pragma unroll
-      for (int v = 1; v < kFewWaves; ++v) y += s_part[v][t][at];
-      if constexpr (kSwiglu) {
-        f32x4 u = s_part[0][NT + t][at];
-#pragma unroll
-        for (int v = 1; v < kFewWaves; ++v) u += s_part[v][NT + t][at];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
-      }
-      const int f = f0 + 4 * q;
-      if (r0 + i >= count || f >= a.N) continue;
-      const int64_t to = kRows == kRowsIds ? s_row[i] : begin + r0 + i;
-      Out* out = static_cast<Out*>(a.out) + to * a.out_stride + f;
-      if (a.wide_out && f + 4 <= a.N) {
-        if constexpr (std::is_same<Out, float>::value)
-          *reinterpret_cast<f32x4*>(out) = y;
-        else
-          *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+      for (int t = 0; t < kTiles; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (kHold) {
+        w.template products<X>(x, b0, b1, acc);
       } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (f + e < a.N) out[e] = static_cast<Out>(y[e]);
+        for (int s0 = 0; s0 < per; s0 += kStep) {
+          if (s0 > 0) load(w, tile, s0);
+          x.load(a, x_row, x_ok, b0 + s0, b1);
+          w.template products<X>(x, b0 + s0, b1, acc);
+        }
       }
+      // outputs 4g .. 4g+3 of row l16
+      const auto part = s_part[tile & 1];
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) part[wave][t][l16 * 4 + g] = acc[t];
+      lds_barrier();
+      for (int j = tid; j < 64 * NT; j += kFewThreads) {
+        const int i = j / (4 * NT), q = j % (4 * NT), t = q / 4, at = i * 4 + q % 4;  // row i, four outputs
+        f32x4 y = part[0][t][at];
+#pragma unroll
+        for (int v = 1; v < kFewWaves; ++v) y += part[v][t][at];
+        if constexpr (kSwiglu) {
+          f32x4 u = part[0][NT + t][at];
+#pragma unroll
+          for (int v = 1; v < kFewWaves; ++v) u += part[v][NT + t][at];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = swiglu(y[e], u[e]);
+        }
+        const int f = tile * 16 * NT + 4 * q;
+        if (r0 + i >= count || f >= a.N) continue;
+        const int64_t row = kRows == kRowsIds ? s_row[i] : begin + r0 + i;
+        Out* out = static_cast<Out*>(a.out) + row * a.out_stride + f;
+        if (a.wide_out && f + 4 <= a.N) {
+          if constexpr (std::is_same<Out, float>::value)
+            *reinterpret_cast<f32x4*>(out) = y;
+          else
+            *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (f + e < a.N) out[e] = static_cast<Out>(y[e]);
+        }
+      }
+    };
+    for (int tile = from; tile < to; tile += 2) {
+      take(even, odd, tile);
+      if (tile + 1 < to) take(odd, even, tile + 1);
     }
     if (r0 + 16 >= count) return;
-    __syncthreads();
+    load(even, from, 0);
+    lds_barrier();
   }
 }
 
@@ -371,10 +419,12 @@ __global__ __launch_bounds__(kLastThreads) void mx4_last_kernel(LastArgs a) {
     const int64_t row = static_cast<int64_t>(e) * a.p.N + min(f0 + l16, a.p.N - 1);
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     constexpr int kStep = 3;
-    WeightBlocks<1, kStep> w;
+    WeightBlocks<1, kStep, false> w;
+    XBlocks<X, kStep> x;
     for (int s0 = 0; s0 < per; s0 += kStep) {
       w.load(a.p, &row, b0 + s0, b1);
-      w.template products<X>(a.p, pair, l16 == 0, b0 + s0, b1, &acc);
+      x.load(a.p, pair, l16 == 0, b0 + s0, b1);
+      w.template products<X>(x, b0 + s0, b1, &acc);
     }
     sum += gate * acc;
   }
@@ -411,31 +461,6 @@ template <int kPieces>
 __device__ __forceinline__ int swizzled(int row, int c) {
   return c ^ ((row / (8 / kPieces)) % kPieces);
 }
-
-// A row's scale bytes, four blocks at a time, read whole and in bounds: near the
-// end of all scales (at least four) the word starts earlier.
-struct ScaleRow {
-  const uint8_t* p;
-  int last;  // the last block at which a word may start
-  __device__ __forceinline__ ScaleRow(const uint8_t* scales, int64_t row, int nb, int64_t total) {
-    p = scales + row * nb;
-    last = static_cast<int>(min(total - 4 - row * nb, int64_t{1} << 20));
-  }
-  __device__ __forceinline__ uint32_t load(int b) const {
-    uint32_t w;
-    __builtin_memcpy(&w, p + min(b, last), 4);
-    return w;
-  }
-  // kBlocks bytes from block b on of what load(b) gave; 1 past the row's end
-  template <int kBlocks>
-  __device__ __forceinline__ uint32_t bytes(uint32_t w, int b, int nb) const {
-    w >>= 8 * (b - min(b, last));
-#pragma unroll
-    for (int j = 1; j < kBlocks; ++j)
-      if (b + j >= nb) w = (w & ~(255u << (8 * j))) | static_cast<uint32_t>(kOne) << (8 * j);
-    return w;
-  }
-};
 
 template <int SEL>
 __device__ __forceinline__ f32x16 mfma_mx4_32(u32x4 w, uint32_t w_scales, u32x4 x, uint32_t x_scales, f32x16 c) {
@@ -506,10 +531,6 @@ __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt((kLeft & 15) | 0x0f70 | (kLeft >> 4) << 14);
   __builtin_amdgcn_sched_barrier(0);
 }
-
-// A barrier for LDS reads and writes that leaves loads into LDS on their way:
-// __syncthreads() would wait for them.
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // A workgroup takes 256 weight rows (128 outputs of both matrices for SwiGLU)
 // and 32 * CT rows of one group; K goes through LDS in three buffers, loaded two
@@ -881,23 +902,35 @@ int few_outputs(const ProductArgs& a, int64_t groups, bool swiglu, int step) {
   return 1;
 }
 
+constexpr int kRunGroups = 768;  // workgroups that are resident together, about
+
+template <int X, bool kSwiglu, int NT, int kStep, typename Out, int kRows>
+hipError_t launch_few(ProductArgs a, int64_t groups, bool hold, hipStream_t st) {
+  const int tiles = (a.N + 16 * NT - 1) / (16 * NT);
+  a.run = static_cast<int>(std::min<int64_t>(std::max<int64_t>(groups * tiles / kRunGroups, 1), 8));
+  auto kernel = hold ? mx4_few_kernel<X, kSwiglu, NT, kStep, true, false, Out, kRows>
+                     : mx4_few_kernel<X, kSwiglu, NT, kStep, false, false, Out, kRows>;
+  if constexpr (kRows == kRowsStart && NT == 1 && kStep == 2)
+    if (a.blocks < 4) kernel = mx4_few_kernel<X, kSwiglu, NT, kStep, true, true, Out, kRows>;
+  return launch2(kernel, static_cast<unsigned>((tiles + a.run - 1) / a.run), static_cast<unsigned>(groups), kFewThreads, a, st);
+}
+
 template <int X, bool kSwiglu, int NT, typename Out, int kRows>
-hipError_t launch_few(const ProductArgs& a, int64_t groups, int step, hipStream_t st) {
-  const auto kernel = step == 4   ? mx4_few_kernel<X, kSwiglu, NT, 4, Out, kRows>
-                      : step == 3 ? mx4_few_kernel<X, kSwiglu, NT, 3, Out, kRows>
-                                  : mx4_few_kernel<X, kSwiglu, NT, 2, Out, kRows>;
-  return launch2(kernel, static_cast<unsigned>((a.N + 16 * NT - 1) / (16 * NT)), static_cast<unsigned>(groups), kFewThreads,
-                 a, st);
+hipError_t launch_few(const ProductArgs& a, int64_t groups, int step, bool hold, hipStream_t st) {
+  return step == 4   ? launch_few<X, kSwiglu, NT, 4, Out, kRows>(a, groups, hold, st)
+         : step == 3 ? launch_few<X, kSwiglu, NT, 3, Out, kRows>(a, groups, hold, st)
+                     : launch_few<X, kSwiglu, NT, 2, Out, kRows>(a, groups, hold, st);
 }
 
 template <int X, bool kSwiglu, typename Out, int kRows>
 hipError_t launch_few(ProductArgs a, int64_t groups, hipStream_t st) {
   a.wide_out = wide_rows(a.out, a.out_stride, sizeof(Out));
-  const int step = few_step((a.nb + 4 * kFewWaves - 1) / (4 * kFewWaves)), nt = few_outputs(a, groups, kSwiglu, step);
+  const int per = (a.nb + 4 * kFewWaves - 1) / (4 * kFewWaves);
+  const int step = few_step(per), nt = few_outputs(a, groups, kSwiglu, step);
   if constexpr (!kSwiglu)
-    if (nt == 4) return launch_few<X, kSwiglu, 4, Out, kRows>(a, groups, step, st);
-  return nt == 2 ? launch_few<X, kSwiglu, 2, Out, kRows>(a, groups, step, st)
-                 : launch_few<X, kSwiglu, 1, Out, kRows>(a, groups, step, st);
+    if (nt == 4) return launch_few<X, kSwiglu, 4, Out, kRows>(a, groups, step, per <= step, st);
+  return nt == 2 ? launch_few<X, kSwiglu, 2, Out, kRows>(a, groups, step, per <= step, st)
+                 : launch_few<X, kSwiglu, 1, Out, kRows>(a, groups, step, per <= step, st);
 }
 
 template <int X, bool kSwiglu, typename Out, int CT>
