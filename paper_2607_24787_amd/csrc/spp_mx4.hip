@@ -159,15 +159,15 @@ struct XBlocks {
   static constexpr int kParts = X == kXBf16 ? 4 : 1;
   u32x4 v[kStep][kParts];
   uint32_t byte[kStep];
-  // blocks b .. b + kStep - 1, zeros from b1 on, or for no row
-  __device__ __forceinline__ void load(const ProductArgs& a, int64_t row, bool have, int b, int b1) {
+  // blocks b .. b + kStep - 1, zeros outside [b0, b1) or for no row
+  __device__ __forceinline__ void load(const ProductArgs& a, int64_t row, bool have, int b, int b0, int b1) {
     const uint8_t* p = static_cast<const uint8_t*>(a.x) + row * a.x_stride;
 #pragma unroll
     for (int s = 0; s < kStep; ++s) {
       byte[s] = kOne;
 #pragma unroll
       for (int q = 0; q < kParts; ++q) v[s][q] = u32x4{0, 0, 0, 0};
-      if (!have || b + s >= b1) continue;
+      if (!have || b + s < b0 || b + s >= b1) continue;
       if constexpr (X == kXCodes) {
         v[s][0] = reinterpret_cast<const u32x4*>(p)[b + s];
         byte[s] = a.x_scales[row * a.nb + b + s];
@@ -200,39 +200,42 @@ constexpr int kFewWaves = kFewThreads / 64;
 // free as long as both operands agree: the matrix instruction's sum goes by lane
 // and place, whatever the blocks' order in K.  Here a lane's blocks follow one
 // another, so that its loads share cache lines and its scales a word.  kTiny:
-// fewer scales than a word's in all.
+// rows of fewer blocks, or fewer scales than a word's in all.
 template <int kTiles, int kStep, bool kTiny>
 struct WeightBlocks {
   u32x4 codes[kTiles][kStep];
   uint32_t scales[kTiles];
   int shift[kTiles];
-  // blocks b .. b + kStep - 1, those from b1 on not used
-  __device__ __forceinline__ void load(const ProductArgs& a, const int64_t* row, int b, int b1) {
+  // The first of kStep blocks that are in the row, from block b on
+  static __device__ __forceinline__ int window(const ProductArgs& a, int b) { return max(min(b, a.nb - kStep), 0); }
+  // blocks b .. b + kStep - 1 of a window
+  __device__ __forceinline__ void load(const ProductArgs& a, const int64_t* row, int b) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const int first = min(b, a.nb - 1);
       if constexpr (kTiny) {
         const uint8_t* p = a.scales + row[t] * a.nb;
         scales[t] = 0, shift[t] = 0;
-        for (int s = 0; s < 4 && first + s < a.nb; ++s) scales[t] |= static_cast<uint32_t>(p[first + s]) << (8 * s);
+        for (int s = 0; s < kStep && b + s < a.nb; ++s) scales[t] |= static_cast<uint32_t>(p[b + s]) << (8 * s);
       } else {
         const ScaleRow r(a.scales, row[t], a.nb, a.blocks);
-        scales[t] = r.load(first);
-        shift[t] = 8 * (first - min(first, r.last));
+        scales[t] = r.load(b);
+        shift[t] = 8 * (b - min(b, r.last));
       }
+      const u32x4* p = reinterpret_cast<const u32x4*>(a.codes) + row[t] * a.nb + b;
 #pragma unroll
-      for (int s = 0; s < kStep; ++s)
-        codes[t][s] = reinterpret_cast<const u32x4*>(a.codes)[row[t] * a.nb + (b + s < b1 ? b + s : 0)];
+      for (int s = 0; s < kStep; ++s) codes[t][s] = p[kTiny && b + s >= a.nb ? 0 : s];
     }
   }
+  // those in [b0, b1)
   template <int X>
-  __device__ __forceinline__ void products(const XBlocks<X, kStep>& x, int b, int b1, f32x4* acc) const {
+  __device__ __forceinline__ void products(const XBlocks<X, kStep>& x, int b, int b0, int b1, f32x4* acc) const {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       const uint32_t word = scales[t] >> shift[t];
 #pragma unroll
       for (int s = 0; s < kStep; ++s) {
-        const uint32_t byte = b + s < b1 ? (word >> (8 * s)) & 255u : kOne;
+        // what is not to be added: x is zero there, and the scale must be none that makes NaN
+        const uint32_t byte = b + s >= b0 && b + s < b1 ? (word >> (8 * s)) & 255u : kOne;
         if constexpr (X == kXBf16) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) acc[t] = mfma_bf16(cvt8(codes[t][s][q], scale_of(byte)), x.v[s][q], acc[t]);
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
     int64_t row[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) row[t] = first_row + t / NT * a.N + min((tile * NT + t % NT) * 16 + l16, a.N - 1);
-    w.load(a, row, b0 + s0, b1);
+    w.load(a, row, Weights::window(a, b0 + s0));
   };
   Weights even, odd;
   load(even, from, 0);
@@ -331,19 +334,20 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
     int64_t x_row = 0;
     if (x_ok) x_row = kRows == kRowsIds ? s_row[l16] / a.xdiv : begin + r0 + l16;
     XBlocks<X, kStep> x;
-    if (kHold) x.load(a, x_row, x_ok, b0, b1);
+    if (kHold) x.load(a, x_row, x_ok, Weights::window(a, b0), b0, b1);
     const auto take = [&](Weights& w, Weights& next, int tile) {
       if (tile + 1 < to) load(next, tile + 1, 0);
       f32x4 acc[kTiles];
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
       if constexpr (kHold) {
-        w.template products<X>(x, b0, b1, acc);
+        w.template products<X>(x, Weights::window(a, b0), b0, b1, acc);
       } else {
         for (int s0 = 0; s0 < per; s0 += kStep) {
           if (s0 > 0) load(w, tile, s0);
-          x.load(a, x_row, x_ok, b0 + s0, b1);
-          w.template products<X>(x, b0 + s0, b1, acc);
+          const int b = Weights::window(a, b0 + s0);
+          x.load(a, x_row, x_ok, b, b0 + s0, b1);
+          w.template products<X>(x, b, b0 + s0, b1, acc);
         }
       }
       // outputs 4g .. 4g+3 of row l16
@@ -403,7 +407,7 @@ struct LastArgs {
 constexpr int kLastThreads = 512;
 constexpr int kLastWaves = kLastThreads / 64;
 
-template <int X>
+template <int X, int kStep, bool kTiny>
 __global__ __launch_bounds__(kLastThreads) void mx4_last_kernel(LastArgs a) {
   __shared__ f32x4 s_part[kLastWaves][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, l16 = lane & 15;
@@ -418,13 +422,13 @@ __global__ __launch_bounds__(kLastThreads) void mx4_last_kernel(LastArgs a) {
     const int b0 = (i % parts * 4 + g) * per, b1 = min(b0 + per, a.p.nb);
     const int64_t row = static_cast<int64_t>(e) * a.p.N + min(f0 + l16, a.p.N - 1);
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    constexpr int kStep = 3;
-    WeightBlocks<1, kStep, false> w;
+    WeightBlocks<1, kStep, kTiny> w;
     XBlocks<X, kStep> x;
     for (int s0 = 0; s0 < per; s0 += kStep) {
-      w.load(a.p, &row, b0 + s0, b1);
-      x.load(a.p, pair, l16 == 0, b0 + s0, b1);
-      w.template products<X>(x, b0 + s0, b1, &acc);
+      const int b = WeightBlocks<1, kStep, kTiny>::window(a.p, b0 + s0);
+      w.load(a.p, &row, b);
+      x.load(a.p, pair, l16 == 0, b, b0 + s0, b1);
+      w.template products<X>(x, b, b0 + s0, b1, &acc);
     }
     sum += gate * acc;
   }
@@ -902,16 +906,16 @@ int few_outputs(const ProductArgs& a, int64_t groups, bool swiglu, int step) {
   return 1;
 }
 
-constexpr int kRunGroups = 768;  // workgroups that are resident together, about
+constexpr int kRunGroups = 512;  // workgroups that are resident together, about
 
 template <int X, bool kSwiglu, int NT, int kStep, typename Out, int kRows>
 hipError_t launch_few(ProductArgs a, int64_t groups, bool hold, hipStream_t st) {
   const int tiles = (a.N + 16 * NT - 1) / (16 * NT);
-  a.run = static_cast<int>(std::min<int64_t>(std::max<int64_t>(groups * tiles / kRunGroups, 1), 8));
+  a.run = static_cast<int>(std::min<int64_t>((groups * tiles + kRunGroups - 1) / kRunGroups, 16));
   auto kernel = hold ? mx4_few_kernel<X, kSwiglu, NT, kStep, true, false, Out, kRows>
                      : mx4_few_kernel<X, kSwiglu, NT, kStep, false, false, Out, kRows>;
-  if constexpr (kRows == kRowsStart && NT == 1 && kStep == 2)
-    if (a.blocks < 4) kernel = mx4_few_kernel<X, kSwiglu, NT, kStep, true, true, Out, kRows>;
+  if constexpr (NT == 1 && kStep == 2)
+    if (a.nb < kStep || a.blocks < 4) kernel = mx4_few_kernel<X, kSwiglu, NT, kStep, true, true, Out, kRows>;
   return launch2(kernel, static_cast<unsigned>((tiles + a.run - 1) / a.run), static_cast<unsigned>(groups), kFewThreads, a, st);
 }
 
@@ -926,7 +930,8 @@ template <int X, bool kSwiglu, typename Out, int kRows>
 hipError_t launch_few(ProductArgs a, int64_t groups, hipStream_t st) {
   a.wide_out = wide_rows(a.out, a.out_stride, sizeof(Out));
   const int per = (a.nb + 4 * kFewWaves - 1) / (4 * kFewWaves);
-  const int step = few_step(per), nt = few_outputs(a, groups, kSwiglu, step);
+  const bool tiny = a.nb < 4 || a.blocks < 4;
+  const int step = tiny ? 2 : few_step(per), nt = tiny ? 1 : few_outputs(a, groups, kSwiglu, step);
   if constexpr (!kSwiglu)
     if (nt == 4) return launch_few<X, kSwiglu, 4, Out, kRows>(a, groups, step, per <= step, st);
   return nt == 2 ? launch_few<X, kSwiglu, 2, Out, kRows>(a, groups, step, per <= step, st)
@@ -1205,7 +1210,9 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
     l.residual_stride = residual_stride;
     l.K = K;
     void* params[] = {&l};
-    const void* kernel = reinterpret_cast<const void*>(mx4 ? mx4_last_kernel<kXQuantF32> : mx4_last_kernel<kXBf16>);
+    const auto last = d.nb < 3 ? (mx4 ? mx4_last_kernel<kXQuantF32, 1, true> : mx4_last_kernel<kXBf16, 1, true>)
+                               : (mx4 ? mx4_last_kernel<kXQuantF32, 3, false> : mx4_last_kernel<kXBf16, 3, false>);
+    const void* kernel = reinterpret_cast<const void*>(last);
     return launched(hipLaunchKernel(kernel, dim3(static_cast<unsigned>((D + 15) / 16), static_cast<unsigned>(T)),
                                     dim3(kLastThreads), params, 0, st));
   }
