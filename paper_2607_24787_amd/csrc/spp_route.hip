@@ -63,7 +63,143 @@ __device__ __forceinline__ void take_run(const SortArgs& a, int* row, int from, 
   }
 }
 
-// Pairs of each expert in each part, for sorts of several parts
+// Starts of the experts from their pairs (thread e: expert e; n is at most the
+// threads), and all pairs
+__device__ __forceinline__ int starts_of(int all, int* s_sum, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int incl = all;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(incl, d);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 63) s_sum[wave] = incl;
+  __syncthreads();
+  int base = incl - all;
+  *total = 0;
+  for (int w = 0; w < kSortWaves; ++w) {
+    base += w < wave ? s_sum[w] : 0;
+    *total += s_sum[w];
+  }
+  return base;
+}
+
+constexpr int kCountedPairs = 1 << 14;  // sorts that count all pairs in every part
+constexpr int kHeldPairs = 1 << 18;     // sorts whose parts are held in registers
+constexpr int kHeld = 4;                // pairs of a thread
+
+// A stable counting sort: a workgroup places kEach * 1024 pairs, which it holds
+// in registers.  The others it counts by itself (at most 2^14: a launch that
+// would count them costs more than the reads), or finds counted (kCounted).  A
+// wave takes its run of pairs in order and only it writes its row of counts, so
+// a pair's rank does not depend on which lane comes first.
+template <int kEach, bool kCounted>
+__global__ __launch_bounds__(kSortThreads) void expert_sort_once_kernel(SortArgs a) {
+  extern __shared__ int s_row[];  // [kSortWaves][n], then pairs before this part and behind it [2][n]
+  __shared__ int s_sum[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int part = static_cast<int>(blockIdx.x) * kEach * kSortThreads, from = part + wave * 64 * kEach;
+  int id[kEach], rank[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) id[j] = id_at(a, from + 64 * j + lane, a.P);
+  constexpr int kMost = kCounted ? 1 : kCountedPairs / kSortThreads;
+  int e[kMost];  // pairs of other parts
+  if constexpr (!kCounted) {
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+      const int p = j * kSortThreads + tid;
+      e[j] = gridDim.x == 1 || (p >= part && p < part + kEach * kSortThreads) ? -1 : id_at(a, p, a.P);
+    }
+  }
+  for (int i = tid; i < (kSortWaves + 2) * a.n; i += kSortThreads) s_row[i] = 0;
+  __syncthreads();
+  int* row = s_row + wave * a.n;
+  int* other = s_row + kSortWaves * a.n;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const uint64_t same = alike(id[j], a.bits);
+    const int before = __popcll(same & ((uint64_t{1} << lane) - 1));
+    const int base = id[j] >= 0 ? row[id[j]] : 0;
+    rank[j] = base + before;
+    __builtin_amdgcn_wave_barrier();
+    if (id[j] >= 0 && before == 0) row[id[j]] = base + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+  // counts alone: their order does not matter
+  if constexpr (!kCounted) {
+#pragma unroll
+    for (int j = 0; j < kMost; ++j)
+      if (e[j] >= 0) atomicAdd(other + (j * kSortThreads + tid < part ? 0 : a.n) + e[j], 1);
+  }
+  __syncthreads();
+  int all = 0, mine = 0, of_wave[kSortWaves];
+  if (tid < a.n) {
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) of_wave[w] = s_row[w * a.n + tid];
+    if constexpr (kCounted) {
+      constexpr int kBatch = 8;
+      for (int k0 = 0; k0 < a.parts; k0 += kBatch) {
+        int c[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) c[k] = k0 + k < a.parts ? a.total[(k0 + k) * a.n + tid] : 0;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          all += c[k];
+          mine += k0 + k < static_cast<int>(blockIdx.x) ? c[k] : 0;
+        }
+      }
+    } else {
+      mine = other[tid];
+      all = mine + other[a.n + tid];
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) all += of_wave[w];
+    }
+  }
+  int total;
+  const int base = starts_of(all, s_sum, &total);
+  if (tid < a.n) {
+    if (blockIdx.x == 0) {
+      a.start[tid] = base;
+      if (tid == a.n - 1) a.start[a.n] = total;
+    }
+    int at = base + mine;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      s_row[w * a.n + tid] = at;
+      at += of_wave[w];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int p = from + 64 * j + lane;
+    const int at = id[j] >= 0 ? row[id[j]] + rank[j] : -1;
+    if (p < a.P) a.place[p] = at;
+    if (id[j] >= 0) a.pair[at] = p;
+  }
+  // the places of pairs without an expert name no pair
+  for (int i = total + static_cast<int>(blockIdx.x) * kSortThreads + tid; i < a.P;
+       i += static_cast<int>(gridDim.x) * kSortThreads)
+    a.pair[i] = -1;
+}
+
+// Pairs of each expert in each part of kHeld * 1024 pairs; counts alone
+__global__ __launch_bounds__(kSortThreads) void expert_count_held_kernel(SortArgs a) {
+  extern __shared__ int s_row[];  // [n]
+  const int tid = threadIdx.x, part = static_cast<int>(blockIdx.x) * kHeld * kSortThreads;
+  int id[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) id[j] = id_at(a, part + j * kSortThreads + tid, a.P);
+  for (int i = tid; i < a.n; i += kSortThreads) s_row[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (id[j] >= 0) atomicAdd(s_row + id[j], 1);
+  __syncthreads();
+  if (tid < a.n) a.total[blockIdx.x * a.n + tid] = s_row[tid];
+}
+
+// Pairs of each expert in each part, for larger sorts
 __global__ __launch_bounds__(kSortThreads) void expert_count_kernel(SortArgs a) {
   extern __shared__ int s_row[];  // [kSortWaves][n]
   const int wave = threadIdx.x >> 6, run = a.each / kSortWaves;
@@ -80,13 +216,13 @@ __global__ __launch_bounds__(kSortThreads) void expert_count_kernel(SortArgs a) 
   }
 }
 
-// A stable counting sort.  A wave counts its run of pairs by expert; the counts
+// A stable counting sort of more pairs.  A wave counts its run of pairs by expert; the counts
 // become starts (experts before, parts before, waves before); the wave goes
 // through its run again and gives every pair its place.
 __global__ __launch_bounds__(kSortThreads) void expert_sort_kernel(SortArgs a) {
   extern __shared__ int s_row[];  // [kSortWaves][n]
   __shared__ int s_sum[kSortWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, run = a.each / kSortWaves;
+  const int tid = threadIdx.x, wave = tid >> 6, run = a.each / kSortWaves;
   for (int i = tid; i < kSortWaves * a.n; i += kSortThreads) s_row[i] = 0;
   __syncthreads();
   const int64_t from64 = static_cast<int64_t>(blockIdx.x) * a.each + wave * run;
@@ -108,19 +244,8 @@ __global__ __launch_bounds__(kSortThreads) void expert_sort_kernel(SortArgs a) {
       }
     }
   }
-  int incl = all;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(incl, d);
-    if (lane >= d) incl += o;
-  }
-  if (lane == 63) s_sum[wave] = incl;
-  __syncthreads();
-  int base = incl - all, total = 0;
-  for (int w = 0; w < kSortWaves; ++w) {
-    base += w < wave ? s_sum[w] : 0;
-    total += s_sum[w];
-  }
+  int total;
+  const int base = starts_of(all, s_sum, &total);
   if (tid < a.n) {
     if (blockIdx.x == 0) {
       a.start[tid] = base;
@@ -209,6 +334,8 @@ struct RowOf {
   }
 };
 
+constexpr int kRowBatch = 8;  // rows whose loads are in flight together
+
 // A token's row is read once and written to its pairs' places.
 __global__ __launch_bounds__(kRowThreads) void expert_gather_kernel(RowArgs a) {
   const RowOf r(a);
@@ -218,14 +345,16 @@ __global__ __launch_bounds__(kRowThreads) void expert_gather_kernel(RowArgs a) {
   const u32x4* from = row_at(a.x, a.x_stride, r.t);
   for (int i = r.first; i < a.pieces; i += r.step) {
     const u32x4 v = from[i];
-    for (int k = 0; k < a.K; ++k) {
-      const int at = place[k];
-      if (static_cast<unsigned>(at) < static_cast<unsigned>(P)) row_at(a.out, a.out_stride, at)[i] = v;
+    for (int k0 = 0; k0 < a.K; k0 += kRowBatch) {
+      int at[kRowBatch];
+#pragma unroll
+      for (int k = 0; k < kRowBatch; ++k) at[k] = k0 + k < a.K ? place[k0 + k] : -1;
+#pragma unroll
+      for (int k = 0; k < kRowBatch; ++k)
+        if (static_cast<unsigned>(at[k]) < static_cast<unsigned>(P)) row_at(a.out, a.out_stride, at[k])[i] = v;
     }
   }
 }
-
-constexpr int kRowBatch = 8;  // rows whose loads are in flight together
 
 // Where pair p's row is; negative or too large: nowhere
 __device__ __forceinline__ int place_of(const RowArgs& a, int64_t p) {
@@ -257,7 +386,7 @@ __global__ __launch_bounds__(kRowThreads) void expert_combine_kernel(RowArgs a) 
         have[k] = static_cast<unsigned>(at) < static_cast<unsigned>(P);
 #pragma unroll
         for (int q = 0; q < Q; ++q)
-          if (have[k]) v[k][q] = row_at(a.x, a.x_stride, at)[i * Q + q];
+          if (have[k]) v[k][q] = __builtin_nontemporal_load(row_at(a.x, a.x_stride, at) + i * Q + q);
         if constexpr (kWeights) w[k] = have[k] ? a.weight[p0 + k0 + k] : 0.f;
       }
 #pragma unroll
@@ -305,7 +434,7 @@ __global__ __launch_bounds__(kRowThreads) void expert_combine_grad_kernel(RowArg
       float f[E], g[E];
       widen<T>(d[i], f);
       if (a.d_weight) {
-        widen<T>(y[i], g);
+        widen<T>(__builtin_nontemporal_load(y + i), g);
 #pragma unroll
         for (int j = 0; j < E; ++j) dot = fmaf(f[j], g[j], dot);
       }
@@ -331,7 +460,7 @@ const char* pairs_why(int32_t T, int32_t K) {
 }
 
 // Parts of a sort at most
-int64_t most_parts(int64_t P) { return std::min<int64_t>(kMaxParts, std::max<int64_t>(1, P / kMinPart)); }
+int64_t most_parts(int64_t P) { return std::min<int64_t>(kMaxParts, std::max<int64_t>(1, (P + kMinPart - 1) / kMinPart)); }
 
 // Parts of a sort, and pairs of one
 void parts_of(int64_t P, int* parts, int* each) {
@@ -392,9 +521,24 @@ hipError_t launch_expert_sort(const int32_t* topk, int64_t P, int32_t n, int32_t
   a.P = static_cast<int>(P);
   a.n = n;
   while (1 << a.bits < n) ++a.bits;
+  void* params[] = {&a};
+  if (P <= kHeldPairs) {
+    const int each = (P <= kSortThreads ? 1 : kHeld) * kSortThreads;
+    a.parts = static_cast<int>(std::max<int64_t>(1, (P + each - 1) / each));
+    const bool counted = P > kCountedPairs;
+    if (counted) {
+      const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(expert_count_held_kernel), dim3(a.parts),
+                                           dim3(kSortThreads), params, static_cast<unsigned>(n * sizeof(int)), st);
+      if (e != hipSuccess) return e;
+    }
+    const auto kernel = counted               ? expert_sort_once_kernel<kHeld, true>
+                        : P <= kSortThreads ? expert_sort_once_kernel<1, false>
+                                            : expert_sort_once_kernel<kHeld, false>;
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(a.parts), dim3(kSortThreads), params,
+                           static_cast<unsigned>((kSortWaves + 2) * n * sizeof(int)), st);
+  }
   parts_of(P, &a.parts, &a.each);
   const unsigned lds = static_cast<unsigned>(kSortWaves * n * sizeof(int));
-  void* params[] = {&a};
   if (a.parts > 1) {
     const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(expert_count_kernel), dim3(a.parts),
                                          dim3(kSortThreads), params, lds, st);
