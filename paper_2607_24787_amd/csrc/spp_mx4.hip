@@ -446,87 +446,24 @@ __global__ __launch_bounds__(kLastThreads) void mx4_last_kernel(LastArgs a) {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kTileThreads = 256;
+constexpr int kTileThreads = 512;
 constexpr int kTileWaves = kTileThreads / 64;
-constexpr int kTileRows = 64 * kTileWaves;  // weight rows of a workgroup
+constexpr int kTileRows = 256;  // weight rows of a tile
 constexpr int kXcds = 8;
+constexpr int kTileWorkgroups = 256;  // one on each compute unit
+constexpr int kBuffers = 3;
+constexpr int kSchedProducts = 0x008, kSchedReads = 0x100;  // matrix instructions, LDS reads
 
 __device__ const u32x4 kZeros = {0, 0, 0, 0};
+
+template <int N>
+using Const = std::integral_constant<int, N>;
 
 // 16 bytes from global memory to `to` + 16 * lane of LDS
 __device__ __forceinline__ void to_lds(const uint8_t* from, uint8_t* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
                                    (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
 }
-
-// Where 16-byte piece c of a row of `pieces` goes: 8 neighbouring rows' pieces c
-// spread over the banks.
-template <int kPieces>
-__device__ __forceinline__ int swizzled(int row, int c) {
-  return c ^ ((row / (8 / kPieces)) % kPieces);
-}
-
-template <int SEL>
-__device__ __forceinline__ f32x16 mfma_mx4_32(u32x4 w, uint32_t w_scales, u32x4 x, uint32_t x_scales, f32x16 c) {
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(w), wide(x), c, 4, 4, SEL, static_cast<int>(w_scales), SEL,
-                                                         static_cast<int>(x_scales));
-}
-
-// Row tile `tile` of kTile rows over all groups' rows, group after group: its
-// group, first row and rows.  Every wave finds it by itself.
-struct Tile {
-  int group, first, count;
-};
-
-template <int kTile>
-__device__ __forceinline__ int tiles_of(const ProductArgs& a, int g, int* first, int* count) {
-  *first = min(max(a.start[g], 0), a.M);
-  *count = max(min(max(a.start[g + 1], 0), a.M) - *first, 0);
-  return (*count + kTile - 1) / kTile;
-}
-
-template <int kTile>
-__device__ __forceinline__ int total_tiles(const ProductArgs& a, int* before) {
-  const int lane = threadIdx.x & 63;
-  const int per = (a.groups + 63) / 64;
-  int sum = 0;
-  for (int j = 0; j < per; ++j) {
-    const int g = lane * per + j;
-    int first, count;
-    if (g < a.groups) sum += tiles_of<kTile>(a, g, &first, &count);
-  }
-  int incl = sum;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(incl, d);
-    if (lane >= d) incl += o;
-  }
-  *before = incl - sum;
-  return __shfl(incl, 63);
-}
-
-template <int kTile>
-__device__ __forceinline__ Tile find_tile(const ProductArgs& a, int before, int tile) {
-  const int lane = threadIdx.x & 63;
-  const int per = (a.groups + 63) / 64;
-  int group = -1, first = 0, count = 0;
-  for (int j = 0; j < per; ++j) {
-    const int g = lane * per + j;
-    if (g >= a.groups) break;
-    int f, c;
-    const int t = tiles_of<kTile>(a, g, &f, &c);
-    if (tile >= before && tile < before + t) {
-      group = g;
-      first = f + (tile - before) * kTile;
-      count = min(c - (tile - before) * kTile, kTile);
-    }
-    before += t;
-  }
-  const int from = max(__ffsll(static_cast<long long>(__ballot(group >= 0))) - 1, 0);
-  return Tile{__shfl(group, from), __shfl(first, from), __shfl(count, from)};
-}
-
-constexpr int kBuffers = 3;
 
 // Waits until at most kLeft of this wave's loads are on their way
 template <int kLeft>
@@ -536,133 +473,216 @@ __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// A workgroup takes 256 weight rows (128 outputs of both matrices for SwiGLU)
-// and 32 * CT rows of one group; K goes through LDS in three buffers, loaded two
-// stages ahead.  A wave takes 64 of the weight rows and all rows of x.
+// Where 16-byte piece c of a row of `kPieces` goes: piece c of the neighbouring
+// rows that 16 lanes read together is spread over 256 bytes, all of the banks.
+template <int kPieces>
+__device__ __forceinline__ int swizzled(int row, int c) {
+  return c ^ ((row / (16 / kPieces)) % kPieces);
+}
+
+template <int SEL>
+__device__ __forceinline__ f32x16 mfma_mx4_32(u32x4 w, uint32_t w_scales, u32x4 x, uint32_t x_scales, f32x16 c) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(w), wide(x), c, 4, 4, SEL, static_cast<int>(w_scales), SEL,
+                                                         static_cast<int>(x_scales));
+}
+
+// Rows of a group
+__device__ __forceinline__ int rows_of(const ProductArgs& a, int g, int* first) {
+  *first = min(max(a.start[g], 0), a.M);
+  return max(min(max(a.start[g + 1], 0), a.M) - *first, 0);
+}
+
+// A tile is 256 weight rows (128 outputs of both matrices for SwiGLU) by 64 * CT
+// rows of one group.  A workgroup stays on its compute unit and takes tiles one
+// after the other, neighbouring tiles on one XCD.  K goes through LDS in stages
+// of 128 bytes of a row in 4 bits (64 beside bf16 rows of x, whose stages are 256
+// bytes), in three buffers that are loaded two stages ahead, over the tiles'
+// borders: the next tile's first stages are on their way while this one's last
+// are multiplied and its results written.  A wave takes 64 of the weight rows
+// and half of the rows of x.
+//
+// A tile of 128 rows is bound by LDS (128 KB read a stage of 256 in K, 1,000
+// cycles, beside 1,250 of the matrix units') and by what each compute unit gets
+// from L2 (48 KB a stage).
 template <int X, bool kSwiglu, typename Out, int CT>
 __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a) {
-  constexpr int KB = X == kXCodes ? 2 : 1;  // blocks of a lane and stage
-  constexpr int BL = 2 * KB;                // blocks of a row and stage
-  constexpr int AC = BL, BC = X == kXCodes ? BL : 4 * BL;  // 16-byte pieces of a row
-  constexpr int TM = 32 * CT;
+  constexpr bool kMx4 = X == kXCodes;
+  constexpr int KB = kMx4 ? 4 : 2;                  // blocks of a lane and stage
+  constexpr int BL = 2 * KB;                        // blocks of a row and stage
+  constexpr int AC = BL, BC = kMx4 ? BL : 4 * BL;   // 16-byte pieces of a row
+  constexpr int TM = 64 * CT;
   constexpr int kA = kTileRows * AC * 16, kB = TM * BC * 16;
+  constexpr int AI = kTileRows * AC / kTileThreads, BI = TM * BC / kTileThreads;  // loads of a wave
+  constexpr int kStageLoads = AI + BI + 1;
+  using Word = typename std::conditional<kMx4, uint64_t, uint32_t>::type;  // a row's scales of a stage
   // an array for each buffer: the compiler then sees that reads of one need not
   // wait for loads into another
   __shared__ __attribute__((aligned(16))) uint8_t s_a0[kA], s_a1[kA], s_a2[kA];
   __shared__ __attribute__((aligned(16))) uint8_t s_b0[kB], s_b1[kB], s_b2[kB];
-  __shared__ uint32_t s_sa[kBuffers][kTileRows];
-  __shared__ uint32_t s_sb[X == kXCodes ? kBuffers : 1][kTileThreads];
+  __shared__ Word s_sa[kBuffers][kTileRows];
+  __shared__ Word s_sb[kBuffers][kMx4 ? TM : 1];
+  __shared__ int s_before[spp::kMaxExpertsTopK];  // tiles of the groups before
+  __shared__ int s_sum[kTileWaves];
   const auto a_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_a0 : buf == 1 ? s_a1 : s_a2; };
   const auto b_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_b0 : buf == 1 ? s_b1 : s_b2; };
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, l32 = lane & 31, wf = wave & 3, wt = wave >> 2;
 
-  // the tile: workgroups of one XCD take neighbouring ones
-  int before = 0;
-  const int64_t total = static_cast<int64_t>(a.start ? total_tiles<TM>(a, &before) : (a.M + TM - 1) / TM) * a.columns;
-  const int64_t each = (total + kXcds - 1) / kXcds, at = blockIdx.x / kXcds;
-  const int64_t logical = blockIdx.x % kXcds * each + at;
-  if (at >= each || logical >= total) return;
-  const int tile = static_cast<int>(logical / a.columns), column = static_cast<int>(logical - static_cast<int64_t>(tile) * a.columns);
-  Tile t{0, tile * TM, min(a.M - tile * TM, TM)};
-  if (a.start) t = find_tile<TM>(a, before, tile);
-  if (t.count < 1) return;
-
-  // what this lane loads: rows' addresses, at the piece that goes to its place.
-  // Weight rows lie in one window (two for SwiGLU: a load's rows in one of them).
-  const int64_t first_row = (static_cast<int64_t>(t.group) * (kSwiglu ? 2 : 1)) * a.N;
-  const auto weight_row = [&](int r, int* up) {  // LDS row r's, in its window
-    const int rho = r & 31, w = r >> 6, hh = (rho >> 2) & 1, j = 4 * (rho >> 3) + (rho & 3);
-    *up = (r >> 5) & 1;
-    const int f = kSwiglu ? column * (kTileRows / 2) + w * 32 + 16 * hh + j : column * kTileRows + w * 64 + 32 * hh + 16 * *up + j;
-    return min(f, a.N - 1);
-  };
-  const int window = column * (kSwiglu ? kTileRows / 2 : kTileRows);
-  uint32_t pa[AC];  // bytes from the window's start
-  int ca[AC];
+  // tiles of the groups before each one (thread t: groups 2t and 2t + 1)
+  int row_tiles = (a.M + TM - 1) / TM;
+  if (a.start) {
+    int n[2], first;
 #pragma unroll
-  for (int i = 0; i < AC; ++i) {
-    const int idx = (i * kTileWaves + wave) * 64 + lane, r = idx / AC;
-    ca[i] = swizzled<AC>(r, idx % AC);
-    int up;
-    pa[i] = static_cast<uint32_t>(weight_row(r, &up) - window) * static_cast<uint32_t>(a.nb) * 16;
+    for (int j = 0; j < 2; ++j) n[j] = 2 * tid + j < a.groups ? (rows_of(a, 2 * tid + j, &first) + TM - 1) / TM : 0;
+    int incl = n[0] + n[1];
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    if (lane == 63) s_sum[wave] = incl;
+    __syncthreads();
+    int base = incl - n[0] - n[1];
+    row_tiles = 0;
+#pragma unroll
+    for (int w = 0; w < kTileWaves; ++w) {
+      base += w < wave ? s_sum[w] : 0;
+      row_tiles += s_sum[w];
+    }
+    s_before[2 * tid] = base;
+    s_before[2 * tid + 1] = base + n[0];
+    __syncthreads();
   }
-  const uint8_t* base[2];
-  base[0] = a.codes + (first_row + window) * a.nb * 16;
-  base[1] = kSwiglu ? base[0] + static_cast<int64_t>(a.N) * a.nb * 16 : base[0];
-  constexpr int BI = (TM * BC + kTileThreads - 1) / kTileThreads;
-  const uint8_t* pb[BI];
-  int cb[BI];
+  const int64_t total = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(row_tiles)) * a.columns;
+  const int64_t each = (total + kXcds - 1) / kXcds;
+  const int64_t xcd_first = blockIdx.x % kXcds * each, xcd_end = min(xcd_first + each, total);
+  const int64_t stride = gridDim.x / kXcds;
+  int64_t job = xcd_first + blockIdx.x / kXcds;
+  if (job >= xcd_end) return;
+
+  struct Tile {
+    int group, first, count, column;
+  };
+  const auto find = [&](int64_t j) {
+    const int tile = static_cast<int>(j / a.columns);
+    Tile t{0, tile * TM, min(a.M - tile * TM, TM), static_cast<int>(j - static_cast<int64_t>(tile) * a.columns)};
+    if (a.start) {
+      int n = 0;
+      for (int g = lane; g - lane < a.groups; g += 64) n += __popcll(__ballot(g < a.groups && s_before[g] <= tile));
+      t.group = n - 1;  // the last one with no more tiles before it: those without rows have as many as the next
+      int first;
+      const int rows = rows_of(a, t.group, &first), at = (tile - s_before[t.group]) * TM;
+      t.first = __builtin_amdgcn_readfirstlane(first + at);
+      t.count = __builtin_amdgcn_readfirstlane(min(rows - at, TM));
+    }
+    return t;
+  };
+
+  // what this lane loads: pieces that go to its places, and a row's scales (of the
+  // weights in the first four waves, of x in the others)
+  int ca[AI], cb[BI];
+#pragma unroll
+  for (int i = 0; i < AI; ++i) {
+    const int idx = (i * kTileWaves + wave) * 64 + lane;
+    ca[i] = swizzled<AC>(idx / AC, idx % AC);
+  }
 #pragma unroll
   for (int i = 0; i < BI; ++i) {
-    const int idx = (i * kTileWaves + wave) * 64 + lane, r = min(idx / BC, TM - 1);
-    cb[i] = swizzled<BC>(r, idx % BC);
-    const int p = t.first + min(r, t.count - 1);
-    const int64_t row = (a.pair ? a.pair[p] : p) / a.xdiv;
-    pb[i] = static_cast<const uint8_t*>(a.x) + row * a.x_stride;
+    const int idx = (i * kTileWaves + wave) * 64 + lane;
+    cb[i] = swizzled<BC>(idx / BC, idx % BC);
   }
-  int64_t scale_row, x_row = 0;
-  {
-    int up;
-    const int r = weight_row(tid, &up);
-    scale_row = first_row + (kSwiglu && up ? a.N : 0) + r;
-    if (X == kXCodes) {
-      const int p = t.first + min(tid, t.count - 1);
-      x_row = (a.pair ? a.pair[p] : p) / a.xdiv;
-    }
-  }
-  const ScaleRow scale_a(a.scales, scale_row, a.nb, a.blocks), scale_b(a.x_scales, x_row, a.nb, a.x_blocks);
-  uint32_t wa[kBuffers] = {}, wb[kBuffers] = {};  // of the stages on their way, by buffer
-  constexpr int kStageLoads = AC + (TM * BC) / kTileThreads + (X == kXCodes ? 2 : 1);  // of a wave, at least
-  const auto issue = [&](int st, auto buf) {
-    const int b0 = st * BL;
-    wa[buf] = scale_a.load(b0);
-    if (X == kXCodes) wb[buf] = scale_b.load(b0);
+  const int scale_r = tid < kTileRows ? tid : min(tid - kTileRows, TM - 1);
+  const bool x_scales = kMx4 && wave >= kTileRows / 64;
+  const uint8_t* scale_base = x_scales ? a.x_scales : a.scales;
+
+  // Rows of x of a tile; the pairs' loads are on their way until they are used
+  int x_pair[BI], x_pair_scale = 0;
+  const auto fetch = [&](const Tile& t) {
 #pragma unroll
-    for (int i = 0; i < AC; ++i)
+    for (int i = 0; i < BI; ++i) {
+      const int p = t.first + min(((i * kTileWaves + wave) * 64 + lane) / BC, t.count - 1);
+      x_pair[i] = a.pair ? a.pair[p] : p;
+    }
+    if (kMx4) {
+      const int p = t.first + min(scale_r, t.count - 1);
+      x_pair_scale = a.pair ? a.pair[p] : p;
+    }
+  };
+  uint32_t pa[AI];         // bytes from the start of a window of weight rows
+  const uint8_t* base[2];  // the windows: one, or SwiGLU's two (a load's rows are in one of them)
+  const uint8_t* pb[BI];
+  int64_t scale_at;
+  int scale_last, stage = 0;
+  const auto setup = [&](const Tile& t) {
+    // LDS row r holds the weight row whose sums come to lie where the results are
+    // written from: a lane then has neighbouring outputs
+    const int window = t.column * (kSwiglu ? kTileRows / 2 : kTileRows);
+    const auto weight_row = [&](int r) {
+      const int rho = r & 31, w = r >> 6, hh = (rho >> 2) & 1, j = 4 * (rho >> 3) + (rho & 3), up = (r >> 5) & 1;
+      return min(window + (kSwiglu ? w * 32 + 16 * hh + j : w * 64 + 32 * hh + 16 * up + j), a.N - 1);
+    };
+    const int64_t first_row = static_cast<int64_t>(t.group) * (kSwiglu ? 2 : 1) * a.N;
+    base[0] = a.codes + (first_row + window) * a.nb * 16;
+    base[1] = kSwiglu ? base[0] + static_cast<int64_t>(a.N) * a.nb * 16 : base[0];
+#pragma unroll
+    for (int i = 0; i < AI; ++i)
+      pa[i] = static_cast<uint32_t>(weight_row(((i * kTileWaves + wave) * 64 + lane) / AC) - window) *
+              static_cast<uint32_t>(a.nb) * 16;
+#pragma unroll
+    for (int i = 0; i < BI; ++i) pb[i] = static_cast<const uint8_t*>(a.x) + (x_pair[i] / a.xdiv) * a.x_stride + cb[i] * 16;
+    const int64_t row = x_scales ? x_pair_scale / a.xdiv
+                                 : first_row + (kSwiglu && (scale_r >> 5 & 1) ? a.N : 0) + weight_row(scale_r);
+    scale_at = row * a.nb;
+    scale_last = static_cast<int>(min((x_scales ? a.x_blocks : a.blocks) - static_cast<int64_t>(sizeof(Word)) - scale_at,
+                                      int64_t{1} << 20));
+    stage = 0;
+  };
+
+  const int stages = (a.nb + BL - 1) / BL, padded = (stages + kBuffers - 1) / kBuffers * kBuffers;
+  // of the stages on their way, by buffer: scales, where they begin in their word,
+  // and the blocks left in the row
+  Word word[kBuffers];
+  int begin[kBuffers], left[kBuffers];
+  // The next stage into a buffer: always as many loads, since waits count them
+  const auto issue = [&](auto buf) {
+    const int b0 = stage * BL;
+    const int from = min(b0, scale_last);
+    __builtin_memcpy(&word[buf], scale_base + scale_at + from, sizeof(Word));
+    begin[buf] = min(b0 - from, static_cast<int>(sizeof(Word)) - 1);
+    left[buf] = a.nb - b0;
+#pragma unroll
+    for (int i = 0; i < AI; ++i)
       to_lds(base[((i * kTileWaves + wave) * (64 / AC) >> 5) & 1] + (pa[i] + (b0 + ca[i] < a.nb ? b0 + ca[i] : 0) * 16),
              a_of(buf) + (i * kTileWaves + wave) * 1024);
 #pragma unroll
-    for (int i = 0; i < BI; ++i) {
-      if (BI * kTileThreads != TM * BC && (i * kTileWaves + wave) * 64 >= TM * BC) break;
-      const int block = X == kXCodes ? b0 + cb[i] : b0 + cb[i] / 4;
-      const uint8_t* from = pb[i] + (static_cast<int64_t>(b0) * (BC / BL) + cb[i]) * 16;
-      to_lds(block < a.nb ? from : reinterpret_cast<const uint8_t*>(&kZeros), b_of(buf) + (i * kTileWaves + wave) * 1024);
-    }
+    for (int i = 0; i < BI; ++i)
+      to_lds(b0 + cb[i] / (BC / BL) < a.nb ? pb[i] + static_cast<int64_t>(b0) * (BC / BL * 16)
+                                           : reinterpret_cast<const uint8_t*>(&kZeros),
+             b_of(buf) + (i * kTileWaves + wave) * 1024);
+    ++stage;
   };
-  const auto put_scales = [&](int st, int buf, uint32_t sa, uint32_t sb) {
-    asm volatile("" : "+v"(sa), "+v"(sb));  // not before the wait
-    s_sa[buf][tid] = scale_a.bytes<BL>(sa, st * BL, a.nb);
-    if (X == kXCodes) s_sb[buf][tid] = scale_b.bytes<BL>(sb, st * BL, a.nb);
+  const auto put_scales = [&](auto buf) {
+    Word w = word[buf];
+    asm volatile("" : "+v"(w));  // not before the wait
+    w >>= 8 * begin[buf];
+    if (left[buf] < BL) {  // past the row's end: 1
+      const Word keep = left[buf] <= 0 ? 0 : (Word{1} << (8 * left[buf])) - 1;
+      w = (w & keep) | (static_cast<Word>(0x7f7f7f7f7f7f7f7full) & ~keep);
+    }
+    if (tid < kTileRows)
+      s_sa[buf][tid] = w;
+    else if (kMx4 && tid - kTileRows < TM)
+      s_sb[buf][tid - kTileRows] = w;
   };
 
   f32x16 acc[2][CT];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) acc[i][c][j] = 0.f;
-
-  const int stages = (a.nb + BL - 1) / BL;
-  using Buf0 = std::integral_constant<int, 0>;
-  using Buf1 = std::integral_constant<int, 1>;
-  using Buf2 = std::integral_constant<int, 2>;
-  issue(0, Buf0{});
-  if (stages > 1) {
-    issue(1, Buf1{});
-    wait_loads<kStageLoads>();
-  } else {
-    wait_loads<0>();
-  }
-  put_scales(0, 0, wa[0], wb[0]);
-  lds_barrier();
   // where this lane reads: its row's first piece, and the others by exclusive or
   // with their number; its row's scales of its half.  Hidden from the compiler,
   // which would keep an address of its own for every read of every buffer.
-  uint32_t at_a = (l32 * AC + swizzled<AC>(l32, half * KB)) * 16 + wave * 64 * AC * 16;
-  uint32_t at_b = (l32 * BC + swizzled<BC>(l32, half * (BC / 2))) * 16;
-  uint32_t at_sa = (wave * 64 + l32) * 4 + half * KB, at_sb = l32 * 4 + half * KB;
-  const auto products = [&](const uint8_t* in_a, const uint8_t* in_b, const uint32_t* in_sa, const uint32_t* in_sb) {
+  uint32_t at_a = (l32 * AC + swizzled<AC>(l32, half * KB)) * 16 + wf * 64 * AC * 16;
+  uint32_t at_b = (l32 * BC + swizzled<BC>(l32, half * (BC / 2))) * 16 + wt * 32 * CT * BC * 16;
+  uint32_t at_sa = (wf * 64 + l32) * sizeof(Word) + half * KB, at_sb = (wt * 32 * CT + l32) * sizeof(Word) + half * KB;
+  const auto products = [&](const uint8_t* in_a, const uint8_t* in_b, const Word* in_sa, const Word* in_sb) {
     asm volatile("" : "+v"(at_a), "+v"(at_b), "+v"(at_sa), "+v"(at_sb));
     const auto read_a = [&](int i, int c) {
       return *reinterpret_cast<const u32x4*>(in_a + (at_a ^ (c << 4)) + i * 32 * AC * 16);
@@ -670,136 +690,207 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     const auto read_b = [&](int i, int c) {
       return *reinterpret_cast<const u32x4*>(in_b + (at_b ^ (c << 4)) + i * 32 * BC * 16);
     };
-    const auto scale = [&](const uint32_t* in, uint32_t at, int i) -> uint32_t {
-      const uint8_t* p = reinterpret_cast<const uint8_t*>(in) + at + i * 128;
-      return KB == 2 ? *reinterpret_cast<const uint16_t*>(p) : *p;
+    const auto scale = [&](const Word* in, uint32_t at, int i) -> uint32_t {
+      const uint8_t* p = reinterpret_cast<const uint8_t*>(in) + at + i * 32 * sizeof(Word);
+      return kMx4 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
     };
-    if constexpr (X == kXCodes) {
-      uint32_t sa[2], sb[CT];
+    uint32_t sa[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) sa[i] = scale(in_sa, at_sa, i);
+    for (int i = 0; i < 2; ++i) sa[i] = scale(in_sa, at_sa, i);
+    if constexpr (kMx4) {
+      uint32_t sb[CT];
 #pragma unroll
       for (int i = 0; i < CT; ++i) sb[i] = scale(in_sb, at_sb, i);
-      u32x4 va[2], vb[CT];
+      u32x4 va[KB][2], vb[KB][CT];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) va[i] = read_a(i, 0);
+      for (int b = 0; b < KB; ++b) {
 #pragma unroll
-      for (int i = 0; i < CT; ++i) vb[i] = read_b(i, 0);
+        for (int i = 0; i < 2; ++i) va[b][i] = read_a(i, b);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[i][c] = mfma_mx4_32<0>(va[i], sa[i], vb[c], sb[c], acc[i][c]);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) va[i] = read_a(i, 1);
-#pragma unroll
-      for (int i = 0; i < CT; ++i) vb[i] = read_b(i, 1);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[i][c] = mfma_mx4_32<1>(va[i], sa[i], vb[c], sb[c], acc[i][c]);
-    } else {
-      u32x4 va[2];
-      float sa[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        va[i] = read_a(i, 0);
-        sa[i] = scale_of(scale(in_sa, at_sa, i));
+        for (int i = 0; i < CT; ++i) vb[b][i] = read_b(i, b);
       }
+      const auto block = [&](auto b) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        u32x4 vb[CT];
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int c = 0; c < CT; ++c) vb[c] = read_b(c, q);
+          for (int c = 0; c < CT; ++c) acc[i][c] = mfma_mx4_32<b>(va[b][i], sa[i], vb[b][c], sb[c], acc[i][c]);
+      };
+      block(Const<0>{});
+      block(Const<1>{});
+      block(Const<2>{});
+      block(Const<3>{});
+      // two blocks are read ahead of the products, the others between them
+      constexpr int kReads = 2 + CT;
+      __builtin_amdgcn_sched_group_barrier(kSchedReads, 2 * kReads + 2, 0);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const bf16x8 w = __builtin_bit_cast(bf16x8, cvt8(va[i][q], sa[i]));
+      for (int i = 0; i < 2 * kReads; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kSchedProducts, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedReads, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kSchedProducts, 8 * CT - 2 * kReads, 0);
+    } else {
+      u32x4 va[KB][2];
 #pragma unroll
-          for (int c = 0; c < CT; ++c)
-            acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, vb[c]), acc[i][c], 0, 0, 0);
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) va[b][i] = read_a(i, b);
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          u32x4 vb[CT];
+#pragma unroll
+          for (int c = 0; c < CT; ++c) vb[c] = read_b(c, 4 * b + q);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const bf16x8 w = __builtin_bit_cast(bf16x8, cvt8(va[b][i][q], scale_of((sa[i] >> (8 * b)) & 255u)));
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+              acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, vb[c]), acc[i][c], 0, 0, 0);
+          }
         }
       }
+      // the weights and two quarters of x are read ahead of the products
+      __builtin_amdgcn_sched_group_barrier(kSchedReads, 2 + 2 * KB + 2 * CT, 0);
+#pragma unroll
+      for (int i = 0; i < (4 * KB - 2) * CT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kSchedProducts, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedReads, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kSchedProducts, 4 * CT, 0);
     }
     __builtin_amdgcn_sched_barrier(0);  // the products go before what follows
   };
-  const auto step = [&](int st, auto buf, bool load) {
+  const auto step = [&](int st, auto buf) {
     constexpr int kNext = (buf + 1) % kBuffers, kAfter = (buf + 2) % kBuffers;
-    if (load) issue(st + 2, std::integral_constant<int, kAfter>{});
-    products(a_of(buf), b_of(buf), s_sa[buf], s_sb[X == kXCodes ? buf : 0]);
-    if (load)
-      wait_loads<kStageLoads>();
-    else
-      wait_loads<0>();
-    put_scales(st + 1, kNext, wa[kNext], wb[kNext]);
+    issue(Const<kAfter>{});
+    if (st < stages) products(a_of(buf), b_of(buf), s_sa[buf], s_sb[buf]);
+    wait_loads<kStageLoads>();
+    put_scales(Const<kNext>{});
     lds_barrier();
   };
-  int st = 0;
-  for (; st + 4 < stages; st += kBuffers) {
-    step(st, Buf0{}, true);
-    step(st + 1, Buf1{}, true);
-    step(st + 2, Buf2{}, true);
-  }
-  // one to four are left
-  step(st, Buf0{}, st + 2 < stages);
-  if (st + 1 < stages) step(st + 1, Buf1{}, st + 3 < stages);
-  if (st + 2 < stages) step(st + 2, Buf2{}, false);
-  if (st + 3 < stages) step(st + 3, Buf0{}, false);
 
-  // a lane holds 32 neighbouring outputs of a row (16 of both for SwiGLU)
+  Tile t = find(job);
+  fetch(t);
+  setup(t);
+  issue(Const<0>{});
+  issue(Const<1>{});
+  wait_loads<kStageLoads>();
+  put_scales(Const<0>{});
+  lds_barrier();
+  for (;;) {
+    job += stride;
+    const bool more = job < xcd_end;
+    Tile next = t;
+    if (more) {
+      next = find(job);
+      fetch(next);
+    }
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int r = c * 32 + l32;
-    const int64_t row = t.first + r;
-    const bool ok = r < t.count;
-    if constexpr (kSwiglu) {
-      const int f = column * (kTileRows / 2) + wave * 32 + 16 * half;
-      float y[16];
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) y[j] = swiglu(acc[0][c][j], acc[1][c][j]);
-      if constexpr (X == kXCodes) {
-        uint32_t top = 0;
+      for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(y[j]) & 0x7fffffffu);
-        top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32)));
-        const uint32_t byte = byte_of(top);
-        const float scale = scale_of(byte);
-        u32x2 w;
+        for (int j = 0; j < 16; ++j) acc[i][c][j] = 0.f;
+    for (int st = 0; st < padded; st += kBuffers) {
+      step(st, Const<0>{});
+      if (more && st + kBuffers == padded) setup(next);
+      asm volatile("" : "+v"(scale_at));  // else the load from there is made in both branches, and waited for
+      step(st + 1, Const<1>{});
+      step(st + 2, Const<2>{});
+    }
+
+    // A lane holds 32 neighbouring outputs of a row (16 of both for SwiGLU).  bf16
+    // results go through the third buffer, which nothing is loaded into now, so
+    // that whole cache lines are written.
+    uint8_t* mine = kA >= 8 * 4096 ? s_a2 + wave * 4096 : wave < 4 ? s_a2 + wave * 4096 : s_b2 + (wave - 4) * 4096;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          uint32_t v = 0;
-          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k], y[8 * k + 1], scale, 0);
-          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k + 2], y[8 * k + 3], scale, 1);
-          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k + 4], y[8 * k + 5], scale, 2);
-          v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k + 6], y[8 * k + 7], scale, 3);
-          w[k] = byte == kNanByte ? 0u : v;
-        }
-        if (ok && f < a.N) {
-          *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.out) + (row * a.N + f) / 2) = w;
-          if (half == 0) a.out_scales[(row * a.N + f) / 32] = static_cast<uint8_t>(byte);
-        }
-      } else if (ok && f < a.N) {
-        __bf16* out = static_cast<__bf16*>(a.out) + row * a.N + f;
-        store8(out, y);
-        store8(out + 8, y + 8);
-      }
-    } else {
-      const int f = column * kTileRows + wave * 64 + 32 * half;
-      if (!ok || f >= a.N) continue;
-      Out* out = static_cast<Out*>(a.out) + row * a.out_stride + f;
-      if (a.wide_out && f + 32 <= a.N) {
+    for (int c = 0; c < CT; ++c) {
+      const int r0 = (wt * CT + c) * 32, r = r0 + l32;
+      const int64_t row = t.first + r;
+      const bool ok = r < t.count;
+      if constexpr (kSwiglu) {
+        const int f0 = t.column * (kTileRows / 2) + wf * 32, f = f0 + 16 * half;
+        if (f0 >= a.N) continue;  // N is a multiple of 32
+        float y[16];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float y[8];
+        for (int j = 0; j < 16; ++j) y[j] = swiglu(acc[0][c][j], acc[1][c][j]);
+        if constexpr (kMx4) {
+          uint32_t top = 0;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = acc[k / 2][c][8 * (k % 2) + j];
-          store8(out + 8 * k, y);
+          for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(y[j]) & 0x7fffffffu);
+          top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32)));
+          const uint32_t byte = byte_of(top);
+          const float scale = scale_of(byte);
+          u32x2 w;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            uint32_t v = 0;
+            v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k], y[8 * k + 1], scale, 0);
+            v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k + 2], y[8 * k + 3], scale, 1);
+            v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k + 4], y[8 * k + 5], scale, 2);
+            v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, y[8 * k + 6], y[8 * k + 7], scale, 3);
+            w[k] = byte == kNanByte ? 0u : v;
+          }
+          if (ok) {
+            *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.out) + (row * a.N + f) / 2) = w;
+            if (half == 0) a.out_scales[(row * a.N + f) / 32] = static_cast<uint8_t>(byte);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            store8(reinterpret_cast<__bf16*>(mine + (l32 * 4 + swizzled<4>(l32, half * 2 + k)) * 16), y + 8 * k);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int s = k * 16 + lane / 4, q = lane % 4;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(mine + (s * 4 + swizzled<4>(s, q)) * 16);
+            if (r0 + s < t.count)
+              *reinterpret_cast<u32x4*>(static_cast<__bf16*>(a.out) + static_cast<int64_t>(t.first + r0 + s) * a.N + f0 + 8 * q) = v;
+          }
         }
       } else {
+        const int f0 = t.column * kTileRows + wf * 64, f = f0 + 32 * half;
+        const auto eight = [&](int k, float* y) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (f + j < a.N) out[j] = static_cast<Out>(acc[j / 16][c][j % 16]);
+          for (int j = 0; j < 8; ++j) y[j] = acc[k / 2][c][8 * (k % 2) + j];
+        };
+        if (std::is_same<Out, __bf16>::value && a.wide_out && f0 + 64 <= a.N) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float y[8];
+            eight(k, y);
+            store8(reinterpret_cast<__bf16*>(mine + (l32 * 8 + swizzled<8>(l32, half * 4 + k)) * 16), y);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int s = k * 8 + lane / 8, q = lane % 8;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(mine + (s * 8 + swizzled<8>(s, q)) * 16);
+            if (r0 + s < t.count)
+              *reinterpret_cast<u32x4*>(static_cast<__bf16*>(a.out) + (t.first + r0 + s) * a.out_stride + f0 + 8 * q) = v;
+          }
+          continue;
+        }
+        if (!ok || f >= a.N) continue;
+        Out* out = static_cast<Out*>(a.out) + row * a.out_stride + f;
+        if (a.wide_out && f + 32 <= a.N) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float y[8];
+            eight(k, y);
+            store8(out + 8 * k, y);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (f + j < a.N) out[j] = static_cast<Out>(acc[j / 16][c][j % 16]);
+        }
       }
     }
+    if (!more) break;
+    lds_barrier();  // the third buffer is loaded into again
+    t = next;
   }
+  wait_loads<0>();  // nothing may come to this workgroup's LDS after its end
 }
 
 // ------------------------------------------------------------------ host side
@@ -940,33 +1031,31 @@ hipError_t launch_few(ProductArgs a, int64_t groups, hipStream_t st) {
 
 template <int X, bool kSwiglu, typename Out, int CT>
 hipError_t launch_tile(ProductArgs a, hipStream_t st) {
-  a.columns = (a.N + (kSwiglu ? kTileRows / 2 : kTileRows) - 1) / (kSwiglu ? kTileRows / 2 : kTileRows);
+  constexpr int kOutputs = kSwiglu ? kTileRows / 2 : kTileRows;
+  a.columns = (a.N + kOutputs - 1) / kOutputs;
   a.wide_out = wide_rows(a.out, a.out_stride, sizeof(Out));
   // groups with a last tile of their own: at most one a group, and one a row
-  const int64_t tiles = a.M / (32 * CT) + std::min(a.groups, a.M);
-  const int64_t grid = (tiles * a.columns + kXcds - 1) / kXcds * kXcds;
+  const int64_t tiles = (a.M / (64 * CT) + std::min(a.groups, a.M)) * static_cast<int64_t>(a.columns);
+  const int64_t grid = std::min<int64_t>((tiles + kXcds - 1) / kXcds * kXcds, kTileWorkgroups);
   return launch(mx4_tile_kernel<X, kSwiglu, Out, CT>, static_cast<unsigned>(grid), kTileThreads, a, st);
 }
 
-// Rows of x that a workgroup of the tiled products takes, by the mean of a
-// group's; 0: few rows
+// Rows of x that a tile takes, by the mean of a group's; 0: few rows
 constexpr int kFewRows = 20;
 int tile_rows(int64_t M, int groups) {
   const int64_t mean = M / groups;
-  return mean >= 96 ? 128 : mean >= 48 ? 64 : mean >= kFewRows ? 32 : 0;
+  return mean >= 64 ? 128 : mean >= kFewRows ? 64 : 0;
 }
 
 template <int X, bool kSwiglu, typename Out>
 hipError_t launch_tiles(const ProductArgs& a, int rows, hipStream_t st) {
-  return rows == 128  ? launch_tile<X, kSwiglu, Out, 4>(a, st)
-         : rows == 64 ? launch_tile<X, kSwiglu, Out, 2>(a, st)
-                      : launch_tile<X, kSwiglu, Out, 1>(a, st);
+  return rows == 128 ? launch_tile<X, kSwiglu, Out, 2>(a, st) : launch_tile<X, kSwiglu, Out, 1>(a, st);
 }
 
 template <int X>
 hipError_t launch_product(const ProductArgs& a, int32_t dtype, hipStream_t st) {
   const int rows = tile_rows(a.M, a.groups);
-  if (rows > 0 && a.blocks >= 4)  // fewer scales than a word: the few rows' kernel alone reads them byte by byte
+  if (rows > 0 && a.blocks >= 8)  // fewer scales than a word: the few rows' kernel alone reads them byte by byte
     return dtype == SPP_DTYPE_BF16 ? launch_tiles<X, false, __bf16>(a, rows, st) : launch_tiles<X, false, float>(a, rows, st);
   return dtype == SPP_DTYPE_BF16 ? launch_few<X, false, __bf16, kRowsStart>(a, a.groups, st)
                                  : launch_few<X, false, float, kRowsStart>(a, a.groups, st);
