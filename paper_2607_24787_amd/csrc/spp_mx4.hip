@@ -452,6 +452,7 @@ constexpr int kTileRows = 256;  // weight rows of a tile
 constexpr int kXcds = 8;
 constexpr int kTileWorkgroups = 256;  // one on each compute unit
 constexpr int kBuffers = 3;
+constexpr int kBand = 8;
 constexpr int kSchedProducts = 0x008, kSchedReads = 0x100;  // matrix instructions, LDS reads
 
 __device__ const u32x4 kZeros = {0, 0, 0, 0};
@@ -513,16 +514,20 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   constexpr int TM = 64 * CT;
   constexpr int kA = kTileRows * AC * 16, kB = TM * BC * 16;
   constexpr int AI = kTileRows * AC / kTileThreads, BI = TM * BC / kTileThreads;  // loads of a wave
-  constexpr int kStageLoads = AI + BI + 1;
+  constexpr int kStageLoads = AI + BI;
   using Word = typename std::conditional<kMx4, uint64_t, uint32_t>::type;  // a row's scales of a stage
+  // Scales come four stages at a time, in pieces of 16 bytes: by the stage, every
+  // row would ask for a cache line of its own, as many as its codes do.
+  constexpr int kAtOnce = 4, SC = kAtOnce * BL / 16;
+  constexpr int SI = kMx4 ? 2 : 1;  // loads of a wave: the weights', x's
   // an array for each buffer: the compiler then sees that reads of one need not
   // wait for loads into another
   __shared__ __attribute__((aligned(16))) uint8_t s_a0[kA], s_a1[kA], s_a2[kA];
   __shared__ __attribute__((aligned(16))) uint8_t s_b0[kB], s_b1[kB], s_b2[kB];
-  __shared__ Word s_sa[kBuffers][kTileRows];
-  __shared__ Word s_sb[kBuffers][kMx4 ? TM : 1];
+  __shared__ Word s_sa[kAtOnce][kTileRows];
+  __shared__ Word s_sb[kAtOnce][kMx4 ? TM : 1];
   __shared__ int s_before[spp::kMaxExpertsTopK];  // tiles of the groups before
-  __shared__ int s_sum[kTileWaves];
+  int* s_sum = reinterpret_cast<int*>(s_sa);
   const auto a_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_a0 : buf == 1 ? s_a1 : s_a2; };
   const auto b_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_b0 : buf == 1 ? s_b1 : s_b2; };
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -549,11 +554,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
       base += w < wave ? s_sum[w] : 0;
       row_tiles += s_sum[w];
     }
+    __syncthreads();
     s_before[2 * tid] = base;
     s_before[2 * tid + 1] = base + n[0];
     __syncthreads();
   }
-  const int64_t total = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(row_tiles)) * a.columns;
+  row_tiles = __builtin_amdgcn_readfirstlane(row_tiles);
+  const int64_t total = static_cast<int64_t>(row_tiles) * a.columns;
   const int64_t each = (total + kXcds - 1) / kXcds;
   const int64_t xcd_first = blockIdx.x % kXcds * each, xcd_end = min(xcd_first + each, total);
   const int64_t stride = gridDim.x / kXcds;
@@ -564,8 +571,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     int group, first, count, column;
   };
   const auto find = [&](int64_t j) {
-    const int tile = static_cast<int>(j / a.columns);
-    Tile t{0, tile * TM, min(a.M - tile * TM, TM), static_cast<int>(j - static_cast<int64_t>(tile) * a.columns)};
+    // bands of kBand row tiles, in each of them column by column: those that run
+    // together on an XCD share weights and rows of x in its L2
+    const int band = static_cast<int>(j / (kBand * a.columns)), tiles = min(kBand, row_tiles - band * kBand);
+    const int in_band = static_cast<int>(j - static_cast<int64_t>(band) * kBand * a.columns);
+    const int tile = band * kBand + in_band % tiles;
+    Tile t{0, tile * TM, min(a.M - tile * TM, TM), in_band / tiles};
     if (a.start) {
       int n = 0;
       for (int g = lane; g - lane < a.groups; g += 64) n += __popcll(__ballot(g < a.groups && s_before[g] <= tile));
@@ -591,9 +602,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     const int idx = (i * kTileWaves + wave) * 64 + lane;
     cb[i] = swizzled<BC>(idx / BC, idx % BC);
   }
-  const int scale_r = tid < kTileRows ? tid : min(tid - kTileRows, TM - 1);
-  const bool x_scales = kMx4 && wave >= kTileRows / 64;
-  const uint8_t* scale_base = x_scales ? a.x_scales : a.scales;
+  // of scales: piece scale_c of a row of the weights, and of x (the last row's
+  // again where there are more lanes than rows)
+  const int scale_q = wave * 64 + lane, scale_c = scale_q % SC;
+  const int scale_ra = min(scale_q / SC, kTileRows - 1), scale_rb = min(scale_q / SC, TM - 1);
 
   // Rows of x of a tile; the pairs' loads are on their way until they are used
   int x_pair[BI], x_pair_scale = 0;
@@ -604,15 +616,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
       x_pair[i] = a.pair ? a.pair[p] : p;
     }
     if (kMx4) {
-      const int p = t.first + min(scale_r, t.count - 1);
+      const int p = t.first + min(scale_rb, t.count - 1);
       x_pair_scale = a.pair ? a.pair[p] : p;
     }
   };
   uint32_t pa[AI];         // bytes from the start of a window of weight rows
   const uint8_t* base[2];  // the windows: one, or SwiGLU's two (a load's rows are in one of them)
   const uint8_t* pb[BI];
-  int64_t scale_at;
-  int scale_last, stage = 0;
+  int64_t scale_at[SI];
+  int scale_last[SI], stage = 0;
   const auto setup = [&](const Tile& t) {
     // LDS row r holds the weight row whose sums come to lie where the results are
     // written from: a lane then has neighbouring outputs
@@ -630,26 +642,62 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
               static_cast<uint32_t>(a.nb) * 16;
 #pragma unroll
     for (int i = 0; i < BI; ++i) pb[i] = static_cast<const uint8_t*>(a.x) + (x_pair[i] / a.xdiv) * a.x_stride + cb[i] * 16;
-    const int64_t row = x_scales ? x_pair_scale / a.xdiv
-                                 : first_row + (kSwiglu && (scale_r >> 5 & 1) ? a.N : 0) + weight_row(scale_r);
-    scale_at = row * a.nb;
-    scale_last = static_cast<int>(min((x_scales ? a.x_blocks : a.blocks) - static_cast<int64_t>(sizeof(Word)) - scale_at,
-                                      int64_t{1} << 20));
+#pragma unroll
+    for (int i = 0; i < SI; ++i) {
+      const int64_t row = i == 0 ? first_row + (kSwiglu && (scale_ra >> 5 & 1) ? a.N : 0) + weight_row(scale_ra) : x_pair_scale / a.xdiv;
+      scale_at[i] = row * a.nb;
+      scale_last[i] = static_cast<int>(min((i == 0 ? a.blocks : a.x_blocks) - 16 - scale_at[i], int64_t{1} << 20));
+    }
     stage = 0;
   };
 
   const int stages = (a.nb + BL - 1) / BL, padded = (stages + kBuffers - 1) / kBuffers * kBuffers;
-  // of the stages on their way, by buffer: scales, where they begin in their word,
-  // and the blocks left in the row
-  Word word[kBuffers];
-  int begin[kBuffers], left[kBuffers];
+  struct Scales {
+    u32x4 v[SI];
+    int last[SI];
+  };
+  // A lane's piece of four stages from `st` on, read whole and in bounds: near the
+  // end of all scales (at least 16) it starts earlier
+  const auto load_scales = [&](Scales& to, int st) {
+    const int b = st * BL + 16 * scale_c;
+#pragma unroll
+    for (int i = 0; i < SI; ++i) {
+      to.last[i] = scale_last[i];
+      __builtin_memcpy(&to.v[i], (i == 0 ? a.scales : a.x_scales) + scale_at[i] + min(b, to.last[i]), 16);
+    }
+  };
+  const auto put_scales = [&](const Scales& from, int st) {
+    const int b = st * BL + 16 * scale_c;
+#pragma unroll
+    for (int i = 0; i < SI; ++i) {
+      uint64_t lo = from.v[i][0] | static_cast<uint64_t>(from.v[i][1]) << 32, hi = from.v[i][2] | static_cast<uint64_t>(from.v[i][3]) << 32;
+      int skip = min(b - min(b, from.last[i]), 15);  // bytes before block b
+      if (skip >= 8) lo = hi, hi = 0, skip -= 8;
+      if (skip > 0) {
+        lo = lo >> (8 * skip) | hi << (64 - 8 * skip);
+        hi >>= 8 * skip;
+      }
+      const auto whole = [](uint64_t w, int left) {  // past the row's end: 1
+        const uint64_t keep = left >= 8 ? ~uint64_t{0} : left <= 0 ? 0 : (uint64_t{1} << (8 * left)) - 1;
+        return (w & keep) | (0x7f7f7f7f7f7f7f7full & ~keep);
+      };
+      lo = whole(lo, a.nb - b), hi = whole(hi, a.nb - b - 8);
+      const int r = scale_q / SC;
+      if constexpr (kMx4) {
+        if (i == 0) {
+          s_sa[2 * scale_c][r] = lo, s_sa[2 * scale_c + 1][r] = hi;
+        } else if (r < TM) {
+          s_sb[2 * scale_c][r] = lo, s_sb[2 * scale_c + 1][r] = hi;
+        }
+      } else if (r < kTileRows) {
+        s_sa[0][r] = static_cast<uint32_t>(lo), s_sa[1][r] = static_cast<uint32_t>(lo >> 32);
+        s_sa[2][r] = static_cast<uint32_t>(hi), s_sa[3][r] = static_cast<uint32_t>(hi >> 32);
+      }
+    }
+  };
   // The next stage into a buffer: always as many loads, since waits count them
   const auto issue = [&](auto buf) {
     const int b0 = stage * BL;
-    const int from = min(b0, scale_last);
-    __builtin_memcpy(&word[buf], scale_base + scale_at + from, sizeof(Word));
-    begin[buf] = min(b0 - from, static_cast<int>(sizeof(Word)) - 1);
-    left[buf] = a.nb - b0;
 #pragma unroll
     for (int i = 0; i < AI; ++i)
       to_lds(base[((i * kTileWaves + wave) * (64 / AC) >> 5) & 1] + (pa[i] + (b0 + ca[i] < a.nb ? b0 + ca[i] : 0) * 16),
@@ -661,20 +709,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
              b_of(buf) + (i * kTileWaves + wave) * 1024);
     ++stage;
   };
-  const auto put_scales = [&](auto buf) {
-    Word w = word[buf];
-    asm volatile("" : "+v"(w));  // not before the wait
-    w >>= 8 * begin[buf];
-    if (left[buf] < BL) {  // past the row's end: 1
-      const Word keep = left[buf] <= 0 ? 0 : (Word{1} << (8 * left[buf])) - 1;
-      w = (w & keep) | (static_cast<Word>(0x7f7f7f7f7f7f7f7full) & ~keep);
-    }
-    if (tid < kTileRows)
-      s_sa[buf][tid] = w;
-    else if (kMx4 && tid - kTileRows < TM)
-      s_sb[buf][tid - kTileRows] = w;
-  };
-
   f32x16 acc[2][CT];
   // where this lane reads: its row's first piece, and the others by exclusive or
   // with their number; its row's scales of its half.  Hidden from the compiler,
@@ -761,22 +795,27 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     }
     __builtin_amdgcn_sched_barrier(0);  // the products go before what follows
   };
+  Scales in_tile, of_next;
   const auto step = [&](int st, auto buf) {
-    constexpr int kNext = (buf + 1) % kBuffers, kAfter = (buf + 2) % kBuffers;
-    issue(Const<kAfter>{});
-    if (st < stages) products(a_of(buf), b_of(buf), s_sa[buf], s_sb[buf]);
+    if (st % kAtOnce == 1 && st + kAtOnce - 1 < stages) load_scales(in_tile, st + kAtOnce - 1);
+    issue(Const<(buf + 2) % kBuffers>{});
+    if (st < stages) products(a_of(buf), b_of(buf), s_sa[st % kAtOnce], s_sb[st % kAtOnce]);
     wait_loads<kStageLoads>();
-    put_scales(Const<kNext>{});
+    if (st % kAtOnce == kAtOnce - 1 && st + 1 < stages) {
+      lds_barrier();  // these scales are no longer read
+      put_scales(in_tile, st + 1);
+    }
     lds_barrier();
   };
 
   Tile t = find(job);
   fetch(t);
   setup(t);
+  load_scales(of_next, 0);
   issue(Const<0>{});
   issue(Const<1>{});
   wait_loads<kStageLoads>();
-  put_scales(Const<0>{});
+  put_scales(of_next, 0);
   lds_barrier();
   for (;;) {
     job += stride;
@@ -794,11 +833,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
         for (int j = 0; j < 16; ++j) acc[i][c][j] = 0.f;
     for (int st = 0; st < padded; st += kBuffers) {
       step(st, Const<0>{});
-      if (more && st + kBuffers == padded) setup(next);
-      asm volatile("" : "+v"(scale_at));  // else the load from there is made in both branches, and waited for
+      if (st + kBuffers == padded) {
+        if (more) setup(next);
+        load_scales(of_next, 0);
+      }
       step(st + 1, Const<1>{});
       step(st + 2, Const<2>{});
     }
+    put_scales(of_next, 0);  // read after the barrier below
 
     // A lane holds 32 neighbouring outputs of a row (16 of both for SwiGLU).  bf16
     // results go through the third buffer, which nothing is loaded into now, so
@@ -1055,7 +1097,7 @@ hipError_t launch_tiles(const ProductArgs& a, int rows, hipStream_t st) {
 template <int X>
 hipError_t launch_product(const ProductArgs& a, int32_t dtype, hipStream_t st) {
   const int rows = tile_rows(a.M, a.groups);
-  if (rows > 0 && a.blocks >= 8)  // fewer scales than a word: the few rows' kernel alone reads them byte by byte
+  if (rows > 0 && a.blocks >= 16)  // fewer scales than a piece: the few rows' kernel alone reads them byte by byte
     return dtype == SPP_DTYPE_BF16 ? launch_tiles<X, false, __bf16>(a, rows, st) : launch_tiles<X, false, float>(a, rows, st);
   return dtype == SPP_DTYPE_BF16 ? launch_few<X, false, __bf16, kRowsStart>(a, a.groups, st)
                                  : launch_few<X, false, float, kRowsStart>(a, a.groups, st);

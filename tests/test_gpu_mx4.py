@@ -218,6 +218,14 @@ def test_matmul_groups(torch, M, N, K, G, kind, act):
 
 
 @pytest.mark.parametrize("act", ["bf16", "mx4"])
+@pytest.mark.parametrize("M,N,K,G,kind", [
+    (2500, 3100, 160, 1, ""), (4000, 2100, 2304, 1, ""), (4200, 2050, 1152, 1, ""), (9000, 1030, 64, 1, ""), (5000, 1290, 800, 9, "skewed"),
+    (7000, 1000, 1312, 20, "gaps"), (16000, 520, 32, 40, "skewed")])
+def test_matmul_of_several_tiles_a_workgroup(torch, M, N, K, G, kind, act):
+    check_matmul(np.random.default_rng(M + N + K + G), M, N, K, G, kind, act, "bf16" if N % 4 else "f32")
+
+
+@pytest.mark.parametrize("act", ["bf16", "mx4"])
 @pytest.mark.parametrize("M", [3, 50, 400])
 def test_matmul_strides(torch, act, M):
     for x_pad, out_pad, dtype in ((8, 1, "bf16"), (24, 3, "f32"), (0, 2, "bf16"), (64, 8, "bf16"), (8, 4, "f32")):
