@@ -651,7 +651,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     stage = 0;
   };
 
-  const int stages = (a.nb + BL - 1) / BL, padded = (stages + kBuffers - 1) / kBuffers * kBuffers;
+  const int stages = max((a.nb + BL - 1) / BL, 2);  // two at least: one may be of zeros
   struct Scales {
     u32x4 v[SI];
     int last[SI];
@@ -716,136 +716,84 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   uint32_t at_a = (l32 * AC + swizzled<AC>(l32, half * KB)) * 16 + wf * 64 * AC * 16;
   uint32_t at_b = (l32 * BC + swizzled<BC>(l32, half * (BC / 2))) * 16 + wt * 32 * CT * BC * 16;
   uint32_t at_sa = (wf * 64 + l32) * sizeof(Word) + half * KB, at_sb = (wt * 32 * CT + l32) * sizeof(Word) + half * KB;
-  const auto products = [&](const uint8_t* in_a, const uint8_t* in_b, const Word* in_sa, const Word* in_sb) {
-    asm volatile("" : "+v"(at_a), "+v"(at_b), "+v"(at_sa), "+v"(at_sb));
-    const auto read_a = [&](int i, int c) {
-      return *reinterpret_cast<const u32x4*>(in_a + (at_a ^ (c << 4)) + i * 32 * AC * 16);
-    };
-    const auto read_b = [&](int i, int c) {
-      return *reinterpret_cast<const u32x4*>(in_b + (at_b ^ (c << 4)) + i * 32 * BC * 16);
-    };
+  // Half of a stage's operands: two blocks, or one beside bf16 rows of x
+  constexpr int HA = kMx4 ? 2 : 1, HB = kMx4 ? 2 : 4;
+  struct Half {
+    u32x4 a[HA][2], b[HB][CT];
+  };
+  struct StageScales {
+    uint32_t a[2], b[CT];
+  };
+  const auto read_half = [&](Half& h, const uint8_t* in_a, const uint8_t* in_b, auto which) {
+    asm volatile("" : "+v"(at_a), "+v"(at_b));
+#pragma unroll
+    for (int k = 0; k < HA; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        h.a[k][i] = *reinterpret_cast<const u32x4*>(in_a + (at_a ^ ((which * HA + k) << 4)) + i * 32 * AC * 16);
+#pragma unroll
+    for (int k = 0; k < HB; ++k)
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+        h.b[k][c] = *reinterpret_cast<const u32x4*>(in_b + (at_b ^ ((which * HB + k) << 4)) + c * 32 * BC * 16);
+  };
+  const auto read_scales = [&](StageScales& to, int st) {
+    asm volatile("" : "+v"(at_sa), "+v"(at_sb));
     const auto scale = [&](const Word* in, uint32_t at, int i) -> uint32_t {
       const uint8_t* p = reinterpret_cast<const uint8_t*>(in) + at + i * 32 * sizeof(Word);
       return kMx4 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
     };
-    uint32_t sa[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) sa[i] = scale(in_sa, at_sa, i);
-    if constexpr (kMx4) {
-      uint32_t sb[CT];
+    for (int i = 0; i < 2; ++i) to.a[i] = scale(s_sa[st % kAtOnce], at_sa, i);
 #pragma unroll
-      for (int i = 0; i < CT; ++i) sb[i] = scale(in_sb, at_sb, i);
-      u32x4 va[KB][2], vb[KB][CT];
+    for (int c = 0; c < CT; ++c) to.b[c] = kMx4 ? scale(s_sb[st % kAtOnce], at_sb, c) : 0;
+  };
+  const auto products = [&](const Half& h, const StageScales& scales, auto which) {
 #pragma unroll
-      for (int b = 0; b < KB; ++b) {
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (kMx4) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) va[b][i] = read_a(i, b);
+        for (int c = 0; c < CT; ++c) acc[i][c] = mfma_mx4_32<2 * which>(h.a[0][i], scales.a[i], h.b[0][c], scales.b[c], acc[i][c]);
+      } else {
 #pragma unroll
-        for (int i = 0; i < CT; ++i) vb[b][i] = read_b(i, b);
-      }
-      const auto block = [&](auto b) {
+        for (int q = 0; q < 2; ++q) {
+          const bf16x8 w = __builtin_bit_cast(bf16x8, cvt8(h.a[0][i][q], scale_of((scales.a[i] >> (8 * which)) & 255u)));
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int c = 0; c < CT; ++c) acc[i][c] = mfma_mx4_32<b>(va[b][i], sa[i], vb[b][c], sb[c], acc[i][c]);
-      };
-      block(Const<0>{});
-      block(Const<1>{});
-      block(Const<2>{});
-      block(Const<3>{});
-      // two blocks are read ahead of the products, the others between them
-      constexpr int kReads = 2 + CT;
-      __builtin_amdgcn_sched_group_barrier(kSchedReads, 2 * kReads + 2, 0);
-#pragma unroll
-      for (int i = 0; i < 2 * kReads; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kSchedProducts, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kSchedReads, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(kSchedProducts, 8 * CT - 2 * kReads, 0);
-    } else {
-      u32x4 va[KB][2];
-#pragma unroll
-      for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) va[b][i] = read_a(i, b);
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          u32x4 vb[CT];
-#pragma unroll
-          for (int c = 0; c < CT; ++c) vb[c] = read_b(c, 4 * b + q);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const bf16x8 w = __builtin_bit_cast(bf16x8, cvt8(va[b][i][q], scale_of((sa[i] >> (8 * b)) & 255u)));
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-              acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, vb[c]), acc[i][c], 0, 0, 0);
-          }
+          for (int c = 0; c < CT; ++c)
+            acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, h.b[q][c]), acc[i][c], 0, 0, 0);
         }
       }
-      // the weights and two quarters of x are read ahead of the products
-      __builtin_amdgcn_sched_group_barrier(kSchedReads, 2 + 2 * KB + 2 * CT, 0);
+    }
 #pragma unroll
-      for (int i = 0; i < (4 * KB - 2) * CT; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kSchedProducts, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(kSchedReads, 1, 0);
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (kMx4) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+          acc[i][c] = mfma_mx4_32<2 * which + 1>(h.a[HA - 1][i], scales.a[i], h.b[1][c], scales.b[c], acc[i][c]);
+      } else {
+#pragma unroll
+        for (int q = 2; q < 4; ++q) {
+          const bf16x8 w = __builtin_bit_cast(bf16x8, cvt8(h.a[0][i][q], scale_of((scales.a[i] >> (8 * which)) & 255u)));
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+            acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, h.b[q % HB][c]), acc[i][c], 0, 0, 0);
+        }
       }
-      __builtin_amdgcn_sched_group_barrier(kSchedProducts, 4 * CT, 0);
     }
-    __builtin_amdgcn_sched_barrier(0);  // the products go before what follows
+    // the reads of the other half go between them
+    constexpr int kProducts = (kMx4 ? 4 : 8) * CT;
+#pragma unroll
+    for (int i = 0; i < kProducts; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSchedProducts, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSchedReads, kMx4 ? 2 : 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
-  Scales in_tile, of_next;
-  const auto step = [&](int st, auto buf) {
-    if (st % kAtOnce == 1 && st + kAtOnce - 1 < stages) load_scales(in_tile, st + kAtOnce - 1);
-    issue(Const<(buf + 2) % kBuffers>{});
-    if (st < stages) products(a_of(buf), b_of(buf), s_sa[st % kAtOnce], s_sb[st % kAtOnce]);
-    wait_loads<kStageLoads>();
-    if (st % kAtOnce == kAtOnce - 1 && st + 1 < stages) {
-      lds_barrier();  // these scales are no longer read
-      put_scales(in_tile, st + 1);
-    }
-    lds_barrier();
-  };
-
-  Tile t = find(job);
-  fetch(t);
-  setup(t);
-  load_scales(of_next, 0);
-  issue(Const<0>{});
-  issue(Const<1>{});
-  wait_loads<kStageLoads>();
-  put_scales(of_next, 0);
-  lds_barrier();
-  for (;;) {
-    job += stride;
-    const bool more = job < xcd_end;
-    Tile next = t;
-    if (more) {
-      next = find(job);
-      fetch(next);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) acc[i][c][j] = 0.f;
-    for (int st = 0; st < padded; st += kBuffers) {
-      step(st, Const<0>{});
-      if (st + kBuffers == padded) {
-        if (more) setup(next);
-        load_scales(of_next, 0);
-      }
-      step(st + 1, Const<1>{});
-      step(st + 2, Const<2>{});
-    }
-    put_scales(of_next, 0);  // read after the barrier below
-
-    // A lane holds 32 neighbouring outputs of a row (16 of both for SwiGLU).  bf16
-    // results go through the third buffer, which nothing is loaded into now, so
-    // that whole cache lines are written.
-    uint8_t* mine = kA >= 8 * 4096 ? s_a2 + wave * 4096 : wave < 4 ? s_a2 + wave * 4096 : s_b2 + (wave - 4) * 4096;
+  // A lane holds 32 neighbouring outputs of a row (16 of both for SwiGLU).  bf16
+  // results go through the buffer of the last stage, which nothing is loaded into
+  // now, so that whole cache lines are written.
+  const auto write_out = [&](const Tile& t, auto buf) {
+    uint8_t* mine = kA >= 8 * 4096 || wave < 4 ? a_of(buf) + wave * 4096 : b_of(buf) + (wave - 4) * 4096;
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const int r0 = (wt * CT + c) * 32, r = r0 + l32;
@@ -928,9 +876,74 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
         }
       }
     }
-    if (!more) break;
-    lds_barrier();  // the third buffer is loaded into again
+  };
+
+  Tile t = find(job), next = t;
+  fetch(t);
+  setup(t);
+  Scales scales;
+  Half first, second;
+  StageScales now, then;
+  load_scales(scales, 0);
+  issue(Const<0>{});
+  issue(Const<1>{});
+  wait_loads<kStageLoads>();
+  put_scales(scales, 0);
+  lds_barrier();
+  read_scales(now, 0);
+  read_half(first, s_a0, s_b0, Const<0>{});
+  int st = 0;
+  bool more;
+  const auto begin = [&]() {
+    st = 0;
+    job += stride;
+    more = job < xcd_end;
+    if (more) {
+      next = find(job);
+      fetch(next);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[i][c][j] = 0.f;
+  };
+  // A stage; whether it was the last one.  Its first half is in registers when it
+  // begins, and the next one's when it ends, so that the matrix units have work on
+  // both sides of the barrier that the stage's loads need.
+  const auto step = [&](auto buf) -> bool {
+    constexpr int kNext = (buf + 1) % kBuffers;
+    if (st % kAtOnce == 1 && st + kAtOnce - 1 < stages) load_scales(scales, st + kAtOnce - 1);
+    if (st + 2 == stages && more) {
+      setup(next);
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // scalar loads: not waited for later, with the LDS reads
+    }
+    issue(Const<(buf + 2) % kBuffers>{});
+    read_half(second, a_of(buf), b_of(buf), Const<1>{});
+    products(first, now, Const<0>{});
+    wait_loads<kStageLoads>();
+    lds_barrier();
+    const bool last = st + 1 == stages;
+    if (last || st % kAtOnce == kAtOnce - 1) {  // the scales there are no longer read
+      put_scales(scales, last ? 0 : st + 1);
+      lds_barrier();
+    }
+    if (st + 2 == stages) load_scales(scales, 0);
+    read_scales(then, last ? 0 : st + 1);
+    read_half(first, a_of(Const<kNext>{}), b_of(Const<kNext>{}), Const<0>{});
+    products(second, now, Const<1>{});
+    now = then;
+    if (++st < stages) return false;
+    write_out(t, buf);
+    if (!more) return true;
+    lds_barrier();  // the buffer is loaded into again
     t = next;
+    begin();
+    return false;
+  };
+  begin();
+  while (!step(Const<0>{}) && !step(Const<1>{}) && !step(Const<2>{})) {
   }
   wait_loads<0>();  // nothing may come to this workgroup's LDS after its end
 }
