@@ -497,7 +497,7 @@ __device__ __forceinline__ int rows_of(const ProductArgs& a, int g, int* first) 
 // rows of one group.  A workgroup stays on its compute unit and takes tiles one
 // after the other, neighbouring tiles on one XCD.  K goes through LDS in stages
 // of 128 bytes of a row in 4 bits (64 beside bf16 rows of x, whose stages are 256
-// bytes), in three buffers that are loaded two stages ahead, over the tiles'
+// bytes), in three buffers that are loaded two to three stages ahead, over the tiles'
 // borders: the next tile's first stages are on their way while this one's last
 // are multiplied and its results written.  A wave takes 64 of the weight rows
 // and half of the rows of x.
@@ -514,7 +514,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   constexpr int TM = 64 * CT;
   constexpr int kA = kTileRows * AC * 16, kB = TM * BC * 16;
   constexpr int AI = kTileRows * AC / kTileThreads, BI = TM * BC / kTileThreads;  // loads of a wave
-  constexpr int kStageLoads = AI + BI;
   using Word = typename std::conditional<kMx4, uint64_t, uint32_t>::type;  // a row's scales of a stage
   // Scales come four stages at a time, in pieces of 16 bytes: by the stage, every
   // row would ask for a cache line of its own, as many as its codes do.
@@ -651,7 +650,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     stage = 0;
   };
 
-  const int stages = max((a.nb + BL - 1) / BL, 2);  // two at least: one may be of zeros
+  const int stages = max((a.nb + BL - 1) / BL, kBuffers);  // as many as are on their way: some may be of zeros
   struct Scales {
     u32x4 v[SI];
     int last[SI];
@@ -780,7 +779,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
         }
       }
     }
-    // the reads of the other half go between them
+    // reads of the other half go between them
     constexpr int kProducts = (kMx4 ? 4 : 8) * CT;
 #pragma unroll
     for (int i = 0; i < kProducts; ++i) {
@@ -887,7 +886,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   load_scales(scales, 0);
   issue(Const<0>{});
   issue(Const<1>{});
-  wait_loads<kStageLoads>();
+  issue(Const<2>{});
+  wait_loads<2 * (AI + BI)>();
   put_scales(scales, 0);
   lds_barrier();
   read_scales(now, 0);
@@ -911,18 +911,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   };
   // A stage; whether it was the last one.  Its first half is in registers when it
   // begins, and the next one's when it ends, so that the matrix units have work on
-  // both sides of the barrier that the stage's loads need.
+  // both sides of the barrier that the stage's loads need.  Behind the barrier
+  // nothing reads its buffer any more: it takes the stage after the next two.
   const auto step = [&](auto buf) -> bool {
     constexpr int kNext = (buf + 1) % kBuffers;
     if (st % kAtOnce == 1 && st + kAtOnce - 1 < stages) load_scales(scales, st + kAtOnce - 1);
-    if (st + 2 == stages && more) {
-      setup(next);
-      __builtin_amdgcn_s_waitcnt(0xc07f);  // scalar loads: not waited for later, with the LDS reads
-    }
-    issue(Const<(buf + 2) % kBuffers>{});
     read_half(second, a_of(buf), b_of(buf), Const<1>{});
     products(first, now, Const<0>{});
-    wait_loads<kStageLoads>();
+    wait_loads<AI + BI>();
     lds_barrier();
     const bool last = st + 1 == stages;
     if (last || st % kAtOnce == kAtOnce - 1) {  // the scales there are no longer read
@@ -930,6 +926,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
       lds_barrier();
     }
     if (st + 2 == stages) load_scales(scales, 0);
+    if (!last) {
+      if (st + kBuffers == stages && more) {
+        setup(next);
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // scalar loads: not waited for later, with the LDS reads
+      }
+      issue(buf);
+    }
     read_scales(then, last ? 0 : st + 1);
     read_half(first, a_of(Const<kNext>{}), b_of(Const<kNext>{}), Const<0>{});
     products(second, now, Const<1>{});
@@ -938,6 +941,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     write_out(t, buf);
     if (!more) return true;
     lds_barrier();  // the buffer is loaded into again
+    issue(buf);
     t = next;
     begin();
     return false;
