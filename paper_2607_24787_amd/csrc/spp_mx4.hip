@@ -525,7 +525,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   __shared__ __attribute__((aligned(16))) uint8_t s_b0[kB], s_b1[kB], s_b2[kB];
   __shared__ Word s_sa[kAtOnce][kTileRows];
   __shared__ Word s_sb[kAtOnce][kMx4 ? TM : 1];
-  __shared__ int s_before[spp::kMaxExpertsTopK];  // tiles of the groups before
+  // Tiles of the groups before each one, and where they are few their first rows
+  // and rows, which would take a round trip a tile
+  constexpr int kKept = spp::kMaxExpertsTopK / 3;
+  __shared__ int s_before[spp::kMaxExpertsTopK];
   int* s_sum = reinterpret_cast<int*>(s_sa);
   const auto a_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_a0 : buf == 1 ? s_a1 : s_a2; };
   const auto b_of = [&](auto buf) -> uint8_t* { return buf == 0 ? s_b0 : buf == 1 ? s_b1 : s_b2; };
@@ -535,9 +538,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   // tiles of the groups before each one (thread t: groups 2t and 2t + 1)
   int row_tiles = (a.M + TM - 1) / TM;
   if (a.start) {
-    int n[2], first;
+    int n[2], first[2], rows[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) n[j] = 2 * tid + j < a.groups ? (rows_of(a, 2 * tid + j, &first) + TM - 1) / TM : 0;
+    for (int j = 0; j < 2; ++j) {
+      rows[j] = 2 * tid + j < a.groups ? rows_of(a, 2 * tid + j, &first[j]) : 0;
+      n[j] = (rows[j] + TM - 1) / TM;
+    }
     int incl = n[0] + n[1];
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -554,8 +560,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
       row_tiles += s_sum[w];
     }
     __syncthreads();
-    s_before[2 * tid] = base;
-    s_before[2 * tid + 1] = base + n[0];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int g = 2 * tid + j;
+      if (g >= a.groups) break;
+      s_before[g] = base + (j ? n[0] : 0);
+      if (a.groups <= kKept) s_before[kKept + g] = first[j], s_before[2 * kKept + g] = rows[j];
+    }
     __syncthreads();
   }
   row_tiles = __builtin_amdgcn_readfirstlane(row_tiles);
@@ -580,8 +591,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
       int n = 0;
       for (int g = lane; g - lane < a.groups; g += 64) n += __popcll(__ballot(g < a.groups && s_before[g] <= tile));
       t.group = n - 1;  // the last one with no more tiles before it: those without rows have as many as the next
-      int first;
-      const int rows = rows_of(a, t.group, &first), at = (tile - s_before[t.group]) * TM;
+      int first, rows;
+      if (a.groups <= kKept)
+        first = s_before[kKept + t.group], rows = s_before[2 * kKept + t.group];
+      else
+        rows = rows_of(a, t.group, &first);
+      const int at = (tile - s_before[t.group]) * TM;
       t.first = __builtin_amdgcn_readfirstlane(first + at);
       t.count = __builtin_amdgcn_readfirstlane(min(rows - at, TM));
     }
@@ -792,6 +807,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   // results go through the buffer of the last stage, which nothing is loaded into
   // now, so that whole cache lines are written.
   const auto write_out = [&](const Tile& t, auto buf) {
+    wait_loads<0>();  // the next tile's first two stages
     uint8_t* mine = kA >= 8 * 4096 || wave < 4 ? a_of(buf) + wave * 4096 : b_of(buf) + (wave - 4) * 4096;
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
@@ -887,7 +903,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   issue(Const<0>{});
   issue(Const<1>{});
   issue(Const<2>{});
-  wait_loads<2 * (AI + BI)>();
+  wait_loads<AI + BI>();
   put_scales(scales, 0);
   lds_barrier();
   read_scales(now, 0);
@@ -918,7 +934,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     if (st % kAtOnce == 1 && st + kAtOnce - 1 < stages) load_scales(scales, st + kAtOnce - 1);
     read_half(second, a_of(buf), b_of(buf), Const<1>{});
     products(first, now, Const<0>{});
-    wait_loads<AI + BI>();
+    if (st > 0) wait_loads<AI + BI>();  // a tile's second stage was there before the last one's results were written
     lds_barrier();
     const bool last = st + 1 == stages;
     if (last || st % kAtOnce == kAtOnce - 1) {  // the scales there are no longer read
