@@ -7,6 +7,7 @@
 #include <cstdint>
 #include <cstring>
 #include <type_traits>
+#include <utility>
 
 #include "spp.h"
 #include "spp_fp4.h"
@@ -453,12 +454,21 @@ constexpr int kXcds = 8;
 constexpr int kTileWorkgroups = 256;  // one on each compute unit
 constexpr int kBuffers = 3;
 constexpr int kBand = 8;
-constexpr int kSchedProducts = 0x008, kSchedReads = 0x100;  // matrix instructions, LDS reads
 
 __device__ const u32x4 kZeros = {0, 0, 0, 0};
 
 template <int N>
 using Const = std::integral_constant<int, N>;
+
+template <int... I, typename F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) {
+  (f(Const<I>{}), ...);
+}
+// f(0), f(1), .. f(N - 1), as constants
+template <int N, typename F>
+__device__ __forceinline__ void for_each(F f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
+}
 
 // 16 bytes from global memory to `to` + 16 * lane of LDS
 __device__ __forceinline__ void to_lds(const uint8_t* from, uint8_t* to) {
@@ -497,7 +507,7 @@ __device__ __forceinline__ int rows_of(const ProductArgs& a, int g, int* first) 
 // rows of one group.  A workgroup stays on its compute unit and takes tiles one
 // after the other, neighbouring tiles on one XCD.  K goes through LDS in stages
 // of 128 bytes of a row in 4 bits (64 beside bf16 rows of x, whose stages are 256
-// bytes), in three buffers that are loaded two to three stages ahead, over the tiles'
+// bytes), in three buffers that are loaded two stages ahead, over the tiles'
 // borders: the next tile's first stages are on their way while this one's last
 // are multiplied and its results written.  A wave takes 64 of the weight rows
 // and half of the rows of x.
@@ -665,7 +675,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     stage = 0;
   };
 
-  const int stages = max((a.nb + BL - 1) / BL, kBuffers);  // as many as are on their way: some may be of zeros
+  const int stages = max((a.nb + BL - 1) / BL, 2);  // two at least: one may be of zeros
   struct Scales {
     u32x4 v[SI];
     int last[SI];
@@ -709,19 +719,21 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
       }
     }
   };
-  // The next stage into a buffer: always as many loads, since waits count them
-  const auto issue = [&](auto buf) {
+  // Load l of the next stage into a buffer: always as many, since waits count them
+  constexpr int kLoads = AI + BI;
+  const auto issue = [&](auto l, auto buf) {
     const int b0 = stage * BL;
-#pragma unroll
-    for (int i = 0; i < AI; ++i)
+    if constexpr (l < AI) {
+      constexpr int i = l;
       to_lds(base[((i * kTileWaves + wave) * (64 / AC) >> 5) & 1] + (pa[i] + (b0 + ca[i] < a.nb ? b0 + ca[i] : 0) * 16),
              a_of(buf) + (i * kTileWaves + wave) * 1024);
-#pragma unroll
-    for (int i = 0; i < BI; ++i)
+    } else {
+      constexpr int i = l - AI;
       to_lds(b0 + cb[i] / (BC / BL) < a.nb ? pb[i] + static_cast<int64_t>(b0) * (BC / BL * 16)
                                            : reinterpret_cast<const uint8_t*>(&kZeros),
              b_of(buf) + (i * kTileWaves + wave) * 1024);
-    ++stage;
+    }
+    if constexpr (l == kLoads - 1) ++stage;
   };
   f32x16 acc[2][CT];
   // where this lane reads: its row's first piece, and the others by exclusive or
@@ -738,18 +750,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   struct StageScales {
     uint32_t a[2], b[CT];
   };
-  const auto read_half = [&](Half& h, const uint8_t* in_a, const uint8_t* in_b, auto which) {
-    asm volatile("" : "+v"(at_a), "+v"(at_b));
-#pragma unroll
-    for (int k = 0; k < HA; ++k)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        h.a[k][i] = *reinterpret_cast<const u32x4*>(in_a + (at_a ^ ((which * HA + k) << 4)) + i * 32 * AC * 16);
-#pragma unroll
-    for (int k = 0; k < HB; ++k)
-#pragma unroll
-      for (int c = 0; c < CT; ++c)
-        h.b[k][c] = *reinterpret_cast<const u32x4*>(in_b + (at_b ^ ((which * HB + k) << 4)) + c * 32 * BC * 16);
+  constexpr int kReads = 2 * HA + HB * CT;
+  const auto read = [&](Half& h, const uint8_t* in_a, const uint8_t* in_b, auto which, auto r) {
+    if constexpr (r < 2 * HA) {
+      constexpr int k = r / 2, i = r % 2;
+      h.a[k][i] = *reinterpret_cast<const u32x4*>(in_a + (at_a ^ ((which * HA + k) << 4)) + i * 32 * AC * 16);
+    } else {
+      constexpr int k = (r - 2 * HA) / CT, c = (r - 2 * HA) % CT;
+      h.b[k][c] = *reinterpret_cast<const u32x4*>(in_b + (at_b ^ ((which * HB + k) << 4)) + c * 32 * BC * 16);
+    }
   };
   const auto read_scales = [&](StageScales& to, int st) {
     asm volatile("" : "+v"(at_sa), "+v"(at_sb));
@@ -762,46 +771,36 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
 #pragma unroll
     for (int c = 0; c < CT; ++c) to.b[c] = kMx4 ? scale(s_sb[st % kAtOnce], at_sb, c) : 0;
   };
-  const auto products = [&](const Half& h, const StageScales& scales, auto which) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
+  // The products of half a stage.  Between them, one at a time, go the reads of
+  // the half after it and half of the next stage's loads: eight waves that issue
+  // all of them at once wait 1,300 cycles until they are accepted.
+  const auto products = [&](const Half& h, const StageScales& scales, auto which, Half& next, auto next_buf, auto load_buf) {
+    asm volatile("" : "+v"(at_a), "+v"(at_b));
+    constexpr int kProducts = (kMx4 ? 4 : 8) * CT, kFirst = (kLoads + 1) / 2;
+    constexpr int kFrom = which == 0 ? 0 : kFirst, kCount = which == 0 ? kFirst : kLoads - kFirst;
+    u32x4 w[2];
+    for_each<kProducts>([&](auto k) {
+      constexpr int b = k / (2 * CT), i = k / CT % 2, c = k % CT;
       if constexpr (kMx4) {
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[i][c] = mfma_mx4_32<2 * which>(h.a[0][i], scales.a[i], h.b[0][c], scales.b[c], acc[i][c]);
+        acc[i][c] = mfma_mx4_32<2 * which + b>(h.a[b][i], scales.a[i], h.b[b][c], scales.b[c], acc[i][c]);
       } else {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const bf16x8 w = __builtin_bit_cast(bf16x8, cvt8(h.a[0][i][q], scale_of((scales.a[i] >> (8 * which)) & 255u)));
-#pragma unroll
-          for (int c = 0; c < CT; ++c)
-            acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, h.b[q][c]), acc[i][c], 0, 0, 0);
-        }
+        if constexpr (c == 0) w[i] = cvt8(h.a[0][i][b], scale_of((scales.a[i] >> (8 * which)) & 255u));
+        acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[i]),
+                                                            __builtin_bit_cast(bf16x8, h.b[b][c]), acc[i][c], 0, 0, 0);
       }
-    }
+      for_each<(k + 1) * kReads / kProducts - k * kReads / kProducts>([&](auto r) {
+        read(next, a_of(next_buf), b_of(next_buf), Const<1 - which>{}, Const<k * kReads / kProducts + r>{});
+      });
+      for_each<(k + 1) * kCount / kProducts - k * kCount / kProducts>([&](auto l) {
+        issue(Const<kFrom + k * kCount / kProducts + l>{}, load_buf);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    // else the compiler moves the products over the branches and barriers that follow
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if constexpr (kMx4) {
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
-          acc[i][c] = mfma_mx4_32<2 * which + 1>(h.a[HA - 1][i], scales.a[i], h.b[1][c], scales.b[c], acc[i][c]);
-      } else {
-#pragma unroll
-        for (int q = 2; q < 4; ++q) {
-          const bf16x8 w = __builtin_bit_cast(bf16x8, cvt8(h.a[0][i][q], scale_of((scales.a[i] >> (8 * which)) & 255u)));
-#pragma unroll
-          for (int c = 0; c < CT; ++c)
-            acc[i][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, __builtin_bit_cast(bf16x8, h.b[q % HB][c]), acc[i][c], 0, 0, 0);
-        }
-      }
-    }
-    // reads of the other half go between them
-    constexpr int kProducts = (kMx4 ? 4 : 8) * CT;
-#pragma unroll
-    for (int i = 0; i < kProducts; ++i) {
-      __builtin_amdgcn_sched_group_barrier(kSchedProducts, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kSchedReads, kMx4 ? 2 : 1, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+      for (int c = 0; c < CT; ++c) asm volatile("" : "+v"(acc[i][c]));
   };
   // A lane holds 32 neighbouring outputs of a row (16 of both for SwiGLU).  bf16
   // results go through the buffer of the last stage, which nothing is loaded into
@@ -900,14 +899,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   Half first, second;
   StageScales now, then;
   load_scales(scales, 0);
-  issue(Const<0>{});
-  issue(Const<1>{});
-  issue(Const<2>{});
-  wait_loads<AI + BI>();
+  for_each<kLoads>([&](auto l) { issue(l, Const<0>{}); });
+  for_each<kLoads>([&](auto l) { issue(l, Const<1>{}); });
+  wait_loads<0>();
   put_scales(scales, 0);
   lds_barrier();
   read_scales(now, 0);
-  read_half(first, s_a0, s_b0, Const<0>{});
+  for_each<kReads>([&](auto r) { read(first, s_a0, s_b0, Const<0>{}, r); });
   int st = 0;
   bool more;
   const auto begin = [&]() {
@@ -927,44 +925,37 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   };
   // A stage; whether it was the last one.  Its first half is in registers when it
   // begins, and the next one's when it ends, so that the matrix units have work on
-  // both sides of the barrier that the stage's loads need.  Behind the barrier
-  // nothing reads its buffer any more: it takes the stage after the next two.
+  // both sides of the barrier that the stage's loads need.
   const auto step = [&](auto buf) -> bool {
-    constexpr int kNext = (buf + 1) % kBuffers;
-    if (st % kAtOnce == 1 && st + kAtOnce - 1 < stages) load_scales(scales, st + kAtOnce - 1);
-    read_half(second, a_of(buf), b_of(buf), Const<1>{});
-    products(first, now, Const<0>{});
-    if (st > 0) wait_loads<AI + BI>();  // a tile's second stage was there before the last one's results were written
+    constexpr int kNext = (buf + 1) % kBuffers, kAfter = (buf + 2) % kBuffers;
+    if (st + 2 == stages && more) {
+      setup(next);
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // scalar loads: not waited for later, with the LDS reads
+    }
+    products(first, now, Const<0>{}, second, buf, Const<kAfter>{});
+    wait_loads<(kLoads + 1) / 2>();  // all but what this stage has issued: the next one is there
     lds_barrier();
     const bool last = st + 1 == stages;
     if (last || st % kAtOnce == kAtOnce - 1) {  // the scales there are no longer read
       put_scales(scales, last ? 0 : st + 1);
       lds_barrier();
     }
-    if (st + 2 == stages) load_scales(scales, 0);
-    if (!last) {
-      if (st + kBuffers == stages && more) {
-        setup(next);
-        __builtin_amdgcn_s_waitcnt(0xc07f);  // scalar loads: not waited for later, with the LDS reads
-      }
-      issue(buf);
-    }
+    if (st + 2 == stages || (st % kAtOnce == kAtOnce - 2 && st + 2 < stages)) load_scales(scales, st + 2 == stages ? 0 : st + 2);
     read_scales(then, last ? 0 : st + 1);
-    read_half(first, a_of(Const<kNext>{}), b_of(Const<kNext>{}), Const<0>{});
-    products(second, now, Const<1>{});
+    products(second, now, Const<1>{}, first, Const<kNext>{}, Const<kAfter>{});
     now = then;
     if (++st < stages) return false;
     write_out(t, buf);
     if (!more) return true;
     lds_barrier();  // the buffer is loaded into again
-    issue(buf);
     t = next;
     begin();
     return false;
   };
   begin();
-  while (!step(Const<0>{}) && !step(Const<1>{}) && !step(Const<2>{})) {
-  }
+  if (!step(Const<0>{}))
+    while (!step(Const<1>{}) && !step(Const<2>{}) && !step(Const<0>{})) {
+    }
   wait_loads<0>();  // nothing may come to this workgroup's LDS after its end
 }
 
