@@ -284,7 +284,8 @@ __device__ __forceinline__ int find_pairs(const ProductArgs& a, Ids ids, int gro
 }
 
 // A workgroup takes a.run tiles of 16 * NT outputs (of both matrices for SwiGLU)
-// of one group, for 16 of its rows at a time; its waves share K, kStep blocks of
+// of one group, for 16 of its rows at a time (where groups have more, gridDim.z
+// workgroups take these in turn); its waves share K, kStep blocks of
 // a lane at a time.  A tile's weights are on their way while the one before is
 // multiplied, the first one's before the rows are known; the ids that tell them
 // go before the weights, since loads return in order.  kHold: K is one step, and
@@ -308,7 +309,7 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
       begin = min(max(a.start[group], 0), a.M);
       count = min(max(a.start[group + 1], 0), a.M) - begin;
     }
-    if (count <= 0) return;
+    if (count <= 16 * static_cast<int>(blockIdx.z)) return;
   }
   const int per = (a.nb + 4 * kFewWaves - 1) / (4 * kFewWaves);
   const int b0 = (wave * 4 + g) * per, b1 = min(b0 + per, a.nb);
@@ -324,7 +325,8 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
   };
   Weights even, odd;
   load(even, from, 0);
-  for (int r0 = 0;; r0 += 16) {
+  const int r_first = 16 * static_cast<int>(blockIdx.z), r_step = 16 * static_cast<int>(gridDim.z);
+  for (int r0 = r_first;; r0 += r_step) {
     if constexpr (kRows == kRowsIds) {
       int first;
       count = find_pairs(a, ids, group, r0, s_row, &first);
@@ -388,7 +390,7 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
       take(even, odd, tile);
       if (tile + 1 < to) take(odd, even, tile + 1);
     }
-    if (r0 + 16 >= count) return;
+    if (r0 + r_step >= count) return;
     load(even, from, 0);
     lds_barrier();
   }
@@ -994,10 +996,10 @@ unsigned quant_grid(int64_t words) {
   return static_cast<unsigned>(std::min<int64_t>((words + kQuantThreads - 1) / kQuantThreads, 1 << 20));
 }
 
-hipError_t launch2(void (*kernel)(ProductArgs), unsigned x, unsigned y, unsigned threads, const ProductArgs& a,
+hipError_t launch3(void (*kernel)(ProductArgs), unsigned x, unsigned y, unsigned z, unsigned threads, const ProductArgs& a,
                    hipStream_t st) {
   void* params[] = {const_cast<ProductArgs*>(&a)};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(x, y), dim3(threads), params, 0, st);
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(x, y, z), dim3(threads), params, 0, st);
 }
 
 constexpr int kLastTokens = 2;  // at most, of mx4_last_kernel
@@ -1068,12 +1070,16 @@ constexpr int kRunGroups = 512;  // workgroups that are resident together, about
 template <int X, bool kSwiglu, int NT, int kStep, typename Out, int kRows>
 hipError_t launch_few(ProductArgs a, int64_t groups, bool hold, hipStream_t st) {
   const int tiles = (a.N + 16 * NT - 1) / (16 * NT);
-  a.run = static_cast<int>(std::min<int64_t>((groups * tiles + kRunGroups - 1) / kRunGroups, 16));
+  const int64_t all = groups * tiles, slices = kRows == kRowsStart ? (a.M / groups + 15) / 16 : 1;
+  a.run = static_cast<int>(std::min<int64_t>((all + kRunGroups - 1) / kRunGroups, 16));
+  // rows beyond 16 of a group beside one another, until the card is full
+  const int64_t z = std::min<int64_t>(std::max<int64_t>(kRunGroups * 4 / all, 1), std::max<int64_t>(slices, 1));
   auto kernel = hold ? mx4_few_kernel<X, kSwiglu, NT, kStep, true, false, Out, kRows>
                      : mx4_few_kernel<X, kSwiglu, NT, kStep, false, false, Out, kRows>;
   if constexpr (NT == 1 && kStep == 2)
     if (a.nb < kStep || a.blocks < 4) kernel = mx4_few_kernel<X, kSwiglu, NT, kStep, true, true, Out, kRows>;
-  return launch2(kernel, static_cast<unsigned>((tiles + a.run - 1) / a.run), static_cast<unsigned>(groups), kFewThreads, a, st);
+  return launch3(kernel, static_cast<unsigned>((tiles + a.run - 1) / a.run), static_cast<unsigned>(groups),
+                 static_cast<unsigned>(z), kFewThreads, a, st);
 }
 
 template <int X, bool kSwiglu, int NT, typename Out, int kRows>
@@ -1106,12 +1112,32 @@ hipError_t launch_tile(ProductArgs a, hipStream_t st) {
   return launch(mx4_tile_kernel<X, kSwiglu, Out, CT>, static_cast<unsigned>(grid), kTileThreads, a, st);
 }
 
-// Rows of x that a tile takes, by the mean of a group's; 0: few rows
-constexpr int kFewRows = 20;
-int tile_rows(int64_t M, int groups) {
-  const int64_t mean = M / groups;
-  return mean >= 64 ? 128 : mean >= kFewRows ? 64 : 0;
+// What a product takes, about, in us: rounds of 256 tiles, each of them a start
+// and its stages; 128 rows instead of 64 take 1.2 (x in 4 bits) to 1.45 times as
+// long.  Measured for one round at K = 512 .. 4,096: 7.4 .. 34 (bf16), 6.0 .. 15
+// (4 bits).  A group's last tile is half full on average.
+float tile_us(int rows, int64_t M, int groups, int outputs, int nb, bool mx4) {
+  const int64_t tiles = M / rows + std::max<int64_t>(std::min<int64_t>(groups, M) / 2, 1);
+  const int64_t jobs = tiles * ((outputs + kTileRows - 1) / kTileRows);
+  const float round = mx4 ? 4.9f + 0.62f * ((nb + 7) / 8) : 4.f + 0.85f * ((nb + 3) / 4);
+  return (jobs + kTileWorkgroups - 1) / kTileWorkgroups * round * (rows == 64 ? 1.f : mx4 ? 1.2f : 1.45f);
 }
+
+// Rows of x that a tile takes
+int tile_rows(int64_t M, int groups, int outputs, int nb, bool mx4) {
+  return tile_us(128, M, groups, outputs, nb, mx4) < tile_us(64, M, groups, outputs, nb, mx4) ? 128 : 64;
+}
+
+// Whether the experts' products go by tiles, behind a sort: from 10 pairs an
+// expert on (8 with 4-bit products), and 1 GFLOP.  Measured, few rows against
+// tiles: 128 experts of 2048 x 768 with 8 pairs each 141 : 130 us (bf16), 129 : 92
+// (4 bits), 64 of 1280 x 896 with 9 each 56 : 74 and 51 : 54, with 15 each 90 : 60
+// and 82 : 50; 8 of 1024 x 512 with 24 each (0.6 GFLOP) 21 : 28 and 24 : 25.
+bool by_tiles(int64_t P, int n, int64_t D, int64_t I, bool mx4) {
+  return P >= (mx4 ? 8 : 10) * static_cast<int64_t>(n) && 6 * P * D * I >= 1000000000;
+}
+// The most pairs of a call that goes otherwise
+int64_t most_few_pairs(int n, int64_t D, int64_t I) { return std::max(10 * static_cast<int64_t>(n), 1000000000 / (6 * D * I) + 1); }
 
 template <int X, bool kSwiglu, typename Out>
 hipError_t launch_tiles(const ProductArgs& a, int rows, hipStream_t st) {
@@ -1120,8 +1146,14 @@ hipError_t launch_tiles(const ProductArgs& a, int rows, hipStream_t st) {
 
 template <int X>
 hipError_t launch_product(const ProductArgs& a, int32_t dtype, hipStream_t st) {
-  const int rows = tile_rows(a.M, a.groups);
-  if (rows > 0 && a.blocks >= 16)  // fewer scales than a piece: the few rows' kernel alone reads them byte by byte
+  constexpr bool kMx4 = X == kXCodes;
+  const int rows = tile_rows(a.M, a.groups, a.N, a.nb, kMx4);
+  // Few rows: a start, and 108 (173) TFLOP/s, measured with 5,120 outputs at K =
+  // 2,048: 9.9 us for 32 rows and 26.5 for 128, which tiles take 17.4 and 17.7 for.
+  const float few_us = 3.f + 2e-6f * static_cast<float>(a.M) * static_cast<float>(a.N) * 32.f * static_cast<float>(a.nb) /
+                                 (kMx4 ? 173.f : 108.f);
+  // (tiles read scales 16 bytes at a time: of fewer, the few rows' kernel alone takes any number)
+  if (a.blocks >= 16 && a.M >= 16 && few_us > tile_us(rows, a.M, a.groups, a.N, a.nb, kMx4))
     return dtype == SPP_DTYPE_BF16 ? launch_tiles<X, false, __bf16>(a, rows, st) : launch_tiles<X, false, float>(a, rows, st);
   return dtype == SPP_DTYPE_BF16 ? launch_few<X, false, __bf16, kRowsStart>(a, a.groups, st)
                                  : launch_few<X, false, float, kRowsStart>(a, a.groups, st);
@@ -1247,9 +1279,9 @@ extern "C" spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups
 
 extern "C" size_t spp_mx4_experts_workspace(int32_t n, int32_t D, int32_t I, int32_t T, int32_t K) {
   if (const char* w = experts_why(n, D, I, T, K)) return bad(w), 0;
-  // every smaller call: the largest of few rows, and this one
-  const int64_t P = static_cast<int64_t>(T) * K, few = std::min<int64_t>(P, int64_t{kFewRows} * n);
-  return std::max(few_space(few, D, I).bytes, tile_rows(P, n) > 0 ? tile_space(T, P, n, D, I).bytes : size_t{16});
+  // every smaller call, with either act: the largest of few rows, and this one
+  const int64_t P = static_cast<int64_t>(T) * K, few = std::min<int64_t>(P, most_few_pairs(n, D, I));
+  return std::max(few_space(few, D, I).bytes, by_tiles(P, n, D, I, true) ? tile_space(T, P, n, D, I).bytes : size_t{16});
 }
 
 extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_mx4_matrix* down, int32_t n, int32_t act,
@@ -1280,8 +1312,8 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
       return bad("out must be residual with the same stride, or not overlap it");
   }
   const bool mx4 = act == SPP_ACT_MX4;
-  const int rows = tile_rows(P, n);
-  const Space s = rows > 0 ? tile_space(T, P, n, D, I) : few_space(P, D, I);
+  const bool tiles = by_tiles(P, n, D, I, mx4);
+  const Space s = tiles ? tile_space(T, P, n, D, I) : few_space(P, D, I);
   if (!workspace || !aligned16(workspace)) return bad("workspace must not be NULL, and 16-byte aligned");
   if (workspace_bytes < s.bytes) return bad("the workspace is too small");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -1300,7 +1332,7 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
   c.out = out;
   c.out_stride = out_stride;
 
-  if (rows > 0) {
+  if (tiles) {
     int32_t* start = reinterpret_cast<int32_t*>(space + s.start);
     int32_t* pair = reinterpret_cast<int32_t*>(space + s.pair);
     int32_t* place = reinterpret_cast<int32_t*>(space + s.place);
@@ -1326,6 +1358,7 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
     a.x_scales = space + s.xq_scales;
     a.x_blocks = static_cast<int64_t>(T) * a.nb;
     a.out_scales = space + s.h_scales;
+    int rows = tile_rows(P, n, 2 * I, a.nb, mx4);
     e = mx4 ? launch_tiles<kXCodes, true, __bf16>(a, rows, st) : launch_tiles<kXBf16, true, __bf16>(a, rows, st);
     if (e != hipSuccess) return launched(e);
     ProductArgs d = product_of(*down, n, start, static_cast<int32_t>(P), space + s.y, D);
@@ -1333,6 +1366,7 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
     d.x_stride = mx4 ? I / 2 : static_cast<int64_t>(I) * 2;
     d.x_scales = space + s.h_scales;
     d.x_blocks = P * d.nb;
+    rows = tile_rows(P, n, D, d.nb, mx4);
     e = mx4 ? launch_tiles<kXCodes, false, __bf16>(d, rows, st) : launch_tiles<kXBf16, false, __bf16>(d, rows, st);
     if (e != hipSuccess) return launched(e);
     c.place = place;
