@@ -557,8 +557,8 @@ spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups, const int
  * act SPP_ACT_BF16: the SwiGLU's result is rounded to bf16 between the
  * products.  SPP_ACT_MX4: x and the SwiGLU's result (in fp32) are brought into
  * 4 bits as by spp_mx4_quantize, and both sides of each product are 4-bit.
- * Sums are fp32; the results of each expert are kept in fp32 or, in calls of
- * many tokens, rounded to bf16 before the gates' sum.
+ * Sums are fp32; the results of each expert are kept in fp32 or, with
+ * SPP_ACT_MX4 in calls of many tokens, rounded to bf16 before the gates' sum.
  * n at most 1024, K at most 64, T * K at most 2^24, T * K times D or I at most
  * 2^36.
  * workspace: dev, 16-byte aligned, spp_mx4_experts_workspace bytes for every

@@ -856,40 +856,41 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
         }
       } else {
         const int f0 = t.column * kTileRows + wf * 64, f = f0 + 32 * half;
-        const auto eight = [&](int k, float* y) {
+        if (a.wide_out && f0 + 64 <= a.N) {
+          // 128 bytes of 32 rows at a time: 64 bf16 outputs, or 32 in fp32, which one
+          // half of the lanes holds
+          constexpr bool kF32 = std::is_same<Out, float>::value;
+          constexpr int kEach = 16 / static_cast<int>(sizeof(Out));
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = acc[k / 2][c][8 * (k % 2) + j];
-        };
-        if (std::is_same<Out, __bf16>::value && a.wide_out && f0 + 64 <= a.N) {
+          for (int part = 0; part < (kF32 ? 2 : 1); ++part) {
+            if (!kF32 || half == part) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float y[8];
-            eight(k, y);
-            store8(reinterpret_cast<__bf16*>(mine + (l32 * 8 + swizzled<8>(l32, half * 4 + k)) * 16), y);
-          }
+              for (int k = 0; k < 32 / kEach; ++k) {
+                u32x4 v;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int s = k * 8 + lane / 8, q = lane % 8;
-            const u32x4 v = *reinterpret_cast<const u32x4*>(mine + (s * 8 + swizzled<8>(s, q)) * 16);
-            if (r0 + s < t.count)
-              *reinterpret_cast<u32x4*>(static_cast<__bf16*>(a.out) + (t.first + r0 + s) * a.out_stride + f0 + 8 * q) = v;
+                for (int j = 0; j < 4; ++j) {
+                  const auto y = [&](int m) { return acc[m / 16][c][m % 16]; };
+                  v[j] = kF32 ? __float_as_uint(y(4 * k + j)) : pack_bf16(y((8 * k + 2 * j) % 32), y((8 * k + 2 * j + 1) % 32));
+                }
+                const int piece = kF32 ? k : half * 4 + k;
+                *reinterpret_cast<u32x4*>(mine + (l32 * 8 + swizzled<8>(l32, piece)) * 16) = v;
+              }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int s = k * 8 + lane / 8, q = lane % 8;
+              const u32x4 v = *reinterpret_cast<const u32x4*>(mine + (s * 8 + swizzled<8>(s, q)) * 16);
+              if (r0 + s < t.count)
+                *reinterpret_cast<u32x4*>(static_cast<Out*>(a.out) + (t.first + r0 + s) * a.out_stride + f0 + 32 * part + kEach * q) = v;
+            }
           }
           continue;
         }
         if (!ok || f >= a.N) continue;
         Out* out = static_cast<Out*>(a.out) + row * a.out_stride + f;
-        if (a.wide_out && f + 32 <= a.N) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float y[8];
-            eight(k, y);
-            store8(out + 8 * k, y);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (f + j < a.N) out[j] = static_cast<Out>(acc[j / 16][c][j % 16]);
-        }
+        for (int j = 0; j < 32; ++j)
+          if (f + j < a.N) out[j] = static_cast<Out>(acc[j / 16][c][j % 16]);
       }
     }
   };
@@ -1166,8 +1167,11 @@ struct Space {
 
 size_t up256(size_t n) { return (n + 255) & ~size_t{255}; }
 
-// Few rows an expert: h and y in fp32 at the pairs' own places.  Many: sorted, in
-// bf16 or 4 bits.
+// h: the SwiGLU's results, y: the experts' results.  Few rows an expert: in fp32
+// (h of bf16 products takes half of it) at the pairs' own places.  Many, sorted: h
+// in bf16 or 4 bits, y in fp32, or beside 4-bit products in bf16: its rounding adds
+// less there than h's step, and 4,096 tokens of 8 experts of 2048 would write and
+// read 268 MB more.  After a bf16 h, a bf16 y would make 1.2 times its error.
 Space few_space(int64_t P, int32_t D, int32_t I) {
   Space s{};
   s.y = up256(static_cast<size_t>(P) * I * 4);
@@ -1175,22 +1179,25 @@ Space few_space(int64_t P, int32_t D, int32_t I) {
   return s;
 }
 
-Space tile_space(int64_t T, int64_t P, int32_t n, int32_t D, int32_t I) {
+Space tile_space(int64_t T, int64_t P, int32_t n, int32_t D, int32_t I, bool mx4) {
   Space s{};
-  size_t at = up256(static_cast<size_t>(P) * I * 2);
+  size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t from = at;
     at += up256(bytes);
     return from;
   };
-  s.h_scales = take(static_cast<size_t>(P) * I / 32);
-  s.y = take(static_cast<size_t>(P) * D * 2);
+  s.h = take(static_cast<size_t>(P) * I * 2 / (mx4 ? 4 : 1));
+  s.y = take(static_cast<size_t>(P) * D * (mx4 ? 2 : 4));
   s.start = take((static_cast<size_t>(n) + 1) * 4);
   s.pair = take(static_cast<size_t>(P) * 4);
   s.place = take(static_cast<size_t>(P) * 4);
   s.sort = take(spp::expert_sort_bytes(P, n));
-  s.xq = take(static_cast<size_t>(T) * D / 2);
-  s.xq_scales = take(static_cast<size_t>(T) * D / 32);
+  if (mx4) {
+    s.h_scales = take(static_cast<size_t>(P) * I / 32);
+    s.xq = take(static_cast<size_t>(T) * D / 2);
+    s.xq_scales = take(static_cast<size_t>(T) * D / 32);
+  }
   s.bytes = at;
   return s;
 }
@@ -1281,7 +1288,10 @@ extern "C" size_t spp_mx4_experts_workspace(int32_t n, int32_t D, int32_t I, int
   if (const char* w = experts_why(n, D, I, T, K)) return bad(w), 0;
   // every smaller call, with either act: the largest of few rows, and this one
   const int64_t P = static_cast<int64_t>(T) * K, few = std::min<int64_t>(P, most_few_pairs(n, D, I));
-  return std::max(few_space(few, D, I).bytes, by_tiles(P, n, D, I, true) ? tile_space(T, P, n, D, I).bytes : size_t{16});
+  size_t need = std::max(few_space(few, D, I).bytes, size_t{16});
+  for (const bool mx4 : {false, true})
+    if (by_tiles(P, n, D, I, mx4)) need = std::max(need, tile_space(T, P, n, D, I, mx4).bytes);
+  return need;
 }
 
 extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_mx4_matrix* down, int32_t n, int32_t act,
@@ -1313,7 +1323,7 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
   }
   const bool mx4 = act == SPP_ACT_MX4;
   const bool tiles = by_tiles(P, n, D, I, mx4);
-  const Space s = tiles ? tile_space(T, P, n, D, I) : few_space(P, D, I);
+  const Space s = tiles ? tile_space(T, P, n, D, I, mx4) : few_space(P, D, I);
   if (!workspace || !aligned16(workspace)) return bad("workspace must not be NULL, and 16-byte aligned");
   if (workspace_bytes < s.bytes) return bad("the workspace is too small");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -1349,7 +1359,7 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
       e = launch(mx4_quantize_kernel<__bf16>, quant_grid(q.words), kQuantThreads, q, st);
       if (e != hipSuccess) return launched(e);
     }
-    ProductArgs a = product_of(*gate_up, n, start, static_cast<int32_t>(P), space, I);
+    ProductArgs a = product_of(*gate_up, n, start, static_cast<int32_t>(P), space + s.h, I);
     a.N = I;
     a.pair = pair;
     a.xdiv = K;
@@ -1362,14 +1372,15 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
     e = mx4 ? launch_tiles<kXCodes, true, __bf16>(a, rows, st) : launch_tiles<kXBf16, true, __bf16>(a, rows, st);
     if (e != hipSuccess) return launched(e);
     ProductArgs d = product_of(*down, n, start, static_cast<int32_t>(P), space + s.y, D);
-    d.x = space;
+    d.x = space + s.h;
     d.x_stride = mx4 ? I / 2 : static_cast<int64_t>(I) * 2;
     d.x_scales = space + s.h_scales;
     d.x_blocks = P * d.nb;
     rows = tile_rows(P, n, D, d.nb, mx4);
-    e = mx4 ? launch_tiles<kXCodes, false, __bf16>(d, rows, st) : launch_tiles<kXBf16, false, __bf16>(d, rows, st);
+    e = mx4 ? launch_tiles<kXCodes, false, __bf16>(d, rows, st) : launch_tiles<kXBf16, false, float>(d, rows, st);
     if (e != hipSuccess) return launched(e);
     c.place = place;
+    c.fp32_rows = !mx4;
     return launched(spp::launch_expert_combine(c, st));
   }
 
