@@ -504,7 +504,8 @@ spp_status spp_attention_step(spp_ctx* ctx, int32_t B, const int32_t* pos, int64
  * dev [rows][cols/2], byte j of a row holds elements 2j (low nibble) and 2j+1;
  * scales: dev [rows][cols/32], one byte for 32 elements.  An element is its
  * code's value times 2^(scale - 127), both as in the cache; scale 255 makes
- * the block NaN.  codes 16-byte aligned; rows at most 2^31 - 1, and
+ * the block NaN, and 0, 1, 253 and 254, which no call here writes, give no
+ * certain result.  codes 16-byte aligned; rows at most 2^31 - 1, and
  * rows * cols at most 2^40. */
 typedef struct {
   void* codes;

@@ -260,15 +260,28 @@ struct Ids {
   }
 };
 
+// Where a search for a group's pairs stands
+struct Search {
+  int count;  // pairs with its id
+  int first;  // the first of them
+  int p0, seen;  // where the next 16 are looked for from, and pairs before that
+};
+
 // The pairs with id `group` whose place among them is in [r0, r0 + 16), by one
-// wave; returns how many there are in all.  ids: the first pairs'.  first: the
-// first of all.
-__device__ __forceinline__ int find_pairs(const ProductArgs& a, Ids ids, int group, int r0, int* row, int* first) {
+// wave.  The first search (r0 = 0; ids: the first pairs') counts all of them, the
+// others go on where the one before found what it looked for.
+__device__ __forceinline__ void find_pairs(const ProductArgs& a, Ids ids, int group, int r0, int* row, Search& s) {
   const int lane = threadIdx.x & 63;
-  int seen = 0;
-  *first = a.M;
-  for (int p0 = 0; p0 < a.M; p0 += 64 * kIds) {
+  int p0 = 0, seen = 0;
+  if (r0 > 0) {
+    p0 = s.p0, seen = s.seen;
+  } else {
+    s.first = s.p0 = a.M, s.seen = 0;
+  }
+  bool on = true;  // the next ones' place is not known yet
+  for (; p0 < a.M && (r0 == 0 || on); p0 += 64 * kIds) {
     if (p0 > 0) ids.load(a, p0);
+    const int before = seen;
 #pragma unroll
     for (int j = 0; j < kIds; ++j) {
       const int p = p0 + 64 * j + lane;
@@ -276,11 +289,12 @@ __device__ __forceinline__ int find_pairs(const ProductArgs& a, Ids ids, int gro
       const uint64_t m = __ballot(mine);
       const int at = seen + __popcll(m & ((uint64_t{1} << lane) - 1)) - r0;
       if (mine && at >= 0 && at < 16) row[at] = p;
-      if (seen == 0 && m) *first = p0 + 64 * j + __ffsll(static_cast<long long>(m)) - 1;
+      if (seen == 0 && m) s.first = p0 + 64 * j + __ffsll(static_cast<long long>(m)) - 1;
       seen += __popcll(m);
     }
+    if (on && seen > r0 + 16) s.p0 = p0, s.seen = before, on = false;
   }
-  return seen;
+  if (r0 == 0) s.count = seen;
 }
 
 // A workgroup takes a.run tiles of 16 * NT outputs (of both matrices for SwiGLU)
@@ -323,14 +337,15 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
     for (int t = 0; t < kTiles; ++t) row[t] = first_row + t / NT * a.N + min((tile * NT + t % NT) * 16 + l16, a.N - 1);
     w.load(a, row, Weights::window(a, b0 + s0));
   };
+  Search search;
   Weights even, odd;
   load(even, from, 0);
   const int r_first = 16 * static_cast<int>(blockIdx.z), r_step = 16 * static_cast<int>(gridDim.z);
   for (int r0 = r_first;; r0 += r_step) {
     if constexpr (kRows == kRowsIds) {
-      int first;
-      count = find_pairs(a, ids, group, r0, s_row, &first);
-      if (r0 >= count || (a.by_pair && first != static_cast<int>(blockIdx.y))) return;
+      find_pairs(a, ids, group, r0, s_row, search);
+      count = search.count;
+      if (r0 >= count || (a.by_pair && search.first != static_cast<int>(blockIdx.y))) return;
       __builtin_amdgcn_wave_barrier();
     }
     const bool x_ok = r0 + l16 < count;
@@ -1134,11 +1149,14 @@ int tile_rows(int64_t M, int groups, int outputs, int nb, bool mx4) {
 // tiles: 128 experts of 2048 x 768 with 8 pairs each 141 : 130 us (bf16), 129 : 92
 // (4 bits), 64 of 1280 x 896 with 9 each 56 : 74 and 51 : 54, with 15 each 90 : 60
 // and 82 : 50; 8 of 1024 x 512 with 24 each (0.6 GFLOP) 21 : 28 and 24 : 25.
+// From 64 pairs an expert on in any case: few rows search all pairs.
 bool by_tiles(int64_t P, int n, int64_t D, int64_t I, bool mx4) {
-  return P >= (mx4 ? 8 : 10) * static_cast<int64_t>(n) && 6 * P * D * I >= 1000000000;
+  return P >= int64_t{64} * n || (P >= (mx4 ? 8 : 10) * int64_t{n} && 6 * P * D * I >= 1000000000);
 }
 // The most pairs of a call that goes otherwise
-int64_t most_few_pairs(int n, int64_t D, int64_t I) { return std::max(10 * static_cast<int64_t>(n), 1000000000 / (6 * D * I) + 1); }
+int64_t most_few_pairs(int n, int64_t D, int64_t I) {
+  return std::min(int64_t{64} * n, std::max(int64_t{10} * n, 1000000000 / (6 * D * I) + 1));
+}
 
 template <int X, bool kSwiglu, typename Out>
 hipError_t launch_tiles(const ProductArgs& a, int rows, hipStream_t st) {
