@@ -555,9 +555,10 @@ spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups, const int
  * (multiples of 8, pointers 16-byte aligned; out may be residual with the same
  * stride, else overlaps no input); topk: dev int32 [T][K]; gates: dev fp32
  * [T][K].  An id outside 0 .. n-1 adds nothing; an id may occur twice.
- * act SPP_ACT_BF16: the SwiGLU's result is rounded to bf16 between the
- * products.  SPP_ACT_MX4: x and the SwiGLU's result (in fp32) are brought into
- * 4 bits as by spp_mx4_quantize, and both sides of each product are 4-bit.
+ * act SPP_ACT_BF16: the SwiGLU's result goes into the second product as two
+ * bf16 terms (16 bits), or in calls of many tokens rounded to bf16.
+ * SPP_ACT_MX4: x and the SwiGLU's result (in fp32) are brought into 4 bits as by
+ * spp_mx4_quantize, and both sides of each product are 4-bit.
  * Sums are fp32; the results of each expert are kept in fp32 or, with
  * SPP_ACT_MX4 in calls of many tokens, rounded to bf16 before the gates' sum.
  * n at most 1024, K at most 64, T * K at most 2^24, T * K times D or I at most

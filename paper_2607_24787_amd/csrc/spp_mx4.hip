@@ -68,7 +68,11 @@ __global__ __launch_bounds__(kQuantThreads) void mx4_load_kernel(RowsQ a) {
 // --------------------------------------------------------- products of few rows
 
 // What a product's rows of x are
-enum { kXBf16 = 0, kXCodes = 1, kXQuantBf16 = 2, kXQuantF32 = 3 };
+// (rows of two bf16 terms, the second one half a stride behind: kXTerms multiplies
+// one after the other, kXTermRows as neighbouring rows of x, of one row)
+enum { kXBf16 = 0, kXCodes = 1, kXQuantBf16 = 2, kXQuantF32 = 3, kXTerms = 4, kXTermRows = 5 };
+// A result as such terms, which keep 16 bits
+struct Terms {};
 // Which rows a group has: start[g] .. start[g+1] - 1 (or all), or the pairs
 // with its id
 enum { kRowsStart = 0, kRowsIds = 1 };
@@ -153,35 +157,52 @@ __device__ __forceinline__ i32x8 wide(u32x4 c) {
 // __syncthreads() would wait for them.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// kStep blocks of a row of x: bf16 rows as four operands of 8 elements each, rows
-// in 4 bits as codes with their scale byte
+// kStep blocks of a row of x: bf16 rows as four operands of 8 elements each, split
+// rows as four and four, rows in 4 bits as codes with their scale byte
 template <int X, int kStep>
 struct XBlocks {
-  static constexpr int kParts = X == kXBf16 ? 4 : 1;
+  static constexpr int kParts = X == kXBf16 || X == kXTermRows ? 4 : X == kXTerms ? 8 : 1;
   u32x4 v[kStep][kParts];
   uint32_t byte[kStep];
-  // blocks b .. b + kStep - 1, zeros outside [b0, b1) or for no row
+  // blocks b .. b + kStep - 1, zeros outside [b0, b1) or for no row (`row` is one
+  // that can be read all the same)
   __device__ __forceinline__ void load(const ProductArgs& a, int64_t row, bool have, int b, int b0, int b1) {
     const uint8_t* p = static_cast<const uint8_t*>(a.x) + row * a.x_stride;
+    if constexpr (X == kXTermRows) p += threadIdx.x & 1 ? a.x_stride / 2 : 0;
+    if constexpr (X != kXQuantBf16 && X != kXQuantF32) {
+#pragma unroll
+      for (int s = 0; s < kStep; ++s) {
+        byte[s] = kOne;
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) v[s][q] = u32x4{0, 0, 0, 0};
+        if (!have || b + s < b0 || b + s >= b1) continue;
+        if constexpr (X == kXCodes) {
+          v[s][0] = reinterpret_cast<const u32x4*>(p)[b + s];
+          byte[s] = a.x_scales[row * a.nb + b + s];
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            v[s][q] = reinterpret_cast<const u32x4*>(p)[4 * (b + s) + q];
+            if constexpr (X == kXTerms) v[s][4 + q] = reinterpret_cast<const u32x4*>(p + a.x_stride / 2)[4 * (b + s) + q];
+          }
+        }
+      }
+      return;
+    }
+    // converted: all lanes load, so that no load is waited for inside a branch
+    using T = typename std::conditional<X == kXQuantBf16, __bf16, float>::type;
+    float y[kStep][32];
+#pragma unroll
+    for (int s = 0; s < kStep; ++s)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) load8(reinterpret_cast<const T*>(p) + 32 * min(b + s, a.nb - 1) + 8 * q, y[s] + 8 * q);
 #pragma unroll
     for (int s = 0; s < kStep; ++s) {
-      byte[s] = kOne;
-#pragma unroll
-      for (int q = 0; q < kParts; ++q) v[s][q] = u32x4{0, 0, 0, 0};
-      if (!have || b + s < b0 || b + s >= b1) continue;
-      if constexpr (X == kXCodes) {
-        v[s][0] = reinterpret_cast<const u32x4*>(p)[b + s];
-        byte[s] = a.x_scales[row * a.nb + b + s];
-      } else if constexpr (X == kXBf16) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[s][q] = reinterpret_cast<const u32x4*>(p)[4 * (b + s) + q];
-      } else {
-        using T = typename std::conditional<X == kXQuantF32, float, __bf16>::type;
-        float y[32];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) load8(reinterpret_cast<const T*>(p) + 32 * (b + s) + 8 * q, y + 8 * q);
-        v[s][0] = quantise32(y, &byte[s]);
-      }
+      const bool ok = have && b + s >= b0 && b + s < b1;
+      uint32_t scale;
+      const u32x4 codes = quantise32(y[s], &scale);
+      v[s][0] = ok ? codes : u32x4{0, 0, 0, 0};
+      byte[s] = ok ? scale : kOne;
     }
   }
 };
@@ -237,9 +258,13 @@ struct WeightBlocks {
       for (int s = 0; s < kStep; ++s) {
         // what is not to be added: x is zero there, and the scale must be none that makes NaN
         const uint32_t byte = b + s >= b0 && b + s < b1 ? (word >> (8 * s)) & 255u : kOne;
-        if constexpr (X == kXBf16) {
+        if constexpr (X == kXBf16 || X == kXTerms || X == kXTermRows) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) acc[t] = mfma_bf16(cvt8(codes[t][s][q], scale_of(byte)), x.v[s][q], acc[t]);
+          for (int q = 0; q < 4; ++q) {
+            const u32x4 w = cvt8(codes[t][s][q], scale_of(byte));
+            acc[t] = mfma_bf16(w, x.v[s][q], acc[t]);
+            if constexpr (X == kXTerms) acc[t] = mfma_bf16(w, x.v[s][4 + q], acc[t]);
+          }
         } else {
           acc[t] = mfma_mx4<0>(codes[t][s], byte, x.v[s][0], x.byte[s], acc[t]);
         }
@@ -388,16 +413,30 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
         const int f = tile * 16 * NT + 4 * q;
         if (r0 + i >= count || f >= a.N) continue;
         const int64_t row = kRows == kRowsIds ? s_row[i] : begin + r0 + i;
-        Out* out = static_cast<Out*>(a.out) + row * a.out_stride + f;
-        if (a.wide_out && f + 4 <= a.N) {
-          if constexpr (std::is_same<Out, float>::value)
-            *reinterpret_cast<f32x4*>(out) = y;
-          else
-            *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
-        } else {
+        if constexpr (std::is_same<Out, Terms>::value) {  // N is a multiple of 32
+          __bf16* out = static_cast<__bf16*>(a.out) + row * 2 * a.N + f;
+          u32x2 high{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])}, low;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (f + e < a.N) out[e] = static_cast<Out>(y[e]);
+          for (int e = 0; e < 2; ++e) {
+            // what is infinite or NaN is so in the first term, and the second adds nothing
+            const float l0 = y[2 * e] - bf16_lo(high[e]), l1 = y[2 * e + 1] - bf16_hi(high[e]);
+            low[e] = pack_bf16(l0 == l0 ? l0 : 0.f, l1 == l1 ? l1 : 0.f);
+          }
+          *reinterpret_cast<u32x2*>(out) = high;
+          *reinterpret_cast<u32x2*>(out + a.N) = low;
+          continue;
+        } else {
+          Out* out = static_cast<Out*>(a.out) + row * a.out_stride + f;
+          if (a.wide_out && f + 4 <= a.N) {
+            if constexpr (std::is_same<Out, float>::value)
+              *reinterpret_cast<f32x4*>(out) = y;
+            else
+              *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (f + e < a.N) out[e] = static_cast<Out>(y[e]);
+          }
         }
       }
     };
@@ -427,6 +466,7 @@ constexpr int kLastWaves = kLastThreads / 64;
 
 template <int X, int kStep, bool kTiny>
 __global__ __launch_bounds__(kLastThreads) void mx4_last_kernel(LastArgs a) {
+  constexpr int kTerms = X == kXTermRows ? 2 : 1;  // columns of the matrix instruction that the token takes
   __shared__ f32x4 s_part[kLastWaves][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, l16 = lane & 15;
   const int parts = a.K >= kLastWaves ? 1 : kLastWaves / a.K;
@@ -445,11 +485,14 @@ __global__ __launch_bounds__(kLastThreads) void mx4_last_kernel(LastArgs a) {
     for (int s0 = 0; s0 < per; s0 += kStep) {
       const int b = WeightBlocks<1, kStep, kTiny>::window(a.p, b0 + s0);
       w.load(a.p, &row, b);
-      x.load(a.p, pair, l16 == 0, b, b0 + s0, b1);
+      x.load(a.p, pair, l16 < kTerms, b, b0 + s0, b1);
       w.template products<X>(x, b, b0 + s0, b1, &acc);
     }
     sum += gate * acc;
   }
+  if constexpr (kTerms == 2)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] += __shfl_down(sum[j], 1);
   if (l16 == 0) s_part[wave][g] = sum;
   __syncthreads();
   if (tid >= 16 || f0 + tid >= a.p.N) return;
@@ -1186,7 +1229,8 @@ struct Space {
 size_t up256(size_t n) { return (n + 255) & ~size_t{255}; }
 
 // h: the SwiGLU's results, y: the experts' results.  Few rows an expert: in fp32
-// (h of bf16 products takes half of it) at the pairs' own places.  Many, sorted: h
+// at the pairs' own places; the weights' reads bound such calls, and h goes into
+// the second product as two terms.  Many, sorted: h
 // in bf16 or 4 bits, y in fp32, or beside 4-bit products in bf16: its rounding adds
 // less there than h's step, and 4,096 tokens of 8 experts of 2048 would write and
 // read 268 MB more.  After a bf16 h, a bf16 y would make 1.2 times its error.
@@ -1411,11 +1455,11 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
   a.by_pair = P < n;
   const int64_t groups = std::min<int64_t>(P, n);
   hipError_t e = mx4 ? launch_few<kXQuantBf16, true, float, kRowsIds>(a, groups, st)
-                     : launch_few<kXBf16, true, __bf16, kRowsIds>(a, groups, st);
+                     : launch_few<kXBf16, true, Terms, kRowsIds>(a, groups, st);
   if (e != hipSuccess) return launched(e);
   ProductArgs d = product_of(*down, n, nullptr, static_cast<int32_t>(P), space + s.y, D);
   d.x = space + s.h;
-  d.x_stride = static_cast<int64_t>(I) * (mx4 ? 4 : 2);
+  d.x_stride = static_cast<int64_t>(I) * 4;
   d.ids = topk;
   d.by_pair = P < n;
   if (T <= kLastTokens) {
@@ -1428,14 +1472,14 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
     l.residual_stride = residual_stride;
     l.K = K;
     void* params[] = {&l};
-    const auto last = d.nb < 3 ? (mx4 ? mx4_last_kernel<kXQuantF32, 1, true> : mx4_last_kernel<kXBf16, 1, true>)
-                               : (mx4 ? mx4_last_kernel<kXQuantF32, 3, false> : mx4_last_kernel<kXBf16, 3, false>);
+    const auto last = d.nb < 3 ? (mx4 ? mx4_last_kernel<kXQuantF32, 1, true> : mx4_last_kernel<kXTermRows, 1, true>)
+                               : (mx4 ? mx4_last_kernel<kXQuantF32, 3, false> : mx4_last_kernel<kXTermRows, 3, false>);
     const void* kernel = reinterpret_cast<const void*>(last);
     return launched(hipLaunchKernel(kernel, dim3(static_cast<unsigned>((D + 15) / 16), static_cast<unsigned>(T)),
                                     dim3(kLastThreads), params, 0, st));
   }
   e = mx4 ? launch_few<kXQuantF32, false, float, kRowsIds>(d, groups, st)
-          : launch_few<kXBf16, false, float, kRowsIds>(d, groups, st);
+          : launch_few<kXTerms, false, float, kRowsIds>(d, groups, st);
   if (e != hipSuccess) return launched(e);
   c.ids = topk;
   c.n = n;
