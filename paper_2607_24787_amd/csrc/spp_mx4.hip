@@ -32,7 +32,9 @@ struct RowsQ {
 
 constexpr int kQuantThreads = 256;
 
-// A lane takes 8 elements, four lanes a block.
+// A lane takes 8 elements, four lanes a block: a row's reads and writes are whole
+// cache lines.  Bound by memory: 98,304 bf16 rows of 2,048 take 113 us (510 MB, 4.5
+// TB/s) here, and 97 us (5.3 TB/s) to be read back by mx4_load_kernel.
 template <typename T>
 __global__ __launch_bounds__(kQuantThreads) void mx4_quantize_kernel(RowsQ a) {
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kQuantThreads + threadIdx.x; i < a.words;
@@ -329,6 +331,12 @@ __device__ __forceinline__ void find_pairs(const ProductArgs& a, Ids ids, int gr
 // multiplied, the first one's before the rows are known; the ids that tell them
 // go before the weights, since loads return in order.  kHold: K is one step, and
 // x stays in registers over the tiles.
+// Bound by the weights' reads: the SwiGLU half of 64 tokens over 128 experts (K =
+// 2,048, 214 MB) takes 46 us, 4.6 TB/s, the other (K = 768, 107 MB) 28 to 31.  One
+// tile a workgroup, rows first and the weights behind them took 67 and 81: a
+// workgroup then waits for three round trips one after the other.  One token's 8
+// experts are latency (7.7 us: a launch, ids, weights, join), and so are 5,120
+// outputs of one row (4.8 us).
 template <int X, bool kSwiglu, int NT, int kStep, bool kHold, bool kTiny, typename Out, int kRows>
 __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
   constexpr int kTiles = kSwiglu ? 2 * NT : NT;
@@ -451,7 +459,8 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
 }
 
 // The second product of one or a few tokens with the gates' sum, one launch for
-// both: a workgroup takes 16 outputs of token blockIdx.y, its waves its experts
+// both (5.3 us for 8 experts of 2048 x 768; two launches took 6.3 and 4.4): a
+// workgroup takes 16 outputs of token blockIdx.y, its waves its experts
 // (and shares of K where there are fewer experts than waves).
 struct LastArgs {
   ProductArgs p;  // x: the SwiGLU's results, row t * K + k; ids
@@ -572,9 +581,17 @@ __device__ __forceinline__ int rows_of(const ProductArgs& a, int g, int* first) 
 // are multiplied and its results written.  A wave takes 64 of the weight rows
 // and half of the rows of x.
 //
-// A tile of 128 rows is bound by LDS (128 KB read a stage of 256 in K, 1,000
-// cycles, beside 1,250 of the matrix units') and by what each compute unit gets
-// from L2 (48 KB a stage).
+// What bounds it: with bf16 rows the matrix instructions (32 of each wave a stage,
+// 2,370 cycles of a SIMD; 8,192 x 5,120 outputs at K = 2,048 take 152 us, 1.13
+// PFLOP/s, a library's bf16 product of 8,192^3 reaches 1.14 to 1.35).  With both
+// sides in 4 bits (1,320 cycles) what a compute unit gets from L2, 48 KB a stage,
+// which takes 900 to 1,300 cycles: 60 us, 2.9 PFLOP/s, of them about 12 for the
+// results' 84 MB, and 3.6 PFLOP/s at K = 16,384 (the instructions by themselves reach
+// 8.0, and 2.2 in bf16).  Whole lines matter: L2 gives 55 bytes a cycle where a
+// load's rows are 128 bytes and 29 where they are 64, and a 64-byte stage of 256 x
+// 128 tiles, two workgroups of four waves a compute unit, took 87 us.  Loads that
+// are issued together hold up the products behind them (53,000 of a workgroup's
+// 124,000 cycles), so they go between them, one at a time.
 template <int X, bool kSwiglu, typename Out, int CT>
 __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a) {
   constexpr bool kMx4 = X == kXCodes;

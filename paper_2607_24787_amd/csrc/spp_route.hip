@@ -92,7 +92,9 @@ constexpr int kHeld = 4;                // pairs of a thread
 // in registers.  The others it counts by itself (at most 2^14: a launch that
 // would count them costs more than the reads), or finds counted (kCounted).  A
 // wave takes its run of pairs in order and only it writes its row of counts, so
-// a pair's rank does not depend on which lane comes first.
+// a pair's rank does not depend on which lane comes first.  Latency: 512 pairs of
+// 128 experts take 4 us, 6,144 of 64 take 8.4 (two parts), 65,536 of 128 take 4.7 +
+// 7.9; with the pairs read twice, in a loop, 12, and 5.9 + 13.
 template <int kEach, bool kCounted>
 __global__ __launch_bounds__(kSortThreads) void expert_sort_once_kernel(SortArgs a) {
   extern __shared__ int s_row[];  // [kSortWaves][n], then pairs before this part and behind it [2][n]
@@ -336,7 +338,9 @@ struct RowOf {
 
 constexpr int kRowBatch = 8;  // rows whose loads are in flight together
 
-// A token's row is read once and written to its pairs' places.
+// A token's row is read once and written to its pairs' places.  Bound by the
+// writes: 8,192 bf16 rows of 2,048 to 8 places each take 47 to 58 us (302 MB, 5.2 to
+// 6.4 TB/s).
 __global__ __launch_bounds__(kRowThreads) void expert_gather_kernel(RowArgs a) {
   const RowOf r(a);
   if (r.t >= a.T) return;
@@ -363,7 +367,9 @@ __device__ __forceinline__ int place_of(const RowArgs& a, int64_t p) {
 }
 
 // Sums in fp32, in the order of a token's experts.  Rows in T, or fp32 rows of
-// bf16 outputs.
+// bf16 outputs.  Bound by the rows' reads, which go past the caches: 65,536 bf16
+// rows of 2,048 take 64 us with weights and a residual (335 MB, 5.2 TB/s), 98
+// through the caches.
 template <typename T, typename Rows, bool kWeights>
 __global__ __launch_bounds__(kRowThreads) void expert_combine_kernel(RowArgs a) {
   constexpr int E = 16 / static_cast<int>(sizeof(T));
@@ -415,7 +421,9 @@ __global__ __launch_bounds__(kRowThreads) void expert_combine_kernel(RowArgs a) 
 }
 
 // One wave per pair: d_row = w * d_out, d_w = <d_out, row>.  The waves of a
-// token are neighbours and find its d_out in the caches.
+// token are neighbours and find its d_out in the caches.  Bound by memory: 65,536
+// bf16 rows of 2,048 read and written take 126 us (570 MB, 4.5 TB/s; a copy reaches
+// 5.2).
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void expert_combine_grad_kernel(RowArgs a) {
   constexpr int E = 16 / static_cast<int>(sizeof(T));
