@@ -758,7 +758,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     int last[SI];
   };
   // A lane's piece of four stages from `st` on, read whole and in bounds: near the
-  // end of all scales (at least 16) it starts earlier
+  // end of all scales it starts earlier, by up to 15 bytes.  All are at least 16, but
+  // for those of x that the experts' call quantises itself: its codes, 256 bytes or
+  // more of the workspace, lie in front of them
   const auto load_scales = [&](Scales& to, int st) {
     const int b = st * BL + 16 * scale_c;
 #pragma unroll

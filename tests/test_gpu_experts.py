@@ -260,7 +260,8 @@ class Experts:
     (1, 1, 1, 32, 32, "any"), (1, 128, 8, 256, 96, "distinct"), (1, 64, 6, 1280, 896, "distinct"), (2, 40, 8, 512, 768, "distinct"),
     (3, 8, 2, 96, 64, "any"), (5, 3, 4, 160, 160, "same"), (16, 16, 3, 64, 128, "bad"), (40, 24, 5, 288, 224, "distinct"),
     (64, 40, 8, 256, 128, "distinct"), (130, 8, 2, 320, 96, "any"), (200, 4, 3, 128, 64, "same"), (300, 24, 8, 256, 160, "distinct"),
-    (700, 8, 4, 192, 288, "bad"), (3000, 4, 2, 64, 32, "any"), (2500, 200, 4, 32, 64, "same"), (1500, 700, 1, 32, 32, "bad"), (1024, 5, 2, 128, 96, "any"), (33, 6, 64, 64, 32, "any"), (4, 1024, 3, 64, 32, "any")])
+    (700, 8, 4, 192, 288, "bad"), (3000, 4, 2, 64, 32, "any"), (2500, 200, 4, 32, 64, "same"), (1500, 700, 1, 32, 32, "bad"), (1024, 5, 2, 128, 96, "any"), (33, 6, 64, 64, 32, "any"), (4, 1024, 3, 64, 32, "any"),
+    (1, 1, 64, 32, 32, "any"), (1, 1, 64, 448, 32, "any"), (3, 2, 64, 96, 64, "any"), (7, 3, 40, 64, 32, "bad")])
 def test_experts(torch, T, n, K, D, I, kind, act):  # noqa: F811
     e = Experts(T, n, K, D, I, kind, seed=T + n, residual=T % 2 == 0)
     e.check(act, e.run(act))
