@@ -559,8 +559,7 @@ spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups, const int
  * bf16 terms (16 bits), or in calls of many tokens rounded to bf16.
  * SPP_ACT_MX4: x and the SwiGLU's result (in fp32) are brought into 4 bits as by
  * spp_mx4_quantize, and both sides of each product are 4-bit.
- * Sums are fp32; the results of each expert are kept in fp32 or, with
- * SPP_ACT_MX4 in calls of many tokens, rounded to bf16 before the gates' sum.
+ * Sums are fp32, and so is the result of each expert until the gates' sum.
  * n at most 1024, K at most 64, T * K at most 2^24, T * K times D or I at most
  * 2^36.
  * workspace: dev, 16-byte aligned, spp_mx4_experts_workspace bytes for every

@@ -93,10 +93,12 @@ def groups_of(start, M):
     return [np.arange(a, b) for a, b in zip(at[:-1], at[1:])]
 
 
-def experts(x, gate_up, down, topk, gates, residual, mx4):
+def experts(x, gate_up, down, topk, gates, residual, mx4, u_h=U16, u_y=U16, sums=True):
     """(out, bound) of the routed experts before the output's rounding.
 
     x [T, D]; gate_up [n, 2I, D], down [n, D, I] values; topk, gates [T, K]; residual [T, D] or None.
+    u_h: half a step, relative, of what holds the SwiGLU's result (with mx4: 4 bits); u_y: of each expert's result.
+    sums=False: the first product's sums are exact in fp32, as the inputs see to.
     """
     T, D = x.shape
     n, I = gate_up.shape[0], gate_up.shape[1] // 2
@@ -111,6 +113,7 @@ def experts(x, gate_up, down, topk, gates, residual, mx4):
         if t.size == 0:
             continue
         gu, err = product(x[t], gate_up[e])
+        err = err if sums else 0 * err
         g, u = gu[:, :I], gu[:, I:]
         s = g / (1 + np.exp(-g))
         h = s * u
@@ -119,9 +122,9 @@ def experts(x, gate_up, down, topk, gates, residual, mx4):
         if mx4:
             h, err_h = quantised(h, err_h)
         else:
-            err_h = err_h + U16 * (np.abs(h) + err_h)
+            err_h = err_h + u_h * (np.abs(h) + err_h)
         y, err_y = product(h, down[e], err_h)
-        err_y = err_y + U16 * (np.abs(y) + err_y)          # rows may be kept in bf16
+        err_y = err_y + u_y * (np.abs(y) + err_y)
         w = gates[t, k][:, None]
         np.add.at(out, t, w * y)
         np.add.at(reach, t, np.abs(w) * (np.abs(y) + err_y))

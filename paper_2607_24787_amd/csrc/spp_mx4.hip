@@ -1247,12 +1247,13 @@ struct Space {
 
 size_t up256(size_t n) { return (n + 255) & ~size_t{255}; }
 
-// h: the SwiGLU's results, y: the experts' results.  Few rows an expert: in fp32
-// at the pairs' own places; the weights' reads bound such calls, and h goes into
-// the second product as two terms.  Many, sorted: h
-// in bf16 or 4 bits, y in fp32, or beside 4-bit products in bf16: its rounding adds
-// less there than h's step, and 4,096 tokens of 8 experts of 2048 would write and
-// read 268 MB more.  After a bf16 h, a bf16 y would make 1.2 times its error.
+// h: the SwiGLU's results, y: the experts' results, which are terms of the gates'
+// sum and stay in fp32.  Few rows an expert: at the pairs' own places; the weights'
+// reads bound such calls, and h goes into the second product as two terms.  Many,
+// sorted: h in bf16 or 4 bits.  Beside 4-bit products too y's fp32 is paid for: 4,096
+// tokens of 8 experts of 2048 write and read 268 MB more than in bf16 (307 us a call in place of 252),
+// which makes their outputs' error that of the output's rounding (0.0017 of their
+// 2-norm) instead of 0.0024.
 Space few_space(int64_t P, int32_t D, int32_t I) {
   Space s{};
   s.y = up256(static_cast<size_t>(P) * I * 4);
@@ -1269,7 +1270,7 @@ Space tile_space(int64_t T, int64_t P, int32_t n, int32_t D, int32_t I, bool mx4
     return from;
   };
   s.h = take(static_cast<size_t>(P) * I * 2 / (mx4 ? 4 : 1));
-  s.y = take(static_cast<size_t>(P) * D * (mx4 ? 2 : 4));
+  s.y = take(static_cast<size_t>(P) * D * 4);
   s.start = take((static_cast<size_t>(n) + 1) * 4);
   s.pair = take(static_cast<size_t>(P) * 4);
   s.place = take(static_cast<size_t>(P) * 4);
@@ -1415,6 +1416,7 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
   c.rows_stride = D;
   c.weights = gates;
   c.dtype = SPP_DTYPE_BF16;
+  c.fp32_rows = 1;
   c.T = T;
   c.K = K;
   c.D = D;
@@ -1458,10 +1460,9 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
     d.x_scales = space + s.h_scales;
     d.x_blocks = P * d.nb;
     rows = tile_rows(P, n, D, d.nb, mx4);
-    e = mx4 ? launch_tiles<kXCodes, false, __bf16>(d, rows, st) : launch_tiles<kXBf16, false, float>(d, rows, st);
+    e = mx4 ? launch_tiles<kXCodes, false, float>(d, rows, st) : launch_tiles<kXBf16, false, float>(d, rows, st);
     if (e != hipSuccess) return launched(e);
     c.place = place;
-    c.fp32_rows = !mx4;
     return launched(spp::launch_expert_combine(c, st));
   }
 
@@ -1502,6 +1503,5 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
   if (e != hipSuccess) return launched(e);
   c.ids = topk;
   c.n = n;
-  c.fp32_rows = 1;
   return launched(spp::launch_expert_combine(c, st));
 }
