@@ -556,7 +556,7 @@ spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups, const int
  * stride, else overlaps no input); topk: dev int32 [T][K]; gates: dev fp32
  * [T][K].  An id outside 0 .. n-1 adds nothing; an id may occur twice.
  * act SPP_ACT_BF16: the SwiGLU's result goes into the second product as two
- * bf16 terms (16 bits), or in calls of many tokens rounded to bf16.
+ * bf16 terms (16 bits).
  * SPP_ACT_MX4: x and the SwiGLU's result (in fp32) are brought into 4 bits as by
  * spp_mx4_quantize, and both sides of each product are 4-bit.
  * Sums are fp32, and so is the result of each expert until the gates' sum.

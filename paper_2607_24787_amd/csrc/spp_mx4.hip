@@ -215,6 +215,15 @@ __device__ __forceinline__ f32x4 mfma_mx4(u32x4 w, uint32_t w_scales, u32x4 x, u
                                                           static_cast<int>(x_byte));
 }
 
+// Two results as bf16 terms of 16 bits together (the first ones; *low: the
+// second): the first is cut off, not rounded, so that a finite result's is finite;
+// the second holds what that leaves, nothing beside an infinity.
+__device__ __forceinline__ uint32_t terms_of(float a, float b, uint32_t* low) {
+  const uint32_t high = __float_as_uint(a) >> 16 | (__float_as_uint(b) & 0xffff0000u);
+  *low = pack_bf16(a == bf16_lo(high) ? 0.f : a - bf16_lo(high), b == bf16_hi(high) ? 0.f : b - bf16_hi(high));
+  return high;
+}
+
 __device__ __forceinline__ float swiglu(float g, float u) { return g / (1.f + expf(-g)) * u; }
 
 constexpr int kFewThreads = 256;
@@ -572,8 +581,13 @@ __device__ __forceinline__ int rows_of(const ProductArgs& a, int g, int* first) 
   return max(min(max(a.start[g + 1], 0), a.M) - *first, 0);
 }
 
+// Rows of x of a tile: with rows of two terms each of them takes two places
+template <int X, int CT>
+constexpr int kTileOf = X == kXTermRows ? 32 * CT : 64 * CT;
+
 // A tile is 256 weight rows (128 outputs of both matrices for SwiGLU) by 64 * CT
-// rows of one group.  A workgroup stays on its compute unit and takes tiles one
+// rows of one group (kXTermRows: 64 rows of two terms, each of a wave's 32 rows in
+// two of its columns, which are added at the tile's end).  A workgroup stays on its compute unit and takes tiles one
 // after the other, neighbouring tiles on one XCD.  K goes through LDS in stages
 // of 128 bytes of a row in 4 bits (64 beside bf16 rows of x, whose stages are 256
 // bytes), in three buffers that are loaded two stages ahead, over the tiles'
@@ -598,7 +612,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   constexpr int KB = kMx4 ? 4 : 2;                  // blocks of a lane and stage
   constexpr int BL = 2 * KB;                        // blocks of a row and stage
   constexpr int AC = BL, BC = kMx4 ? BL : 4 * BL;   // 16-byte pieces of a row
-  constexpr int TM = 64 * CT;
+  constexpr bool kTerms = X == kXTermRows;
+  static_assert(!kTerms || CT == 2, "a column for each term");
+  constexpr int TM = 64 * CT, TR = kTileOf<X, CT>;  // places for rows of x, and rows
   constexpr int kA = kTileRows * AC * 16, kB = TM * BC * 16;
   constexpr int AI = kTileRows * AC / kTileThreads, BI = TM * BC / kTileThreads;  // loads of a wave
   using Word = typename std::conditional<kMx4, uint64_t, uint32_t>::type;  // a row's scales of a stage
@@ -623,13 +639,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   const int half = lane >> 5, l32 = lane & 31, wf = wave & 3, wt = wave >> 2;
 
   // tiles of the groups before each one (thread t: groups 2t and 2t + 1)
-  int row_tiles = (a.M + TM - 1) / TM;
+  int row_tiles = (a.M + TR - 1) / TR;
   if (a.start) {
     int n[2], first[2], rows[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       rows[j] = 2 * tid + j < a.groups ? rows_of(a, 2 * tid + j, &first[j]) : 0;
-      n[j] = (rows[j] + TM - 1) / TM;
+      n[j] = (rows[j] + TR - 1) / TR;
     }
     int incl = n[0] + n[1];
 #pragma unroll
@@ -673,7 +689,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
     const int band = static_cast<int>(j / (kBand * a.columns)), tiles = min(kBand, row_tiles - band * kBand);
     const int in_band = static_cast<int>(j - static_cast<int64_t>(band) * kBand * a.columns);
     const int tile = band * kBand + in_band % tiles;
-    Tile t{0, tile * TM, min(a.M - tile * TM, TM), in_band / tiles};
+    Tile t{0, tile * TR, min(a.M - tile * TR, TR), in_band / tiles};
     if (a.start) {
       int n = 0;
       for (int g = lane; g - lane < a.groups; g += 64) n += __popcll(__ballot(g < a.groups && s_before[g] <= tile));
@@ -683,9 +699,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
         first = s_before[kKept + t.group], rows = s_before[2 * kKept + t.group];
       else
         rows = rows_of(a, t.group, &first);
-      const int at = (tile - s_before[t.group]) * TM;
+      const int at = (tile - s_before[t.group]) * TR;
       t.first = __builtin_amdgcn_readfirstlane(first + at);
-      t.count = __builtin_amdgcn_readfirstlane(min(rows - at, TM));
+      t.count = __builtin_amdgcn_readfirstlane(min(rows - at, TR));
     }
     return t;
   };
@@ -708,12 +724,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   const int scale_q = wave * 64 + lane, scale_c = scale_q % SC;
   const int scale_ra = min(scale_q / SC, kTileRows - 1), scale_rb = min(scale_q / SC, TM - 1);
 
+  // The place in LDS that load i of this lane goes to, of TM
+  const auto place_at = [&](int i) { return ((i * kTileWaves + wave) * 64 + lane) / BC; };
   // Rows of x of a tile; the pairs' loads are on their way until they are used
   int x_pair[BI], x_pair_scale = 0;
   const auto fetch = [&](const Tile& t) {
 #pragma unroll
     for (int i = 0; i < BI; ++i) {
-      const int p = t.first + min(((i * kTileWaves + wave) * 64 + lane) / BC, t.count - 1);
+      const int r = place_at(i), p = t.first + min(kTerms ? r / 64 * 32 + r % 32 : r, t.count - 1);
       x_pair[i] = a.pair ? a.pair[p] : p;
     }
     if (kMx4) {
@@ -742,7 +760,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
       pa[i] = static_cast<uint32_t>(weight_row(((i * kTileWaves + wave) * 64 + lane) / AC) - window) *
               static_cast<uint32_t>(a.nb) * 16;
 #pragma unroll
-    for (int i = 0; i < BI; ++i) pb[i] = static_cast<const uint8_t*>(a.x) + (x_pair[i] / a.xdiv) * a.x_stride + cb[i] * 16;
+    for (int i = 0; i < BI; ++i)
+      pb[i] = static_cast<const uint8_t*>(a.x) + (x_pair[i] / a.xdiv) * a.x_stride + cb[i] * 16 +
+              (kTerms && place_at(i) & 32 ? a.x_stride / 2 : 0);
 #pragma unroll
     for (int i = 0; i < SI; ++i) {
       const int64_t row = i == 0 ? first_row + (kSwiglu && (scale_ra >> 5 & 1) ? a.N : 0) + weight_row(scale_ra) : x_pair_scale / a.xdiv;
@@ -887,9 +907,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
   const auto write_out = [&](const Tile& t, auto buf) {
     wait_loads<0>();  // the next tile's first two stages
     uint8_t* mine = kA >= 8 * 4096 || wave < 4 ? a_of(buf) + wave * 4096 : b_of(buf) + (wave - 4) * 4096;
+    constexpr int kColumns = TR / 64;
+    if constexpr (kTerms) acc[0][0] += acc[0][1], acc[1][0] += acc[1][1];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      const int r0 = (wt * CT + c) * 32, r = r0 + l32;
+    for (int c = 0; c < kColumns; ++c) {
+      const int r0 = (wt * kColumns + c) * 32, r = r0 + l32;
       const int64_t row = t.first + r;
       const bool ok = r < t.count;
       if constexpr (kSwiglu) {
@@ -920,15 +942,26 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
             if (half == 0) a.out_scales[(row * a.N + f) / 32] = static_cast<uint8_t>(byte);
           }
         } else {
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-            store8(reinterpret_cast<__bf16*>(mine + (l32 * 4 + swizzled<4>(l32, half * 2 + k)) * 16), y + 8 * k);
+          // two terms (Out), 64 bytes of 32 rows each
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const int s = k * 16 + lane / 4, q = lane % 4;
-            const u32x4 v = *reinterpret_cast<const u32x4*>(mine + (s * 4 + swizzled<4>(s, q)) * 16);
+            u32x4 high, low;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t l;
+              high[j] = terms_of(y[8 * k + 2 * j], y[8 * k + 2 * j + 1], &l);
+              low[j] = l;
+            }
+            uint8_t* to = mine + (l32 * 4 + swizzled<4>(l32, half * 2 + k)) * 16;
+            *reinterpret_cast<u32x4*>(to) = high;
+            *reinterpret_cast<u32x4*>(to + 2048) = low;
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int s = k % 2 * 16 + lane / 4, q = lane % 4, term = k / 2;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(mine + term * 2048 + (s * 4 + swizzled<4>(s, q)) * 16);
             if (r0 + s < t.count)
-              *reinterpret_cast<u32x4*>(static_cast<__bf16*>(a.out) + static_cast<int64_t>(t.first + r0 + s) * a.N + f0 + 8 * q) = v;
+              *reinterpret_cast<u32x4*>(static_cast<__bf16*>(a.out) + (int64_t{2} * (t.first + r0 + s) + term) * a.N + f0 + 8 * q) = v;
           }
         }
       } else {
@@ -1185,7 +1218,7 @@ hipError_t launch_tile(ProductArgs a, hipStream_t st) {
   a.columns = (a.N + kOutputs - 1) / kOutputs;
   a.wide_out = wide_rows(a.out, a.out_stride, sizeof(Out));
   // groups with a last tile of their own: at most one a group, and one a row
-  const int64_t tiles = (a.M / (64 * CT) + std::min(a.groups, a.M)) * static_cast<int64_t>(a.columns);
+  const int64_t tiles = (a.M / kTileOf<X, CT> + std::min(a.groups, a.M)) * static_cast<int64_t>(a.columns);
   const int64_t grid = std::min<int64_t>((tiles + kXcds - 1) / kXcds * kXcds, kTileWorkgroups);
   return launch(mx4_tile_kernel<X, kSwiglu, Out, CT>, static_cast<unsigned>(grid), kTileThreads, a, st);
 }
@@ -1248,12 +1281,13 @@ struct Space {
 size_t up256(size_t n) { return (n + 255) & ~size_t{255}; }
 
 // h: the SwiGLU's results, y: the experts' results, which are terms of the gates'
-// sum and stay in fp32.  Few rows an expert: at the pairs' own places; the weights'
-// reads bound such calls, and h goes into the second product as two terms.  Many,
-// sorted: h in bf16 or 4 bits.  Beside 4-bit products too y's fp32 is paid for: 4,096
-// tokens of 8 experts of 2048 write and read 268 MB more than in bf16 (307 us a call in place of 252),
-// which makes their outputs' error that of the output's rounding (0.0017 of their
-// 2-norm) instead of 0.0024.
+// sum and stay in fp32.  h goes into the second product as two bf16 terms, or in 4
+// bits.  Few rows an expert: at the pairs' own places, h in fp32 or terms (the
+// weights' reads bound such calls).  Many: sorted.  There too both are paid for, so
+// that what a call keeps does not go by its number of tokens: with h rounded to bf16
+// 1,024 tokens of 6 of 64 experts of 1280 x 896 take 112 us instead of 127, with y in
+// bf16 beside 4-bit products 4,096 tokens of 8 of 128 of 2048 x 768 take 252 instead
+// of 305 (268 MB less), and each makes 1.4 times the error of the output's rounding.
 Space few_space(int64_t P, int32_t D, int32_t I) {
   Space s{};
   s.y = up256(static_cast<size_t>(P) * I * 4);
@@ -1269,7 +1303,7 @@ Space tile_space(int64_t T, int64_t P, int32_t n, int32_t D, int32_t I, bool mx4
     at += up256(bytes);
     return from;
   };
-  s.h = take(static_cast<size_t>(P) * I * 2 / (mx4 ? 4 : 1));
+  s.h = take(mx4 ? static_cast<size_t>(P) * I / 2 : static_cast<size_t>(P) * I * 4);
   s.y = take(static_cast<size_t>(P) * D * 4);
   s.start = take((static_cast<size_t>(n) + 1) * 4);
   s.pair = take(static_cast<size_t>(P) * 4);
@@ -1452,15 +1486,15 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
     a.x_blocks = static_cast<int64_t>(T) * a.nb;
     a.out_scales = space + s.h_scales;
     int rows = tile_rows(P, n, 2 * I, a.nb, mx4);
-    e = mx4 ? launch_tiles<kXCodes, true, __bf16>(a, rows, st) : launch_tiles<kXBf16, true, __bf16>(a, rows, st);
+    e = mx4 ? launch_tiles<kXCodes, true, __bf16>(a, rows, st) : launch_tiles<kXBf16, true, Terms>(a, rows, st);
     if (e != hipSuccess) return launched(e);
     ProductArgs d = product_of(*down, n, start, static_cast<int32_t>(P), space + s.y, D);
     d.x = space + s.h;
-    d.x_stride = mx4 ? I / 2 : static_cast<int64_t>(I) * 2;
+    d.x_stride = mx4 ? I / 2 : static_cast<int64_t>(I) * 4;
     d.x_scales = space + s.h_scales;
     d.x_blocks = P * d.nb;
     rows = tile_rows(P, n, D, d.nb, mx4);
-    e = mx4 ? launch_tiles<kXCodes, false, float>(d, rows, st) : launch_tiles<kXBf16, false, float>(d, rows, st);
+    e = mx4 ? launch_tiles<kXCodes, false, float>(d, rows, st) : launch_tile<kXTermRows, false, float, 2>(d, st);
     if (e != hipSuccess) return launched(e);
     c.place = place;
     return launched(spp::launch_expert_combine(c, st));

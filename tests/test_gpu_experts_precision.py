@@ -62,6 +62,6 @@ def test_results_of_4_bit_products_stay_in_fp32(torch, T, n, K, D, I, kind):  # 
     check_kept(exact_experts(T, n, K, D, I, kind, T + I), "mx4")
 
 
-@pytest.mark.parametrize("T,n,K,D,I,kind", FEW)
+@pytest.mark.parametrize("T,n,K,D,I,kind", FEW + TILES)
 def test_swiglu_results_keep_16_bits(torch, T, n, K, D, I, kind):  # noqa: F811
     check_kept(exact_experts(T, n, K, D, I, kind, T + I), "bf16")
