@@ -432,15 +432,9 @@ __global__ __launch_bounds__(kFewThreads) void mx4_few_kernel(ProductArgs a) {
         const int64_t row = kRows == kRowsIds ? s_row[i] : begin + r0 + i;
         if constexpr (std::is_same<Out, Terms>::value) {  // N is a multiple of 32
           __bf16* out = static_cast<__bf16*>(a.out) + row * 2 * a.N + f;
-          u32x2 high{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])}, low;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            // what is infinite or NaN is so in the first term, and the second adds nothing
-            const float l0 = y[2 * e] - bf16_lo(high[e]), l1 = y[2 * e + 1] - bf16_hi(high[e]);
-            low[e] = pack_bf16(l0 == l0 ? l0 : 0.f, l1 == l1 ? l1 : 0.f);
-          }
-          *reinterpret_cast<u32x2*>(out) = high;
-          *reinterpret_cast<u32x2*>(out + a.N) = low;
+          uint32_t low0, low1;
+          *reinterpret_cast<u32x2*>(out) = u32x2{terms_of(y[0], y[1], &low0), terms_of(y[2], y[3], &low1)};
+          *reinterpret_cast<u32x2*>(out + a.N) = u32x2{low0, low1};
           continue;
         } else {
           Out* out = static_cast<Out*>(a.out) + row * a.out_stride + f;

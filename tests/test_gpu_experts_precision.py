@@ -65,3 +65,32 @@ def test_results_of_4_bit_products_stay_in_fp32(torch, T, n, K, D, I, kind):  # 
 @pytest.mark.parametrize("T,n,K,D,I,kind", FEW + TILES)
 def test_swiglu_results_keep_16_bits(torch, T, n, K, D, I, kind):  # noqa: F811
     check_kept(exact_experts(T, n, K, D, I, kind, T + I), "bf16")
+
+
+@pytest.mark.parametrize("T,n,K", [(1, 4, 2), (2, 8, 3), (5, 8, 2), (40, 4, 3), (300, 4, 2)])
+@pytest.mark.parametrize("u_exp,finite", [(64, True), (66, False), (-60, True)])
+def test_swiglu_results_at_the_largest_floats(torch, T, n, K, u_exp, finite):  # noqa: F811
+    """h = 1.99994 * 2^127 is finite in fp32 and would round to infinity in bf16; 4 h is infinite, and so is its output."""
+    D, I = 96, 64
+    e = Experts(T, n, K, D, I, "distinct", residual=False)
+    gu, dn = np.zeros((n, 2 * I, D)), np.zeros((n, D, I))
+    gu[:, 0, :2] = 1.0                                   # g = x0 + x1
+    gu[:, I, 2] = 1.0                                    # u = x2
+    dn[:, :, 0] = 1.5
+    for m, v in ((e.gu, gu), (e.dn, dn)):
+        m.codes, m.scales = ox.quantise(v.reshape(m.codes.shape))
+        m.upload()
+        assert np.array_equal(m.v, v.reshape(m.codes.shape))
+    e.dn.scales = e.dn.scales - 60
+    e.dn.upload()
+    x = np.zeros((T, D))
+    x[:, :3] = [255 / 128 * 2.0 ** 63, 127 / 128 * 2.0 ** 56, 2.0 ** u_exp]
+    e.x[:, :D] = dev(x, "bf16")
+    assert np.array_equal(host(e.x[:, :D]), x)
+    got = host(e.run("bf16"))[:T, :D]
+    h = (x[:, 0] + x[:, 1]) * x[:, 2]
+    want = h * 1.5 * 2.0 ** -60 * host(e.gates).sum(1)
+    if finite:      # h's 16 bits, sums of K fp32 gates, the output's rounding
+        assert np.all(np.abs(got - want[:, None]) <= (U_TERMS + (K + 3) * 2 * ox.U32 + U["bf16"]) * want[:, None] * (1 + 1e-3))
+    else:
+        assert np.isposinf(got).all()
