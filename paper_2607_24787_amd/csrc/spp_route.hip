@@ -500,7 +500,9 @@ RowArgs rows_of(int32_t T, int32_t K, int32_t D, int elem) {
   a.T = T;
   a.K = K;
   a.pieces = D * elem / 16;
-  while (a.shift < 8 && 1 << a.shift < a.pieces) ++a.shift;
+  // a launch has fewer than 2^32 threads: of 2^24 tokens none gets a whole workgroup
+  const int most = T < kMaxPairs ? 8 : 7;
+  while (a.shift < most && 1 << a.shift < a.pieces) ++a.shift;
   return a;
 }
 
