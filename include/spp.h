@@ -498,7 +498,8 @@ spp_status spp_attention_step(spp_ctx* ctx, int32_t B, const int32_t* pos, int64
  * back.  Operators on explicit device pointers, as the attention's above: no
  * context, no allocation, no host wait, work enqueued on hip_stream of the
  * current device, fit for capture into a graph; a call with nothing to do
- * returns SPP_OK; EINVAL before anything is enqueued.
+ * returns SPP_OK; EINVAL before anything is enqueued.  Arrays overlap where
+ * they share a byte: column ranges of one buffer's rows do not.
  *
  * Matrix: rows x cols elements, cols a multiple of 32, at most 2^17.  codes:
  * dev [rows][cols/2], byte j of a row holds elements 2j (low nibble) and 2j+1;

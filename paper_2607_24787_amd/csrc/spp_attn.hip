@@ -1354,26 +1354,6 @@ uint64_t extent(int64_t stride, int64_t T, int heads, int d, int elem) {
   return static_cast<uint64_t>((T - 1) * stride + static_cast<int64_t>(heads) * d) * static_cast<uint64_t>(elem);
 }
 
-// Whether T rows of na bytes, sa bytes apart, and T rows of nb bytes, sb apart,
-// have a byte in common (a stride is at least its row).  Rows of one fused
-// product lie between each other without.
-bool rows_overlap(const void* a, int64_t sa, int64_t na, const void* b, int64_t sb, int64_t nb, int64_t T) {
-  const int64_t span_a = (T - 1) * sa + na, span_b = (T - 1) * sb + nb;
-  if (!overlap(a, static_cast<uint64_t>(span_a), b, static_cast<uint64_t>(span_b))) return false;
-  const int64_t off = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
-  const auto below = [](int64_t x, int64_t y) { return x / y - (x % y < 0); };  // floor(x / y)
-  // rows of a from the first that ends past row u of b to the last that starts before its end
-  const auto meets = [&](int64_t u) {
-    const int64_t at = off + u * sb;
-    return std::max<int64_t>(0, below(at - na, sa) + 1) <= std::min<int64_t>(T - 1, below(at + nb - 1, sa));
-  };
-  // with one stride all of b's rows lie alike to a's: its first and last are the ones that meet the most
-  if (sa == sb) return meets(0) || meets(T - 1);
-  for (int64_t u = 0; u < T; ++u)
-    if (meets(u)) return true;
-  return false;
-}
-
 template <typename T>
 hipError_t launch_store(const StoreArgs& a, int d, unsigned grid, hipStream_t st) {
   return d == 128 ? launch(kv4_store_kernel<T, 128>, grid, 256, a, st) : launch(kv4_store_kernel<T, 64>, grid, 256, a, st);
@@ -1537,10 +1517,9 @@ extern "C" spp_status spp_kv4_store(const spp_attn_desc* desc, void* cache, int3
     if (!same && overlap(q, extent(q_stride, T, desc->n_heads, d, elem), q_out, out_bytes))
       return bad("q_out must be q with the same stride, or not overlap it");
     const int64_t kv_bytes = static_cast<int64_t>(desc->n_kv_heads) * d * elem;
-    for (const auto& [rows, stride] : {std::pair{k, k_stride}, std::pair{v, v_stride}})
-      if (rows_overlap(q_out, q_out_stride * elem, static_cast<int64_t>(desc->n_heads) * d * elem, rows, stride * elem,
-                       kv_bytes, T))
-        return bad("q_out must not overlap rows of k or v");
+    const Rows q_rows{q_out, static_cast<int64_t>(desc->n_heads) * d * elem, q_out_stride * elem, T};
+    for (const auto& [at, stride] : {std::pair{k, k_stride}, std::pair{v, v_stride}})
+      if (meet(q_rows, Rows{at, kv_bytes, stride * elem, T})) return bad("q_out must not overlap rows of k or v");
   }
   StoreArgs a{};
   a.cache = cache_of(desc, cache);
@@ -1579,7 +1558,7 @@ extern "C" spp_status spp_kv4_load(const spp_attn_desc* desc, const void* cache,
   if (k_out) SPP_BAD(rows_why(k_out, k_stride, desc->n_kv_heads, d, elem));
   if (v_out) SPP_BAD(rows_why(v_out, v_stride, desc->n_kv_heads, d, elem));
   const int64_t row_bytes = static_cast<int64_t>(desc->n_kv_heads) * d * elem;
-  if (k_out && v_out && rows_overlap(k_out, k_stride * elem, row_bytes, v_out, v_stride * elem, row_bytes, T))
+  if (meet(Rows{k_out, row_bytes, k_stride * elem, T}, Rows{v_out, row_bytes, v_stride * elem, T}))
     return bad("k_out must not overlap rows of v_out");
   LoadArgs a{};
   a.cache = cache_of(desc, cache);

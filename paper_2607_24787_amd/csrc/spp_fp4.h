@@ -5,8 +5,10 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <type_traits>
+#include <utility>
 
 #include "spp.h"
 #include "spp_internal.h"
@@ -121,6 +123,45 @@ spp_status bad(const char* why) { return spp::set_error(SPP_EINVAL, why); }
 bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
+}
+
+// `count` rows of `bytes` each, `stride` bytes apart (at least a row); an array is one row
+struct Rows {
+  const void* at;
+  int64_t bytes, stride, count;
+};
+
+Rows array(const void* p, int64_t bytes) { return {p, bytes, bytes, 1}; }
+Rows rows_from(const void* p, int64_t stride, int64_t row, int64_t count, int elem) { return {p, row * elem, stride * elem, count}; }
+
+// Whether they have a byte in common.  Column ranges of one buffer lie between
+// each other without.
+bool meet(Rows a, Rows b) {
+  if (!a.at || !b.at || a.count < 1 || b.count < 1) return false;
+  if (a.count < b.count) std::swap(a, b);
+  if (!overlap(a.at, static_cast<uint64_t>((a.count - 1) * a.stride + a.bytes), b.at,
+               static_cast<uint64_t>((b.count - 1) * b.stride + b.bytes)))
+    return false;
+  const int64_t off = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.at) - reinterpret_cast<uintptr_t>(a.at));
+  const auto below = [](int64_t x, int64_t y) { return x / y - (x % y < 0); };  // floor(x / y)
+  // rows of a, before the first and behind the last too, from the first that ends past row u of b to the last that
+  // starts before its end
+  const auto first = [&](int64_t u) { return below(off + u * b.stride - a.bytes, a.stride) + 1; };
+  const auto last = [&](int64_t u) { return below(off + u * b.stride + b.bytes - 1, a.stride); };
+  if (a.stride == b.stride) {  // row u meets the rows that row 0 meets, u further on
+    const int64_t f = first(0), l = last(0);
+    return f <= l && std::max<int64_t>(0, -l) <= std::min<int64_t>(b.count - 1, a.count - 1 - f);
+  }
+  for (int64_t u = 0; u < b.count; ++u)
+    if (std::max<int64_t>(0, first(u)) <= std::min<int64_t>(a.count - 1, last(u))) return true;
+  return false;
+}
+
+const char* rows_why(const void* p, int64_t stride, int64_t row, int elem) {
+  if (!p) return "a pointer to rows is NULL";
+  if (stride < row || stride > int64_t{1} << 30) return "a row stride must be at least a row, at most 2^30 elements";
+  if (!aligned16(p) || stride * elem % 16 != 0) return "rows must be 16-byte aligned, their stride a multiple of 16 bytes";
+  return nullptr;
 }
 
 const char* dtype_why(int32_t dtype) {

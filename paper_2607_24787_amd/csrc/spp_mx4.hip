@@ -1068,18 +1068,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a
 
 // ------------------------------------------------------------------ host side
 
-const char* rows_why(const void* p, int64_t stride, int64_t row, int elem) {
-  if (!p) return "a pointer to rows is NULL";
-  if (stride < row || stride > int64_t{1} << 30) return "a row stride must be at least a row, at most 2^30 elements";
-  if (!aligned16(p) || stride * elem % 16 != 0) return "rows must be 16-byte aligned, their stride a multiple of 16 bytes";
-  return nullptr;
-}
-
-// The end of rows as bytes from their start
-uint64_t span(int64_t rows, int64_t stride, int64_t row, int elem) {
-  return rows < 1 ? 0 : static_cast<uint64_t>((rows - 1) * stride + row) * static_cast<uint64_t>(elem);
-}
-
 const char* matrix_why(const spp_mx4_matrix* m) {
   if (!m) return "a matrix is NULL";
   if (m->cols < 32 || m->cols > 1 << 17 || m->cols % 32 != 0) return "cols must be a multiple of 32, at most 2^17";
@@ -1090,11 +1078,11 @@ const char* matrix_why(const spp_mx4_matrix* m) {
   return nullptr;
 }
 
-uint64_t code_bytes(const spp_mx4_matrix& m) { return static_cast<uint64_t>(m.rows) * (m.cols / 2); }
-uint64_t scale_bytes(const spp_mx4_matrix& m) { return static_cast<uint64_t>(m.rows) * (m.cols / 32); }
+int64_t code_bytes(const spp_mx4_matrix& m) { return m.rows * (m.cols / 2); }
+int64_t scale_bytes(const spp_mx4_matrix& m) { return m.rows * (m.cols / 32); }
 
-bool over(const spp_mx4_matrix& m, const void* p, uint64_t bytes) {
-  return overlap(m.codes, code_bytes(m), p, bytes) || overlap(m.scales, scale_bytes(m), p, bytes);
+bool over(const spp_mx4_matrix& m, const Rows& r) {
+  return meet(r, array(m.codes, code_bytes(m))) || meet(r, array(m.scales, scale_bytes(m)));
 }
 
 unsigned quant_grid(int64_t words) {
@@ -1127,8 +1115,8 @@ const char* product_why(const spp_mx4_matrix* w, int32_t groups, const int32_t* 
   if (M == 0) return nullptr;
   if (!out || !aligned(out, dtype == SPP_DTYPE_BF16 ? 2 : 4)) return "out must not be NULL, and aligned to its elements";
   if (out_stride < N || out_stride > int64_t{1} << 30) return "out's stride must be at least a row, at most 2^30 elements";
-  const uint64_t bytes = span(M, out_stride, N, dtype == SPP_DTYPE_BF16 ? 2 : 4);
-  if (over(*w, out, bytes) || (start && overlap(start, static_cast<uint64_t>(groups + 1) * 4, out, bytes)))
+  const Rows to = rows_from(out, out_stride, N, M, dtype == SPP_DTYPE_BF16 ? 2 : 4);
+  if (over(*w, to) || meet(to, array(start, (groups + 1) * 4)))
     return "out must not overlap an input";
   return nullptr;
 }
@@ -1331,7 +1319,7 @@ extern "C" spp_status spp_mx4_quantize(int32_t dtype, const void* x, int64_t x_s
   if (q->rows == 0) return SPP_OK;
   const int elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
   SPP_BAD(rows_why(x, x_stride, q->cols, elem));
-  if (over(*q, x, span(q->rows, x_stride, q->cols, elem)) || overlap(q->codes, code_bytes(*q), q->scales, scale_bytes(*q)))
+  if (over(*q, rows_from(x, x_stride, q->cols, q->rows, elem)) || meet(array(q->codes, code_bytes(*q)), array(q->scales, scale_bytes(*q))))
     return bad("x, codes and scales must not overlap");
   RowsQ a{};
   a.x = x;
@@ -1351,7 +1339,7 @@ extern "C" spp_status spp_mx4_load(const spp_mx4_matrix* q, int32_t dtype, void*
   if (q->rows == 0) return SPP_OK;
   const int elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
   SPP_BAD(rows_why(out, out_stride, q->cols, elem));
-  if (over(*q, out, span(q->rows, out_stride, q->cols, elem))) return bad("out must not overlap codes or scales");
+  if (over(*q, rows_from(out, out_stride, q->cols, q->rows, elem))) return bad("out must not overlap codes or scales");
   RowsQ a{};
   a.out = out;
   a.out_stride = out_stride;
@@ -1369,8 +1357,8 @@ extern "C" spp_status spp_mx4_matmul(const spp_mx4_matrix* w, int32_t groups, co
   SPP_BAD(product_why(w, groups, start, M, dtype, out, out_stride));
   if (M == 0) return SPP_OK;
   SPP_BAD(rows_why(x, x_stride, w->cols, 2));
-  const uint64_t bytes = span(M, out_stride, w->rows / groups, dtype == SPP_DTYPE_BF16 ? 2 : 4);
-  if (overlap(x, span(M, x_stride, w->cols, 2), out, bytes)) return bad("out must not overlap an input");
+  if (meet(rows_from(out, out_stride, w->rows / groups, M, dtype == SPP_DTYPE_BF16 ? 2 : 4), rows_from(x, x_stride, w->cols, M, 2)))
+    return bad("out must not overlap an input");
   ProductArgs a = product_of(*w, groups, start, M, out, out_stride);
   a.x = x;
   a.x_stride = x_stride * 2;
@@ -1384,8 +1372,8 @@ extern "C" spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups
   SPP_BAD(matrix_why(x));
   if (x->rows != M || x->cols != w->cols) return bad("x must have M rows and the weights' cols");
   if (M == 0) return SPP_OK;
-  const uint64_t bytes = span(M, out_stride, w->rows / groups, dtype == SPP_DTYPE_BF16 ? 2 : 4);
-  if (over(*x, out, bytes)) return bad("out must not overlap an input");
+  if (over(*x, rows_from(out, out_stride, w->rows / groups, M, dtype == SPP_DTYPE_BF16 ? 2 : 4)))
+    return bad("out must not overlap an input");
   ProductArgs a = product_of(*w, groups, start, M, out, out_stride);
   a.x = x->codes;
   a.x_stride = x->cols / 2;
@@ -1421,14 +1409,13 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
   if (!topk || !gates || !aligned(topk, 4) || !aligned(gates, 4))
     return bad("topk and gates must not be NULL, and aligned to their elements");
   const int64_t P = static_cast<int64_t>(T) * K;
-  const uint64_t out_bytes = span(T, out_stride, D, 2), each = static_cast<uint64_t>(P) * 4;
-  if (overlap(x, span(T, x_stride, D, 2), out, out_bytes) || overlap(topk, each, out, out_bytes) ||
-      overlap(gates, each, out, out_bytes) || over(*gate_up, out, out_bytes) || over(*down, out, out_bytes))
+  const Rows to = rows_from(out, out_stride, D, T, 2);
+  if (meet(to, rows_from(x, x_stride, D, T, 2)) || meet(to, array(topk, P * 4)) || meet(to, array(gates, P * 4)) ||
+      over(*gate_up, to) || over(*down, to))
     return bad("out must not overlap an input");
   if (residual) {
     SPP_BAD(rows_why(residual, residual_stride, D, 2));
-    if (!(residual == out && residual_stride == out_stride) &&
-        overlap(residual, span(T, residual_stride, D, 2), out, out_bytes))
+    if (!(residual == out && residual_stride == out_stride) && meet(to, rows_from(residual, residual_stride, D, T, 2)))
       return bad("out must be residual with the same stride, or not overlap it");
   }
   const bool mx4 = act == SPP_ACT_MX4;

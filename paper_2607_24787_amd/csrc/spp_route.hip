@@ -478,21 +478,10 @@ void parts_of(int64_t P, int* parts, int* each) {
   *parts = static_cast<int>(std::max<int64_t>(1, (P + e - 1) / e));
 }
 
-const char* expert_rows_why(const void* p, int64_t stride, int64_t row, int elem) {
-  if (!p) return "a pointer to rows is NULL";
-  if (stride < row || stride > int64_t{1} << 30) return "a row stride must be at least a row, at most 2^30 elements";
-  if (!aligned16(p) || stride * elem % 16 != 0) return "rows must be 16-byte aligned, their stride a multiple of 16 bytes";
-  return nullptr;
-}
-
 const char* width_why(int32_t D, int elem) {
   return D < 1 || D > 1 << 20 || static_cast<int64_t>(D) * elem % 16 != 0
              ? "D must be positive, at most 2^20, and a row a multiple of 16 bytes"
              : nullptr;
-}
-
-uint64_t span(int64_t rows, int64_t stride, int64_t row, int elem) {
-  return static_cast<uint64_t>((rows - 1) * stride + row) * static_cast<uint64_t>(elem);
 }
 
 RowArgs rows_of(int32_t T, int32_t K, int32_t D, int elem) {
@@ -616,11 +605,11 @@ extern "C" spp_status spp_expert_gather(int32_t dtype, const void* x, int64_t x_
   const int elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
   SPP_BAD(width_why(D, elem));
   if (T == 0) return SPP_OK;
-  SPP_BAD(expert_rows_why(x, x_stride, D, elem));
-  SPP_BAD(expert_rows_why(rows, rows_stride, D, elem));
+  SPP_BAD(rows_why(x, x_stride, D, elem));
+  SPP_BAD(rows_why(rows, rows_stride, D, elem));
   if (!place || !aligned(place, 4)) return bad("place must not be NULL, and aligned to its elements");
-  if (overlap(x, span(T, x_stride, D, elem), rows, span(static_cast<int64_t>(T) * K, rows_stride, D, elem)))
-    return bad("rows must not overlap x");
+  const Rows to = rows_from(rows, rows_stride, D, static_cast<int64_t>(T) * K, elem);
+  if (meet(to, rows_from(x, x_stride, D, T, elem))) return bad("rows must not overlap x");
   RowArgs a = rows_of(T, K, D, elem);
   a.x = x;
   a.x_stride = x_stride * elem;
@@ -638,17 +627,15 @@ extern "C" spp_status spp_expert_combine(int32_t dtype, const void* rows, int64_
   const int elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
   SPP_BAD(width_why(D, elem));
   if (T == 0) return SPP_OK;
-  SPP_BAD(expert_rows_why(rows, rows_stride, D, elem));
-  SPP_BAD(expert_rows_why(out, out_stride, D, elem));
+  SPP_BAD(rows_why(rows, rows_stride, D, elem));
+  SPP_BAD(rows_why(out, out_stride, D, elem));
   if (!place || !aligned(place, 4) || !aligned(weights, 4))
     return bad("place must not be NULL, place and weights aligned to their elements");
-  const uint64_t out_bytes = span(T, out_stride, D, elem);
-  if (overlap(rows, span(static_cast<int64_t>(T) * K, rows_stride, D, elem), out, out_bytes))
-    return bad("out must not overlap rows");
+  const Rows to = rows_from(out, out_stride, D, T, elem);
+  if (meet(to, rows_from(rows, rows_stride, D, static_cast<int64_t>(T) * K, elem))) return bad("out must not overlap rows");
   if (residual) {
-    SPP_BAD(expert_rows_why(residual, residual_stride, D, elem));
-    if (!(residual == out && residual_stride == out_stride) &&
-        overlap(residual, span(T, residual_stride, D, elem), out, out_bytes))
+    SPP_BAD(rows_why(residual, residual_stride, D, elem));
+    if (!(residual == out && residual_stride == out_stride) && meet(to, rows_from(residual, residual_stride, D, T, elem)))
       return bad("out must be residual with the same stride, or not overlap it");
   }
   const spp::ExpertSum sum{rows, rows_stride, place,    nullptr,         weights, 0,          dtype,
@@ -665,21 +652,18 @@ extern "C" spp_status spp_expert_combine_grad(int32_t dtype, const void* d_out, 
   const int elem = dtype == SPP_DTYPE_BF16 ? 2 : 4;
   SPP_BAD(width_why(D, elem));
   if (T == 0 || (!d_rows && !d_weights)) return SPP_OK;
-  SPP_BAD(expert_rows_why(d_out, d_out_stride, D, elem));
+  SPP_BAD(rows_why(d_out, d_out_stride, D, elem));
   if (!place || !aligned(place, 4) || !aligned(weights, 4) || !aligned(d_weights, 4))
     return bad("place must not be NULL, place, weights and d_weights aligned to their elements");
   const int64_t P = static_cast<int64_t>(T) * K;
-  const uint64_t d_bytes = span(T, d_out_stride, D, elem);
-  if (d_weights) SPP_BAD(expert_rows_why(rows, rows_stride, D, elem));
+  if (d_weights) SPP_BAD(rows_why(rows, rows_stride, D, elem));
   if (d_rows) {
-    SPP_BAD(expert_rows_why(d_rows, d_rows_stride, D, elem));
-    const uint64_t bytes = span(P, d_rows_stride, D, elem);
-    if (overlap(d_rows, bytes, d_out, d_bytes)) return bad("d_rows must not overlap d_out");
-    if (d_weights && !(rows == d_rows && rows_stride == d_rows_stride) &&
-        overlap(d_rows, bytes, rows, span(P, rows_stride, D, elem)))
+    SPP_BAD(rows_why(d_rows, d_rows_stride, D, elem));
+    const Rows to = rows_from(d_rows, d_rows_stride, D, P, elem);
+    if (meet(to, rows_from(d_out, d_out_stride, D, T, elem))) return bad("d_rows must not overlap d_out");
+    if (d_weights && !(rows == d_rows && rows_stride == d_rows_stride) && meet(to, rows_from(rows, rows_stride, D, P, elem)))
       return bad("d_rows must be rows with the same stride, or not overlap them");
-    if (d_weights && overlap(d_rows, bytes, d_weights, static_cast<uint64_t>(P) * 4))
-      return bad("d_weights must not overlap d_rows");
+    if (meet(to, array(d_weights, P * 4))) return bad("d_weights must not overlap d_rows");
   }
   RowArgs a = rows_of(T, K, D, elem);
   a.x = rows;

@@ -2,7 +2,8 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_mx4 import blank, dev, host, stream, torch  # noqa: F401
+from tests.test_gpu_experts import Experts, Sorted, ids
+from tests.test_gpu_mx4 import Matrix, blank, dev, host, stream, torch  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +32,36 @@ def test_gather_and_combine_of_the_most_tokens(torch):  # noqa: F811
     assert (x[T] == 3.0).all() and (rows[T] == 3.0).all()
     del x, rows
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("M", [1, 9, 300])
+def test_inputs_and_outputs_as_columns_of_one_buffer(torch, M):  # noqa: F811
+    """The bits of calls with buffers of their own, and nothing else of the buffer changed."""
+    from paper_2607_24787_amd import spp
+    rng = np.random.default_rng(M)
+    D, W, n, bf16 = 64, 200, 5, spp.DTYPE_BF16
+    w, start = Matrix(rng, n * 40, D), dev(np.sort(np.r_[0, rng.integers(0, M + 1, n - 1), M]).astype(np.int32))
+    e = Experts(M, n, 1, D, 32, pad=0, residual=False)
+    s = Sorted(ids(rng, M, 1, n, "any"), n)
+    gates = dev(rng.random(M).astype(np.float32))
+    x = dev(rng.normal(size=(M, D)), "bf16")
+    calls = {
+        "matmul": (40, lambda x, xs, y, ys: spp.spp_mx4_matmul(w.desc, n, start.data_ptr(), x, xs, M, bf16, y, ys, stream())),
+        "experts": (D, lambda x, xs, y, ys: spp.spp_mx4_experts(
+            e.gu.desc, e.dn.desc, n, spp.ACT_MX4, x, xs, e.topk_dev.data_ptr(), e.gates.data_ptr(), M, 1, 0, 0, y, ys,
+            e.space.data_ptr(), e.size, stream())),
+        "gather": (D, lambda x, xs, y, ys: spp.spp_expert_gather(bf16, x, xs, s.place.data_ptr(), M, 1, D, y, ys, stream())),
+        "combine": (D, lambda x, xs, y, ys: spp.spp_expert_combine(bf16, x, xs, s.place.data_ptr(), gates.data_ptr(), M, 1, D, 0, 0,
+                                                                   y, ys, stream())),
+        "gradient": (D, lambda x, xs, y, ys: spp.spp_expert_combine_grad(bf16, x, xs, 0, 0, s.place.data_ptr(), gates.data_ptr(), M,
+                                                                         1, D, y, ys, 0, stream()))}
+    for name, (N, call) in calls.items():
+        alone, both = blank((M, N), "bf16"), blank((M + 1, W), "bf16")
+        call(x.data_ptr(), D, alone.data_ptr(), N)
+        both[:M, 72:72 + D] = x
+        call(both.data_ptr() + 2 * 72, W, both.data_ptr() + 2 * 8, W)
+        got = host(both)
+        assert np.array_equal(got[:M, 8:8 + N], host(alone)), name
+        assert np.array_equal(got[:M, 72:72 + D], host(x)), name
+        got[:M, 8:8 + N] = got[:M, 72:72 + D] = np.nan
+        assert np.isnan(got).all(), name
