@@ -565,7 +565,8 @@ spp_status spp_mx4_matmul_mx4(const spp_mx4_matrix* w, int32_t groups, const int
  * 2^36.
  * workspace: dev, 16-byte aligned, spp_mx4_experts_workspace bytes for every
  * call of at most T tokens (with either act); its contents do not matter, and
- * are undefined afterwards.  A call holds it until the stream has passed it:
+ * are undefined afterwards.  It overlaps nothing else that the call is given.
+ * A call holds it until the stream has passed it:
  * calls (and captured graphs) that may run at the same time need one each. */
 size_t spp_mx4_experts_workspace(int32_t n, int32_t D, int32_t I, int32_t T, int32_t K);
 spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_mx4_matrix* down, int32_t n, int32_t act,
@@ -579,6 +580,7 @@ spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_mx4_matrix* 
  * dev int32 [T][K]; start: dev int32 [n + 1]; pair, place: dev int32 [T * K].
  * A pair whose id is outside 0 .. n-1 has no place (place[p] = -1); the last
  * places then have no pair (pair[i] = -1).  n at most 1024, T * K at most 2^24.
+ * No array may overlap another.
  * workspace: as for spp_mx4_experts, spp_expert_sort_workspace bytes for every
  * call of at most T tokens. */
 size_t spp_expert_sort_workspace(int32_t T, int32_t K, int32_t n);
@@ -591,7 +593,8 @@ spp_status spp_expert_sort(const int32_t* topk, int32_t T, int32_t K, int32_t n,
  * the calls below).  place: of spp_expert_sort, or any other int32 [T * K]: an
  * entry outside 0 .. T*K-1 takes no row, rows that no entry names are left as
  * they were, and a row that two entries name holds either one's.  The gradient
- * of x is spp_expert_combine of the rows' gradients, without weights. */
+ * of x is spp_expert_combine of the rows' gradients, without weights.  rows
+ * overlaps neither x nor place. */
 spp_status spp_expert_gather(int32_t dtype, const void* x, int64_t x_stride, const int32_t* place, int32_t T, int32_t K,
                              int32_t D, void* rows, int64_t rows_stride, void* hip_stream);
 /* out[t] = [residual[t] +] sum_k weights[t][k] rows[place[t * K + k]], sums in
@@ -607,7 +610,8 @@ spp_status spp_expert_combine(int32_t dtype, const void* rows, int64_t rows_stri
  * NULL: 1.  d_rows may be rows with the same stride.  A pair without a place
  * gets d_weights 0, rows that no pair names are left as they were; a row that
  * two pairs name holds either one's (and d_rows must then not be rows).  The
- * residual's gradient is d_out itself. */
+ * residual's gradient is d_out itself.  But for rows, d_rows and d_weights overlap
+ * no input, and not each other. */
 spp_status spp_expert_combine_grad(int32_t dtype, const void* d_out, int64_t d_out_stride, const void* rows,
                                    int64_t rows_stride, const int32_t* place, const float* weights, int32_t T,
                                    int32_t K, int32_t D, void* d_rows, int64_t d_rows_stride, float* d_weights,

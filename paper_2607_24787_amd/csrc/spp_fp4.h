@@ -137,7 +137,7 @@ Rows rows_from(const void* p, int64_t stride, int64_t row, int64_t count, int el
 // Whether they have a byte in common.  Column ranges of one buffer lie between
 // each other without.
 bool meet(Rows a, Rows b) {
-  if (!a.at || !b.at || a.count < 1 || b.count < 1) return false;
+  if (!a.at || !b.at || a.count < 1 || b.count < 1 || a.bytes < 1 || b.bytes < 1) return false;
   if (a.count < b.count) std::swap(a, b);
   if (!overlap(a.at, static_cast<uint64_t>((a.count - 1) * a.stride + a.bytes), b.at,
                static_cast<uint64_t>((b.count - 1) * b.stride + b.bytes)))

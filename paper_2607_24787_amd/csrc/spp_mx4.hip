@@ -1423,6 +1423,10 @@ extern "C" spp_status spp_mx4_experts(const spp_mx4_matrix* gate_up, const spp_m
   const Space s = tiles ? tile_space(T, P, n, D, I, mx4) : few_space(P, D, I);
   if (!workspace || !aligned16(workspace)) return bad("workspace must not be NULL, and 16-byte aligned");
   if (workspace_bytes < s.bytes) return bad("the workspace is too small");
+  const Rows used = array(workspace, static_cast<int64_t>(s.bytes));
+  if (meet(used, to) || meet(used, rows_from(x, x_stride, D, T, 2)) || meet(used, rows_from(residual, residual_stride, D, T, 2)) ||
+      meet(used, array(topk, P * 4)) || meet(used, array(gates, P * 4)) || over(*gate_up, used) || over(*down, used))
+    return bad("the workspace must not overlap an input or the output");
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   uint8_t* space = static_cast<uint8_t*>(workspace);
 

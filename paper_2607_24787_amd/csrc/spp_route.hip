@@ -586,15 +586,16 @@ extern "C" spp_status spp_expert_sort(const int32_t* topk, int32_t T, int32_t K,
   if (!aligned(topk, 4) || !aligned(start, 4) || !aligned(pair, 4) || !aligned(place, 4))
     return bad("topk, start, pair and place must be aligned to their elements");
   const int64_t P = static_cast<int64_t>(T) * K;
-  const uint64_t each = static_cast<uint64_t>(P) * 4, starts = static_cast<uint64_t>(n + 1) * 4;
-  if (overlap(topk, each, pair, each) || overlap(topk, each, place, each) || overlap(topk, each, start, starts) ||
-      overlap(pair, each, place, each) || overlap(pair, each, start, starts) || overlap(place, each, start, starts))
-    return bad("topk, start, pair and place must not overlap");
   const size_t need = spp::expert_sort_bytes(P, n);
   if (need > 0) {
     if (!workspace || !aligned16(workspace)) return bad("workspace must not be NULL, and 16-byte aligned");
     if (workspace_bytes < need) return bad("the workspace is too small");
   }
+  const Rows all[] = {array(topk, P * 4), array(pair, P * 4), array(place, P * 4), array(start, (n + 1) * 4),
+                      array(need > 0 ? workspace : nullptr, static_cast<int64_t>(need))};
+  for (const Rows& one : all)
+    for (const Rows* other = all; other < &one; ++other)
+      if (meet(one, *other)) return bad("topk, start, pair, place and workspace must not overlap");
   return launched(spp::launch_expert_sort(topk, P, n, start, pair, place, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -610,6 +611,7 @@ extern "C" spp_status spp_expert_gather(int32_t dtype, const void* x, int64_t x_
   if (!place || !aligned(place, 4)) return bad("place must not be NULL, and aligned to its elements");
   const Rows to = rows_from(rows, rows_stride, D, static_cast<int64_t>(T) * K, elem);
   if (meet(to, rows_from(x, x_stride, D, T, elem))) return bad("rows must not overlap x");
+  if (meet(to, array(place, static_cast<int64_t>(T) * K * 4))) return bad("rows must not overlap place");
   RowArgs a = rows_of(T, K, D, elem);
   a.x = x;
   a.x_stride = x_stride * elem;
@@ -633,6 +635,8 @@ extern "C" spp_status spp_expert_combine(int32_t dtype, const void* rows, int64_
     return bad("place must not be NULL, place and weights aligned to their elements");
   const Rows to = rows_from(out, out_stride, D, T, elem);
   if (meet(to, rows_from(rows, rows_stride, D, static_cast<int64_t>(T) * K, elem))) return bad("out must not overlap rows");
+  const int64_t each = static_cast<int64_t>(T) * K * 4;
+  if (meet(to, array(place, each)) || meet(to, array(weights, each))) return bad("out must not overlap place or weights");
   if (residual) {
     SPP_BAD(rows_why(residual, residual_stride, D, elem));
     if (!(residual == out && residual_stride == out_stride) && meet(to, rows_from(residual, residual_stride, D, T, elem)))
@@ -663,8 +667,14 @@ extern "C" spp_status spp_expert_combine_grad(int32_t dtype, const void* d_out, 
     if (meet(to, rows_from(d_out, d_out_stride, D, T, elem))) return bad("d_rows must not overlap d_out");
     if (d_weights && !(rows == d_rows && rows_stride == d_rows_stride) && meet(to, rows_from(rows, rows_stride, D, P, elem)))
       return bad("d_rows must be rows with the same stride, or not overlap them");
+    if (meet(to, array(place, P * 4)) || meet(to, array(weights, P * 4)))
+      return bad("d_rows must not overlap place or weights");
     if (meet(to, array(d_weights, P * 4))) return bad("d_weights must not overlap d_rows");
   }
+  const Rows dots = array(d_weights, P * 4);
+  if (meet(dots, array(place, P * 4)) || meet(dots, array(weights, P * 4)) || meet(dots, rows_from(d_out, d_out_stride, D, T, elem)) ||
+      meet(dots, rows_from(rows, rows_stride, D, P, elem)))
+    return bad("d_weights must not overlap an input");
   RowArgs a = rows_of(T, K, D, elem);
   a.x = rows;
   a.x_stride = rows_stride * elem;

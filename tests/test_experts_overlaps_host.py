@@ -69,3 +69,61 @@ def test_products_whose_rows_share_a_byte_are_refused_and_no_others():
     (spp.spp_expert_combine_grad, GRAD, dict(rows_stride=192, d_rows_dev=2 * GOOD + 256, d_rows_stride=192))])
 def test_column_ranges_of_one_buffer_are_accepted(call, good, change):
     _not_refused(lambda: call(**{**good, **change}))
+
+
+OUTSIDE = 10 * GOOD    # where EXPERTS has its workspace
+EXPERTS_T = {**EXPERTS, "T": 300, "residual_dev": 0, "workspace_bytes": 1 << 30}
+
+
+@pytest.mark.parametrize("call,good,change", [
+    (spp.spp_expert_gather, GATHER, dict(rows_dev=2 * GOOD)),
+    (spp.spp_expert_gather, GATHER, dict(rows_dev=2 * GOOD + 32)),
+    (spp.spp_expert_gather, GATHER, dict(place_dev=3 * GOOD + 10 * 128 - 4)),
+    (spp.spp_expert_combine, COMBINE, dict(out_dev=2 * GOOD)),
+    (spp.spp_expert_combine, COMBINE, dict(out_dev=3 * GOOD)),
+    (spp.spp_expert_combine, COMBINE, dict(out_dev=3 * GOOD + 32)),
+    (spp.spp_expert_combine, COMBINE, dict(place_dev=5 * GOOD + 5 * 128 - 4)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_rows_dev=3 * GOOD)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_rows_dev=4 * GOOD + 32)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_rows_dev=4 * GOOD + 32, d_weights_dev=0)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_weights_dev=GOOD + 636)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_weights_dev=2 * GOOD)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_weights_dev=3 * GOOD)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_weights_dev=4 * GOOD)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_weights_dev=4 * GOOD - 36, d_rows_dev=0)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=9 * GOOD)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=8 * GOOD + 256)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=7 * GOOD)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=6 * GOOD + 16)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=5 * GOOD)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=GOOD + 320 * 32 - 16)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=3 * GOOD)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=2 * GOOD)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=4 * GOOD + 304)),
+    (spp.spp_mx4_experts, EXPERTS_T, dict(topk_dev=OUTSIDE + 4096)),
+    (spp.spp_mx4_experts, EXPERTS_T, dict(out_dev=OUTSIDE - 16)),
+] + [(spp.spp_expert_sort, {"topk_dev": GOOD, "T": 5000, "K": 4, "n": 8, "start_dev": 2 * GOOD, "pair_dev": 3 * GOOD,
+                            "place_dev": 4 * GOOD, "workspace_dev": 5 * GOOD, "workspace_bytes": 1 << 20},
+      dict(workspace_dev=at)) for at in (GOOD, 2 * GOOD + 32, 3 * GOOD + 79984, 4 * GOOD + 16)])
+def test_outputs_and_workspaces_over_other_arrays_are_refused(call, good, change):
+    _not_refused(lambda: call(**good))
+    _refused(lambda: call(**{**good, **change}))
+
+
+@pytest.mark.parametrize("call,good,change", [
+    (spp.spp_expert_gather, GATHER, dict(rows_dev=2 * GOOD + 48)),
+    (spp.spp_expert_combine, COMBINE, dict(out_dev=3 * GOOD + 48)),
+    (spp.spp_expert_combine, COMBINE, dict(weights_dev=0, out_dev=3 * GOOD)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_weights_dev=4 * GOOD + 40)),
+    (spp.spp_expert_combine_grad, GRAD, dict(d_rows_dev=4 * GOOD - 1280)),
+    (spp.spp_mx4_experts, EXPERTS, dict(workspace_dev=9 * GOOD + 384)),
+    (spp.spp_expert_sort, {"topk_dev": GOOD, "T": 40, "K": 4, "n": 8, "start_dev": 2 * GOOD, "pair_dev": 3 * GOOD,
+                           "place_dev": 4 * GOOD, "workspace_dev": GOOD, "workspace_bytes": 16}, dict())])
+def test_neighbouring_arrays_are_accepted(call, good, change):
+    _not_refused(lambda: call(**{**good, **change}))
+
+
+def test_arrays_of_no_element_overlap_nothing():
+    spp_sort = dict(topk_dev=GOOD + 4, T=0, K=4, n=8, start_dev=GOOD, pair_dev=GOOD + 8, place_dev=GOOD + 12, workspace_dev=0,
+                    workspace_bytes=0)
+    _not_refused(lambda: spp.spp_expert_sort(**spp_sort))
