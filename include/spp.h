@@ -592,9 +592,9 @@ spp_status spp_expert_sort(const int32_t* topk, int32_t T, int32_t K, int32_t n,
  * 16-byte aligned, a row and the strides multiples of 16 bytes (the same for
  * the calls below).  place: of spp_expert_sort, or any other int32 [T * K]: an
  * entry outside 0 .. T*K-1 takes no row, rows that no entry names are left as
- * they were, and a row that two entries name holds either one's.  The gradient
- * of x is spp_expert_combine of the rows' gradients, without weights.  rows
- * overlaps neither x nor place. */
+ * they were, and a row that two entries name holds no certain result (16 bytes
+ * of the one's, 16 of the other's).  The gradient of x is spp_expert_combine of
+ * the rows' gradients, without weights.  rows overlaps neither x nor place. */
 spp_status spp_expert_gather(int32_t dtype, const void* x, int64_t x_stride, const int32_t* place, int32_t T, int32_t K,
                              int32_t D, void* rows, int64_t rows_stride, void* hip_stream);
 /* out[t] = [residual[t] +] sum_k weights[t][k] rows[place[t * K + k]], sums in
@@ -609,7 +609,7 @@ spp_status spp_expert_combine(int32_t dtype, const void* rows, int64_t rows_stri
  * and d_weights may each be NULL; rows may be NULL without d_weights; weights
  * NULL: 1.  d_rows may be rows with the same stride.  A pair without a place
  * gets d_weights 0, rows that no pair names are left as they were; a row that
- * two pairs name holds either one's (and d_rows must then not be rows).  The
+ * two pairs name holds no certain result (and d_rows must then not be rows).  The
  * residual's gradient is d_out itself.  But for rows, d_rows and d_weights overlap
  * no input, and not each other. */
 spp_status spp_expert_combine_grad(int32_t dtype, const void* d_out, int64_t d_out_stride, const void* rows,

@@ -65,3 +65,24 @@ def test_inputs_and_outputs_as_columns_of_one_buffer(torch, M):  # noqa: F811
         assert np.array_equal(got[:M, 72:72 + D], host(x)), name
         got[:M, 8:8 + N] = got[:M, 72:72 + D] = np.nan
         assert np.isnan(got).all(), name
+
+
+@pytest.mark.parametrize("T,K,D", [(3, 2, 8), (400, 3, 2048), (2000, 2, 4104)])
+def test_rows_that_two_pairs_name(torch, T, K, D):  # noqa: F811
+    """Each 16 bytes are one of the pairs'; rows that one pair names are its own, the others as they were."""
+    from paper_2607_24787_amd import spp
+    rng = np.random.default_rng(T)
+    P = T * K
+    place = rng.integers(0, P, size=P)
+    x, place_dev = dev(rng.normal(size=(T, D)), "bf16"), dev(place.astype(np.int32))
+    rows, d_rows = blank((P, D), "bf16"), blank((P, D), "bf16")
+    spp.spp_expert_gather(spp.DTYPE_BF16, x.data_ptr(), D, place_dev.data_ptr(), T, K, D, rows.data_ptr(), D, stream())
+    spp.spp_expert_combine_grad(spp.DTYPE_BF16, x.data_ptr(), D, 0, 0, place_dev.data_ptr(), 0, T, K, D, d_rows.data_ptr(), D, 0,
+                                stream())
+    sent = host(x).reshape(T, D // 8, 8)
+    for got in (host(rows).reshape(P, D // 8, 8), host(d_rows).reshape(P, D // 8, 8)):
+        fine = np.zeros((P, D // 8), dtype=bool)
+        for p in range(P):
+            fine[place[p]] |= (got[place[p]] == sent[p // K]).all(-1)
+        named = np.isin(np.arange(P), place)
+        assert fine[named].all() and np.isnan(got[~named]).all() and 0 < named.sum() < P
