@@ -115,15 +115,6 @@ struct ScaleRow {
     __builtin_memcpy(&w, p + min(b, last), 4);
     return w;
   }
-  // kBlocks bytes from block b on of what load(b) gave; 1 past the row's end
-  template <int kBlocks>
-  __device__ __forceinline__ uint32_t bytes(uint32_t w, int b, int nb) const {
-    w >>= 8 * (b - min(b, last));
-#pragma unroll
-    for (int j = 1; j < kBlocks; ++j)
-      if (b + j >= nb) w = (w & ~(255u << (8 * j))) | static_cast<uint32_t>(kOne) << (8 * j);
-    return w;
-  }
 };
 
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
@@ -209,9 +200,8 @@ struct XBlocks {
   }
 };
 
-template <int SEL>
-__device__ __forceinline__ f32x4 mfma_mx4(u32x4 w, uint32_t w_scales, u32x4 x, uint32_t x_byte, f32x4 c) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(w), wide(x), c, 4, 4, SEL, static_cast<int>(w_scales), 0,
+__device__ __forceinline__ f32x4 mfma_mx4(u32x4 w, uint32_t w_byte, u32x4 x, uint32_t x_byte, f32x4 c) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(w), wide(x), c, 4, 4, 0, static_cast<int>(w_byte), 0,
                                                           static_cast<int>(x_byte));
 }
 
@@ -277,7 +267,7 @@ struct WeightBlocks {
             if constexpr (X == kXTerms) acc[t] = mfma_bf16(w, x.v[s][4 + q], acc[t]);
           }
         } else {
-          acc[t] = mfma_mx4<0>(codes[t][s], byte, x.v[s][0], x.byte[s], acc[t]);
+          acc[t] = mfma_mx4(codes[t][s], byte, x.v[s][0], x.byte[s], acc[t]);
         }
       }
     }

@@ -236,14 +236,10 @@ __global__ __launch_bounds__(kSortThreads) void expert_sort_kernel(SortArgs a) {
   // thread e: expert e (n is at most the threads)
   int all = 0, mine = 0;  // pairs of the expert: in all parts, and in the parts before this one
   if (tid < a.n) {
-    if (a.parts == 1) {
-      for (int w = 0; w < kSortWaves; ++w) all += s_row[w * a.n + tid];
-    } else {
-      for (int k = 0; k < a.parts; ++k) {
-        const int c = a.total[static_cast<size_t>(k) * a.n + tid];
-        all += c;
-        mine += k < static_cast<int>(blockIdx.x) ? c : 0;
-      }
+    for (int k = 0; k < a.parts; ++k) {
+      const int c = a.total[static_cast<size_t>(k) * a.n + tid];
+      all += c;
+      mine += k < static_cast<int>(blockIdx.x) ? c : 0;
     }
   }
   int total;
@@ -289,9 +285,6 @@ struct RowArgs {
 };
 
 constexpr int kRowThreads = 256;
-
-template <typename T>
-__device__ __forceinline__ int elems() { return 16 / static_cast<int>(sizeof(T)); }
 
 // 16 bytes to fp32 values and back
 template <typename T>
@@ -470,12 +463,11 @@ const char* pairs_why(int32_t T, int32_t K) {
 // Parts of a sort at most
 int64_t most_parts(int64_t P) { return std::min<int64_t>(kMaxParts, std::max<int64_t>(1, (P + kMinPart - 1) / kMinPart)); }
 
-// Parts of a sort, and pairs of one
+// Parts of a sort whose parts are not held, and pairs of one
 void parts_of(int64_t P, int* parts, int* each) {
-  const int64_t n = most_parts(P);
-  const int64_t e = std::max<int64_t>(1, ((P + n - 1) / n + kSortThreads - 1) / kSortThreads) * kSortThreads;
+  const int64_t e = ((P + kMaxParts - 1) / kMaxParts + kSortThreads - 1) / kSortThreads * kSortThreads;
   *each = static_cast<int>(e);
-  *parts = static_cast<int>(std::max<int64_t>(1, (P + e - 1) / e));
+  *parts = static_cast<int>((P + e - 1) / e);
 }
 
 const char* width_why(int32_t D, int elem) {
@@ -538,11 +530,9 @@ hipError_t launch_expert_sort(const int32_t* topk, int64_t P, int32_t n, int32_t
   }
   parts_of(P, &a.parts, &a.each);
   const unsigned lds = static_cast<unsigned>(kSortWaves * n * sizeof(int));
-  if (a.parts > 1) {
-    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(expert_count_kernel), dim3(a.parts),
-                                         dim3(kSortThreads), params, lds, st);
-    if (e != hipSuccess) return e;
-  }
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(expert_count_kernel), dim3(a.parts),
+                                       dim3(kSortThreads), params, lds, st);
+  if (e != hipSuccess) return e;
   return hipLaunchKernel(reinterpret_cast<const void*>(expert_sort_kernel), dim3(a.parts), dim3(kSortThreads), params,
                          lds, st);
 }
