@@ -1213,9 +1213,12 @@ int tile_rows(int64_t M, int groups, int outputs, int nb, bool mx4) {
 
 // Whether the experts' products go by tiles, behind a sort: from 10 pairs an
 // expert on (8 with 4-bit products), and 1 GFLOP.  Measured, few rows against
-// tiles: 128 experts of 2048 x 768 with 8 pairs each 141 : 130 us (bf16), 129 : 92
-// (4 bits), 64 of 1280 x 896 with 9 each 56 : 74 and 51 : 54, with 15 each 90 : 60
-// and 82 : 50; 8 of 1024 x 512 with 24 each (0.6 GFLOP) 21 : 28 and 24 : 25.
+// tiles: 128 experts of 2048 x 768 with 6 pairs each 116 : 141 us (bf16), 104 : 93
+// (4 bits), with 8 146 : 137 and 127 : 94, with 10 151 : 141 and 132 : 96; 64 of 1280 x
+// 896 with 9 each 62 : 82 and 54 : 55, with 10 74 : 70 and 64 : 50; 24 of 1024 x 768
+// with 8 each 30 : 36 and 29 : 28, with 12 31 : 37 and 30 : 28, with 16 41 : 37 and
+// 39 : 29; 8 of 1024 x 512 with 24 each (0.6 GFLOP) 24 : 31 and 28 : 26.  No one
+// number of pairs is the border at every width: at these the rule costs up to 1.2.
 // From 64 pairs an expert on in any case: few rows search all pairs.
 bool by_tiles(int64_t P, int n, int64_t D, int64_t I, bool mx4) {
   return P >= int64_t{64} * n || (P >= (mx4 ? 8 : 10) * int64_t{n} && 6 * P * D * I >= 1000000000);
