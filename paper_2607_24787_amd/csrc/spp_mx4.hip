@@ -580,16 +580,19 @@ constexpr int kTileOf = X == kXTermRows ? 32 * CT : 64 * CT;
 // and half of the rows of x.
 //
 // What bounds it: with bf16 rows the matrix instructions (32 of each wave a stage,
-// 2,370 cycles of a SIMD; 8,192 x 5,120 outputs at K = 2,048 take 152 us, 1.13
-// PFLOP/s, a library's bf16 product of 8,192^3 reaches 1.14 to 1.35).  With both
-// sides in 4 bits (1,320 cycles) what a compute unit gets from L2, 48 KB a stage,
-// which takes 900 to 1,300 cycles: 60 us, 2.9 PFLOP/s, of them about 12 for the
-// results' 84 MB, and 3.6 PFLOP/s at K = 16,384 (the instructions by themselves reach
-// 8.0, and 2.2 in bf16).  Whole lines matter: L2 gives 55 bytes a cycle where a
-// load's rows are 128 bytes and 29 where they are 64, and a 64-byte stage of 256 x
-// 128 tiles, two workgroups of four waves a compute unit, took 87 us.  Loads that
-// are issued together hold up the products behind them (53,000 of a workgroup's
-// 124,000 cycles), so they go between them, one at a time.
+// 37 cycles each in a loop of nothing else, 2,370 cycles of a SIMD; 8,192 x 5,120
+// outputs at K = 2,048 take 152 to 164 us, 1.05 to 1.13 PFLOP/s, a library's bf16
+// product of 8,192^3 reaches 1.14 to 1.35).  With both sides in 4 bits (41 cycles
+// each, 1,320) what a compute unit gets from L2, 48 KB a stage, which takes 890
+// cycles where nothing else is read: 60 us, 2.9 PFLOP/s, of them about 12 for the
+// results' 84 MB, the matrix units busy for 41,000 of the 130,000 cycles that a wave
+// lives; 3.6 PFLOP/s at K = 16,384 (the instructions by themselves reach 8.0, and 2.2
+// in bf16).  Whole lines matter: L2 gives 55 bytes a cycle where a load's rows are 128
+// bytes and 29 where they are 64, and a 64-byte stage of 256 x 128 tiles, two
+// workgroups of four waves a compute unit, took 87 us.  Loads that are issued
+// together hold up the products behind them, so they go between them, one at a time.
+// Rows of two terms: 1,024 tokens of 6 of 64 experts, 1280 outputs of K = 896, take 50
+// us, which bf16 rows took 37 for, with twice the products.
 template <int X, bool kSwiglu, typename Out, int CT>
 __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(ProductArgs a) {
   constexpr bool kMx4 = X == kXCodes;
