@@ -86,3 +86,22 @@ def test_rows_that_two_pairs_name(torch, T, K, D):  # noqa: F811
             fine[place[p]] |= (got[place[p]] == sent[p // K]).all(-1)
         named = np.isin(np.arange(P), place)
         assert fine[named].all() and np.isnan(got[~named]).all() and 0 < named.sum() < P
+
+
+@pytest.mark.parametrize("M", [1, 20, 700])
+def test_products_of_subnormal_activations(torch, M):  # noqa: F811
+    """A bf16 below 2^-126 times a weight of 6 * 2^125 is a number like any other."""
+    from oracle import experts as ox
+    from paper_2607_24787_amd import spp
+    rng = np.random.default_rng(M)
+    N, K = 300, 96
+    codes, scales = rng.integers(0, 16, size=(N, K)).astype(np.uint8), np.full((N, K // 32), 252, dtype=np.uint8)
+    x = dev(rng.integers(-127, 128, size=(M, K)) * 2.0 ** -133, "bf16")
+    b, s, out = dev(ox.pack(codes)), dev(scales), blank((M, N), "f32")
+    spp.spp_mx4_matmul(spp.make_mx4(b.data_ptr(), s.data_ptr(), N, K), 1, 0, x.data_ptr(), K, M, spp.DTYPE_F32, out.data_ptr(), N,
+                       stream())
+    v = x.view(torch.int16).cpu().numpy().astype(np.int64)
+    exact = np.where(v < 0, -1.0, 1.0) * (v & 0x7fff) * 2.0 ** -133
+    assert np.abs(exact).max() < 2.0 ** -126 and np.abs(exact).max() > 0
+    want, bound = ox.product(exact, ox.values(codes, scales))
+    assert np.all(np.abs(host(out) - want) <= bound + ox.U32 * np.abs(want))
